@@ -20,7 +20,7 @@
  *  - Layout: q, k, v, w, o, d_o, dq, dk, dv, dw are contiguous [B, H, L, d];
  *    beta, dbeta, lse are contiguous [B, H, L] (the *_layout and *_varlen entry
  *    points also take [B, L, H, d] and packed sequences).  w and beta are per
- *    token and per head.  No grouped-query sharing.
+ *    token and per head.  No grouped-query sharing (but for the path_paged_* calls).
  *  - dtype `dt` is the storage type of q,k,v,w,beta,o and of all gradients
  *    (PATH_F32: float, PATH_BF16: bfloat16).  lse is always float.
  *  - Arithmetic.  PATH_F32 contracts on fp32 MFMA throughout.  PATH_BF16 accumulates
@@ -337,6 +337,56 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
                                    const void* log_f, void* kcache, void* vcache, float* ccache, int n, int Lmax,
                                    void* o, float* lse, int B, int H, int d, float scale, path_dtype_t dt,
                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Serving from paged caches (Sec. 3.4 with sequences of different lengths, several new tokens a call, and cache memory handed out
+ * in pages).  The caches hold what the decode path's hold -- keys carried to the sequence's last token, k_i^(n) = H_{n-1} .. H_{i+1} k_i,
+ * and values; with gates the running sums c_i -- in pools of pages:
+ *   kpages, vpages [num_pages, H, page_size, d] (dt), cpages [num_pages, H, page_size] (fp32; NULL for plain PaTH).
+ *   page_size a power of two from 16 to 4096; slot j of a head in page p holds the tokens i with page_table[s][i / page_size] = p, i % page_size = j.
+ * Lengths and tables are DEVICE int32 arrays, read when the kernels run (a captured call follows them through its replays):
+ *   page_table [nseq, pages_per_seq]; cached [nseq], tokens of each sequence in the cache; cu_new [nseq + 1], not decreasing: sequence s
+ *   brings the new tokens cu_new[s] .. cu_new[s+1]-1 of q, k, v, w, beta, log_f, o, lse, packed along the token axis.  No new tokens, none cached: allowed.
+ * Host arguments bound them: T tokens in the packed tensors, at most max_new new and max_cached cached tokens a sequence (both choose the
+ * grids and how the cache is split; close bounds are fast).  Values past the bounds are held to them; rows of o and lse that belong to no sequence are left
+ * as they are.  A page_table entry outside [0, num_pages) is a hole: its tokens take no part, nothing is read or written there.
+ *
+ * Shapes: q, o [T, H * group, d], lse [T, H * group] (fp32); k, v, w [T, H, d]; beta, log_f [T, H]; all contiguous.  Query heads
+ * h * group .. h * group + group - 1 share key head h with its w, beta and gates (group 1: as everywhere else).
+ *
+ *   path_paged_attn    o, lse of the new tokens: each attends to its sequence's cached tokens and to the new ones up to itself.  The
+ *                      caches are only read (drafted tokens can be looked at and dropped; pages may be shared between sequences).
+ *   path_paged_append  the new tokens' transitions applied to the cached keys, in place, and the new keys (carried to the last new token),
+ *                      values and gate sums written behind them.  The caller owns `cached` and adds the new tokens to it
+ *                      afterwards.  Room: tokens past pages_per_seq * page_size are not stored.  Pages that it reaches belong to one sequence only
+ *                      (keys carried on by two sequences are nobody's: copy the pages first; the call then leaves undefined keys, no fault).
+ *   path_paged_extend  both, in the order attention, append; up to 16 new tokens and 64 rows (new tokens x group) a sequence in one pass over its cache.
+ *
+ * Attention uses the cached keys as they stand: the logit is formed from x = H_{n} .. H_{n+a} q with the stored key, where path_decode_step
+ * rounds the refreshed key first.  A server may put appends off: the new tokens of path_paged_attn are then all tokens since the
+ * last append (keys are read and written back, and rounded, once per append instead of once per token).
+ * Arithmetic with PATH_BF16: up to 16 new tokens, X and the transitions as sums of two bf16 operands (no range rule); longer chunks
+ * carry queries, keys and transitions as fp16 operands under the range rule above (the logits inside a tile of 64 new tokens in fp32).
+ * workspace: path_paged_workspace_bytes(...) bytes (0 for arguments that the calls reject), 256-byte aligned; contents undefined before and after.
+ * Errors: PATH_ERR_SHAPE for nseq, H, group or max_new < 1, group > 64, T or max_cached < 0, a page size that is not allowed, or max_cached >
+ * pages_per_seq * page_size; PATH_ERR_NULL also if only one of log_f and cpages is given.  T = 0 does nothing.
+ */
+size_t path_paged_workspace_bytes(int nseq, int T, int max_new, int max_cached, int H, int group, int d, path_dtype_t dt);
+path_status_t path_paged_attn(const void* q, const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                              const void* kpages, const void* vpages, const float* cpages, const int* page_table,
+                              const int* cached, const int* cu_new, void* o, float* lse, int nseq, int T, int max_new,
+                              int max_cached, int num_pages, int page_size, int pages_per_seq, int H, int group, int d,
+                              float scale, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream);
+path_status_t path_paged_append(const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                                void* kpages, void* vpages, float* cpages, const int* page_table, const int* cached,
+                                const int* cu_new, int nseq, int T, int max_new, int max_cached, int num_pages,
+                                int page_size, int pages_per_seq, int H, int d, path_dtype_t dt, void* workspace,
+                                size_t workspace_bytes, void* stream);
+path_status_t path_paged_extend(const void* q, const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                                void* kpages, void* vpages, float* cpages, const int* page_table, const int* cached,
+                                const int* cu_new, void* o, float* lse, int nseq, int T, int max_new, int max_cached,
+                                int num_pages, int page_size, int pages_per_seq, int H, int group, int d, float scale,
+                                path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Sequence-parallel forward: ONE device's share of the ring of paper Sec. 3.5 ("context parallelism": the

@@ -7,6 +7,7 @@ CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -119,6 +120,14 @@ def load_library():
     lib.path_decode_static_scratch_bytes.argtypes = []
     lib.path_decode_step_static.restype = ci
     lib.path_decode_step_static.argtypes = [vp] * 7 + [ci, ci, vp, vp, ci, ci, ci, cf, ci, vp]
+    lib.path_paged_workspace_bytes.restype = sz
+    lib.path_paged_workspace_bytes.argtypes = [ci] * 8
+    lib.path_paged_attn.restype = ci
+    lib.path_paged_attn.argtypes = [vp] * 14 + [ci] * 10 + [cf, ci, vp, sz, vp]
+    lib.path_paged_append.restype = ci
+    lib.path_paged_append.argtypes = [vp] * 11 + [ci] * 10 + [vp, sz, vp]
+    lib.path_paged_extend.restype = ci
+    lib.path_paged_extend.argtypes = [vp] * 14 + [ci] * 10 + [cf, ci, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -536,3 +545,90 @@ def path_attn_varlen_bwd(q, k, v, w, beta, o, lse, d_o, cu_seqlens, log_f=None, 
                                                *[_ptr(x) for x in outs], _opt(dlog_f), arr, n, H, d, 1, scale, dt,
                                                _ptr(workspace), workspace.numel(), _stream_handle(stream)))
     return tuple(outs) + ((dlog_f,) if dlog_f is not None else ())
+
+
+def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) -> int:
+    """Bytes of scratch that the path_paged_* calls need for these bounds (more of any of them: not less)."""
+    return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
+
+
+def _paged(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, log_f, cpages, o, lse, workspace, max_new, max_cached):
+    """Checks that every tensor is what the kernels take it for; (nseq, T, num_pages, page_size, pages_per_seq, H, group, d, dt, workspace)."""
+    import torch
+    if k.dim() != 3 or kpages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k is [T,H,d], kpages [num_pages,H,page_size,d], page_table [nseq,pages_per_seq]")
+    T, H, d = k.shape
+    num_pages, _, page_size, _ = kpages.shape
+    nseq, per_seq = page_table.shape
+    dt = _dt_of(k)
+    group = 1
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
+            raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
+        group = q.shape[1] // H
+    want = [("v", v, (T, H, d), k.dtype), ("w", w, (T, H, d), k.dtype), ("beta", beta, (T, H), k.dtype),
+            ("kpages", kpages, (num_pages, H, page_size, d), k.dtype), ("vpages", vpages, tuple(kpages.shape), k.dtype),
+            ("page_table", page_table, (nseq, per_seq), torch.int32), ("cached", cached, (nseq,), torch.int32), ("cu_new", cu_new, (nseq + 1,), torch.int32)]
+    if q is not None:
+        want += [("q", q, tuple(q.shape), k.dtype), ("o", o, tuple(q.shape), k.dtype), ("lse", lse, (T, H * group), torch.float32)]
+    if log_f is not None:
+        want.append(("log_f", log_f, (T, H), k.dtype))
+    if cpages is not None:
+        want.append(("cpages", cpages, (num_pages, H, page_size), torch.float32))
+    for name, t, shape, dtype in [("k", k, (T, H, d), k.dtype), *want]:
+        if t is None:
+            continue
+        if tuple(t.shape) != shape or t.dtype != dtype:
+            raise ValueError(f"{name} is {shape}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
+        if not t.is_cuda or t.device != k.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
+    if workspace is None:
+        workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
+    elif workspace.device != k.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the GPU that k is on")
+    return nseq, T, num_pages, page_size, per_seq, H, group, d, dt, workspace
+
+
+def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream):
+    import torch
+    max_new, max_cached = int(max_new), int(max_cached)
+    if q is not None:
+        o = torch.empty_like(q) if o is None else o
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+    nseq, T, num_pages, page_size, per_seq, H, group, d, dt, workspace = _paged(
+        q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, log_f, cpages, o, lse, workspace, max_new, max_cached)
+    if T == 0:
+        return o, lse
+    call = getattr(load_library(), name)
+    cache = (_ptr(k), _ptr(v), _ptr(w), _ptr(beta), _opt(log_f), _ptr(kpages), _ptr(vpages), _opt(cpages), _ptr(page_table), _ptr(cached), _ptr(cu_new))
+    sizes = (nseq, T, max_new, max_cached, num_pages, page_size, per_seq, H)
+    here = torch.cuda.current_device() == k.device.index
+    with (contextlib.nullcontext() if here else torch.cuda.device(k.device)):      # (launches go to the tensors' GPU)
+        if q is None:
+            _check(call(*cache, *sizes, d, dt, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+        else:
+            scale = float(d ** -0.5 if scale is None else scale)
+            _check(call(_ptr(q), *cache, _ptr(o), _ptr(lse), *sizes, group, d, scale, dt, _ptr(workspace), workspace.numel() * workspace.element_size(),
+                        _stream_handle(stream)))
+    return o, lse
+
+
+def path_paged_attn(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f=None, cpages=None,
+                    scale=None, o=None, lse=None, workspace=None, stream=None):
+    """Attention of packed new tokens over paged caches, which are only read: q [T,H*group,d], k, v, w [T,H,d], beta (and log_f) [T,H];
+    kpages, vpages [num_pages,H,page_size,d] (cpages [num_pages,H,page_size] fp32); page_table [nseq,pages_per_seq], cached [nseq], cu_new [nseq+1]
+    int32 on the GPU.  Returns (o [T,H*group,d], lse [T,H*group]); rows of no sequence are left as they are."""
+    return _paged_call("path_paged_attn", q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream)
+
+
+def path_paged_append(k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f=None, cpages=None,
+                      workspace=None, stream=None):
+    """Appends packed new tokens to paged caches: cached keys take the new tokens' transitions in place, new keys, values (and gate
+    sums) are written behind them.  ``cached`` stays as it is: the caller adds the new tokens to it."""
+    _paged_call("path_paged_append", None, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, None, None, None, workspace, stream)
+
+
+def path_paged_extend(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f=None, cpages=None,
+                      scale=None, o=None, lse=None, workspace=None, stream=None):
+    """path_paged_attn, then path_paged_append; few new tokens a sequence (one, or drafts) in one pass over its cache."""
+    return _paged_call("path_paged_extend", q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream)

@@ -18,6 +18,7 @@ hipError_t launch_attn_states(const FwdParams& p, int d, int is_bf16, hipStream_
 #include "bwd_decl.h"
 #include "decode_decl.h"
 #include "fox_decl.h"
+#include "paged_decl.h"
 namespace path {
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -943,4 +944,140 @@ extern "C" path_status_t path_attn_varlen_bwd(const void* q, const void* k, cons
     if (st != PATH_OK) return st;
     return bwd_impl(BWD_FULL, BWD_STAGE_ALL, ul, q, k, v, w, beta, log_f, o, lse, d_o, dq, dk, dv, dw, dbeta, dlog_f, nseq, H, lmax, d,
                     causal, scale, dt, rest, rest_bytes, stream);
+}
+
+// ---- paged caches ----
+namespace {
+struct PagedPlan {
+    bool few, many;              // which of the two ways sequences may go
+    int few_limit, few_m, few_splits, few_len, tiles, many_splits, many_len;
+    size_t few_o, few_ml, x, crow, many_o, many_ml, kt, wt, zt, vt, sd, pt, total;
+};
+}  // namespace
+
+static bool paged_shape_ok(int nseq, int T, int max_new, int max_cached, int H, int group, int d) {
+    if (nseq < 1 || T < 0 || max_new < 1 || max_cached < 0 || H < 1 || group < 1 || group > PAGED_FEW_ROWS) return false;
+    if (d != 64 && d != 128) return false;
+    if ((long long)nseq * H > 65535 || (long long)H * group > 65535 || max_cached > (1 << 30)) return false;
+    return ((long long)T / 64 + nseq) * 64 * H * group <= (1LL << 31) / 4;      // 32-bit grids
+}
+
+static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H, int group, int d, size_t es) {
+    PagedPlan p{};
+    const int mn = max_new < T ? max_new : T, room = PAGED_FEW_ROWS / group, lim = room < PAGED_FEW ? room : PAGED_FEW;
+    p.many = mn > lim;
+    p.few = !p.many || nseq > 1;      // (one sequence that may be long is taken for long)
+    p.few_limit = p.few ? lim : 0;
+    p.few_m = mn < lim ? mn : lim;
+    auto pieces = [&](long long units, long long want, int least, int& len) {      // the cache in pieces so that about `want` workgroups run
+        const long long most = (max_cached + least - 1) / least;
+        long long n = (want + units - 1) / units;
+        n = n < 1 ? 1 : n > most ? most : n;
+        len = n > 0 ? (int)(((max_cached + n - 1) / n + 127) / 128 * 128) : 128;
+        return (max_cached + len - 1) / len;
+    };
+    p.few_splits = pieces((long long)nseq * H, 1024, 128, p.few_len);
+    if (p.few_splits < 1) p.few_splits = 1;
+    p.tiles = T / 64 + nseq;
+    const long long tiles = T / 64 > 1 ? T / 64 : 1;
+    p.many_splits = pieces(tiles * H * group, 512, 512, p.many_len);
+
+    size_t off = 0;
+    auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
+    const size_t Hq = (size_t)H * group, rows = (size_t)T * Hq;
+    if (p.few) {
+        const size_t slots = p.few_splits > 1 ? (size_t)p.few_splits * nseq * p.few_m * Hq : 0;
+        take(p.few_o, slots * d * 4);
+        take(p.few_ml, slots * 2 * 4);
+    }
+    if (p.many) {
+        const size_t th = (size_t)p.tiles * H;
+        take(p.x, rows * d * 4);
+        take(p.crow, (size_t)T * H * 4);
+        take(p.many_o, (size_t)(1 + p.many_splits) * rows * d * 4);
+        take(p.many_ml, (size_t)(1 + p.many_splits) * rows * 2 * 4);
+        for (size_t* f : {&p.kt, &p.wt, &p.zt, &p.vt}) take(*f, th * CHUNK * d * es);
+        take(p.sd, (size_t)p.tiles * Hq * CHUNK * CHUNK * 4);
+        take(p.pt, (size_t)nseq * H * d * d * es);
+    }
+    p.total = off > 256 ? off : 256;
+    return p;
+}
+
+extern "C" size_t path_paged_workspace_bytes(int nseq, int T, int max_new, int max_cached, int H, int group, int d, path_dtype_t dt) {
+    if (dt != PATH_F32 && dt != PATH_BF16) return 0;
+    if (!paged_shape_ok(nseq, T, max_new, max_cached, H, group, d)) return 0;
+    return paged_plan(nseq, T, max_new, max_cached, H, group, d, dt == PATH_F32 ? 4 : 2).total;
+}
+
+static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!a.k || !a.v || !a.w || !a.beta || !a.kpages || !a.vpages || !a.table || !a.cached || !a.cu || !workspace) return PATH_ERR_NULL;
+    if (a.attn && (!a.q || !a.o || !a.lse)) return PATH_ERR_NULL;
+    if (!a.log_f != !a.cpages) return PATH_ERR_NULL;
+    if (dt != PATH_F32 && dt != PATH_BF16) return PATH_ERR_DTYPE;
+    if (!paged_shape_ok(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d) || a.num_pages < 1 || a.per_seq < 1) return PATH_ERR_SHAPE;
+    if (page_size < PAGED_GROUP || page_size > 4096 || (page_size & (page_size - 1))) return PATH_ERR_SHAPE;
+    if (a.max_cached > (long long)a.per_seq * page_size) return PATH_ERR_SHAPE;
+    if (a.attn && !(a.scale > 0.f)) return PATH_ERR_UNSUPPORTED;
+    while ((1 << a.page_shift) < page_size) ++a.page_shift;
+    const PagedPlan p = paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, dt == PATH_F32 ? 4 : 2);
+    if (workspace_bytes < p.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
+    const void* al[] = {a.q, a.k, a.v, a.w, a.kpages, a.vpages, a.cpages, a.o};
+    for (const void* ptr : al) if (misaligned(ptr)) return PATH_ERR_ALIGN;
+    if (a.T == 0) return PATH_OK;
+    clear_inherited_error();
+    char* const ws = static_cast<char*>(workspace);
+    auto f = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+    a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len;
+    a.few_o = f(p.few_o); a.few_ml = f(p.few_ml);
+    a.tiles = p.tiles; a.many_splits = p.many_splits; a.many_len = p.many_len;
+    a.x = f(p.x); a.crow = f(p.crow); a.many_o = f(p.many_o); a.many_ml = f(p.many_ml);
+    a.kt = ws + p.kt; a.wt = ws + p.wt; a.zt = ws + p.zt; a.vt = ws + p.vt; a.sd = f(p.sd); a.pt = ws + p.pt;
+    const int bf = dt == PATH_BF16 ? 1 : 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (p.few) {
+        if (!hip_ok(launch_paged_rows(a, d, bf, st), "paged cache, few new tokens")) return PATH_ERR_HIP;
+        if (a.attn && p.few_splits > 1 && !hip_ok(launch_paged_merge_few(a, d, bf, st), "paged cache, pieces joined")) return PATH_ERR_HIP;
+    }
+    if (p.many) {
+        if (!hip_ok(launch_paged_chunk(a, d, bf, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
+        if (a.attn) {
+            if (!hip_ok(launch_paged_sweep(a, d, bf, st), "paged cache, sweep over the new tokens")) return PATH_ERR_HIP;
+            if (p.many_splits > 0 && !hip_ok(launch_paged_rows_many(a, d, bf, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
+            if (!hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
+        }
+        if (a.append) {
+            if (!hip_ok(launch_paged_scan(a, d, bf, st), "paged cache, scan over the new tokens")) return PATH_ERR_HIP;
+            if (a.max_cached > 0 && !hip_ok(launch_paged_refresh(a, d, bf, st), "paged cache, keys carried on")) return PATH_ERR_HIP;
+        }
+    }
+    return PATH_OK;
+}
+
+extern "C" path_status_t path_paged_attn(const void* q, const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                                         const void* kpages, const void* vpages, const float* cpages, const int* page_table,
+                                         const int* cached, const int* cu_new, void* o, float* lse, int nseq, int T, int max_new,
+                                         int max_cached, int num_pages, int page_size, int pages_per_seq, int H, int group, int d,
+                                         float scale, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream) {
+    PagedArgs a{q, k, v, w, beta, log_f, const_cast<void*>(kpages), const_cast<void*>(vpages), const_cast<float*>(cpages), page_table, cached, cu_new,
+                o, lse, nseq, T, max_new, max_cached, num_pages, 0, pages_per_seq, H, group, scale, 1, 0};
+    return paged_call(a, page_size, d, dt, workspace, workspace_bytes, stream);
+}
+extern "C" path_status_t path_paged_append(const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                                           void* kpages, void* vpages, float* cpages, const int* page_table, const int* cached,
+                                           const int* cu_new, int nseq, int T, int max_new, int max_cached, int num_pages,
+                                           int page_size, int pages_per_seq, int H, int d, path_dtype_t dt, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+    PagedArgs a{nullptr, k, v, w, beta, log_f, kpages, vpages, cpages, page_table, cached, cu_new,
+                nullptr, nullptr, nseq, T, max_new, max_cached, num_pages, 0, pages_per_seq, H, 1, 1.f, 0, 1};
+    return paged_call(a, page_size, d, dt, workspace, workspace_bytes, stream);
+}
+extern "C" path_status_t path_paged_extend(const void* q, const void* k, const void* v, const void* w, const void* beta, const void* log_f,
+                                           void* kpages, void* vpages, float* cpages, const int* page_table, const int* cached,
+                                           const int* cu_new, void* o, float* lse, int nseq, int T, int max_new, int max_cached,
+                                           int num_pages, int page_size, int pages_per_seq, int H, int group, int d, float scale,
+                                           path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream) {
+    PagedArgs a{q, k, v, w, beta, log_f, kpages, vpages, cpages, page_table, cached, cu_new,
+                o, lse, nseq, T, max_new, max_cached, num_pages, 0, pages_per_seq, H, group, scale, 1, 1};
+    return paged_call(a, page_size, d, dt, workspace, workspace_bytes, stream);
 }
