@@ -950,7 +950,7 @@ extern "C" path_status_t path_attn_varlen_bwd(const void* q, const void* k, cons
 namespace {
 struct PagedPlan {
     bool few, many;              // which of the two ways sequences may go
-    int few_limit, few_m, few_splits, few_len, tiles, many_splits, many_len;
+    int few_limit, few_m, few_splits, few_len, tiles, row_blocks, many_splits, many_len;
     size_t few_o, few_ml, x, crow, many_o, many_ml, kt, wt, zt, vt, sd, pt, total;
 };
 }  // namespace
@@ -979,8 +979,9 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
     p.few_splits = pieces((long long)nseq * H, 1024, 128, p.few_len);
     if (p.few_splits < 1) p.few_splits = 1;
     p.tiles = T / 64 + nseq;
-    const long long tiles = T / 64 > 1 ? T / 64 : 1;
-    p.many_splits = pieces(tiles * H * group, 512, 512, p.many_len);
+    p.row_blocks = (int)((long long)T * group / 128) + nseq;
+    const long long blocks = (long long)T * group / 128;
+    p.many_splits = pieces((blocks > 1 ? blocks : 1) * H, 512, 512, p.many_len);
 
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
@@ -1030,7 +1031,7 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     auto f = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
     a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len;
     a.few_o = f(p.few_o); a.few_ml = f(p.few_ml);
-    a.tiles = p.tiles; a.many_splits = p.many_splits; a.many_len = p.many_len;
+    a.tiles = p.tiles; a.row_blocks = p.row_blocks; a.joined = dt == PATH_BF16; a.many_splits = p.many_splits; a.many_len = p.many_len;
     a.x = f(p.x); a.crow = f(p.crow); a.many_o = f(p.many_o); a.many_ml = f(p.many_ml);
     a.kt = ws + p.kt; a.wt = ws + p.wt; a.zt = ws + p.zt; a.vt = ws + p.vt; a.sd = f(p.sd); a.pt = ws + p.pt;
     const int bf = dt == PATH_BF16 ? 1 : 0;
@@ -1043,8 +1044,8 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
         if (!hip_ok(launch_paged_chunk(a, d, bf, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
         if (a.attn) {
             if (!hip_ok(launch_paged_sweep(a, d, bf, st), "paged cache, sweep over the new tokens")) return PATH_ERR_HIP;
-            if (p.many_splits > 0 && !hip_ok(launch_paged_rows_many(a, d, bf, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
-            if (!hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
+            if (p.many_splits > 0 && !hip_ok(bf ? launch_paged_attn(a, d, st) : launch_paged_rows_many(a, d, 0, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
+            if (p.many_splits > a.joined && !hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
         }
         if (a.append) {
             if (!hip_ok(launch_paged_scan(a, d, bf, st), "paged cache, scan over the new tokens")) return PATH_ERR_HIP;

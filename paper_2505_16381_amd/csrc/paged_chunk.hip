@@ -392,7 +392,18 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
         }
     } else {
         l_run = sum_rows(l_run);
-        if (there) {
+        if (there && q.n == 0) {      // nothing cached: that was all
+            const float inv = 1.f / l_run;
+            typedef T V4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                V4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (T)(O[t][i] * inv);
+                *reinterpret_cast<V4*>(reinterpret_cast<T*>(a.o) + at * D + 16 * t + 4 * g) = v;
+            }
+            if (g == 0) a.lse[at] = (m_run + __builtin_amdgcn_logf(l_run)) * LN2;
+        } else if (there) {
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 *reinterpret_cast<f32x4*>(a.x + at * D + 16 * t + 4 * g) = x[t];

@@ -37,6 +37,8 @@ struct PagedArgs {
     float *few_o, *few_ml;                         // [split][nseq * few_m * H * G][d], [..][2]
     // the others: tiles of 64 new tokens (tile c of sequence s: first_tile(s) + c < tiles)
     int tiles, many_splits, many_len;
+    int row_blocks;                                // blocks of 128 rows, first_block(s) + i < row_blocks
+    int joined;                                    // the attention kernel joins a single piece with record 0 itself
     float *x, *crow;                               // [T][H*G][d] X; [T][H] c of the new tokens (gates)
     float *many_o, *many_ml;                       // [1 + split][T * H * G][d], [..][2]; record 0: the new tokens' own
     void *kt, *wt, *zt, *vt;                       // [tiles][H]: operand tiles of the new tokens, see paged_chunk.hip
@@ -53,6 +55,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int s) {
 }
 // The tiles of a sequence start here: sequences before it have at most t0 / 64 + s tiles, each at most one part tile.
 __device__ __forceinline__ int first_tile(const PagedArgs& a, int s) { return (min(max(a.cu[s], 0), a.T) >> 6) + s; }
+// The same for blocks of 128 rows (token, query head of the group).
+__device__ __forceinline__ int first_block(const PagedArgs& a, int s) { return min(max(a.cu[s], 0), a.T) * a.G / 128 + s; }
 
 // Where 16 cached tokens of a head lie, and how many of them there are: pos a multiple of 16 below n.  An entry of the page table outside the
 // pool is a hole: nothing is read or written there.
@@ -78,6 +82,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rsrc(const void* pages, 
     const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)p), hi = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32));
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0,
                                              __builtin_amdgcn_readfirstlane(valid * row_bytes), 0x00020000);
+}
+
+// 16 bytes per lane of such a buffer straight to LDS, one lane behind the other.  (Written inside a kernel template, the builtin keeps the host pass from
+// emitting the kernel: a function
+// of its own.)
+__device__ __forceinline__ void paged_to_lds(__amdgpu_buffer_rsrc_t r, unsigned char* lds, int offset) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, offset, 0, 0, 0);
 }
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
@@ -113,6 +124,7 @@ template <int E, typename T> __device__ __forceinline__ void load_f32(const T* p
 
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int is_bf16, hipStream_t st);       // few new tokens: everything; d = 64, 128
 hipError_t launch_paged_rows_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st);  // X rows from the workspace
+hipError_t launch_paged_attn(const PagedArgs& a, int d, hipStream_t st);                    // the same, bf16
 hipError_t launch_paged_merge_few(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
 hipError_t launch_paged_merge_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
 hipError_t launch_paged_chunk(const PagedArgs& a, int d, int is_bf16, hipStream_t st);      // tiles of the new tokens

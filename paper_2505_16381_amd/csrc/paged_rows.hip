@@ -559,6 +559,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
         const PagedSeq q = paged_seq(a, s);
         if (tok - q.t0 < 0 || tok - q.t0 >= q.m || q.m <= a.few_limit) return;
         used = 1 + (q.n + a.many_len - 1) / a.many_len;
+        if (used <= 1 + a.joined) return;      // (the sweep or the attention kernel has finished it)
         at = slot = row;
     }
     constexpr int E = D / 64;
