@@ -997,7 +997,9 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
         take(p.crow, (size_t)T * H * 4);
         take(p.many_o, (size_t)(1 + p.many_splits) * rows * d * 4);
         take(p.many_ml, (size_t)(1 + p.many_splits) * rows * 2 * 4);
-        for (size_t* f : {&p.kt, &p.wt, &p.zt, &p.vt}) take(*f, th * CHUNK * d * es);
+        // kt, zt: fp32, or pairs of bf16 tiles; w and v are taken as they are with bf16
+        for (size_t* f : {&p.kt, &p.zt}) take(*f, th * CHUNK * d * 4);
+        for (size_t* f : {&p.wt, &p.vt}) take(*f, es == 4 ? th * CHUNK * d * 4 : 0);
         take(p.sd, (size_t)p.tiles * Hq * CHUNK * CHUNK * 4);
         take(p.pt, (size_t)nseq * H * d * d * es);
     }
@@ -1041,16 +1043,18 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
         if (a.attn && p.few_splits > 1 && !hip_ok(launch_paged_merge_few(a, d, bf, st), "paged cache, pieces joined")) return PATH_ERR_HIP;
     }
     if (p.many) {
-        if (!hip_ok(launch_paged_chunk(a, d, bf, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
-        if (a.attn) {
-            if (!hip_ok(launch_paged_sweep(a, d, bf, st), "paged cache, sweep over the new tokens")) return PATH_ERR_HIP;
-            if (p.many_splits > 0 && !hip_ok(bf ? launch_paged_attn(a, d, st) : launch_paged_rows_many(a, d, 0, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
-            if (p.many_splits > a.joined && !hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
+        if (bf) {
+            if (!hip_ok(launch_paged_chunk16(a, d, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
+            if (!hip_ok(launch_paged_sweep16(a, d, st), "paged cache, sweep over the new tokens")) return PATH_ERR_HIP;
+            if (a.attn && p.many_splits > 0 && !hip_ok(launch_paged_attn(a, d, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
+        } else {
+            if (!hip_ok(launch_paged_chunk(a, d, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
+            if (a.attn && !hip_ok(launch_paged_sweep(a, d, st), "paged cache, sweep over the new tokens")) return PATH_ERR_HIP;
+            if (a.attn && p.many_splits > 0 && !hip_ok(launch_paged_rows_many(a, d, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
+            if (a.append && !hip_ok(launch_paged_scan(a, d, st), "paged cache, scan over the new tokens")) return PATH_ERR_HIP;
         }
-        if (a.append) {
-            if (!hip_ok(launch_paged_scan(a, d, bf, st), "paged cache, scan over the new tokens")) return PATH_ERR_HIP;
-            if (a.max_cached > 0 && !hip_ok(launch_paged_refresh(a, d, bf, st), "paged cache, keys carried on")) return PATH_ERR_HIP;
-        }
+        if (a.attn && p.many_splits > a.joined && !hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
+        if (a.append && a.max_cached > 0 && !hip_ok(launch_paged_refresh(a, d, bf, st), "paged cache, keys carried on")) return PATH_ERR_HIP;
     }
     return PATH_OK;
 }

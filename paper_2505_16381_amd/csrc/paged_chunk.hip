@@ -1,5 +1,5 @@
-// Chunks of new tokens for a paged cache: the triangular transform of tiles of 64 tokens, the queries' way through the tiles to
-// the chunk's start, and the keys' and the transitions' to its end.
+// Chunks of new tokens for a paged cache, fp32: the triangular transform of tiles of 64 tokens, the queries' way through the tiles to
+// the chunk's start, and the keys' and the transitions' to its end.  (bf16: paged_chunk16.hip.)
 //
 // Per tile and key head (paged_chunk_kernel), with the matrices of paged_decl.h restricted to the tile's tokens:
 //     kt  K - (T D)^T W       keys carried to the tile's right edge
@@ -7,28 +7,20 @@
 //                             what one with the d x d matrix costs at d = 128
 //     x   Q - (L T) W         queries as they stand at the tile's left edge
 //     sd  Q K^T - L (T D)     logits inside the tile
-// All in fp32: the inputs are exact there, and these logits are the ones that short sequences consist of.
 //
 // paged_sweep_kernel carries rows X through earlier tiles, right to left: S = kt X^T, then X^T -= Z^T (W X^T).  Rows are the queries of
 // a tile (with softmax and values beside it), or, for the append, rows of the identity: then S is a row of every key of the tile
 // carried to the chunk's END, and what is left of X at the chunk's start are the rows of H_{m-1} .. H_0.
-// A wave has 16 rows; results stay in registers and are the next product's operand, so the index that is summed over runs in the
-// result's order: element 16 (2 s + j / 4) + 4 g + j % 4 in place j of lane group g of the 32-wide slab s (16-bit), which is how kt, wt, zt
-// and vt are stored; fp32 products take 4 at a time in natural order.
+// A wave has 16 rows; results stay in registers and are the next product's operand.  Bound by the fp32 matrix rate and, for few tiles, by the chain.
 #include "paged_decl.h"
 
 namespace path {
 
-template <typename T> __device__ __forceinline__ int slab_place(int i) {      // where index i of a summed axis is stored
-    return sizeof(T) == 2 ? (i & ~31) + 8 * ((i & 15) >> 2) + 4 * ((i >> 4) & 1) + (i & 3) : i;
-}
-
 constexpr int LDT = 68;      // row length of a 64 x 64 matrix in LDS
 template <int D> constexpr size_t chunk_smem() { return (size_t)(3 * 64 * (D + 4) + 3 * 64 * LDT + 64 + 256) * 4; }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
-    typedef typename Compute<T>::type CT;
     constexpr int LD = D + 4;
     extern __shared__ __attribute__((aligned(16))) float sm[];
     float* const W = sm;
@@ -50,11 +42,11 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
     if (q.m <= a.few_limit || c < 0 || m <= 0) return;
     const int tok0 = q.t0 + 64 * c;
 
-    const T* const kg = reinterpret_cast<const T*>(a.k);
-    const T* const vg = reinterpret_cast<const T*>(a.v);
-    const T* const wg = reinterpret_cast<const T*>(a.w);
-    const T* const qg = reinterpret_cast<const T*>(a.q);
-    auto stage = [&](float* dst, const T* src, int heads, int head) {
+    const float* const kg = reinterpret_cast<const float*>(a.k);
+    const float* const vg = reinterpret_cast<const float*>(a.v);
+    const float* const wg = reinterpret_cast<const float*>(a.w);
+    const float* const qg = reinterpret_cast<const float*>(a.q);
+    auto stage = [&](float* dst, const float* src, int heads, int head) {
         for (int i = tid; i < 64 * D / 4; i += 256) {
             const int t = i / (D / 4), e = (i % (D / 4)) * 4;
             float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -64,11 +56,11 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
     };
     stage(W, wg, a.H, h);
     stage(K, kg, a.H, h);
-    if (tid < 64) beta[tid] = tid < m ? (float)reinterpret_cast<const T*>(a.beta)[(long long)(tok0 + tid) * a.H + h] : 0.f;
+    if (tid < 64) beta[tid] = tid < m ? reinterpret_cast<const float*>(a.beta)[(long long)(tok0 + tid) * a.H + h] : 0.f;
     if (a.cpages) {      // gate sums: c of the last cached token, the earlier tiles' gates, then one by one
-        const T* const fg = reinterpret_cast<const T*>(a.log_f);
+        const float* const fg = reinterpret_cast<const float*>(a.log_f);
         float x = 0.f;
-        for (int t = tid; t < 64 * c; t += 256) x += (float)fg[(long long)(q.t0 + t) * a.H + h];
+        for (int t = tid; t < 64 * c; t += 256) x += fg[(long long)(q.t0 + t) * a.H + h];
         red[tid] = x;
         __syncthreads();
         if (wv == 0) {
@@ -76,7 +68,7 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
             for (int o = 32; o; o >>= 1) y += __shfl_xor(y, o);
             const long long r = q.n > 0 ? paged_row(a, s, h, q.n - 1) : -1;
             y += r >= 0 ? a.cpages[r] : 0.f;
-            float z = lane < m ? (float)fg[(long long)(tok0 + lane) * a.H + h] : 0.f;
+            float z = lane < m ? fg[(long long)(tok0 + lane) * a.H + h] : 0.f;
             for (int o = 1; o < 64; o <<= 1) { const float b = __shfl_up(z, o); if (lane >= o) z += b; }
             if (lane < m) a.crow[(long long)(tok0 + lane) * a.H + h] = y + z;
             if (a.append && lane < m) {
@@ -86,24 +78,23 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
         }
     }
     const size_t th = (size_t)tile * a.H + h;
-    CT* const kt = reinterpret_cast<CT*>(a.kt) + th * 64 * D;
-    CT* const wt = reinterpret_cast<CT*>(a.wt) + th * 64 * D;
-    CT* const zt = reinterpret_cast<CT*>(a.zt) + th * 64 * D;
-    T* const vt = reinterpret_cast<T*>(a.vt) + th * 64 * D;
+    float* const kt = reinterpret_cast<float*>(a.kt) + th * 64 * D;
+    float* const wt = reinterpret_cast<float*>(a.wt) + th * 64 * D;
+    float* const zt = reinterpret_cast<float*>(a.zt) + th * 64 * D;
+    float* const vt = reinterpret_cast<float*>(a.vt) + th * 64 * D;
     __syncthreads();
 
-    for (int i = tid; i < 64 * D; i += 256) wt[(i / D) * D + slab_place<CT>(i % D)] = (CT)W[(i / D) * LD + i % D];
+    for (int i = tid; i < 64 * D; i += 256) wt[(i / D) * D + (i % D)] = W[(i / D) * LD + i % D];
     if (a.attn)
         for (int i = tid; i < 64 * D; i += 256) {
             const int t = i / D, e = i % D;
-            vt[e * 64 + slab_place<T>(t)] = t < m ? vg[((long long)(tok0 + t) * a.H + h) * D + e] : (T)0.f;
+            vt[e * 64 + (t)] = t < m ? vg[((long long)(tok0 + t) * a.H + h) * D + e] : 0.f;
         }
     if (a.append)
         for (int i = tid; i < 64 * (D / 4); i += 256) {
             const int t = i / (D / 4), e = (i % (D / 4)) * 4;
             const long long r = t < m ? paged_row(a, s, h, q.n + 64 * c + t) : -1;
-            typedef T V4 __attribute__((ext_vector_type(4)));
-            if (r >= 0) *reinterpret_cast<V4*>(reinterpret_cast<T*>(a.vpages) + r * D + e) = *reinterpret_cast<const V4*>(vg + ((long long)(tok0 + t) * a.H + h) * D + e);
+            if (r >= 0) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.vpages) + r * D + e) = *reinterpret_cast<const f32x4*>(vg + ((long long)(tok0 + t) * a.H + h) * D + e);
         }
 
     const int rb = wv >> 1, cb = wv & 1;      // this wave's 32 x 32 block of a 64 x 64 matrix
@@ -173,7 +164,7 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
         f32x16 v = zero16();
         mm<float, 64, true, false>(v, W, LD, r0, B2, LDT, c0, l32, hh);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) zt[(r0 + acc_row(j, hh)) * 64 + slab_place<CT>(c0 + l32)] = (CT)-v[j];
+        for (int j = 0; j < 16; ++j) zt[(r0 + acc_row(j, hh)) * 64 + (c0 + l32)] = -v[j];
     }
     __syncthreads();
     for (int b = wv; b < D / 32 * 2; b += 4) {      // kt = K - (T D)^T W
@@ -183,7 +174,7 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const int r = r0 + acc_row(j, hh);
-            kt[r * D + slab_place<CT>(c0 + l32)] = (CT)(K[r * LD + c0 + l32] - v[j]);
+            kt[r * D + (c0 + l32)] = (K[r * LD + c0 + l32] - v[j]);
         }
     }
     if (!a.attn) return;
@@ -225,36 +216,7 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
 }
 
 // Products with 16 rows of results per wave whose right operand is packed from results.
-template <typename CT, int KD> struct SweepOperand;
-template <int KD> struct SweepOperand<half_t, KD> {
-    halfx8 f[KD / 32];
-    __device__ __forceinline__ void pack(const f32x4* x) {
-#pragma unroll
-        for (int s = 0; s < KD / 32; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[s][j] = (half_t)x[2 * s + (j >> 2)][j & 3];
-    }
-    __device__ __forceinline__ f32x4 left(const half_t* row, int g, f32x4 c) const {
-#pragma unroll
-        for (int s = 0; s < KD / 32; ++s) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const halfx8*>(row + 32 * s + 8 * g), f[s], c, 0, 0, 0);
-        return c;
-    }
-};
-template <int KD> struct SweepOperand<bf16_t, KD> {
-    bf16x8 f[KD / 32];
-    __device__ __forceinline__ void pack(const f32x4* x) {
-#pragma unroll
-        for (int s = 0; s < KD / 32; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[s][j] = (bf16_t)x[2 * s + (j >> 2)][j & 3];
-    }
-    __device__ __forceinline__ f32x4 left(const bf16_t* row, int g, f32x4 c) const {
-#pragma unroll
-        for (int s = 0; s < KD / 32; ++s) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(row + 32 * s + 8 * g), f[s], c, 0, 0, 0);
-        return c;
-    }
-};
-template <int KD> struct SweepOperand<float, KD> {
+template <int KD> struct SweepOperand {
     f32x4 f[KD / 16];
     __device__ __forceinline__ void pack(const f32x4* x) {
 #pragma unroll
@@ -271,9 +233,8 @@ template <int KD> struct SweepOperand<float, KD> {
     }
 };
 
-template <typename T, int D, bool SCAN>
+template <int D, bool SCAN>
 __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
-    typedef typename Compute<T>::type CT;
     constexpr int DT = D / 16;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, Hq = a.H * a.G;
     int s, h, hq = 0, tile, r0 = 0;
@@ -337,9 +298,9 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) { S[b][i] = __builtin_amdgcn_exp2f(S[b][i] - base); sum += S[b][i]; }
         l_run = l_run * f + sum;
-        SweepOperand<T, 64> P;
+        SweepOperand<64> P;
         P.pack(S);
-        const T* const vt = reinterpret_cast<const T*>(a.vt) + ((size_t)(first + j) * a.H + h) * 64 * D;
+        const float* const vt = reinterpret_cast<const float*>(a.vt) + ((size_t)(first + j) * a.H + h) * 64 * D;
 #pragma unroll
         for (int t = 0; t < DT; ++t) O[t] = P.left(vt + (16 * t + c) * 64, g, O[t] * f);
     };
@@ -352,10 +313,10 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
     }
     for (int j = ct - 1; j >= 0; --j) {
         const size_t th = ((size_t)(first + j) * a.H + h) * 64 * D;
-        const CT* const kt = reinterpret_cast<const CT*>(a.kt) + th;
-        const CT* const wt = reinterpret_cast<const CT*>(a.wt) + th;
-        const CT* const zt = reinterpret_cast<const CT*>(a.zt) + th;
-        SweepOperand<CT, D> X;
+        const float* const kt = reinterpret_cast<const float*>(a.kt) + th;
+        const float* const wt = reinterpret_cast<const float*>(a.wt) + th;
+        const float* const zt = reinterpret_cast<const float*>(a.zt) + th;
+        SweepOperand<D> X;
         X.pack(x);
         f32x4 S[4], Y[4];
 #pragma unroll
@@ -363,7 +324,7 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
             S[b] = X.left(kt + (16 * b + c) * D, g, f32x4{0.f, 0.f, 0.f, 0.f});
             Y[b] = X.left(wt + (16 * b + c) * D, g, f32x4{0.f, 0.f, 0.f, 0.f});
         }
-        SweepOperand<CT, 64> YB;
+        SweepOperand<64> YB;
         YB.pack(Y);
 #pragma unroll
         for (int t = 0; t < DT; ++t) x[t] = YB.left(zt + (16 * t + c) * 64, g, x[t]);
@@ -374,33 +335,31 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
                 for (int i = 0; i < 4; ++i) {
                     const int t = 64 * j + 16 * b + 4 * g + i;
                     const long long r = t < q.m ? paged_row(a, s, h, q.n + t) : -1;
-                    if (r >= 0) reinterpret_cast<T*>(a.kpages)[r * D + row] = (T)S[b][i];
+                    if (r >= 0) reinterpret_cast<float*>(a.kpages)[r * D + row] = S[b][i];
                 }
         } else {
             attend(j, S, false);
         }
     }
     if constexpr (SCAN) {
-        CT* const p = reinterpret_cast<CT*>(a.pt) + (((size_t)s * a.H + h) * D + row) * D;
-        typedef CT V4 __attribute__((ext_vector_type(4)));
+        float* const p = reinterpret_cast<float*>(a.pt) + (((size_t)s * a.H + h) * D + row) * D;
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
-            V4 v;
+            f32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (CT)(x[t][i] - (16 * t + 4 * g + i == row ? 1.f : 0.f));
-            *reinterpret_cast<V4*>(p + 16 * t + 4 * g) = v;
+            for (int i = 0; i < 4; ++i) v[i] = (x[t][i] - (16 * t + 4 * g + i == row ? 1.f : 0.f));
+            *reinterpret_cast<f32x4*>(p + 16 * t + 4 * g) = v;
         }
     } else {
         l_run = sum_rows(l_run);
         if (there && q.n == 0) {      // nothing cached: that was all
             const float inv = 1.f / l_run;
-            typedef T V4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-                V4 v;
+                f32x4 v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (T)(O[t][i] * inv);
-                *reinterpret_cast<V4*>(reinterpret_cast<T*>(a.o) + at * D + 16 * t + 4 * g) = v;
+                for (int i = 0; i < 4; ++i) v[i] = (O[t][i] * inv);
+                *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o) + at * D + 16 * t + 4 * g) = v;
             }
             if (g == 0) a.lse[at] = (m_run + __builtin_amdgcn_logf(l_run)) * LN2;
         } else if (there) {
@@ -414,32 +373,23 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
     }
 }
 
-template <typename T, int D>
+template <int D>
 static hipError_t launch_chunk_t(const PagedArgs& a, hipStream_t st) {
     constexpr size_t bytes = chunk_smem<D>();
     static_assert(bytes <= 160 * 1024, "LDS");
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_chunk_kernel<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_chunk_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((paged_chunk_kernel<T, D>), dim3((unsigned)(a.tiles * a.H)), dim3(256), bytes, st, a);
+    hipLaunchKernelGGL((paged_chunk_kernel<D>), dim3((unsigned)(a.tiles * a.H)), dim3(256), bytes, st, a);
     return hipGetLastError();
 }
-hipError_t launch_paged_chunk(const PagedArgs& a, int d, int is_bf16, hipStream_t st) {
-    if (is_bf16) return d == 64 ? launch_chunk_t<bf16_t, 64>(a, st) : launch_chunk_t<bf16_t, 128>(a, st);
-    return d == 64 ? launch_chunk_t<float, 64>(a, st) : launch_chunk_t<float, 128>(a, st);
-}
-template <typename T, int D, bool SCAN>
+hipError_t launch_paged_chunk(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_chunk_t<64>(a, st) : launch_chunk_t<128>(a, st); }
+template <int D, bool SCAN>
 static hipError_t launch_sweep_t(const PagedArgs& a, hipStream_t st) {
     const unsigned grid = SCAN ? (unsigned)(a.nseq * a.H * (D / 64)) : (unsigned)(a.tiles * a.H * a.G);
-    hipLaunchKernelGGL((paged_sweep_kernel<T, D, SCAN>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((paged_sweep_kernel<D, SCAN>), dim3(grid), dim3(256), 0, st, a);
     return hipGetLastError();
 }
-hipError_t launch_paged_sweep(const PagedArgs& a, int d, int is_bf16, hipStream_t st) {
-    if (is_bf16) return d == 64 ? launch_sweep_t<bf16_t, 64, false>(a, st) : launch_sweep_t<bf16_t, 128, false>(a, st);
-    return d == 64 ? launch_sweep_t<float, 64, false>(a, st) : launch_sweep_t<float, 128, false>(a, st);
-}
-hipError_t launch_paged_scan(const PagedArgs& a, int d, int is_bf16, hipStream_t st) {
-    if (is_bf16) return d == 64 ? launch_sweep_t<bf16_t, 64, true>(a, st) : launch_sweep_t<bf16_t, 128, true>(a, st);
-    return d == 64 ? launch_sweep_t<float, 64, true>(a, st) : launch_sweep_t<float, 128, true>(a, st);
-}
+hipError_t launch_paged_sweep(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_sweep_t<64, false>(a, st) : launch_sweep_t<128, false>(a, st); }
+hipError_t launch_paged_scan(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_sweep_t<64, true>(a, st) : launch_sweep_t<128, true>(a, st); }
 
 }  // namespace path

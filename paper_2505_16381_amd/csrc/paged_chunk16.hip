@@ -1,0 +1,586 @@
+// Chunks of new tokens for a paged cache, bf16: the triangular transform of tiles of 64 tokens, the queries' way through the tiles
+// to the chunk's start, and the keys' and the transitions' to its end.  (fp32, and what the quantities are: paged_chunk.hip.)
+//
+// Inputs are bf16 numbers and multiplied as they are.  What is computed from them -- T, T D, L, L T, Z, the carried keys, X and W X -- is
+// multiplied as a sum of two bf16 numbers, hi + lo (17 bits; products hi hi + hi lo + lo hi): one fp16 number each
+// leaves the log-sum-exp 2e-6 of itself off, through errors that all keys of a row share; so 1e-7, and with bf16's range.
+// On the matrix units that is little: these products are a small part of the call, and a chain of short steps.
+#include <type_traits>
+
+#include "lds_tile.h"
+#include "paged_decl.h"
+
+namespace path {
+
+constexpr int C16_THREADS = 512, C16_LT = 72, C16_LF = 68;      // row lengths in LDS: 64 x 64 pairs, 64 x 64 fp32
+template <int D> constexpr size_t chunk16_smem() { return (size_t)3 * 64 * (D + 8) * 2 + 2 * 64 * C16_LF * 4 + 4 * 2 * 64 * C16_LT * 2 + 64 * 4 + 256 * 4; }
+
+struct Pair { bf16_t *hi, *lo; };
+__device__ __forceinline__ void put_pair(const Pair& p, int i, float x) {
+    const bf16_t h = (bf16_t)x;
+    p.hi[i] = h;
+    p.lo[i] = (bf16_t)(x - (float)h);
+}
+template <int K, bool TA, bool TB>
+__device__ __forceinline__ void mm_pairs(f32x16& acc, const Pair& A, int lda, int ar, const Pair& B, int ldb, int br, int l32, int h) {
+    mm<bf16_t, K, TA, TB>(acc, A.hi, lda, ar, B.hi, ldb, br, l32, h);
+    mm<bf16_t, K, TA, TB>(acc, A.hi, lda, ar, B.lo, ldb, br, l32, h);
+    mm<bf16_t, K, TA, TB>(acc, A.lo, lda, ar, B.hi, ldb, br, l32, h);
+}
+
+// One workgroup per tile and key head; 32 x 32 blocks by the eight waves, two 64 x 64 matrices at a time or one of d x 64.
+template <int D>
+__global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs a) {
+    constexpr int LD = D + 8, LT = C16_LT, LF = C16_LF, NT = C16_THREADS;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    bf16_t* const W = reinterpret_cast<bf16_t*>(smem);
+    bf16_t* const K = W + 64 * LD;
+    bf16_t* const Q = K + 64 * LD;
+    float* const F1 = reinterpret_cast<float*>(Q + 64 * LD);      // N; then, with F2, the pair L T
+    float* const F2 = F1 + 64 * LF;                               // (I + N)^{-1}
+    bf16_t* const pairs = reinterpret_cast<bf16_t*>(F2 + 64 * LF);
+    const Pair Tp{pairs, pairs + 64 * LT}, Dt{pairs + 2 * 64 * LT, pairs + 3 * 64 * LT}, Lp{pairs + 4 * 64 * LT, pairs + 5 * 64 * LT},
+        Ut{pairs + 6 * 64 * LT, pairs + 7 * 64 * LT}, LTp{reinterpret_cast<bf16_t*>(F1), reinterpret_cast<bf16_t*>(F1) + 64 * LT};
+    static_assert(2 * 64 * LT * 2 <= 2 * 64 * LF * 4, "L T fits where N and its inverse were");
+    float* const beta = reinterpret_cast<float*>(pairs + 8 * 64 * LT);
+    float* const red = beta + 64;
+
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
+    const int tile = blockIdx.x % a.tiles, h = blockIdx.x / a.tiles, Hq = a.H * a.G;
+    int s = 0;
+    for (int i = 0; i < a.nseq; i += 64) s += __popcll(__ballot(i + lane < a.nseq && first_tile(a, min(i + lane, a.nseq - 1)) <= tile));
+    s = __builtin_amdgcn_readfirstlane(max(0, s - 1));
+    const PagedSeq q = paged_seq(a, s);
+    const int c = tile - first_tile(a, s), m = q.m - 64 * c;
+    if (q.m <= a.few_limit || c < 0 || m <= 0) return;
+    const int tok0 = q.t0 + 64 * c;
+
+    const bf16_t* const vg = reinterpret_cast<const bf16_t*>(a.v);
+    auto stage = [&](bf16_t* dst, const void* src, int heads, int head) {
+        const bf16_t* const p = reinterpret_cast<const bf16_t*>(src);
+#pragma unroll
+        for (int i0 = 0; i0 < 64 * D / 8; i0 += NT) {
+            const int i = i0 + tid, t = i / (D / 8), e = (i % (D / 8)) * 8;
+            u32x4 x = {0, 0, 0, 0};
+            if (t < m) x = *reinterpret_cast<const u32x4*>(p + ((long long)(tok0 + t) * heads + head) * D + e);
+            *reinterpret_cast<u32x4*>(dst + t * LD + e) = x;
+        }
+    };
+    stage(W, a.w, a.H, h);
+    stage(K, a.k, a.H, h);
+    if (a.attn) stage(Q, a.q, Hq, h * a.G);
+    if (tid < 64) beta[tid] = tid < m ? (float)reinterpret_cast<const bf16_t*>(a.beta)[(long long)(tok0 + tid) * a.H + h] : 0.f;
+    if (a.cpages) {      // gate sums: c of the last cached token, the earlier tiles' gates, then one by one
+        const bf16_t* const fg = reinterpret_cast<const bf16_t*>(a.log_f);
+        if (tid < 256) {
+            float x = 0.f;
+            for (int t = tid; t < 64 * c; t += 256) x += (float)fg[(long long)(q.t0 + t) * a.H + h];
+            red[tid] = x;
+        }
+        __syncthreads();
+        if (wv == 0) {
+            float y = red[lane] + red[64 + lane] + red[128 + lane] + red[192 + lane];
+            for (int o = 32; o; o >>= 1) y += __shfl_xor(y, o);
+            const long long r = q.n > 0 ? paged_row(a, s, h, q.n - 1) : -1;
+            y += r >= 0 ? a.cpages[r] : 0.f;
+            float z = lane < m ? (float)fg[(long long)(tok0 + lane) * a.H + h] : 0.f;
+            for (int o = 1; o < 64; o <<= 1) { const float b = __shfl_up(z, o); if (lane >= o) z += b; }
+            if (lane < m) a.crow[(long long)(tok0 + lane) * a.H + h] = y + z;
+            if (a.append && lane < m) {
+                const long long w = paged_row(a, s, h, q.n + 64 * c + lane);
+                if (w >= 0) a.cpages[w] = y + z;
+            }
+        }
+    }
+    if (a.append)
+        for (int i = tid; i < 64 * (D / 8); i += NT) {
+            const int t = i / (D / 8), e = (i % (D / 8)) * 8;
+            const long long r = t < m ? paged_row(a, s, h, q.n + 64 * c + t) : -1;
+            if (r >= 0) *reinterpret_cast<u32x4*>(reinterpret_cast<bf16_t*>(a.vpages) + r * D + e) = *reinterpret_cast<const u32x4*>(vg + ((long long)(tok0 + t) * a.H + h) * D + e);
+        }
+    const size_t th = ((size_t)tile * a.H + h) * 64 * D;
+    const size_t lo = (size_t)a.tiles * a.H * 64 * D;      // kt, zt: all hi tiles, then all lo tiles
+    bf16_t* const kt = reinterpret_cast<bf16_t*>(a.kt) + th;
+    bf16_t* const zt = reinterpret_cast<bf16_t*>(a.zt) + th;
+    __syncthreads();
+
+    const bool first = wv < 4;                            // which of two 64 x 64 matrices
+    const int rb = (wv >> 1) & 1, cb = wv & 1;
+    auto each = [&](const f32x16& v, auto f) {            // f(row, column, value) of this wave's block of a 64 x 64 matrix
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f(32 * rb + acc_row(j, hh), 32 * cb + l32, v[j]);
+    };
+    auto lower = [&]() {                                  // L = lower(Q W^T)
+        f32x16 v = zero16();
+        mm<bf16_t, D, false, false>(v, Q, LD, 32 * rb, W, LD, 32 * cb, l32, hh);
+        each(v, [&](int r, int k, float x) { put_pair(Lp, r * LT + k, k <= r ? x : 0.f); });
+    };
+    {   // N = diag(beta) strictLower(W W^T); D^T = strictUpper(K W^T)
+        f32x16 v = zero16();
+        mm<bf16_t, D, false, false>(v, first ? W : K, LD, 32 * rb, W, LD, 32 * cb, l32, hh);
+        if (first) each(v, [&](int r, int k, float x) { F1[r * LF + k] = k < r ? beta[r] * x : 0.f; F2[r * LF + k] = 0.f; });
+        else each(v, [&](int r, int k, float x) { put_pair(Dt, r * LT + k, k > r ? x : 0.f); });
+    }
+    __syncthreads();
+    // (I + N)^{-1}: the 16 x 16 blocks on the diagonal by substitution, a column per thread
+    if (wv == 0) {
+        const int b = lane & ~15, j = lane & 15;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float y = i == j ? 1.f : 0.f;
+#pragma unroll
+            for (int t = 0; t < i; ++t) y -= F1[(b + i) * LF + b + t] * x[t];
+            x[i] = y;
+            F2[(b + i) * LF + b + j] = y;
+        }
+    } else if (!first && a.attn) lower();
+    __syncthreads();
+    // ... then twice the lower left quarter, -T22 (N21 T11), by 16 x 16 blocks; a product's result is the next one's right operand as it stands
+    const int g = lane >> 4, c16 = lane & 15;
+    auto quarter = [&](auto half, int b, int rq, int cq) {
+        constexpr int HB = decltype(half)::value, NB = HB / 16;
+        f32x4 tmp[NB];
+#pragma unroll
+        for (int r = 0; r < NB; ++r) {
+            tmp[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < HB; k += 4)
+                tmp[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(F1[(b + HB + 16 * r + c16) * LF + b + k + g], F2[(b + k + g) * LF + b + 16 * cq + c16], tmp[r], 0, 0, 0);
+        }
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < NB; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                y = __builtin_amdgcn_mfma_f32_16x16x4f32(F2[(b + HB + 16 * rq + c16) * LF + b + HB + 16 * r + 4 * g + i], tmp[r][i], y, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) F2[(b + HB + 16 * rq + 4 * g + i) * LF + b + 16 * cq + c16] = -y[i];
+    };
+    if (wv < 2) quarter(std::integral_constant<int, 16>(), 32 * wv, 0, 0);
+    __syncthreads();
+    if (wv < 4) quarter(std::integral_constant<int, 32>(), 0, wv >> 1, wv & 1);
+    __syncthreads();
+    for (int i = tid; i < 64 * 64; i += NT) put_pair(Tp, (i >> 6) * LT + (i & 63), F2[(i >> 6) * LF + (i & 63)] * beta[i & 63]);      // T
+    __syncthreads();
+    if (first) {   // (T D)^T
+        f32x16 v = zero16();
+        mm_pairs<64, false, false>(v, Dt, LT, 32 * rb, Tp, LT, 32 * cb, l32, hh);
+        each(v, [&](int r, int k, float x) { put_pair(Ut, r * LT + k, x); });
+    }
+    typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+    auto turned_product = [&](int b, const Pair& B, auto f) {      // block b of W^T B^T: f(row of B, first of 4 d, values)
+        const int r0 = 32 * (b >> 1), c0 = 32 * (b & 1);
+        f32x16 v = zero16();
+        mm<bf16_t, 64, true, false>(v, W, LD, r0, B.hi, LT, c0, l32, hh);
+        mm<bf16_t, 64, true, false>(v, W, LD, r0, B.lo, LT, c0, l32, hh);
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) f(c0 + l32, r0 + acc_row(j, hh), f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]});
+    };
+    auto store_pair = [&](bf16_t* p, int i, f32x4 v) {
+        V4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = (bf16_t)v[e]; y[e] = (bf16_t)(v[e] - (float)x[e]); }
+        *reinterpret_cast<V4*>(p + i) = x;
+        *reinterpret_cast<V4*>(p + lo + i) = y;
+    };
+    if (!first)      // -Z = -T W
+        for (int b = wv - 4; b < D / 16; b += 4) turned_product(b, Tp, [&](int t, int d, f32x4 v) { store_pair(zt, t * D + d, -v); });
+    __syncthreads();
+    for (int b = wv; b < D / 16; b += 8)      // carried keys K - (T D)^T W
+        turned_product(b, Ut, [&](int t, int d, f32x4 v) {
+            const V4 k = *reinterpret_cast<const V4*>(K + t * LD + d);
+            store_pair(kt, t * D + d, f32x4{(float)k[0], (float)k[1], (float)k[2], (float)k[3]} - v);
+        });
+    if (!a.attn) return;
+    for (int gq = 0; gq < a.G; ++gq) {
+        const int hq = h * a.G + gq;
+        if (gq > 0) {
+            __syncthreads();
+            stage(Q, a.q, Hq, hq);
+            __syncthreads();
+            if (first) lower();
+            __syncthreads();
+        }
+        if (first) {      // logits, transposed: K Q^T - (T D)^T L^T
+            f32x16 v = zero16(), u = zero16();
+            mm<bf16_t, D, false, false>(v, K, LD, 32 * rb, Q, LD, 32 * cb, l32, hh);
+            mm_pairs<64, false, false>(u, Ut, LT, 32 * rb, Lp, LT, 32 * cb, l32, hh);
+            float* const sd = a.sd + ((size_t)tile * Hq + hq) * 4096 + (32 * cb + l32) * 64 + 32 * rb;
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<f32x4*>(sd + acc_row(j, hh)) = f32x4{v[j] - u[j], v[j + 1] - u[j + 1], v[j + 2] - u[j + 2], v[j + 3] - u[j + 3]};
+        } else {          // L T
+            f32x16 v = zero16();
+            mm_pairs<64, false, true>(v, Lp, LT, 32 * rb, Tp, LT, 32 * cb, l32, hh);
+            each(v, [&](int r, int k, float x) { put_pair(LTp, r * LT + k, x); });
+        }
+        __syncthreads();
+        for (int b = wv; b < D / 16; b += 8)      // X = Q - (L T) W
+            turned_product(b, LTp, [&](int t, int d, f32x4 v) {
+                if (t >= m) return;
+                const V4 k = *reinterpret_cast<const V4*>(Q + t * LD + d);
+                *reinterpret_cast<f32x4*>(a.x + ((long long)(tok0 + t) * Hq + hq) * D + d) = f32x4{(float)k[0], (float)k[1], (float)k[2], (float)k[3]} - v;
+            });
+    }
+}
+
+// ---- the way through the tiles ----
+//
+// 64 rows per workgroup, 16 per wave, and two waves for each 16 rows, which share a step's work:
+//     wave a   S = kt X^T (64 tokens x 16 rows), softmax, O^T += V^T P^T        scan: S are rows of keys, stored
+//     wave b   Y = W X^T, X^T -= Z^T Y, and X as operands to LDS for wave a's next step
+// The tile's operands come to LDS in two sets, each while the other is worked on: carried keys (hi, lo) and W; -Z (hi, lo) and V.
+// Bound by LDS (3.5 thousand cycles a step at 128 bytes a cycle) and, with few tiles, by the steps' chain; one wave for both halves,
+// alone on its SIMD, took 4.2 us a step.
+// The first workgroups are those of the append's scan, whose way is the longest: rows of the identity, of which S are rows of the
+// keys carried to the chunk's end, and what is left of X the rows of H_{m-1} .. H_0.
+// Row r = 4 g + i of X^T's block t is element 32 (t / 2) + 8 g + 4 (t % 2) + i, so that as an operand a lane holds eight elements in a row,
+// as it reads them of the keys and of W.
+constexpr int S16_THREADS = 512;
+template <int D> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)4 * (D / 32) * 2 * 64 * 16; }
+
+// Fragments (16 d x 32 tokens) of a tile's transpose for four blocks of 16 d, by eight reads of rows 32 u + 4 g + 0..3 and 16 further on: a is
+// the lane's address for the first two blocks (eight bytes apart), b for the others.  The waits are in the block.
+template <int OFF, int ROWB>
+__device__ __forceinline__ void turned_tr(unsigned a, unsigned b, bf16x8 (&f)[4]) {
+    union U { unsigned long long v[2]; bf16x8 f; } u[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %1, %8 offset:%11\n\t"
+                 "ds_read_b64_tr_b16 %2, %8 offset:%10+8\n\tds_read_b64_tr_b16 %3, %8 offset:%11+8\n\t"
+                 "ds_read_b64_tr_b16 %4, %9 offset:%10\n\tds_read_b64_tr_b16 %5, %9 offset:%11\n\t"
+                 "ds_read_b64_tr_b16 %6, %9 offset:%10+8\n\tds_read_b64_tr_b16 %7, %9 offset:%11+8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1])
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB) : "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = u[k].f;
+}
+// The same of a pair of tiles, one behind the other.
+template <int OFF, int ROWB>
+__device__ __forceinline__ void turned_tr_pair(unsigned a, unsigned b, bf16x8 (&f)[4], bf16x8 (&l)[4]) {
+    constexpr int T = 64 * ROWB;
+    union U { unsigned long long v[2]; bf16x8 f; } u[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%18\n\tds_read_b64_tr_b16 %1, %16 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %2, %16 offset:%18+8\n\tds_read_b64_tr_b16 %3, %16 offset:%19+8\n\t"
+                 "ds_read_b64_tr_b16 %4, %17 offset:%18\n\tds_read_b64_tr_b16 %5, %17 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %6, %17 offset:%18+8\n\tds_read_b64_tr_b16 %7, %17 offset:%19+8\n\t"
+                 "ds_read_b64_tr_b16 %8, %16 offset:%20\n\tds_read_b64_tr_b16 %9, %16 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %10, %16 offset:%20+8\n\tds_read_b64_tr_b16 %11, %16 offset:%21+8\n\t"
+                 "ds_read_b64_tr_b16 %12, %17 offset:%20\n\tds_read_b64_tr_b16 %13, %17 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %14, %17 offset:%20+8\n\tds_read_b64_tr_b16 %15, %17 offset:%21+8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1]),
+                   "=&v"(u[4].v[0]), "=&v"(u[4].v[1]), "=&v"(u[5].v[0]), "=&v"(u[5].v[1]), "=&v"(u[6].v[0]), "=&v"(u[6].v[1]), "=&v"(u[7].v[0]), "=&v"(u[7].v[1])
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + T), "n"(OFF + T + 16 * ROWB) : "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { f[k] = u[k].f; l[k] = u[4 + k].f; }
+}
+// Results (16 (2 s + j / 4) + 4 g + j % 4 in place j of slab s) as operands
+template <int N> __device__ __forceinline__ void pack_pairs(const f32x4* x, bf16x8* hi, bf16x8* lo) {
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float v = x[2 * s + (j >> 2)][j & 3];
+            hi[s][j] = (bf16_t)v;
+            lo[s][j] = (bf16_t)(v - (float)hi[s][j]);
+        }
+}
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+template <int D, bool SCAN>
+__device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem, int s, int h, int hq, int ct, int r0) {
+    typedef TurnedTile<D> L;
+    constexpr int ROWB = D * 2, TILE = 64 * ROWB, DT = D / 16, DS = D / 32, PPR = D / 8, RPI = 64 / PPR, GI = 8 / RPI;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, Hq = a.H * a.G;
+    const int rw = wv & 3;                  // its 16 rows
+    const bool carries = wv >= 4;           // wave b
+    const PagedSeq q = paged_seq(a, s);
+    const int first = first_tile(a, s), row = r0 + 16 * rw + c;
+    const int tok = SCAN ? 0 : q.t0 + 64 * ct + row;
+    const bool there = SCAN || 64 * ct + row < q.m;
+    const long long at = (long long)tok * Hq + hq;
+    const size_t lo = (size_t)a.tiles * a.H * 64 * D;
+    const bf16_t* const kt = reinterpret_cast<const bf16_t*>(a.kt);
+    const bf16_t* const zt = reinterpret_cast<const bf16_t*>(a.zt);
+    bf16x8* const sx = reinterpret_cast<bf16x8*>(smem + 6 * TILE) + rw * DS * 2 * 64 + lane;      // X of the 16 rows: [slab][hi, lo][lane]
+
+    // copies: wave w brings rows 8 w .. + 7 of each tile, a row's pieces exchanged by its turn; rows of w and v past the last token: that token's
+    const int q4 = lane / PPR;
+    auto copy = [&](int slot, const bf16_t* src, long long stride, int last) {
+#pragma unroll
+        for (int i = 0; i < GI; ++i) {
+            const int r = 8 * wv + i * RPI + q4;
+            const bf16_t* const p = src + min(r, last) * stride + ((lane % PPR) ^ L::turn(r)) * 8;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                             (__attribute__((address_space(3))) void*)(smem + slot * TILE + (8 * wv + i * RPI) * ROWB), 16, 0, 0);
+        }
+    };
+    auto tile_at = [&](int j) { return ((size_t)(first + j) * a.H + h) * 64 * D; };
+    auto user = [&](const void* p, int j) { return reinterpret_cast<const bf16_t*>(p) + ((long long)(q.t0 + 64 * j) * a.H + h) * D; };
+    auto bring0 = [&](int j) {
+        copy(0, kt + tile_at(j), D, 63);
+        copy(1, kt + lo + tile_at(j), D, 63);
+        copy(2, user(a.w, j), (long long)a.H * D, q.m - 64 * j - 1);
+    };
+    auto bring1 = [&](int j) {
+        copy(3, zt + tile_at(j), D, 63);
+        copy(4, zt + lo + tile_at(j), D, 63);
+        if (!SCAN) copy(5, user(a.v, j), (long long)a.H * D, q.m - 64 * j - 1);
+    };
+    if (!SCAN) copy(5, user(a.v, ct), (long long)a.H * D, q.m - 64 * ct - 1);
+    else bring1(ct - 1);
+    if (ct > 0) bring0(ct - 1);
+
+    const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const unsigned tr = base + 3 * TILE + L::at(4 * g + (c >> 2), 8 * (c & 3)) * 2;      // of set 1; d block t: exclusive or 64 (t / 2), plus 8 (t % 2)
+    const unsigned nat = L::at(c, 8 * g) * 2;                                            // of a tile; d slab s: exclusive or 64 s
+    auto frag = [&](int slot, int b, int sl) { return *reinterpret_cast<const bf16x8*>(smem + slot * TILE + b * 16 * ROWB + (nat ^ (64 * sl))); };
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    if (!carries) {
+        f32x4 O[SCAN ? 1 : DT], S[4];
+        float m_run = -INFINITY, l_run = 0.f, cq = 0.f;
+        const float sl2 = a.scale * LOG2E;
+        bf16x8 P[2];
+        auto softmax = [&](int j, bool own) {
+            float top = -INFINITY, ck[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ck[i] = 0.f;
+            if (a.cpages) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ck[i] = a.crow[(long long)min(q.t0 + 64 * j + 16 * (i >> 2) + 4 * g + (i & 3), a.T - 1) * a.H + h];
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y = S[b][i] * sl2 + (cq - ck[4 * b + i]) * LOG2E;      // (no gates: both are zero)
+                    if (own) y = 16 * b + 4 * g + i <= row ? y : -INFINITY;
+                    S[b][i] = y;
+                    top = fmaxf(top, y);
+                }
+            const float now = fmaxf(m_run, max_rows(top)), ref = now == -INFINITY ? 0.f : now, f = __builtin_amdgcn_exp2f(m_run - ref);
+            m_run = now;
+            float sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { S[b][i] = __builtin_amdgcn_exp2f(S[b][i] - ref); sum += S[b][i]; }
+            l_run = l_run * f + sum;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) O[t] *= f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) P[u][k] = (bf16_t)S[2 * u + (k >> 2)][k & 3];
+        };
+        auto values = [&]() {
+#pragma unroll
+            for (int t = 0; t < DT; t += 4) {      // four blocks at a time, none waiting for its own last product
+                bf16x8 v[4];
+                turned_tr<2 * TILE, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[0], O[t + k]);
+                turned_tr<2 * TILE + 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[1], O[t + k]);
+            }
+        };
+        long long place[4];      // SCAN: where this lane's key of each block goes
+        auto places = [&](int j) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int t = 64 * j + 16 * b + c;
+                place[b] = t < q.m ? paged_row(a, s, h, q.n + t) : -1;
+            }
+        };
+        if constexpr (SCAN) {
+            places(ct - 1);
+            wait_async_and_sync();
+            lds_barrier();
+        } else {      // the tile's own logits are there
+#pragma unroll
+            for (int t = 0; t < DT; ++t) O[t] = zero;
+            if (a.cpages && there) cq = a.crow[(long long)tok * a.H + h];
+            const float* const sd = a.sd + ((size_t)(first + ct) * Hq + hq) * 4096 + row * 64;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) S[b] = *reinterpret_cast<const f32x4*>(sd + 16 * b + 4 * g);
+            softmax(ct, true);
+            wait_async_and_sync();
+            values();
+            lds_barrier();
+            if (ct > 0) bring1(ct - 1);
+        }
+        for (int j = ct - 1; j >= 0; --j) {
+            // set 0 and X are there
+#pragma unroll
+            for (int b = 0; b < 4; ++b) S[b] = zero;
+#pragma unroll
+            for (int sl = 0; sl < DS; ++sl) {
+                const bf16x8 xh = sx[(2 * sl) * 64], xl = sx[(2 * sl + 1) * 64];
+                bf16x8 kh[4], kl[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) { kh[b] = frag(0, b, sl); kl[b] = frag(1, b, sl); }
+                // (scan: transposed, a lane has four consecutive elements of a key)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xh, kh[b], S[b]) : mfma32(kh[b], xh, S[b]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xl, kh[b], S[b]) : mfma32(kh[b], xl, S[b]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xh, kl[b], S[b]) : mfma32(kl[b], xh, S[b]);
+            }
+            wait_async_and_sync();      // set 1 is there, set 0 and X are free
+            if (j > 0) bring0(j - 1);
+            if constexpr (SCAN) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    bf16x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)S[b][i];
+                    if (place[b] >= 0) *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.kpages) + place[b] * D + r0 + 16 * rw + 4 * g) = v;
+                }
+                if (j > 0) places(j - 1);
+            }
+            if constexpr (!SCAN) {
+                softmax(j, false);
+                values();
+            }
+            wait_async_and_sync();      // set 0 and X are there, set 1 is free
+            if (j > 0) bring1(j - 1);
+        }
+        if constexpr (!SCAN) {
+            l_run = sum_rows(l_run);
+            if (there && q.n == 0) {      // nothing cached: that was all
+                const float inv = 1.f / l_run;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    bf16x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(O[t][i] * inv);
+                    *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.o) + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = v;
+                }
+                if (g == 0) a.lse[at] = (m_run + __builtin_amdgcn_logf(l_run)) * LN2;
+            } else if (there) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.many_o + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = O[t];
+                if (g == 0) { a.many_ml[2 * at] = m_run; a.many_ml[2 * at + 1] = l_run; }
+            }
+        }
+    } else {
+        f32x4 x[DT], Y[4];
+        bf16x8 xh[DS], xl[DS], yh[2], yl[2];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            x[t] = zero;
+            if constexpr (SCAN) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[t][i] = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + i == row ? 1.f : 0.f;
+            } else if (there) {
+                x[t] = *reinterpret_cast<const f32x4*>(a.x + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1));
+            }
+        }
+        auto hand_over = [&]() {
+            pack_pairs<DS>(x, xh, xl);
+#pragma unroll
+            for (int sl = 0; sl < DS; ++sl) { sx[(2 * sl) * 64] = xh[sl]; sx[(2 * sl + 1) * 64] = xl[sl]; }
+        };
+        if (ct > 0) hand_over();
+        wait_async_and_sync();
+        lds_barrier();
+        if (!SCAN && ct > 0) bring1(ct - 1);
+        for (int j = ct - 1; j >= 0; --j) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) Y[b] = zero;
+#pragma unroll
+            for (int sl = 0; sl < DS; ++sl)
+            {
+                bf16x8 w[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) w[b] = frag(2, b, sl);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) Y[b] = mfma32(w[b], xh[sl], Y[b]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) Y[b] = mfma32(w[b], xl[sl], Y[b]);
+            }
+            pack_pairs<2>(Y, yh, yl);
+            wait_async_and_sync();
+            if (j > 0) bring0(j - 1);
+            auto carry = [&](int t, auto ut) {
+                constexpr int u = decltype(ut)::value;
+                bf16x8 zh[4], zl[4];
+                turned_tr_pair<u * 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), zh, zl);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zh[k], yh[u], x[t + k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zh[k], yl[u], x[t + k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zl[k], yh[u], x[t + k]);
+            };
+#pragma unroll
+            for (int t = 0; t < DT; t += 4) {
+                carry(t, std::integral_constant<int, 0>());
+                carry(t, std::integral_constant<int, 1>());
+            }
+            if (j > 0) hand_over();
+            wait_async_and_sync();
+            if (j > 0) bring1(j - 1);
+        }
+        if constexpr (SCAN) {
+            half_t* const p = reinterpret_cast<half_t*>(a.pt) + (((size_t)s * a.H + h) * D + row) * D;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1);
+                halfx4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (half_t)(x[t][i] - (d + i == row ? 1.f : 0.f));
+                *reinterpret_cast<halfx4*>(p + d) = v;
+            }
+        } else if (there && q.n > 0) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.x + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = x[t];
+        }
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(S16_THREADS, 1) void paged_sweep16_kernel(PagedArgs a) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, Hq = a.H * a.G, scans = a.append ? a.nseq * a.H * (D / 64) : 0;
+    int x = blockIdx.x;
+    if (x < scans) {
+        const int r0 = 64 * (x % (D / 64)); x /= D / 64;
+        const int s = x / a.H, m = paged_seq(a, s).m;
+        if (m <= a.few_limit) return;
+        sweep16<D, true>(a, smem, s, x % a.H, 0, (m + 63) >> 6, r0);
+        return;
+    }
+    x -= scans;
+    const int tile = a.tiles - 1 - x / Hq, hq = x % Hq;      // (the last tiles have the longest way)
+    int s = 0;
+    for (int i = 0; i < a.nseq; i += 64) s += __popcll(__ballot(i + lane < a.nseq && first_tile(a, min(i + lane, a.nseq - 1)) <= tile));
+    s = __builtin_amdgcn_readfirstlane(max(0, s - 1));
+    const int m = paged_seq(a, s).m, ct = tile - first_tile(a, s);
+    if (m <= a.few_limit || ct < 0 || 64 * ct >= m) return;
+    sweep16<D, false>(a, smem, s, hq / a.G, hq, __builtin_amdgcn_readfirstlane(ct), 0);
+}
+
+template <int D>
+static hipError_t launch_chunk16_t(const PagedArgs& a, hipStream_t st) {
+    constexpr size_t bytes = chunk16_smem<D>();
+    static_assert(bytes <= 160 * 1024, "LDS");
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_chunk16_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((paged_chunk16_kernel<D>), dim3((unsigned)(a.tiles * a.H)), dim3(C16_THREADS), bytes, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_paged_chunk16(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_chunk16_t<64>(a, st) : launch_chunk16_t<128>(a, st); }
+template <int D>
+static hipError_t launch_sweep16_t(const PagedArgs& a, hipStream_t st) {
+    constexpr size_t bytes = sweep16_smem<D>();
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_sweep16_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (attr != hipSuccess) return attr;
+    const unsigned grid = (unsigned)((a.append ? a.nseq * a.H * (D / 64) : 0) + (a.attn ? a.tiles * a.H * a.G : 0));
+    hipLaunchKernelGGL((paged_sweep16_kernel<D>), dim3(grid), dim3(S16_THREADS), bytes, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_paged_sweep16(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_sweep16_t<64>(a, st) : launch_sweep16_t<128>(a, st); }
+
+}  // namespace path

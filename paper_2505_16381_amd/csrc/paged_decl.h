@@ -11,8 +11,8 @@
 //
 // A sequence goes one of two ways, by its own number of new tokens (few_limit).  Few: every workgroup forms X and Z itself by
 // walking the tokens' transitions (paged_rows.hip), and one pass over the cache does the attention, the append or both.  More:
-// tiles of 64 new tokens (paged_chunk.hip) leave X, the attention among the new tokens and H_{m-1} .. H_0; then the cache
-// is attended to (paged_attn.hip, paged_rows.hip) and carried on (paged_refresh.hip).
+// tiles of 64 new tokens (paged_chunk16.hip, fp32 paged_chunk.hip) leave X, the attention among the new tokens and H_{m-1} .. H_0;
+// then the cache is attended to (paged_attn.hip, fp32 paged_rows.hip) and carried on (paged_refresh.hip).
 #pragma once
 #include "path_common.h"
 
@@ -41,9 +41,9 @@ struct PagedArgs {
     int joined;                                    // the attention kernel joins a single piece with record 0 itself
     float *x, *crow;                               // [T][H*G][d] X; [T][H] c of the new tokens (gates)
     float *many_o, *many_ml;                       // [1 + split][T * H * G][d], [..][2]; record 0: the new tokens' own
-    void *kt, *wt, *zt, *vt;                       // [tiles][H]: operand tiles of the new tokens, see paged_chunk.hip
+    void *kt, *wt, *zt, *vt;                       // [tiles][H]: operand tiles of the new tokens, see paged_chunk.hip (bf16: kt, zt only, [hi, lo][tiles][H])
     float* sd;                                     // [tiles][H*G][64][64] logits inside a tile
-    void* pt;                                      // [nseq][H][d][d]: W^T Z of all new tokens
+    void* pt;                                      // [nseq][H][d][d]: H_{m-1} .. H_0 - I of all new tokens (fp32, fp16)
 };
 
 struct PagedSeq { int n, t0, m; };
@@ -123,13 +123,15 @@ template <int E, typename T> __device__ __forceinline__ void load_f32(const T* p
 }
 
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int is_bf16, hipStream_t st);       // few new tokens: everything; d = 64, 128
-hipError_t launch_paged_rows_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st);  // X rows from the workspace
+hipError_t launch_paged_rows_many(const PagedArgs& a, int d, hipStream_t st);               // X rows from the workspace, fp32
 hipError_t launch_paged_attn(const PagedArgs& a, int d, hipStream_t st);                    // the same, bf16
 hipError_t launch_paged_merge_few(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
 hipError_t launch_paged_merge_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
-hipError_t launch_paged_chunk(const PagedArgs& a, int d, int is_bf16, hipStream_t st);      // tiles of the new tokens
-hipError_t launch_paged_sweep(const PagedArgs& a, int d, int is_bf16, hipStream_t st);      // attention among the new tokens, X
-hipError_t launch_paged_scan(const PagedArgs& a, int d, int is_bf16, hipStream_t st);       // the new keys, W^T Z of all tokens
-hipError_t launch_paged_refresh(const PagedArgs& a, int d, int is_bf16, hipStream_t st);    // cached keys <- (I - W^T Z) keys
+hipError_t launch_paged_chunk(const PagedArgs& a, int d, hipStream_t st);                   // tiles of the new tokens, fp32
+hipError_t launch_paged_sweep(const PagedArgs& a, int d, hipStream_t st);                   // attention among the new tokens, X
+hipError_t launch_paged_scan(const PagedArgs& a, int d, hipStream_t st);                    // the new keys, H_{m-1} .. H_0
+hipError_t launch_paged_chunk16(const PagedArgs& a, int d, hipStream_t st);                 // bf16: the tiles
+hipError_t launch_paged_sweep16(const PagedArgs& a, int d, hipStream_t st);                 // sweep and scan in one launch
+hipError_t launch_paged_refresh(const PagedArgs& a, int d, int is_bf16, hipStream_t st);    // cached keys <- H_{m-1} .. H_0 keys
 
 }  // namespace path

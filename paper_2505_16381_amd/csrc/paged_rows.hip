@@ -19,10 +19,10 @@ namespace path {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 
-template <typename T, int D> struct RowsCfg {
+template <typename T, int D, int NRT, bool BOTH> struct RowsCfg {
     static constexpr int ES = sizeof(T), ROWB = D * ES;
     static constexpr int KR = ROWB / 64;                 // 16-byte registers of 16 rows per lane
-    static constexpr int U = ES == 2 ? 2 : 1;            // groups of 16 tokens per step
+    static constexpr int U = ES == 2 && !(D == 128 && (NRT == 4 || BOTH)) ? 2 : 1;      // groups of 16 tokens per step: what 256 registers hold two steps of
     static constexpr int PPR = ROWB / 16;                // 16-byte pieces per row
     static constexpr int VBYTES = 4 * U * 16 * ROWB;     // value tiles of the four waves
     static constexpr int LDX = D + 4;
@@ -31,10 +31,10 @@ template <typename T, int D> struct RowsCfg {
         if (ES == 2) return r * PPR + (cp ^ (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)));
         return r * PPR + (cp ^ (((r >> 2) & 3) * 4));
     }
-    static constexpr size_t floats_before(int NRT, bool append) { return (size_t)16 * D + (size_t)16 * NRT * LDX + (append ? 16 * LDX : 0) + 16 * NRT * 17 + 32 + 16 * NRT * 2; }
-    static constexpr size_t merge_bytes(int NRT) { return (size_t)2 * (NRT * (D / 16) * 1024 + NRT * 512); }
-    static constexpr size_t smem(int NRT, bool append) {
-        const size_t f = (floats_before(NRT, append) * 4 + 255) / 256 * 256, a = VBYTES, b = merge_bytes(NRT), c = 16 * D * 4;
+    static constexpr size_t floats_before(bool append) { return (size_t)16 * D + (size_t)16 * NRT * LDX + (append ? 16 * LDX : 0) + 16 * NRT * 17 + 32 + 16 * NRT * 2; }
+    static constexpr size_t merge_bytes() { return (size_t)2 * (NRT * (D / 16) * 1024 + NRT * 512); }
+    static constexpr size_t smem(bool append) {
+        const size_t f = (floats_before(append) * 4 + 255) / 256 * 256, a = VBYTES, b = merge_bytes(), c = 16 * D * 4;
         return f + (a > b ? (a > c ? a : c) : (b > c ? b : c));
     }
 };
@@ -148,8 +148,8 @@ template <int D> struct Directions<float, D> {
 
 // WALK: few new tokens, X and Z formed here; else 16 NRT rows of X from the workspace (no append).
 template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND>
-__global__ __launch_bounds__(256, NRT == 1 ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
-    using C = RowsCfg<T, D>;
+__global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && ATTN && APPEND) ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
+    using C = RowsCfg<T, D, NRT, ATTN && APPEND>;
     constexpr int KR = C::KR, U = C::U, ROWB = C::ROWB, ROWS = 16 * NRT, LDX = C::LDX, DT = D / 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* const sw = reinterpret_cast<float*>(smem);           // [16][D] w of the new tokens
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, NRT == 1 ? 2 : 1) void paged_rows_kernel(Paged
     float* const sn = sz + (APPEND ? 16 * LDX : 0);             // [ROWS][17] logits with the new tokens
     float* const sb = sn + ROWS * 17;                           // [16] beta, [16] c of the new tokens
     float* const sml = sb + 32;                                 // [ROWS][2] maximum, sum
-    unsigned char* const sv = smem + (C::floats_before(NRT, APPEND) * 4 + 255) / 256 * 256;      // value tiles; the new keys; the waves' results
+    unsigned char* const sv = smem + (C::floats_before(APPEND) * 4 + 255) / 256 * 256;      // value tiles; the new keys; the waves' results
 
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     const int Hq = a.H * a.G;
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(256, NRT == 1 ? 2 : 1) void paged_rows_kernel(Paged
     if constexpr (ATTN) {
 #pragma unroll
     for (int t = 0; t < NRT; ++t) l_run[t] = sum_rows(l_run[t]);
-    constexpr size_t PER = C::merge_bytes(NRT) / 2;
+    constexpr size_t PER = C::merge_bytes() / 2;
     for (int half = 2; half >= 1; half >>= 1) {
         __syncthreads();
         if (wv >= half && wv < 2 * half) {
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
 
 template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND>
 static hipError_t launch_rows_t(const PagedArgs& a, long long grid, hipStream_t st) {
-    constexpr size_t bytes = RowsCfg<T, D>::smem(NRT, APPEND);
+    constexpr size_t bytes = RowsCfg<T, D, NRT, ATTN && APPEND>::smem(APPEND);
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_rows_kernel<T, D, NRT, WALK, ATTN, APPEND>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
@@ -606,14 +606,11 @@ hipError_t launch_paged_rows(const PagedArgs& a, int d, int is_bf16, hipStream_t
     if (is_bf16) return d == 64 ? launch_rows_d<bf16_t, 64>(a, st) : launch_rows_d<bf16_t, 128>(a, st);
     return d == 64 ? launch_rows_d<float, 64>(a, st) : launch_rows_d<float, 128>(a, st);
 }
-template <typename T, int D>
+template <int D>
 static hipError_t launch_rows_many_d(const PagedArgs& a, hipStream_t st) {
-    return launch_rows_t<T, D, 4, false, true, false>(a, (long long)a.tiles * a.G * a.H * a.many_splits, st);
+    return launch_rows_t<float, D, 4, false, true, false>(a, (long long)a.tiles * a.G * a.H * a.many_splits, st);
 }
-hipError_t launch_paged_rows_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st) {
-    if (is_bf16) return d == 64 ? launch_rows_many_d<bf16_t, 64>(a, st) : launch_rows_many_d<bf16_t, 128>(a, st);
-    return d == 64 ? launch_rows_many_d<float, 64>(a, st) : launch_rows_many_d<float, 128>(a, st);
-}
+hipError_t launch_paged_rows_many(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_rows_many_d<64>(a, st) : launch_rows_many_d<128>(a, st); }
 template <typename T, int D, bool FEW>
 static hipError_t launch_merge_t(const PagedArgs& a, hipStream_t st) {
     const long long rows = FEW ? (long long)a.nseq * a.few_m * a.H * a.G : (long long)a.T * a.H * a.G;
