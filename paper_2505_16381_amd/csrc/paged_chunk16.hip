@@ -7,7 +7,6 @@
 // On the matrix units that is little: these products are a small part of the call, and a chain of short steps.
 #include <type_traits>
 
-#include "lds_tile.h"
 #include "paged_decl.h"
 
 namespace path {
@@ -234,41 +233,62 @@ __global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs
 // alone on its SIMD, took 4.2 us a step.
 // The first workgroups are those of the append's scan, whose way is the longest: rows of the identity, of which S are rows of the
 // keys carried to the chunk's end, and what is left of X the rows of H_{m-1} .. H_0.
-// Row r = 4 g + i of X^T's block t is element 32 (t / 2) + 8 g + 4 (t % 2) + i, so that as an operand a lane holds eight elements in a row,
-// as it reads them of the keys and of W.
+// As an operand a lane holds elements 32 s + 4 g + 0..3 and 16 further on, as results have them; two eight-byte reads of the keys and of W, which like the
+// transposing reads take whole sixteen-byte pieces off the banks (eight elements in a row cost the latter twice their time).
 constexpr int S16_THREADS = 512;
 template <int D> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)4 * (D / 32) * 2 * 64 * 16; }
 
-// Fragments (16 d x 32 tokens) of a tile's transpose for four blocks of 16 d, by eight reads of rows 32 u + 4 g + 0..3 and 16 further on: a is
-// the lane's address for the first two blocks (eight bytes apart), b for the others.  The waits are in the block.
+// Place of an element in a tile of 64 rows: sixteen-byte pieces of a row exchanged by its turn, such that 32 lanes' eight bytes fall on all banks
+// once, both of one piece's two halves in 16 rows (fragments along the row) and of 32 bytes in 8 rows (transposing reads).
+template <int W> struct Turned16 {
+    static __host__ __device__ __forceinline__ int turn(int row) {
+        return W == 128 ? ((row & 3) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1) : (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+    }
+    static __host__ __device__ __forceinline__ int at(int row, int col) { return row * W + ((((col >> 3) ^ turn(row)) << 3) | (col & 7)); }
+};
+// Fragments of four blocks of 16 rows: eight bytes at a and at b each.  (Left to the compiler these become reads of two rows at once, which take four
+// times as long.)
 template <int OFF, int ROWB>
-__device__ __forceinline__ void turned_tr(unsigned a, unsigned b, bf16x8 (&f)[4]) {
+__device__ __forceinline__ void rows_frags(unsigned a, unsigned b, bf16x8 (&f)[4]) {
     union U { unsigned long long v[2]; bf16x8 f; } u[4];
-    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %1, %8 offset:%11\n\t"
-                 "ds_read_b64_tr_b16 %2, %8 offset:%10+8\n\tds_read_b64_tr_b16 %3, %8 offset:%11+8\n\t"
-                 "ds_read_b64_tr_b16 %4, %9 offset:%10\n\tds_read_b64_tr_b16 %5, %9 offset:%11\n\t"
-                 "ds_read_b64_tr_b16 %6, %9 offset:%10+8\n\tds_read_b64_tr_b16 %7, %9 offset:%11+8\n\ts_waitcnt lgkmcnt(0)"
+    asm volatile("ds_read_b64 %0, %8 offset:%10\n\tds_read_b64 %1, %9 offset:%10\n\tds_read_b64 %2, %8 offset:%11\n\tds_read_b64 %3, %9 offset:%11\n\t"
+                 "ds_read_b64 %4, %8 offset:%12\n\tds_read_b64 %5, %9 offset:%12\n\tds_read_b64 %6, %8 offset:%13\n\tds_read_b64 %7, %9 offset:%13\n\t"
+                 "s_waitcnt lgkmcnt(0)"
                  : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1])
-                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB) : "memory");
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + 32 * ROWB), "n"(OFF + 48 * ROWB) : "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = u[k].f;
+}
+// Fragments (16 d x 32 tokens) of a tile's transpose for four blocks of 16 d, whose addresses are a0 .. a3: reads of rows 32 u + 4 g + 0..3 and
+// of those 16 further on.  The waits are in the block.
+template <int OFF, int ROWB>
+__device__ __forceinline__ void turned_tr(unsigned a0, unsigned a1, unsigned a2, unsigned a3, bf16x8 (&f)[4]) {
+    union U { unsigned long long v[2]; bf16x8 f; } u[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1])
+                 : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(OFF), "n"(OFF + 16 * ROWB) : "memory");
 #pragma unroll
     for (int k = 0; k < 4; ++k) f[k] = u[k].f;
 }
 // The same of a pair of tiles, one behind the other.
 template <int OFF, int ROWB>
-__device__ __forceinline__ void turned_tr_pair(unsigned a, unsigned b, bf16x8 (&f)[4], bf16x8 (&l)[4]) {
+__device__ __forceinline__ void turned_tr_pair(unsigned a0, unsigned a1, unsigned a2, unsigned a3, bf16x8 (&f)[4], bf16x8 (&l)[4]) {
     constexpr int T = 64 * ROWB;
     union U { unsigned long long v[2]; bf16x8 f; } u[8];
-    asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%18\n\tds_read_b64_tr_b16 %1, %16 offset:%19\n\t"
-                 "ds_read_b64_tr_b16 %2, %16 offset:%18+8\n\tds_read_b64_tr_b16 %3, %16 offset:%19+8\n\t"
-                 "ds_read_b64_tr_b16 %4, %17 offset:%18\n\tds_read_b64_tr_b16 %5, %17 offset:%19\n\t"
-                 "ds_read_b64_tr_b16 %6, %17 offset:%18+8\n\tds_read_b64_tr_b16 %7, %17 offset:%19+8\n\t"
-                 "ds_read_b64_tr_b16 %8, %16 offset:%20\n\tds_read_b64_tr_b16 %9, %16 offset:%21\n\t"
-                 "ds_read_b64_tr_b16 %10, %16 offset:%20+8\n\tds_read_b64_tr_b16 %11, %16 offset:%21+8\n\t"
-                 "ds_read_b64_tr_b16 %12, %17 offset:%20\n\tds_read_b64_tr_b16 %13, %17 offset:%21\n\t"
-                 "ds_read_b64_tr_b16 %14, %17 offset:%20+8\n\tds_read_b64_tr_b16 %15, %17 offset:%21+8\n\ts_waitcnt lgkmcnt(0)"
+    asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%20\n\tds_read_b64_tr_b16 %1, %16 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %2, %17 offset:%20\n\tds_read_b64_tr_b16 %3, %17 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %4, %18 offset:%20\n\tds_read_b64_tr_b16 %5, %18 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %6, %19 offset:%20\n\tds_read_b64_tr_b16 %7, %19 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %8, %16 offset:%22\n\tds_read_b64_tr_b16 %9, %16 offset:%23\n\t"
+                 "ds_read_b64_tr_b16 %10, %17 offset:%22\n\tds_read_b64_tr_b16 %11, %17 offset:%23\n\t"
+                 "ds_read_b64_tr_b16 %12, %18 offset:%22\n\tds_read_b64_tr_b16 %13, %18 offset:%23\n\t"
+                 "ds_read_b64_tr_b16 %14, %19 offset:%22\n\tds_read_b64_tr_b16 %15, %19 offset:%23\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1]),
                    "=&v"(u[4].v[0]), "=&v"(u[4].v[1]), "=&v"(u[5].v[0]), "=&v"(u[5].v[1]), "=&v"(u[6].v[0]), "=&v"(u[6].v[1]), "=&v"(u[7].v[0]), "=&v"(u[7].v[1])
-                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + T), "n"(OFF + T + 16 * ROWB) : "memory");
+                 : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + T), "n"(OFF + T + 16 * ROWB) : "memory");
 #pragma unroll
     for (int k = 0; k < 4; ++k) { f[k] = u[k].f; l[k] = u[4 + k].f; }
 }
@@ -287,7 +307,7 @@ __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __
 
 template <int D, bool SCAN>
 __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem, int s, int h, int hq, int ct, int r0) {
-    typedef TurnedTile<D> L;
+    typedef Turned16<D> L;
     constexpr int ROWB = D * 2, TILE = 64 * ROWB, DT = D / 16, DS = D / 32, PPR = D / 8, RPI = 64 / PPR, GI = 8 / RPI;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, Hq = a.H * a.G;
     const int rw = wv & 3;                  // its 16 rows
@@ -330,9 +350,8 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
     if (ct > 0) bring0(ct - 1);
 
     const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const unsigned tr = base + 3 * TILE + L::at(4 * g + (c >> 2), 8 * (c & 3)) * 2;      // of set 1; d block t: exclusive or 64 (t / 2), plus 8 (t % 2)
-    const unsigned nat = L::at(c, 8 * g) * 2;                                            // of a tile; d slab s: exclusive or 64 s
-    auto frag = [&](int slot, int b, int sl) { return *reinterpret_cast<const bf16x8*>(smem + slot * TILE + b * 16 * ROWB + (nat ^ (64 * sl))); };
+    const unsigned tr = base + 3 * TILE + L::at(4 * g + (c >> 2), 4 * (c & 3)) * 2;      // of set 1; d block t: exclusive or 32 t
+    const unsigned nat = base + L::at(c, 4 * g) * 2;                                     // of set 0; d slab s: exclusive or 64 s, its second half + 32
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     if (!carries) {
@@ -376,10 +395,10 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
 #pragma unroll
             for (int t = 0; t < DT; t += 4) {      // four blocks at a time, none waiting for its own last product
                 bf16x8 v[4];
-                turned_tr<2 * TILE, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), v);
+                turned_tr<2 * TILE, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), v);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[0], O[t + k]);
-                turned_tr<2 * TILE + 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), v);
+                turned_tr<2 * TILE + 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), v);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[1], O[t + k]);
             }
@@ -417,8 +436,8 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             for (int sl = 0; sl < DS; ++sl) {
                 const bf16x8 xh = sx[(2 * sl) * 64], xl = sx[(2 * sl + 1) * 64];
                 bf16x8 kh[4], kl[4];
-#pragma unroll
-                for (int b = 0; b < 4; ++b) { kh[b] = frag(0, b, sl); kl[b] = frag(1, b, sl); }
+                rows_frags<0, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), kh);
+                rows_frags<TILE, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), kl);
                 // (scan: transposed, a lane has four consecutive elements of a key)
 #pragma unroll
                 for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xh, kh[b], S[b]) : mfma32(kh[b], xh, S[b]);
@@ -455,12 +474,12 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
                     bf16x4 v;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(O[t][i] * inv);
-                    *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.o) + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = v;
+                    *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.o) + at * D + 16 * t + 4 * g) = v;
                 }
                 if (g == 0) a.lse[at] = (m_run + __builtin_amdgcn_logf(l_run)) * LN2;
             } else if (there) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.many_o + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = O[t];
+                for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.many_o + at * D + 16 * t + 4 * g) = O[t];
                 if (g == 0) { a.many_ml[2 * at] = m_run; a.many_ml[2 * at + 1] = l_run; }
             }
         }
@@ -472,9 +491,9 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             x[t] = zero;
             if constexpr (SCAN) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[t][i] = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + i == row ? 1.f : 0.f;
+                for (int i = 0; i < 4; ++i) x[t][i] = 16 * t + 4 * g + i == row ? 1.f : 0.f;
             } else if (there) {
-                x[t] = *reinterpret_cast<const f32x4*>(a.x + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1));
+                x[t] = *reinterpret_cast<const f32x4*>(a.x + at * D + 16 * t + 4 * g);
             }
         }
         auto hand_over = [&]() {
@@ -493,8 +512,7 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             for (int sl = 0; sl < DS; ++sl)
             {
                 bf16x8 w[4];
-#pragma unroll
-                for (int b = 0; b < 4; ++b) w[b] = frag(2, b, sl);
+                rows_frags<2 * TILE, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), w);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) Y[b] = mfma32(w[b], xh[sl], Y[b]);
 #pragma unroll
@@ -506,7 +524,7 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             auto carry = [&](int t, auto ut) {
                 constexpr int u = decltype(ut)::value;
                 bf16x8 zh[4], zl[4];
-                turned_tr_pair<u * 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 64), zh, zl);
+                turned_tr_pair<u * 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), zh, zl);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zh[k], yh[u], x[t + k]);
 #pragma unroll
@@ -527,7 +545,7 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             half_t* const p = reinterpret_cast<half_t*>(a.pt) + (((size_t)s * a.H + h) * D + row) * D;
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-                const int d = 32 * (t >> 1) + 8 * g + 4 * (t & 1);
+                const int d = 16 * t + 4 * g;
                 halfx4 v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = (half_t)(x[t][i] - (d + i == row ? 1.f : 0.f));
@@ -535,7 +553,7 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             }
         } else if (there && q.n > 0) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.x + at * D + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = x[t];
+            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.x + at * D + 16 * t + 4 * g) = x[t];
         }
     }
 }
