@@ -225,18 +225,18 @@ __global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs
 
 // ---- the way through the tiles ----
 //
-// 64 rows per workgroup, 16 per wave, and two waves for each 16 rows, which share a step's work:
-//     wave a   S = kt X^T (64 tokens x 16 rows), softmax, O^T += V^T P^T        scan: S are rows of keys, stored
-//     wave b   Y = W X^T, X^T -= Z^T Y, and X as operands to LDS for wave a's next step
+// 64 rows per workgroup, and four waves for each 16 of them, which share a step's work:
+//     waves a   S = kt X^T (32 of the tile's 64 tokens each), softmax, O^T += V^T P^T: two online softmaxes, joined at the end.  scan: S are rows of keys, stored
+//     waves b   Y = W X^T (32 tokens each), exchanged; X^T -= Z^T Y (half of d each), and X as operands to LDS for the next step
 // The tile's operands come to LDS in two sets, each while the other is worked on: carried keys (hi, lo) and W; -Z (hi, lo) and V.
-// Bound by LDS (3.5 thousand cycles a step at 128 bytes a cycle) and, with few tiles, by the steps' chain; one wave for both halves,
-// alone on its SIMD, took 4.2 us a step.
+// Bound by the chain of steps: 72 products a SIMD (1.1 us) and 2.2 thousand cycles of LDS each.  One wave for all of a row's work took 4.2 us a step,
+// two 2.7.
 // The first workgroups are those of the append's scan, whose way is the longest: rows of the identity, of which S are rows of the
 // keys carried to the chunk's end, and what is left of X the rows of H_{m-1} .. H_0.
 // As an operand a lane holds elements 32 s + 4 g + 0..3 and 16 further on, as results have them; two eight-byte reads of the keys and of W, which like the
 // transposing reads take whole sixteen-byte pieces off the banks (eight elements in a row cost the latter twice their time).
-constexpr int S16_THREADS = 512;
-template <int D> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)4 * (D / 32) * 2 * 64 * 16; }
+constexpr int S16_THREADS = 1024;
+template <int D> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)4 * (D / 32) * 2 * 64 * 16 + 4 * 2 * 2 * 64 * 16; }
 
 // Place of an element in a tile of 64 rows: sixteen-byte pieces of a row exchanged by its turn, such that 32 lanes' eight bytes fall on all banks
 // once, both of one piece's two halves in 16 rows (fragments along the row) and of 32 bytes in 8 rows (transposing reads).
@@ -246,18 +246,31 @@ template <int W> struct Turned16 {
     }
     static __host__ __device__ __forceinline__ int at(int row, int col) { return row * W + ((((col >> 3) ^ turn(row)) << 3) | (col & 7)); }
 };
-// Fragments of four blocks of 16 rows: eight bytes at a and at b each.  (Left to the compiler these become reads of two rows at once, which take four
-// times as long.)
+// Fragments of two blocks of 16 rows: eight bytes at a and at b each; of a tile and of the one behind it, or of one.  (Left to the compiler these become
+// reads of two rows at once, which take four times as long.)
 template <int OFF, int ROWB>
-__device__ __forceinline__ void rows_frags(unsigned a, unsigned b, bf16x8 (&f)[4]) {
+__device__ __forceinline__ void rows_pair(unsigned a, unsigned b, bf16x8 (&f)[2], bf16x8 (&l)[2]) {
+    constexpr int T = 64 * ROWB;
     union U { unsigned long long v[2]; bf16x8 f; } u[4];
     asm volatile("ds_read_b64 %0, %8 offset:%10\n\tds_read_b64 %1, %9 offset:%10\n\tds_read_b64 %2, %8 offset:%11\n\tds_read_b64 %3, %9 offset:%11\n\t"
                  "ds_read_b64 %4, %8 offset:%12\n\tds_read_b64 %5, %9 offset:%12\n\tds_read_b64 %6, %8 offset:%13\n\tds_read_b64 %7, %9 offset:%13\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1])
-                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + 32 * ROWB), "n"(OFF + 48 * ROWB) : "memory");
-#pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = u[k].f;
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB), "n"(OFF + T), "n"(OFF + T + 16 * ROWB) : "memory");
+    f[0] = u[0].f;
+    f[1] = u[1].f;
+    l[0] = u[2].f;
+    l[1] = u[3].f;
+}
+template <int OFF, int ROWB>
+__device__ __forceinline__ void rows_one(unsigned a, unsigned b, bf16x8 (&f)[2]) {
+    union U { unsigned long long v[2]; bf16x8 f; } u[2];
+    asm volatile("ds_read_b64 %0, %4 offset:%6\n\tds_read_b64 %1, %5 offset:%6\n\tds_read_b64 %2, %4 offset:%7\n\tds_read_b64 %3, %5 offset:%7\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1])
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 16 * ROWB) : "memory");
+    f[0] = u[0].f;
+    f[1] = u[1].f;
 }
 // Fragments (16 d x 32 tokens) of a tile's transpose for four blocks of 16 d, whose addresses are a0 .. a3: reads of rows 32 u + 4 g + 0..3 and
 // of those 16 further on.  The waits are in the block.
@@ -308,10 +321,10 @@ __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __
 template <int D, bool SCAN>
 __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem, int s, int h, int hq, int ct, int r0) {
     typedef Turned16<D> L;
-    constexpr int ROWB = D * 2, TILE = 64 * ROWB, DT = D / 16, DS = D / 32, PPR = D / 8, RPI = 64 / PPR, GI = 8 / RPI;
+    constexpr int ROWB = D * 2, TILE = 64 * ROWB, DT = D / 16, DS = D / 32, HT = DT / 2, HS = DS / 2, PPR = D / 8, RPI = 64 / PPR;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, Hq = a.H * a.G;
-    const int rw = wv & 3;                  // its 16 rows
-    const bool carries = wv >= 4;           // wave b
+    const int rw = wv & 3, part = (wv >> 2) & 1;      // its 16 rows, and which half of the work on them
+    const bool carries = wv >= 8;                     // waves b
     const PagedSeq q = paged_seq(a, s);
     const int first = first_tile(a, s), row = r0 + 16 * rw + c;
     const int tok = SCAN ? 0 : q.t0 + 64 * ct + row;
@@ -320,17 +333,16 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
     const size_t lo = (size_t)a.tiles * a.H * 64 * D;
     const bf16_t* const kt = reinterpret_cast<const bf16_t*>(a.kt);
     const bf16_t* const zt = reinterpret_cast<const bf16_t*>(a.zt);
-    bf16x8* const sx = reinterpret_cast<bf16x8*>(smem + 6 * TILE) + rw * DS * 2 * 64 + lane;      // X of the 16 rows: [slab][hi, lo][lane]
+    bf16x8* const sx = reinterpret_cast<bf16x8*>(smem + 6 * TILE) + rw * DS * 2 * 64 + lane;                            // X of the 16 rows: [slab][hi, lo][lane]
+    bf16x8* const sy = reinterpret_cast<bf16x8*>(smem + 6 * TILE + 4 * DS * 2 * 64 * 16) + rw * 2 * 2 * 64 + lane;      // Y: the same, two slabs
 
-    // copies: wave w brings rows 8 w .. + 7 of each tile, a row's pieces exchanged by its turn; rows of w and v past the last token: that token's
-    const int q4 = lane / PPR;
+    // copies: the waves share a tile's rows, a row's pieces exchanged by its turn; rows of w and v past the last token: that token's
+    const int copied = RPI * wv + lane / PPR;
     auto copy = [&](int slot, const bf16_t* src, long long stride, int last) {
-#pragma unroll
-        for (int i = 0; i < GI; ++i) {
-            const int r = 8 * wv + i * RPI + q4;
-            const bf16_t* const p = src + min(r, last) * stride + ((lane % PPR) ^ L::turn(r)) * 8;
+        if (RPI * wv < 64) {
+            const bf16_t* const p = src + min(copied, last) * stride + ((lane % PPR) ^ L::turn(copied)) * 8;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                             (__attribute__((address_space(3))) void*)(smem + slot * TILE + (8 * wv + i * RPI) * ROWB), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(smem + slot * TILE + RPI * wv * ROWB), 16, 0, 0);
         }
     };
     auto tile_at = [&](int j) { return ((size_t)(first + j) * a.H + h) * 64 * D; };
@@ -351,28 +363,28 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
 
     const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     const unsigned tr = base + 3 * TILE + L::at(4 * g + (c >> 2), 4 * (c & 3)) * 2;      // of set 1; d block t: exclusive or 32 t
-    const unsigned nat = base + L::at(c, 4 * g) * 2;                                     // of set 0; d slab s: exclusive or 64 s, its second half + 32
+    const unsigned nat = base + part * 32 * ROWB + L::at(c, 4 * g) * 2;                  // of set 0, its 32 tokens; d slab s: exclusive or 64 s, its second half + 32
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     if (!carries) {
-        f32x4 O[SCAN ? 1 : DT], S[4];
+        f32x4 O[SCAN ? 1 : DT], S[2];
         float m_run = -INFINITY, l_run = 0.f, cq = 0.f;
         const float sl2 = a.scale * LOG2E;
-        bf16x8 P[2];
+        bf16x8 P;
         auto softmax = [&](int j, bool own) {
-            float top = -INFINITY, ck[16];
+            float top = -INFINITY, ck[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ck[i] = 0.f;
+            for (int i = 0; i < 8; ++i) ck[i] = 0.f;
             if (a.cpages) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) ck[i] = a.crow[(long long)min(q.t0 + 64 * j + 16 * (i >> 2) + 4 * g + (i & 3), a.T - 1) * a.H + h];
+                for (int i = 0; i < 8; ++i) ck[i] = a.crow[(long long)min(q.t0 + 64 * j + 32 * part + 16 * (i >> 2) + 4 * g + (i & 3), a.T - 1) * a.H + h];
             }
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float y = S[b][i] * sl2 + (cq - ck[4 * b + i]) * LOG2E;      // (no gates: both are zero)
-                    if (own) y = 16 * b + 4 * g + i <= row ? y : -INFINITY;
+                    if (own) y = 32 * part + 16 * b + 4 * g + i <= row ? y : -INFINITY;
                     S[b][i] = y;
                     top = fmaxf(top, y);
                 }
@@ -380,34 +392,30 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             m_run = now;
             float sum = 0.f;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { S[b][i] = __builtin_amdgcn_exp2f(S[b][i] - ref); sum += S[b][i]; }
             l_run = l_run * f + sum;
 #pragma unroll
             for (int t = 0; t < DT; ++t) O[t] *= f;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) P[u][k] = (bf16_t)S[2 * u + (k >> 2)][k & 3];
+            for (int k = 0; k < 8; ++k) P[k] = (bf16_t)S[k >> 2][k & 3];
         };
         auto values = [&]() {
+            const unsigned v0 = tr + part * 32 * ROWB;
 #pragma unroll
             for (int t = 0; t < DT; t += 4) {      // four blocks at a time, none waiting for its own last product
                 bf16x8 v[4];
-                turned_tr<2 * TILE, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), v);
+                turned_tr<2 * TILE, ROWB>(v0 ^ (32 * t), v0 ^ (32 * t + 32), v0 ^ (32 * t + 64), v0 ^ (32 * t + 96), v);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[0], O[t + k]);
-                turned_tr<2 * TILE + 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), v);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P[1], O[t + k]);
+                for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P, O[t + k]);
             }
         };
-        long long place[4];      // SCAN: where this lane's key of each block goes
+        long long place[2];      // SCAN: where this lane's key of each block goes
         auto places = [&](int j) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int t = 64 * j + 16 * b + c;
+            for (int b = 0; b < 2; ++b) {
+                const int t = 64 * j + 32 * part + 16 * b + c;
                 place[b] = t < q.m ? paged_row(a, s, h, q.n + t) : -1;
             }
         };
@@ -419,9 +427,9 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
 #pragma unroll
             for (int t = 0; t < DT; ++t) O[t] = zero;
             if (a.cpages && there) cq = a.crow[(long long)tok * a.H + h];
-            const float* const sd = a.sd + ((size_t)(first + ct) * Hq + hq) * 4096 + row * 64;
+            const float* const sd = a.sd + ((size_t)(first + ct) * Hq + hq) * 4096 + row * 64 + 32 * part;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) S[b] = *reinterpret_cast<const f32x4*>(sd + 16 * b + 4 * g);
+            for (int b = 0; b < 2; ++b) S[b] = *reinterpret_cast<const f32x4*>(sd + 16 * b + 4 * g);
             softmax(ct, true);
             wait_async_and_sync();
             values();
@@ -430,112 +438,151 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
         }
         for (int j = ct - 1; j >= 0; --j) {
             // set 0 and X are there
+            f32x4 R[2];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) S[b] = zero;
+            for (int b = 0; b < 2; ++b) S[b] = R[b] = zero;
 #pragma unroll
             for (int sl = 0; sl < DS; ++sl) {
                 const bf16x8 xh = sx[(2 * sl) * 64], xl = sx[(2 * sl + 1) * 64];
-                bf16x8 kh[4], kl[4];
-                rows_frags<0, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), kh);
-                rows_frags<TILE, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), kl);
+                bf16x8 kh[2], kl[2];
+                rows_pair<0, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), kh, kl);
                 // (scan: transposed, a lane has four consecutive elements of a key)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xh, kh[b], S[b]) : mfma32(kh[b], xh, S[b]);
+                for (int b = 0; b < 2; ++b) S[b] = SCAN ? mfma32(xh, kh[b], S[b]) : mfma32(kh[b], xh, S[b]);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xl, kh[b], S[b]) : mfma32(kh[b], xl, S[b]);
+                for (int b = 0; b < 2; ++b) R[b] = SCAN ? mfma32(xl, kh[b], R[b]) : mfma32(kh[b], xl, R[b]);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) S[b] = SCAN ? mfma32(xh, kl[b], S[b]) : mfma32(kl[b], xh, S[b]);
+                for (int b = 0; b < 2; ++b) S[b] = SCAN ? mfma32(xh, kl[b], S[b]) : mfma32(kl[b], xh, S[b]);
             }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) S[b] += R[b];
             wait_async_and_sync();      // set 1 is there, set 0 and X are free
             if (j > 0) bring0(j - 1);
             if constexpr (SCAN) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                for (int b = 0; b < 2; ++b) {
                     bf16x4 v;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[i] = (bf16_t)S[b][i];
                     if (place[b] >= 0) *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.kpages) + place[b] * D + r0 + 16 * rw + 4 * g) = v;
                 }
                 if (j > 0) places(j - 1);
-            }
-            if constexpr (!SCAN) {
+            } else {
                 softmax(j, false);
                 values();
             }
             wait_async_and_sync();      // set 0 and X are there, set 1 is free
             if (j > 0) bring1(j - 1);
         }
-        if constexpr (!SCAN) {
+        if constexpr (!SCAN) {      // the two halves' softmaxes joined, where set 0 was
             l_run = sum_rows(l_run);
-            if (there && q.n == 0) {      // nothing cached: that was all
-                const float inv = 1.f / l_run;
+            float* const p = reinterpret_cast<float*>(smem) + rw * (DT * 256 + 128);
+            if (part == 1) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    bf16x4 v;
+                for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(p + t * 256 + lane * 4) = O[t];
+                p[DT * 256 + lane] = m_run;
+                p[DT * 256 + 64 + lane] = l_run;
+            }
+            lds_barrier();
+            if (part == 0 && there) {
+                const float m2 = p[DT * 256 + lane], now = fmaxf(m_run, m2), f1 = __builtin_amdgcn_exp2f(m_run - now), f2 = __builtin_amdgcn_exp2f(m2 - now);      // (the own tile's first half has the row's first keys: now is finite)
+                l_run = l_run * f1 + p[DT * 256 + 64 + lane] * f2;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(O[t][i] * inv);
-                    *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.o) + at * D + 16 * t + 4 * g) = v;
+                for (int t = 0; t < DT; ++t) O[t] = O[t] * f1 + *reinterpret_cast<const f32x4*>(p + t * 256 + lane * 4) * f2;
+                if (q.n == 0) {      // nothing cached: that was all
+                    const float inv = 1.f / l_run;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        bf16x4 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(O[t][i] * inv);
+                        *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16_t*>(a.o) + at * D + 16 * t + 4 * g) = v;
+                    }
+                    if (g == 0) a.lse[at] = (now + __builtin_amdgcn_logf(l_run)) * LN2;
+                } else {
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.many_o + at * D + 16 * t + 4 * g) = O[t];
+                    if (g == 0) { a.many_ml[2 * at] = now; a.many_ml[2 * at + 1] = l_run; }
                 }
-                if (g == 0) a.lse[at] = (m_run + __builtin_amdgcn_logf(l_run)) * LN2;
-            } else if (there) {
-#pragma unroll
-                for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.many_o + at * D + 16 * t + 4 * g) = O[t];
-                if (g == 0) { a.many_ml[2 * at] = m_run; a.many_ml[2 * at + 1] = l_run; }
             }
         }
     } else {
-        f32x4 x[DT], Y[4];
-        bf16x8 xh[DS], xl[DS], yh[2], yl[2];
+        f32x4 x[HT], Y[2];      // its half of X
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
+        for (int t = 0; t < HT; ++t) {
+            const int d = 16 * (HT * part + t) + 4 * g;
             x[t] = zero;
             if constexpr (SCAN) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[t][i] = 16 * t + 4 * g + i == row ? 1.f : 0.f;
+                for (int i = 0; i < 4; ++i) x[t][i] = d + i == row ? 1.f : 0.f;
             } else if (there) {
-                x[t] = *reinterpret_cast<const f32x4*>(a.x + at * D + 16 * t + 4 * g);
+                x[t] = *reinterpret_cast<const f32x4*>(a.x + at * D + d);
             }
         }
         auto hand_over = [&]() {
-            pack_pairs<DS>(x, xh, xl);
+            bf16x8 xh[HS], xl[HS];
+            pack_pairs<HS>(x, xh, xl);
 #pragma unroll
-            for (int sl = 0; sl < DS; ++sl) { sx[(2 * sl) * 64] = xh[sl]; sx[(2 * sl + 1) * 64] = xl[sl]; }
+            for (int sl = 0; sl < HS; ++sl) { sx[(2 * (HS * part + sl)) * 64] = xh[sl]; sx[(2 * (HS * part + sl) + 1) * 64] = xl[sl]; }
         };
         if (ct > 0) hand_over();
         wait_async_and_sync();
         lds_barrier();
         if (!SCAN && ct > 0) bring1(ct - 1);
         for (int j = ct - 1; j >= 0; --j) {
+            bf16x8 xh[DS], xl[DS];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) Y[b] = zero;
+            for (int sl = 0; sl < DS; ++sl) { xh[sl] = sx[(2 * sl) * 64]; xl[sl] = sx[(2 * sl + 1) * 64]; }
+            f32x4 R[2];
 #pragma unroll
-            for (int sl = 0; sl < DS; ++sl)
-            {
-                bf16x8 w[4];
-                rows_frags<2 * TILE, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), w);
+            for (int b = 0; b < 2; ++b) Y[b] = R[b] = zero;
 #pragma unroll
-                for (int b = 0; b < 4; ++b) Y[b] = mfma32(w[b], xh[sl], Y[b]);
+            for (int sl = 0; sl < DS; ++sl) {
+                bf16x8 w[2];
+                rows_one<2 * TILE, ROWB>(nat ^ (64 * sl), nat ^ (64 * sl + 32), w);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) Y[b] = mfma32(w[b], xl[sl], Y[b]);
+                for (int b = 0; b < 2; ++b) Y[b] = mfma32(w[b], xh[sl], Y[b]);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) R[b] = mfma32(w[b], xl[sl], R[b]);
             }
-            pack_pairs<2>(Y, yh, yl);
+            bf16x8 yh[2], yl[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) Y[b] += R[b];
+            pack_pairs<1>(Y, yh, yl);
+            sy[(2 * part) * 64] = yh[0];
+            sy[(2 * part + 1) * 64] = yl[0];
             wait_async_and_sync();
             if (j > 0) bring0(j - 1);
-            auto carry = [&](int t, auto ut) {
-                constexpr int u = decltype(ut)::value;
-                bf16x8 zh[4], zl[4];
-                turned_tr_pair<u * 32 * ROWB, ROWB>(tr ^ (32 * t), tr ^ (32 * t + 32), tr ^ (32 * t + 64), tr ^ (32 * t + 96), zh, zl);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zh[k], yh[u], x[t + k]);
+            for (int u = 0; u < 2; ++u) { yh[u] = sy[(2 * u) * 64]; yl[u] = sy[(2 * u + 1) * 64]; }
+            const unsigned z0 = tr ^ (32 * HT * part);
+            bf16x8 zh[4], zl[4];
+            if constexpr (HT == 4) {
+                turned_tr_pair<0, ROWB>(z0, z0 ^ 32, z0 ^ 64, z0 ^ 96, zh, zl);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zh[k], yl[u], x[t + k]);
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zh[k], yh[0], x[k]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[t + k] = mfma32(zl[k], yh[u], x[t + k]);
-            };
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zh[k], yl[0], x[k]);
 #pragma unroll
-            for (int t = 0; t < DT; t += 4) {
-                carry(t, std::integral_constant<int, 0>());
-                carry(t, std::integral_constant<int, 1>());
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zl[k], yh[0], x[k]);
+                turned_tr_pair<32 * ROWB, ROWB>(z0, z0 ^ 32, z0 ^ 64, z0 ^ 96, zh, zl);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zh[k], yh[1], x[k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zh[k], yl[1], x[k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = mfma32(zl[k], yh[1], x[k]);
+            } else {      // two blocks, both slabs
+                turned_tr_pair<0, ROWB>(z0, z0 ^ 32, z0 + 32 * ROWB, (z0 ^ 32) + 32 * ROWB, zh, zl);
+                f32x4 y[2] = {zero, zero};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { f32x4& v = k < 2 ? x[k] : y[k - 2]; v = mfma32(zh[k], yh[k >> 1], v); }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { f32x4& v = k < 2 ? x[k] : y[k - 2]; v = mfma32(zh[k], yl[k >> 1], v); }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { f32x4& v = k < 2 ? x[k] : y[k - 2]; v = mfma32(zl[k], yh[k >> 1], v); }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[k] += y[k];
             }
             if (j > 0) hand_over();
             wait_async_and_sync();
@@ -544,16 +591,19 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
         if constexpr (SCAN) {
             half_t* const p = reinterpret_cast<half_t*>(a.pt) + (((size_t)s * a.H + h) * D + row) * D;
 #pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const int d = 16 * t + 4 * g;
+            for (int t = 0; t < HT; ++t) {
+                const int d = 16 * (HT * part + t) + 4 * g;
                 halfx4 v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = (half_t)(x[t][i] - (d + i == row ? 1.f : 0.f));
                 *reinterpret_cast<halfx4*>(p + d) = v;
             }
-        } else if (there && q.n > 0) {
+        } else {
+            if (there && q.n > 0) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(a.x + at * D + 16 * t + 4 * g) = x[t];
+                for (int t = 0; t < HT; ++t) *reinterpret_cast<f32x4*>(a.x + at * D + 16 * (HT * part + t) + 4 * g) = x[t];
+            }
+            lds_barrier();      // (where waves a join their halves)
         }
     }
 }
