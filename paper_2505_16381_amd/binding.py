@@ -7,7 +7,6 @@ CPU fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -552,64 +551,63 @@ def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) ->
     return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
 
 
-def _paged(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, log_f, cpages, o, lse, workspace, max_new, max_cached):
-    """Checks that every tensor is what the kernels take it for; (nseq, T, num_pages, page_size, pages_per_seq, H, group, d, dt, workspace)."""
-    import torch
-    if k.dim() != 3 or kpages.dim() != 4 or page_table.dim() != 2:
-        raise ValueError("k is [T,H,d], kpages [num_pages,H,page_size,d], page_table [nseq,pages_per_seq]")
-    T, H, d = k.shape
-    num_pages, _, page_size, _ = kpages.shape
-    nseq, per_seq = page_table.shape
-    dt = _dt_of(k)
-    group = 1
-    if q is not None:
-        if q.dim() != 3 or q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
-            raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
-        group = q.shape[1] // H
-    want = [("v", v, (T, H, d), k.dtype), ("w", w, (T, H, d), k.dtype), ("beta", beta, (T, H), k.dtype),
-            ("kpages", kpages, (num_pages, H, page_size, d), k.dtype), ("vpages", vpages, tuple(kpages.shape), k.dtype),
-            ("page_table", page_table, (nseq, per_seq), torch.int32), ("cached", cached, (nseq,), torch.int32), ("cu_new", cu_new, (nseq + 1,), torch.int32)]
-    if q is not None:
-        want += [("q", q, tuple(q.shape), k.dtype), ("o", o, tuple(q.shape), k.dtype), ("lse", lse, (T, H * group), torch.float32)]
-    if log_f is not None:
-        want.append(("log_f", log_f, (T, H), k.dtype))
-    if cpages is not None:
-        want.append(("cpages", cpages, (num_pages, H, page_size), torch.float32))
-    for name, t, shape, dtype in [("k", k, (T, H, d), k.dtype), *want]:
-        if t is None:
-            continue
-        if tuple(t.shape) != shape or t.dtype != dtype:
-            raise ValueError(f"{name} is {shape}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
-        if not t.is_cuda or t.device != k.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
-    if workspace is None:
-        workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
-    elif workspace.device != k.device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous and on the GPU that k is on")
-    return nseq, T, num_pages, page_size, per_seq, H, group, d, dt, workspace
+def _paged_tensor(name, t, shape, dtype, dev):
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} is {tuple(shape)}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
+    return t.data_ptr()
 
 
 def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream):
+    """Checks that every tensor is what the kernels take it for, and calls; (a call of short kernels is bound by this function: one look at each)."""
     import torch
-    max_new, max_cached = int(max_new), int(max_cached)
+    if k.dim() != 3 or kpages.dim() != 4 or page_table.dim() != 2 or (q is not None and q.dim() != 3):
+        raise ValueError("q, k are [T,heads,d], kpages [num_pages,H,page_size,d], page_table [nseq,pages_per_seq]")
+    shape, pages, td, i32, dev = k.shape, kpages.shape, k.dtype, torch.int32, k.get_device()
+    T, H, d = shape
+    num_pages, _, page_size, _ = pages
+    nseq, per_seq = page_table.shape
+    dt = PATH_BF16 if td == torch.bfloat16 else _dt_of(k)
+    if dev < 0:
+        raise ValueError("k must be on a GPU")
+    max_new, max_cached, group = int(max_new), int(max_cached), 1
     if q is not None:
-        o = torch.empty_like(q) if o is None else o
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
-    nseq, T, num_pages, page_size, per_seq, H, group, d, dt, workspace = _paged(
-        q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, log_f, cpages, o, lse, workspace, max_new, max_cached)
+        if q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
+            raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
+        group = q.shape[1] // H
+        if o is None:
+            o = torch.empty_like(q)
+        if lse is None:
+            lse = q.new_empty((T, H * group), dtype=torch.float32)
+    if (log_f is None) != (cpages is None):
+        raise ValueError("log_f and cpages go together")
+    one = shape[:2]
+    args = [_paged_tensor("k", k, shape, td, dev), _paged_tensor("v", v, shape, td, dev), _paged_tensor("w", w, shape, td, dev),
+            _paged_tensor("beta", beta, one, td, dev), None if log_f is None else _paged_tensor("log_f", log_f, one, td, dev),
+            _paged_tensor("kpages", kpages, (num_pages, H, page_size, d), td, dev), _paged_tensor("vpages", vpages, pages, td, dev),
+            None if cpages is None else _paged_tensor("cpages", cpages, pages[:3], torch.float32, dev),
+            _paged_tensor("page_table", page_table, (nseq, per_seq), i32, dev), _paged_tensor("cached", cached, (nseq,), i32, dev),
+            _paged_tensor("cu_new", cu_new, (nseq + 1,), i32, dev)]
+    if q is not None:
+        args = [_paged_tensor("q", q, q.shape, td, dev), *args, _paged_tensor("o", o, q.shape, td, dev), _paged_tensor("lse", lse, (T, H * group), torch.float32, dev)]
+    if workspace is None:
+        workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the GPU that k is on")
     if T == 0:
         return o, lse
+    args += [nseq, T, max_new, max_cached, num_pages, page_size, per_seq, H]
+    args += [d] if q is None else [group, d, float(d ** -0.5 if scale is None else scale)]
+    args += [dt, workspace.data_ptr(), workspace.numel() * workspace.element_size()]
     call = getattr(load_library(), name)
-    cache = (_ptr(k), _ptr(v), _ptr(w), _ptr(beta), _opt(log_f), _ptr(kpages), _ptr(vpages), _opt(cpages), _ptr(page_table), _ptr(cached), _ptr(cu_new))
-    sizes = (nseq, T, max_new, max_cached, num_pages, page_size, per_seq, H)
-    here = torch.cuda.current_device() == k.device.index
-    with (contextlib.nullcontext() if here else torch.cuda.device(k.device)):      # (launches go to the tensors' GPU)
-        if q is None:
-            _check(call(*cache, *sizes, d, dt, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_handle(stream)))
-        else:
-            scale = float(d ** -0.5 if scale is None else scale)
-            _check(call(_ptr(q), *cache, _ptr(o), _ptr(lse), *sizes, group, d, scale, dt, _ptr(workspace), workspace.numel() * workspace.element_size(),
-                        _stream_handle(stream)))
+    if torch.cuda.current_device() == dev:
+        code = call(*args, _stream_handle(stream))
+    else:
+        with torch.cuda.device(dev):      # launches go to the tensors' GPU
+            code = call(*args, _stream_handle(stream))
+    if code:
+        _check(code)
     return o, lse
 
 

@@ -950,10 +950,15 @@ extern "C" path_status_t path_attn_varlen_bwd(const void* q, const void* k, cons
 namespace {
 struct PagedPlan {
     bool few, many;              // which of the two ways sequences may go
-    int few_limit, few_m, few_splits, few_len, tiles, row_blocks, many_splits, many_len;
+    int few_limit, few_m, few_splits, few_len, few_waves, tiles, row_blocks, many_splits, many_len;
     size_t few_o, few_ml, x, crow, many_o, many_ml, kt, wt, zt, vt, sd, pt, total;
 };
 }  // namespace
+
+// Cached keys of a head up to so many bytes are taken by one workgroup of eight waves (up to 128 tokens four), which leaves nothing to join.  us replayed /
+// eager, one workgroup against pieces, 16 heads, one token: d = 64, 512 tokens attn 7.6 / 15.4, 10.6 / 18.3, extend 10.2 / 15.7, 12.7 / 18.4; d = 128, 512
+// tokens 11.6 / 15.3, 12.7 / 18.6 and 15.6 / 15.6, 14.0 / 18.6; 700 tokens 15.0 / 15.4, 13.5 / 18.6 and 19.0 / 18.9, 15.0 / 18.5; 128 heads 17.4, 17.1 and 23.9, 23.4.
+static constexpr int PAGED_SHORT_BYTES = 128 * 1024;
 
 static bool paged_shape_ok(int nseq, int T, int max_new, int max_cached, int H, int group, int d) {
     if (nseq < 1 || T < 0 || max_new < 1 || max_cached < 0 || H < 1 || group < 1 || group > PAGED_FEW_ROWS) return false;
@@ -962,7 +967,7 @@ static bool paged_shape_ok(int nseq, int T, int max_new, int max_cached, int H, 
     return ((long long)T / 64 + nseq) * 64 * H * group <= (1LL << 31) / 4;      // 32-bit grids
 }
 
-static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H, int group, int d, size_t es) {
+static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H, int group, int d, size_t es, bool attn) {
     PagedPlan p{};
     const int mn = max_new < T ? max_new : T, room = PAGED_FEW_ROWS / group, lim = room < PAGED_FEW ? room : PAGED_FEW;
     p.many = mn > lim;
@@ -976,8 +981,17 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
         len = n > 0 ? (int)(((max_cached + n - 1) / n + 127) / 128 * 128) : 128;
         return (max_cached + len - 1) / len;
     };
-    p.few_splits = pieces((long long)nseq * H, 1024, 128, p.few_len);
+    // Pieces of the cache that fill the chip once: two workgroups per CU, one with more than 16 rows; for the append, which has nothing to join,
+    // smaller ones that even out unequal lengths.  16 sequences of up to 4000 tokens, 8 heads, 24 rows: 1024 workgroups 52 us, 512 48, 256 40; 8 of up to 3001,
+    // 16 heads, d = 64: 1024 41, 512 33 (join included); append to 16 of up to 4000, 16 heads: 1024 92, 512 93, 2048 81.
+    p.few_splits = pieces((long long)nseq * H, !attn ? 2048 : p.few_m * group <= 16 ? 512 : 256, 128, p.few_len);
     if (p.few_splits < 1) p.few_splits = 1;
+    p.few_waves = 4;
+    if (attn && p.few_m * group <= 16 && (size_t)max_cached * d * es <= PAGED_SHORT_BYTES) {
+        p.few_waves = max_cached <= 128 ? 4 : 8;
+        p.few_splits = 1;
+        p.few_len = max_cached > 128 ? max_cached : 128;
+    }
     p.tiles = T / 64 + nseq;
     p.row_blocks = (int)((long long)T * group / 128) + nseq;
     const long long blocks = (long long)T * group / 128;
@@ -985,14 +999,15 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
 
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
-    const size_t Hq = (size_t)H * group, rows = (size_t)T * Hq;
+    const size_t Hq = (size_t)H * group;
     if (p.few) {
-        const size_t slots = p.few_splits > 1 ? (size_t)p.few_splits * nseq * p.few_m * Hq : 0;
+        const size_t slots = attn && p.few_splits > 1 ? (size_t)p.few_splits * nseq * p.few_m * Hq : 0;
         take(p.few_o, slots * d * 4);
         take(p.few_ml, slots * 2 * 4);
     }
     if (p.many) {
         const size_t th = (size_t)p.tiles * H;
+        const size_t rows = attn ? (size_t)T * Hq : 0;
         take(p.x, rows * d * 4);
         take(p.crow, (size_t)T * H * 4);
         take(p.many_o, (size_t)(1 + p.many_splits) * rows * d * 4);
@@ -1000,7 +1015,7 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
         // kt, zt: fp32, or pairs of bf16 tiles; w and v are taken as they are with bf16
         for (size_t* f : {&p.kt, &p.zt}) take(*f, th * CHUNK * d * 4);
         for (size_t* f : {&p.wt, &p.vt}) take(*f, es == 4 ? th * CHUNK * d * 4 : 0);
-        take(p.sd, (size_t)p.tiles * Hq * CHUNK * CHUNK * 4);
+        take(p.sd, attn ? (size_t)p.tiles * Hq * CHUNK * CHUNK * 4 : 0);
         take(p.pt, (size_t)nseq * H * d * d * es);
     }
     p.total = off > 256 ? off : 256;
@@ -1010,7 +1025,7 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
 extern "C" size_t path_paged_workspace_bytes(int nseq, int T, int max_new, int max_cached, int H, int group, int d, path_dtype_t dt) {
     if (dt != PATH_F32 && dt != PATH_BF16) return 0;
     if (!paged_shape_ok(nseq, T, max_new, max_cached, H, group, d)) return 0;
-    return paged_plan(nseq, T, max_new, max_cached, H, group, d, dt == PATH_F32 ? 4 : 2).total;
+    return paged_plan(nseq, T, max_new, max_cached, H, group, d, dt == PATH_F32 ? 4 : 2, true).total;      // (the append needs no records)
 }
 
 static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1023,7 +1038,7 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     if (a.max_cached > (long long)a.per_seq * page_size) return PATH_ERR_SHAPE;
     if (a.attn && !(a.scale > 0.f)) return PATH_ERR_UNSUPPORTED;
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
-    const PagedPlan p = paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, dt == PATH_F32 ? 4 : 2);
+    const PagedPlan p = paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, dt == PATH_F32 ? 4 : 2, a.attn);
     if (workspace_bytes < p.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
     const void* al[] = {a.q, a.k, a.v, a.w, a.kpages, a.vpages, a.cpages, a.o};
     for (const void* ptr : al) if (misaligned(ptr)) return PATH_ERR_ALIGN;
@@ -1031,7 +1046,7 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     clear_inherited_error();
     char* const ws = static_cast<char*>(workspace);
     auto f = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
-    a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len;
+    a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len; a.few_waves = p.few_waves;
     a.few_o = f(p.few_o); a.few_ml = f(p.few_ml);
     a.tiles = p.tiles; a.row_blocks = p.row_blocks; a.joined = dt == PATH_BF16; a.many_splits = p.many_splits; a.many_len = p.many_len;
     a.x = f(p.x); a.crow = f(p.crow); a.many_o = f(p.many_o); a.many_ml = f(p.many_ml);

@@ -33,7 +33,7 @@ struct PagedArgs {
     float scale;
     int attn, append;
     // sequences of at most few_limit new tokens: the cache in few_splits pieces of few_len tokens; records of the pieces
-    int few_limit, few_m, few_splits, few_len;
+    int few_limit, few_m, few_splits, few_len, few_waves;
     float *few_o, *few_ml;                         // [split][nseq * few_m * H * G][d], [..][2]
     // the others: tiles of 64 new tokens (tile c of sequence s: first_tile(s) + c < tiles)
     int tiles, many_splits, many_len;

@@ -1,7 +1,7 @@
 // Attention of up to 64 rows over a paged cache, the append of up to 16 new tokens, and both in one pass.
 //
-// A workgroup has one key head of one sequence and a piece of its cache; its four waves take 32 cached tokens in turn (fp32: 16)
-// and meet only at the end.  Everything is 16x16 products, transposed so that activations stay in registers (lane l = 16 g + c):
+// A workgroup has one key head of one sequence and a piece of its cache; its four waves (eight for a short cache) take 32 cached tokens in turn (fp32 and
+// some others 16) and meet only at the end.  Everything is 16x16 products, transposed so that activations stay in registers (lane l = 16 g + c):
 //
 //     S (16 keys x 16 rows)   = K X^T      A = keys as loaded, B = X      result: lane has row c, keys 4 g + i
 //     C (16 tokens x 16 keys) = Z K^T      A = Z, B = the same registers  result: lane has key c, tokens 4 g + i
@@ -19,23 +19,25 @@ namespace path {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 
-template <typename T, int D, int NRT, bool BOTH> struct RowsCfg {
+template <typename T, int D, int NRT, bool BOTH, int NW> struct RowsCfg {
     static constexpr int ES = sizeof(T), ROWB = D * ES;
     static constexpr int KR = ROWB / 64;                 // 16-byte registers of 16 rows per lane
     static constexpr int U = ES == 2 && !(D == 128 && (NRT == 4 || BOTH)) ? 2 : 1;      // groups of 16 tokens per step: what 256 registers hold two steps of
     static constexpr int PPR = ROWB / 16;                // 16-byte pieces per row
-    static constexpr int VBYTES = 4 * U * 16 * ROWB;     // value tiles of the four waves
+    static constexpr int VBYTES = NW * U * 16 * ROWB;    // value tiles of the waves
     static constexpr int LDX = D + 4;
     // place of piece cp of row r in a value tile: spread over the banks for the reads of 4 (16-bit) or 1 (fp32) row per 16 lanes
     static __device__ __forceinline__ int piece(int r, int cp) {
         if (ES == 2) return r * PPR + (cp ^ (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)));
         return r * PPR + (cp ^ (((r >> 2) & 3) * 4));
     }
-    static constexpr size_t floats_before(bool append) { return (size_t)16 * D + (size_t)16 * NRT * LDX + (append ? 16 * LDX : 0) + 16 * NRT * 17 + 32 + 16 * NRT * 2; }
-    static constexpr size_t merge_bytes() { return (size_t)2 * (NRT * (D / 16) * 1024 + NRT * 512); }
+    static constexpr size_t floats_before(bool append) { return (size_t)2 * 16 * D + (size_t)16 * NRT * LDX + (append ? 16 * LDX : 0) + 16 * NRT * 17 + 32 + 16 * NRT * 2; }
+    static constexpr bool AT_ONCE = NRT <= 2;             // LDS has room for all waves' results
+    static constexpr size_t PER = NRT * (D / 16) * 1024 + NRT * 512;      // bytes of a wave's
+    static constexpr size_t merge_bytes() { return (AT_ONCE ? NW : NW / 2) * PER; }
     static constexpr size_t smem(bool append) {
-        const size_t f = (floats_before(append) * 4 + 255) / 256 * 256, a = VBYTES, b = merge_bytes(), c = 16 * D * 4;
-        return f + (a > b ? (a > c ? a : c) : (b > c ? b : c));
+        const size_t f = (floats_before(append) * 4 + 255) / 256 * 256, a = VBYTES, b = merge_bytes();
+        return f + (a > b ? a : b);
     }
 };
 
@@ -147,18 +149,20 @@ template <int D> struct Directions<float, D> {
 };
 
 // WALK: few new tokens, X and Z formed here; else 16 NRT rows of X from the workspace (no append).
-template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND>
-__global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && ATTN && APPEND) ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
-    using C = RowsCfg<T, D, NRT, ATTN && APPEND>;
+template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 && D == 128 && ATTN && APPEND) ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
+    using C = RowsCfg<T, D, NRT, ATTN && APPEND, NW>;
+    constexpr int NT = 64 * NW;
     constexpr int KR = C::KR, U = C::U, ROWB = C::ROWB, ROWS = 16 * NRT, LDX = C::LDX, DT = D / 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* const sw = reinterpret_cast<float*>(smem);           // [16][D] w of the new tokens
-    float* const sx = sw + 16 * D;                              // [ROWS][LDX] X; at the end O
+    float* const skn = sw + 16 * D;                             // [16][D] the new keys
+    float* const sx = skn + 16 * D;                             // [ROWS][LDX] X; at the end O
     float* const sz = sx + ROWS * LDX;                          // APPEND: [16][LDX] Z
     float* const sn = sz + (APPEND ? 16 * LDX : 0);             // [ROWS][17] logits with the new tokens
     float* const sb = sn + ROWS * 17;                           // [16] beta, [16] c of the new tokens
     float* const sml = sb + 32;                                 // [ROWS][2] maximum, sum
-    unsigned char* const sv = smem + (C::floats_before(APPEND) * 4 + 255) / 256 * 256;      // value tiles; the new keys; the waves' results
+    unsigned char* const sv = smem + (C::floats_before(APPEND) * 4 + 255) / 256 * 256;      // value tiles; the waves' results
 
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     const int Hq = a.H * a.G;
@@ -185,31 +189,34 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
         r0 = (tile - first_tile(a, s)) * 64 * a.G + sub * ROWS;
     }
     s = __builtin_amdgcn_readfirstlane(s);
+    // ---- the pages of this wave's steps, one in each lane (asked for up to the bound: the lengths may still be on their way) ----
+    const int* const table = a.table + (long long)s * a.per_seq;
+    const int len = WALK ? a.few_len : a.many_len, k0 = sp * len;
+    int ids[U];
+    auto fetch_ids = [&](int first) {
+        const int end = min(a.max_cached, k0 + len);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int pos = k0 + ((first + lane) * NW + wv) * 16 * U + 16 * u;
+            ids[u] = pos < end ? table[pos >> a.page_shift] : -1;
+        }
+    };
+    fetch_ids(0);
     const PagedSeq q = paged_seq(a, s);
     const int n = __builtin_amdgcn_readfirstlane(q.n), m = __builtin_amdgcn_readfirstlane(q.m), t0 = __builtin_amdgcn_readfirstlane(q.t0);
     if (WALK ? (m == 0 || m > a.few_limit) : (m <= a.few_limit || r0 >= m * a.G || r0 < 0)) return;
-    const int len = WALK ? a.few_len : a.many_len, used = WALK ? max(1, (n + len - 1) / len) : (n + len - 1) / len;
+    const int used = WALK ? max(1, (n + len - 1) / len) : (n + len - 1) / len;
     if (sp >= used) return;
     const bool last = WALK && sp == used - 1;
-    const int k0 = sp * len, k1 = min(n, k0 + len), rows = min(ROWS, m * a.G - r0);
+    const int k1 = min(n, k0 + len), rows = min(ROWS, m * a.G - r0);
 
-    // ---- the pages of this wave's steps, one in each lane; the first step's loads ----
-    const int* const table = a.table + (long long)s * a.per_seq;
-    int ids[U];
-    auto fetch_ids = [&](int first) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int pos = k0 + ((first + lane) * 4 + wv) * 16 * U + 16 * u;
-            ids[u] = pos < k1 ? table[pos >> a.page_shift] : -1;
-        }
-    };
     struct Step { u32x4 k[U][KR], v[ATTN ? U : 1][ATTN ? KR : 1]; f32x4 cc[U]; long long row[U]; int valid[U]; };
     const int koff = c * ROWB + 16 * g;
     auto fetch = [&](int i, Step& st) {
-        if ((i & 63) == 0) fetch_ids(i);
+        if (i > 0 && (i & 63) == 0) fetch_ids(i);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int pos = k0 + (i * 4 + wv) * 16 * U + 16 * u;
+            const int pos = k0 + (i * NW + wv) * 16 * U + 16 * u;
             const PagedGroup p = paged_group(a, __builtin_amdgcn_readlane(ids[u], i & 63), h, pos, k1);
             st.row[u] = p.row;
             st.valid[u] = p.valid;
@@ -228,32 +235,49 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
             }
         }
     };
-    const int steps = (max(0, k1 - k0 - wv * 16 * U) + 64 * U - 1) / (64 * U);
+    const int steps = (max(0, k1 - k0 - wv * 16 * U) + 16 * NW * U - 1) / (16 * NW * U);
     Step st0, st1;
-    fetch(0, st0);
 
-    // ---- X (and Z): the new tokens' transitions walked ----
+    // ---- X (and Z): the new tokens' transitions walked.  Their loads go out before the cache's, so that the walk is not behind those ----
     const T* const wg = reinterpret_cast<const T*>(a.w);
     const T* const kg = reinterpret_cast<const T*>(a.k);
     const T* const vg = reinterpret_cast<const T*>(a.v);
     constexpr int E = D / 16;
-    float* const skn = reinterpret_cast<float*>(sv);
+    long long new_row = -1;      // APPEND: where token 4 wv + g goes
     if constexpr (WALK) {
-        const bool keys = last && (ATTN || APPEND);
-        for (int i = tid; i < 16 * D / 4; i += 256) {
-            const int t = i / (D / 4), e = (i % (D / 4)) * 4;
-            float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
-            if (t < m) {
-                load_f32<4>(wg + ((long long)(t0 + t) * a.H + h) * D + e, x);
-                if (keys) load_f32<4>(kg + ((long long)(t0 + t) * a.H + h) * D + e, y);
-            }
+        if (APPEND && last && wv < 4 && wv * 4 + g < m) new_row = paged_row(a, s, h, n + wv * 4 + g);
+        constexpr int PER_THREAD = (16 * D / 4 + NT - 1) / NT;
+        float xw[PER_THREAD][4], xk[PER_THREAD][4], xq[E];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sw[t * D + e + j] = x[j];
-                if (keys) skn[t * D + e + j] = y[j];
+        for (int j = 0; j < PER_THREAD; ++j) {
+            const int i = j * NT + tid, t = i / (D / 4), e = (i % (D / 4)) * 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) xw[j][k] = xk[j][k] = 0.f;
+            if (t < m) {
+                load_f32<4>(wg + ((long long)(t0 + t) * a.H + h) * D + e, xw[j]);
+                if (last) load_f32<4>(kg + ((long long)(t0 + t) * a.H + h) * D + e, xk[j]);
             }
         }
-        if (tid < 16) sb[tid] = tid < m ? (float)reinterpret_cast<const T*>(a.beta)[(long long)(t0 + tid) * a.H + h] : 0.f;
+        const float xb = tid < m ? (float)reinterpret_cast<const T*>(a.beta)[(long long)(t0 + tid) * a.H + h] : 0.f;
+        auto query = [&](int r) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) xq[e] = 0.f;
+            if (r < rows) load_f32<E>(reinterpret_cast<const T*>(a.q) + ((long long)(t0 + r / a.G) * Hq + h * a.G + r % a.G) * D + c * E, xq);
+        };
+        if constexpr (ATTN) query(wv * 4 + g);
+        fetch(0, st0);
+#pragma unroll
+        for (int j = 0; j < PER_THREAD; ++j) {
+            const int i = j * NT + tid;
+            if (i < 16 * D / 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    sw[i * 4 + k] = xw[j][k];
+                    if (last) skn[i * 4 + k] = xk[j][k];
+                }
+            }
+        }
+        if (tid < 16) sb[tid] = xb;
         if (a.cpages && tid == 64) {
             const long long r = n > 0 ? paged_row(a, s, h, n - 1) : -1;
             float x = r >= 0 ? a.cpages[r] : 0.f;
@@ -264,12 +288,12 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
         }
         __syncthreads();
         if constexpr (ATTN) {
-            for (int r = wv * 4 + g; r < ROWS; r += 16) {
+            for (int r = wv * 4 + g; r < ROWS; r += 4 * NW) {
                 const int tok = r / a.G;
                 float x[E];
+                if (r >= 4 * NW) query(r);
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = 0.f;
-                if (r < rows) load_f32<E>(reinterpret_cast<const T*>(a.q) + ((long long)(t0 + tok) * Hq + h * a.G + r % a.G) * D + c * E, x);
+                for (int e = 0; e < E; ++e) x[e] = xq[e];
                 for (int t = m - 1; t >= 0; --t) {
                     if (last) {
                         float y = 0.f;
@@ -289,7 +313,7 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
                 for (int e = 0; e < E; ++e) sx[r * LDX + c * E + e] = x[e];
             }
         }
-        if constexpr (APPEND) {
+        if (APPEND && wv < 4) {
             const int t1 = wv * 4 + g;
             float x[E];
 #pragma unroll
@@ -315,7 +339,7 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[e] -= y * sw[t * D + c * E + e];
                 }
-                const long long r = paged_row(a, s, h, n + t1);
+                const long long r = new_row;
                 if (r >= 0) {
                     T* const kd = reinterpret_cast<T*>(a.kpages) + r * D + c * E;
                     T* const vd = reinterpret_cast<T*>(a.vpages) + r * D + c * E;
@@ -328,7 +352,8 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
         }
         __syncthreads();
     } else {
-        for (int i = tid; i < ROWS * D / 4; i += 256) {
+        fetch(0, st0);
+        for (int i = tid; i < ROWS * D / 4; i += NT) {
             const int r = i / (D / 4), e = (i % (D / 4)) * 4, row = r0 + r;
             f32x4 x = {0.f, 0.f, 0.f, 0.f};
             if (r < rows) x = *reinterpret_cast<const f32x4*>(a.x + ((long long)(t0 + row / a.G) * Hq + h * a.G + row % a.G) * D + e);
@@ -359,7 +384,6 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
         W.load(sw, c, g);
     }
     unsigned char* const myv = sv + wv * (U * 16 * ROWB);
-    __syncthreads();      // (the new keys lay where the value tiles go)
 
     auto process = [&](Step& st) {
         if constexpr (ATTN) {
@@ -444,12 +468,23 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
     }
     if constexpr (!ATTN) return;
 
-    // ---- the four waves' results: 2, 3 into 0, 1, then 1 into 0 ----
+    // ---- the waves' results: the upper half's into the lower's, until one is left ----
     if constexpr (ATTN) {
 #pragma unroll
     for (int t = 0; t < NRT; ++t) l_run[t] = sum_rows(l_run[t]);
-    constexpr size_t PER = C::merge_bytes() / 2;
-    for (int half = 2; half >= 1; half >>= 1) {
+    constexpr size_t PER = C::PER;
+    if constexpr (C::AT_ONCE) {      // all results to LDS; whoever writes an element joins it
+        __syncthreads();
+        float* const p = reinterpret_cast<float*>(sv + wv * PER);
+#pragma unroll
+        for (int t = 0; t < NRT; ++t) {
+#pragma unroll
+            for (int b = 0; b < DT; ++b) *reinterpret_cast<f32x4*>(p + (t * DT + b) * 256 + lane * 4) = O[t][b];
+            p[NRT * DT * 256 + t * 128 + lane] = m_run[t];
+            p[NRT * DT * 256 + t * 128 + 64 + lane] = l_run[t];
+        }
+    } else {
+    for (int half = NW / 2; half >= 1; half >>= 1) {
         __syncthreads();
         if (wv >= half && wv < 2 * half) {
             float* const p = reinterpret_cast<float*>(sv + (wv - half) * PER);
@@ -484,14 +519,37 @@ __global__ __launch_bounds__(256, NRT == 1 && !(sizeof(T) == 4 && D == 128 && AT
             if (g == 0) { sml[2 * (16 * t + c)] = m_run[t]; sml[2 * (16 * t + c) + 1] = l_run[t]; }
         }
     }
+    }
     __syncthreads();
 
     // ---- the new tokens' keys and values; the result, or this piece's record ----
-    for (int i = tid; i < rows * (D / 4); i += 256) {
+    for (int i = tid; i < rows * (D / 4); i += NT) {
         const int r = i / (D / 4), e = (i % (D / 4)) * 4, row = r0 + r, tok = row / a.G;
         const long long at = (long long)(t0 + tok) * Hq + h * a.G + row % a.G;
-        f32x4 o = *reinterpret_cast<const f32x4*>(sx + r * LDX + e);
-        float mx = sml[2 * r], l = sml[2 * r + 1];
+        f32x4 o;
+        float mx, l;
+        if constexpr (C::AT_ONCE) {
+            const int t = r >> 4, from = 16 * ((e & 15) >> 2) + (r & 15);      // the lane that has it
+            const float* const p = reinterpret_cast<const float*>(sv);
+            constexpr int STEP = PER / 4, ML = NRT * DT * 256;
+            float mw[NW];
+            mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) { mw[w] = p[w * STEP + ML + t * 128 + from]; mx = fmaxf(mx, mw[w]); }
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            o = f32x4{0.f, 0.f, 0.f, 0.f};
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = __builtin_amdgcn_exp2f(mw[w] - ref);
+                l += f * p[w * STEP + ML + t * 128 + 64 + from];
+                o += *reinterpret_cast<const f32x4*>(p + w * STEP + (t * DT + (e >> 4)) * 256 + from * 4) * f;
+            }
+        } else {
+            o = *reinterpret_cast<const f32x4*>(sx + r * LDX + e);
+            mx = sml[2 * r];
+            l = sml[2 * r + 1];
+        }
         if (last) {
             float now = mx;
             auto logit = [&](int t) { return sn[r * 17 + t] * sl2 + (a.cpages ? (sb[16 + tok] - sb[16 + t]) * LOG2E : 0.f); };
@@ -584,14 +642,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     if (lane == 0) a.lse[at] = (mx + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND>
+template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND, int NW = 4>
 static hipError_t launch_rows_t(const PagedArgs& a, long long grid, hipStream_t st) {
-    constexpr size_t bytes = RowsCfg<T, D, NRT, ATTN && APPEND>::smem(APPEND);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_rows_kernel<T, D, NRT, WALK, ATTN, APPEND>),
+    constexpr size_t bytes = RowsCfg<T, D, NRT, ATTN && APPEND, NW>::smem(APPEND);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_rows_kernel<T, D, NRT, WALK, ATTN, APPEND, NW>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((paged_rows_kernel<T, D, NRT, WALK, ATTN, APPEND>), dim3((unsigned)grid), dim3(256), bytes, st, a);
+    hipLaunchKernelGGL((paged_rows_kernel<T, D, NRT, WALK, ATTN, APPEND, NW>), dim3((unsigned)grid), dim3(64 * NW), bytes, st, a);
     return hipGetLastError();
 }
 template <typename T, int D>
@@ -599,6 +657,7 @@ static hipError_t launch_rows_d(const PagedArgs& a, hipStream_t st) {
     const long long grid = (long long)a.nseq * a.H * a.few_splits;
     const int rows = a.few_m * a.G;
     if (!a.attn) return launch_rows_t<T, D, 1, true, false, true>(a, grid, st);
+    if (rows <= 16 && a.few_waves == 8) return a.append ? launch_rows_t<T, D, 1, true, true, true, 8>(a, grid, st) : launch_rows_t<T, D, 1, true, true, false, 8>(a, grid, st);
     if (a.append) return rows <= 16 ? launch_rows_t<T, D, 1, true, true, true>(a, grid, st) : rows <= 32 ? launch_rows_t<T, D, 2, true, true, true>(a, grid, st) : launch_rows_t<T, D, 4, true, true, true>(a, grid, st);
     return rows <= 16 ? launch_rows_t<T, D, 1, true, true, false>(a, grid, st) : rows <= 32 ? launch_rows_t<T, D, 2, true, true, false>(a, grid, st) : launch_rows_t<T, D, 4, true, true, false>(a, grid, st);
 }
