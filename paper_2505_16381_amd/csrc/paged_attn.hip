@@ -11,7 +11,10 @@
 // by 2e-6 of itself and more, 1e-7 so).  P is one bf16 number, as everywhere in the library.
 // A piece of 16 rows in LDS is 16-byte pieces exchanged as in lds_tile.h, such that neither fragments along a row nor transposing reads
 // meet on a bank; the copies fetch them in that order.  Past the end of the sequence and in holes they bring zeros (the buffer's bounds).
-// Two workgroups share a CU (64 KB of LDS, 256 registers): the softmax of one runs under the products of the other.  The
+// Two workgroups share a CU (64 KB of LDS, 256 registers): the softmax of one runs under the products of the other.  512 rows over 8192 tokens and 2048 over
+// 16384, 16 query heads, d = 128: 61 and 380 us, 730 TFLOP/s of logits and P V or 1.1 PFLOP/s of products; bound by the matrix units at the clock that
+// power leaves them (half of their cycles): without X's second part 82 us less, with a stage's exponentials put between the next one's products, by hand or in a
+// pipeline of half stages, the same.  The
 // accumulator is rescaled only when a row's maximum has grown by more than 8 (2^8 in P and its sum is exact enough: both are floating).
 // Numbered so that the row blocks of a key head and piece run on one XCD, which then reads its keys and values once from memory.
 #include <type_traits>
@@ -128,15 +131,15 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a) {
         const int4 valid = *reinterpret_cast<const int4*>(sval + PAR * 4);
         if (u + 1 < stages) fetch(u + 1);
         f32x16 S[2];
+        S[0] = S[1] = zero16();
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            S[kb] = zero16();
-#pragma unroll
-            for (int i = 0; i < DS; ++i) {
-                const bf16x8 k = *reinterpret_cast<const bf16x8*>(smem + BUF + kb * 32 * ROWB + (kaddr ^ (32 * i)));
-                S[kb] = Tr<bf16_t>::mma(k, xh[i], S[kb]);
-                S[kb] = Tr<bf16_t>::mma(k, xl[i], S[kb]);
-            }
+        for (int i = 0; i < DS; ++i) {      // two chains of products, neither waiting for its own last one
+            const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(smem + BUF + (kaddr ^ (32 * i)));
+            const bf16x8 k1 = *reinterpret_cast<const bf16x8*>(smem + BUF + 32 * ROWB + (kaddr ^ (32 * i)));
+            S[0] = Tr<bf16_t>::mma(k0, xh[i], S[0]);
+            S[1] = Tr<bf16_t>::mma(k1, xh[i], S[1]);
+            S[0] = Tr<bf16_t>::mma(k0, xl[i], S[0]);
+            S[1] = Tr<bf16_t>::mma(k1, xl[i], S[1]);
         }
         float top = -INFINITY;
         const bool whole = __builtin_amdgcn_readfirstlane(min(min(valid.x, valid.y), min(valid.z, valid.w))) == PAGED_GROUP;
@@ -148,8 +151,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a) {
                 if (GATES) ck = *reinterpret_cast<const f32x4*>(smem + 4 * TILE + PAR * PATTN_KEYS * 4 + (32 * kb + 8 * g + 4 * h) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    S[kb][4 * g + e] *= sl2;
-                    if (GATES) S[kb][4 * g + e] += (crow - ck[e]) * LOG2E;
+                    if (GATES) S[kb][4 * g + e] = S[kb][4 * g + e] * sl2 + (crow - ck[e]) * LOG2E;
                 }
             }
         if (!whole)
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a) {
             for (int j = 0; j < 16; ++j) top = fmaxf(top, S[kb][j]);
         {
             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * (GATES ? 1.f : sl2);
         }
         if (__any(top > m_run + 8.f)) {
             const float now = fmaxf(m_run, top), f = __builtin_amdgcn_exp2f(m_run - (now == -INFINITY ? 0.f : now));
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a) {
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                S[kb][j] = __builtin_amdgcn_exp2f(S[kb][j] - ref);
+                S[kb][j] = __builtin_amdgcn_exp2f(GATES ? S[kb][j] - ref : S[kb][j] * sl2 - ref);
                 sum += S[kb][j];
             }
             pack_block<bf16_t>(S[kb], P[kb]);
@@ -190,18 +192,18 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedArgs a) {
         l_run += sum;
         auto values = [&](auto bt) {
             constexpr int b = decltype(bt)::value;
-            const unsigned va = vaddr ^ (64 * b), vb = (va ^ 32) + 8 * ROWB;
-            bf16x8 v[4];
+            const unsigned va = vaddr ^ (64 * b), vb = (va ^ 32) + 8 * ROWB, vc = vaddr ^ (64 * b + 64), vd = (vc ^ 32) + 8 * ROWB;
+            bf16x8 v[4], w[4];
             values_tr<BUF + TILE, ROWB>(va, vb, v);
+            values_tr<BUF + TILE, ROWB>(vc, vd, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) O[b] = Tr<bf16_t>::mma(v[i], P[i >> 1][i & 1], O[b]);
+            for (int i = 0; i < 4; ++i) {
+                O[b] = Tr<bf16_t>::mma(v[i], P[i >> 1][i & 1], O[b]);
+                O[b + 1] = Tr<bf16_t>::mma(w[i], P[i >> 1][i & 1], O[b + 1]);
+            }
         };
         values(std::integral_constant<int, 0>());
-        values(std::integral_constant<int, 1>());
-        if constexpr (DB == 4) {
-            values(std::integral_constant<int, 2>());
-            values(std::integral_constant<int, 3>());
-        }
+        if constexpr (DB == 4) values(std::integral_constant<int, 2>());
     };
     for (int u = 0; u < stages; u += 2) {
         stage(u, std::integral_constant<int, 0>());

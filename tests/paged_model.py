@@ -96,3 +96,10 @@ def expect(x, scale, op):
                 if cp is not None:
                     cp[at, :, i % page] = c[:, t]
     return o, lse, kp, vp, cp
+
+
+def drop_pages(x, holes, num_pages):
+    """The batch with table entries at (sequence, page) in `holes` pointing outside the pool."""
+    for i, (s, p) in enumerate(holes):
+        x["page_table"][s, p] = (-1, num_pages, num_pages + 12345, -2 ** 31)[i % 4]
+    return x
