@@ -551,27 +551,25 @@ def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) ->
     return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
 
 
-def _paged_tensor(name, t, shape, dtype, dev):
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{name} is {tuple(shape)}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
-    if t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
-    return t.data_ptr()
+def _paged_refuse(named, dev):
+    for name, t, shape, dtype in named:
+        if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+            raise ValueError(f"{name} is {tuple(shape)}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
+        if t is not None and (t.get_device() != dev or dev < 0 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
 
 
 def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream):
-    """Checks that every tensor is what the kernels take it for, and calls; (a call of short kernels is bound by this function: one look at each)."""
+    """Checks that every tensor is what the kernels take it for, and calls.  A call of short kernels is bound by this function, so sizes, types and places
+    are looked at in one go, and by name only where something is wrong."""
     import torch
     if k.dim() != 3 or kpages.dim() != 4 or page_table.dim() != 2 or (q is not None and q.dim() != 3):
         raise ValueError("q, k are [T,heads,d], kpages [num_pages,H,page_size,d], page_table [nseq,pages_per_seq]")
-    shape, pages, td, i32, dev = k.shape, kpages.shape, k.dtype, torch.int32, k.get_device()
-    T, H, d = shape
-    num_pages, _, page_size, _ = pages
+    (T, H, d), td, f32, i32, dev = k.shape, k.dtype, torch.float32, torch.int32, k.get_device()
+    num_pages, pH, page_size, pd = kpages.shape
     nseq, per_seq = page_table.shape
-    dt = PATH_BF16 if td == torch.bfloat16 else _dt_of(k)
-    if dev < 0:
-        raise ValueError("k must be on a GPU")
-    max_new, max_cached, group = int(max_new), int(max_cached), 1
+    dt = PATH_BF16 if td is torch.bfloat16 else _dt_of(k)
+    group, n, pool = 1, T * H * d, num_pages * H * page_size * d
     if q is not None:
         if q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
             raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
@@ -579,24 +577,35 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
         if o is None:
             o = torch.empty_like(q)
         if lse is None:
-            lse = q.new_empty((T, H * group), dtype=torch.float32)
+            lse = q.new_empty((T, H * group), dtype=f32)
     if (log_f is None) != (cpages is None):
         raise ValueError("log_f and cpages go together")
-    one = shape[:2]
-    args = [_paged_tensor("k", k, shape, td, dev), _paged_tensor("v", v, shape, td, dev), _paged_tensor("w", w, shape, td, dev),
-            _paged_tensor("beta", beta, one, td, dev), None if log_f is None else _paged_tensor("log_f", log_f, one, td, dev),
-            _paged_tensor("kpages", kpages, (num_pages, H, page_size, d), td, dev), _paged_tensor("vpages", vpages, pages, td, dev),
-            None if cpages is None else _paged_tensor("cpages", cpages, pages[:3], torch.float32, dev),
-            _paged_tensor("page_table", page_table, (nseq, per_seq), i32, dev), _paged_tensor("cached", cached, (nseq,), i32, dev),
-            _paged_tensor("cu_new", cu_new, (nseq + 1,), i32, dev)]
+    looked = [(k, n, td), (v, n, td), (w, n, td), (beta, T * H, td), (kpages, pool, td), (vpages, pool, td), (page_table, nseq * per_seq, i32), (cached, nseq, i32),
+              (cu_new, nseq + 1, i32)]
+    if log_f is not None:
+        looked += [(log_f, T * H, td), (cpages, num_pages * H * page_size, f32)]
     if q is not None:
-        args = [_paged_tensor("q", q, q.shape, td, dev), *args, _paged_tensor("o", o, q.shape, td, dev), _paged_tensor("lse", lse, (T, H * group), torch.float32, dev)]
+        looked += [(q, n * group, td), (o, n * group, td), (lse, T * H * group, f32)]
+    fine = pH == H and pd == d and dev >= 0 and v.shape == k.shape and vpages.shape == kpages.shape
+    for t, size, dtype in looked:
+        if t.numel() != size or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+            fine = False
+    if not fine:
+        _paged_refuse([("k", k, (T, H, d), td), ("v", v, (T, H, d), td), ("w", w, (T, H, d), td), ("beta", beta, (T, H), td), ("log_f", log_f, (T, H), td),
+                       ("kpages", kpages, (num_pages, H, page_size, d), td), ("vpages", vpages, (num_pages, H, page_size, d), td),
+                       ("cpages", cpages, (num_pages, H, page_size), f32), ("page_table", page_table, (nseq, per_seq), i32), ("cached", cached, (nseq,), i32),
+                       ("cu_new", cu_new, (nseq + 1,), i32), ("q", q, (T, H * group, d), td), ("o", o, (T, H * group, d), td), ("lse", lse, (T, H * group), f32)], dev)
+    max_new, max_cached = int(max_new), int(max_cached)
     if workspace is None:
         workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the GPU that k is on")
     if T == 0:
         return o, lse
+    args = [k.data_ptr(), v.data_ptr(), w.data_ptr(), beta.data_ptr(), _opt(log_f), kpages.data_ptr(), vpages.data_ptr(), _opt(cpages), page_table.data_ptr(),
+            cached.data_ptr(), cu_new.data_ptr()]
+    if q is not None:
+        args = [q.data_ptr(), *args, o.data_ptr(), lse.data_ptr()]
     args += [nseq, T, max_new, max_cached, num_pages, page_size, per_seq, H]
     args += [d] if q is None else [group, d, float(d ** -0.5 if scale is None else scale)]
     args += [dt, workspace.data_ptr(), workspace.numel() * workspace.element_size()]

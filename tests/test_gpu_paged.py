@@ -339,3 +339,33 @@ def test_a_call_while_another_device_is_current(gpu):
         got = call(pa, "attn", y, 2, 50, 0.1)
     torch.cuda.synchronize(0)
     assert torch.equal(got[0], want[0])
+
+
+def test_binding_refuses_tensors_of_another_kind(gpu):
+    torch, pa = gpu
+    y = to_gpu(torch, pm.batch([20], [3], 2, 1, 64, 16, "bf16", True))
+    names = ("q", "k", "v", "w", "beta", "kpages", "vpages", "page_table", "cached", "cu_new")
+    run = lambda **k: pa.path_paged_attn(*[{**y, **k}[n] for n in names], 3, 20, log_f=k.get("log_f", y["log_f"]), cpages=k.get("cpages", y["cpages"]),
+                                         o=k.get("o"), lse=k.get("lse"), workspace=k.get("workspace"))
+    run()
+    for n in ("q", "v", "w", "beta", "kpages", "vpages", "log_f"):
+        with pytest.raises(ValueError):
+            run(**{n: y[n].float()})
+        with pytest.raises(ValueError):
+            run(**{n: y[n][..., :-1]})
+        with pytest.raises(ValueError):
+            run(**{n: y[n].cpu()})
+    with pytest.raises(ValueError):
+        run(w=y["w"].transpose(0, 1).contiguous().transpose(0, 1))
+    for n in ("page_table", "cached", "cu_new"):
+        with pytest.raises(ValueError):
+            run(**{n: y[n].long()})
+    with pytest.raises(ValueError):
+        run(cached=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        run(cpages=None)
+    with pytest.raises(ValueError):
+        run(o=torch.empty_like(y["q"])[:2])
+    with pytest.raises(pa.PathAttnError) as e:
+        run(workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    assert e.value.code in (1, 5)
