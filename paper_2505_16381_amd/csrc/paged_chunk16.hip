@@ -167,30 +167,40 @@ __global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs
         mm_pairs<64, false, false>(v, Dt, LT, 32 * rb, Tp, LT, 32 * cb, l32, hh);
         each(v, [&](int r, int k, float x) { put_pair(Ut, r * LT + k, x); });
     }
-    typedef bf16_t V4 __attribute__((ext_vector_type(4)));
-    auto turned_product = [&](int b, const Pair& B, auto f) {      // block b of W^T B^T: f(row of B, first of 4 d, values)
-        const int r0 = 32 * (b >> 1), c0 = 32 * (b & 1);
+    auto product = [&](int b, const Pair& B) {      // block b of B W: rows 32 (b % 2), d 32 (b / 2)
         f32x16 v = zero16();
-        mm<bf16_t, 64, true, false>(v, W, LD, r0, B.hi, LT, c0, l32, hh);
-        mm<bf16_t, 64, true, false>(v, W, LD, r0, B.lo, LT, c0, l32, hh);
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) f(c0 + l32, r0 + acc_row(j, hh), f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]});
+        mm<bf16_t, 64, false, true>(v, B.hi, LT, 32 * (b & 1), W, LD, 32 * (b >> 1), l32, hh);
+        mm<bf16_t, 64, false, true>(v, B.lo, LT, 32 * (b & 1), W, LD, 32 * (b >> 1), l32, hh);
+        return v;
     };
-    auto store_pair = [&](bf16_t* p, int i, f32x4 v) {
-        V4 x, y;
+    // A block as a pair to memory: neighbouring lanes exchange, so that each has two columns of one of two rows, and 64 bytes of a row go out in one piece.
+    // (Four rows' eight bytes per lane, the transposed product, went out in pieces of sixteen: the stores took 4 us more of a tile's 17.)
+    auto store_pair = [&](bf16_t* p, int b, const f32x16& v) {
+        const bool even = !(lane & 1);
+        typedef bf16_t V2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = (bf16_t)v[e]; y[e] = (bf16_t)(v[e] - (float)x[e]); }
-        *reinterpret_cast<V4*>(p + i) = x;
-        *reinterpret_cast<V4*>(p + lo + i) = y;
+        for (int j = 0; j < 16; j += 2) {
+            const float got = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(even ? v[j + 1] : v[j]), 0xb1, 0xf, 0xf, true));
+            const float x0 = even ? v[j] : got, x1 = even ? got : v[j + 1];
+            bf16_t* const at = p + (32 * (b & 1) + acc_row(j, hh) + (even ? 0 : 1)) * D + 32 * (b >> 1) + (l32 & ~1);
+            V2 x, y;
+            x[0] = (bf16_t)x0;
+            x[1] = (bf16_t)x1;
+            y[0] = (bf16_t)(x0 - (float)x[0]);
+            y[1] = (bf16_t)(x1 - (float)x[1]);
+            *reinterpret_cast<V2*>(at) = x;
+            *reinterpret_cast<V2*>(at + lo) = y;
+        }
+    };
+    auto less = [&](const bf16_t* M, int b, f32x16 v) {      // the block of M - v
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = (float)M[(32 * (b & 1) + acc_row(j, hh)) * LD + 32 * (b >> 1) + l32] - v[j];
+        return v;
     };
     if (!first)      // -Z = -T W
-        for (int b = wv - 4; b < D / 16; b += 4) turned_product(b, Tp, [&](int t, int d, f32x4 v) { store_pair(zt, t * D + d, -v); });
+        for (int b = wv - 4; b < D / 16; b += 4) store_pair(zt, b, -product(b, Tp));
     __syncthreads();
-    for (int b = wv; b < D / 16; b += 8)      // carried keys K - (T D)^T W
-        turned_product(b, Ut, [&](int t, int d, f32x4 v) {
-            const V4 k = *reinterpret_cast<const V4*>(K + t * LD + d);
-            store_pair(kt, t * D + d, f32x4{(float)k[0], (float)k[1], (float)k[2], (float)k[3]} - v);
-        });
+    for (int b = wv; b < D / 16; b += 8) store_pair(kt, b, less(K, b, product(b, Ut)));      // carried keys K - (T D)^T W
     if (!a.attn) return;
     for (int gq = 0; gq < a.G; ++gq) {
         const int hq = h * a.G + gq;
@@ -201,25 +211,26 @@ __global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs
             if (first) lower();
             __syncthreads();
         }
-        if (first) {      // logits, transposed: K Q^T - (T D)^T L^T
+        if (first) {      // logits: Q K^T - L (T D)
             f32x16 v = zero16(), u = zero16();
-            mm<bf16_t, D, false, false>(v, K, LD, 32 * rb, Q, LD, 32 * cb, l32, hh);
-            mm_pairs<64, false, false>(u, Ut, LT, 32 * rb, Lp, LT, 32 * cb, l32, hh);
-            float* const sd = a.sd + ((size_t)tile * Hq + hq) * 4096 + (32 * cb + l32) * 64 + 32 * rb;
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) *reinterpret_cast<f32x4*>(sd + acc_row(j, hh)) = f32x4{v[j] - u[j], v[j + 1] - u[j + 1], v[j + 2] - u[j + 2], v[j + 3] - u[j + 3]};
+            mm<bf16_t, D, false, false>(v, Q, LD, 32 * rb, K, LD, 32 * cb, l32, hh);
+            mm_pairs<64, false, false>(u, Lp, LT, 32 * rb, Ut, LT, 32 * cb, l32, hh);
+            float* const sd = a.sd + ((size_t)tile * Hq + hq) * 4096;
+            each(v - u, [&](int r, int k, float x) { sd[r * 64 + k] = x; });
         } else {          // L T
             f32x16 v = zero16();
             mm_pairs<64, false, true>(v, Lp, LT, 32 * rb, Tp, LT, 32 * cb, l32, hh);
             each(v, [&](int r, int k, float x) { put_pair(LTp, r * LT + k, x); });
         }
         __syncthreads();
-        for (int b = wv; b < D / 16; b += 8)      // X = Q - (L T) W
-            turned_product(b, LTp, [&](int t, int d, f32x4 v) {
-                if (t >= m) return;
-                const V4 k = *reinterpret_cast<const V4*>(Q + t * LD + d);
-                *reinterpret_cast<f32x4*>(a.x + ((long long)(tok0 + t) * Hq + hq) * D + d) = f32x4{(float)k[0], (float)k[1], (float)k[2], (float)k[3]} - v;
-            });
+        for (int b = wv; b < D / 16; b += 8) {      // X = Q - (L T) W
+            const f32x16 v = less(Q, b, product(b, LTp));
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int t = 32 * (b & 1) + acc_row(j, hh);
+                if (t < m) a.x[((long long)(tok0 + t) * Hq + hq) * D + 32 * (b >> 1) + l32] = v[j];
+            }
+        }
     }
 }
 
