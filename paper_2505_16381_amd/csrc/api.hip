@@ -950,7 +950,7 @@ extern "C" path_status_t path_attn_varlen_bwd(const void* q, const void* k, cons
 namespace {
 struct PagedPlan {
     bool few, many;              // which of the two ways sequences may go
-    int few_limit, few_m, few_splits, few_len, few_waves, tiles, row_blocks, many_splits, many_len;
+    int few_limit, few_m, few_splits, few_len, few_waves, tiles, row_blocks, many_splits, many_len, refresh_len;
     size_t few_o, few_ml, x, crow, many_o, many_ml, kt, wt, zt, vt, sd, pt, total;
 };
 }  // namespace
@@ -996,6 +996,8 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
     p.row_blocks = (int)((long long)T * group / 128) + nseq;
     const long long blocks = (long long)T * group / 128;
     p.many_splits = pieces((blocks > 1 ? blocks : 1) * H, 512, 512, p.many_len);
+    pieces((long long)nseq * H, 256, 128, p.refresh_len);      // (each loads the d x d matrix: 16 heads of 8192 tokens, 256 workgroups 56 us with the rest of the call, 512 60, 1024 65)
+    if (p.refresh_len > 4096) p.refresh_len = 4096;
 
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
@@ -1046,7 +1048,7 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     clear_inherited_error();
     char* const ws = static_cast<char*>(workspace);
     auto f = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
-    a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len; a.few_waves = p.few_waves;
+    a.few_limit = p.few_limit; a.few_m = p.few_m; a.few_splits = p.few_splits; a.few_len = p.few_len; a.few_waves = p.few_waves; a.refresh_len = p.refresh_len;
     a.few_o = f(p.few_o); a.few_ml = f(p.few_ml);
     a.tiles = p.tiles; a.row_blocks = p.row_blocks; a.joined = dt == PATH_BF16; a.many_splits = p.many_splits; a.many_len = p.many_len;
     a.x = f(p.x); a.crow = f(p.crow); a.many_o = f(p.many_o); a.many_ml = f(p.many_ml);

@@ -37,6 +37,7 @@ struct PagedArgs {
     float *few_o, *few_ml;                         // [split][nseq * few_m * H * G][d], [..][2]
     // the others: tiles of 64 new tokens (tile c of sequence s: first_tile(s) + c < tiles)
     int tiles, many_splits, many_len;
+    int refresh_len;                               // cached tokens per workgroup that carries them on, at most 4096
     int row_blocks;                                // blocks of 128 rows, first_block(s) + i < row_blocks
     int joined;                                    // the attention kernel joins a single piece with record 0 itself
     float *x, *crow;                               // [T][H*G][d] X; [T][H] c of the new tokens (gates)

@@ -9,8 +9,6 @@
 
 namespace path {
 
-constexpr int REFRESH_KEYS = 1024;      // cached tokens per workgroup
-
 template <typename T, int D> constexpr size_t refresh_smem() { return sizeof(T) == 4 ? (size_t)D * (D + 4) * 4 : 0; }
 
 template <typename T, int D>
@@ -18,18 +16,18 @@ __global__ __launch_bounds__(256, 2) void paged_refresh_kernel(PagedArgs a) {
     constexpr int ROWB = D * (int)sizeof(T), KR = ROWB / 64;
     extern __shared__ __attribute__((aligned(16))) float sm[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    const int hs = blockIdx.x % (a.nseq * a.H), s = hs / a.H, h = hs % a.H, k0 = blockIdx.x / (a.nseq * a.H) * REFRESH_KEYS;
+    const int hs = blockIdx.x % (a.nseq * a.H), s = hs / a.H, h = hs % a.H, k0 = blockIdx.x / (a.nseq * a.H) * a.refresh_len;
     const PagedSeq q = paged_seq(a, s);
     const int n = __builtin_amdgcn_readfirstlane(q.n);
     if (q.m <= a.few_limit || k0 >= n) return;
-    const int k1 = min(n, k0 + REFRESH_KEYS);
+    const int k1 = min(n, k0 + a.refresh_len);
     const int* const table = a.table + (long long)s * a.per_seq;
-    const int mine = k0 + (lane * 4 + wv) * 16, id = lane < REFRESH_KEYS / 64 && mine < k1 ? table[mine >> a.page_shift] : -1;
+    const int mine = k0 + (lane * 4 + wv) * 16, id = mine < k1 ? table[mine >> a.page_shift] : -1;
     const int koff = c * ROWB + 16 * g;
-    u32x4 k[KR], kn[KR];
+    u32x4 k[KR], kn[KR], k2[KR], k3[KR];
     auto fetch = [&](int i, u32x4* k) {
         const int pos = k0 + (i * 4 + wv) * 16;
-        const PagedGroup p = paged_group(a, __builtin_amdgcn_readlane(id, i & 63), h, pos, k1);
+        const PagedGroup p = paged_group(a, i < 64 ? __builtin_amdgcn_readlane(id, i & 63) : -1, h, pos, k1);
         const __amdgpu_buffer_rsrc_t r = paged_rsrc(a.kpages, p.row, p.valid, ROWB);
 #pragma unroll
         for (int j = 0; j < KR; ++j) k[j] = __builtin_amdgcn_raw_buffer_load_b128(r, koff + 64 * j, 0, 0);
@@ -37,6 +35,7 @@ __global__ __launch_bounds__(256, 2) void paged_refresh_kernel(PagedArgs a) {
     };
     PagedGroup p = fetch(0, k);
     if constexpr (sizeof(T) == 2) {
+        PagedGroup p1 = fetch(1, kn), p2 = fetch(2, k2);
         const half_t* const M = reinterpret_cast<const half_t*>(a.pt) + (size_t)hs * D * D;
         halfx8 f[D / 16][D / 32];
 #pragma unroll
@@ -44,8 +43,7 @@ __global__ __launch_bounds__(256, 2) void paged_refresh_kernel(PagedArgs a) {
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
                 f[t][j] = *reinterpret_cast<const halfx8*>(M + (32 * (t >> 1) + 8 * (c >> 2) + 4 * (t & 1) + (c & 3)) * D + 32 * j + 8 * g);
-        for (int i = 0; k0 + (i * 4 + wv) * 16 < k1; ++i) {
-            const PagedGroup pn = fetch(i + 1, kn);
+        auto carry = [&](const PagedGroup& p, const u32x4* k) {
             halfx8 kh[KR];
             union { u32x4 u; bf16x8 b; } x[KR];
 #pragma unroll
@@ -67,9 +65,17 @@ __global__ __launch_bounds__(256, 2) void paged_refresh_kernel(PagedArgs a) {
             const __amdgpu_buffer_rsrc_t r = paged_rsrc(a.kpages, p.row, p.valid, ROWB);
 #pragma unroll
             for (int j = 0; j < KR; ++j) __builtin_amdgcn_raw_buffer_store_b128(x[j].u, r, koff + 64 * j, 0, 2);
-            p = pn;
-#pragma unroll
-            for (int j = 0; j < KR; ++j) k[j] = kn[j];
+        };
+        // three groups on their way (past the end: none)
+        for (int i = 0; k0 + (i * 4 + wv) * 16 < k1; i += 4) {
+            const PagedGroup p3 = fetch(i + 3, k3);
+            carry(p, k);
+            p = fetch(i + 4, k);
+            carry(p1, kn);
+            p1 = fetch(i + 5, kn);
+            carry(p2, k2);
+            p2 = fetch(i + 6, k2);
+            carry(p3, k3);
         }
     } else {
         constexpr int LD = D + 4;
@@ -106,7 +112,7 @@ static hipError_t launch_refresh_t(const PagedArgs& a, hipStream_t st) {
     constexpr size_t bytes = refresh_smem<T, D>();
     static const hipError_t attr = bytes ? hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_refresh_kernel<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : hipSuccess;
     if (attr != hipSuccess) return attr;
-    const long long grid = (long long)a.nseq * a.H * ((a.max_cached + REFRESH_KEYS - 1) / REFRESH_KEYS);
+    const long long grid = (long long)a.nseq * a.H * ((a.max_cached + a.refresh_len - 1) / a.refresh_len);
     if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL((paged_refresh_kernel<T, D>), dim3((unsigned)grid), dim3(256), bytes, st, a);
     return hipGetLastError();

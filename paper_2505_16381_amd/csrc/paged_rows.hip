@@ -32,7 +32,7 @@ template <typename T, int D, int NRT, bool BOTH, int NW> struct RowsCfg {
         return r * PPR + (cp ^ (((r >> 2) & 3) * 4));
     }
     static constexpr size_t floats_before(bool append) { return (size_t)2 * 16 * D + (size_t)16 * NRT * LDX + (append ? 16 * LDX : 0) + 16 * NRT * 17 + 32 + 16 * NRT * 2; }
-    static constexpr bool AT_ONCE = NRT <= 2;             // LDS has room for all waves' results
+    static constexpr bool AT_ONCE = NRT == 1;             // LDS has room for all waves' results and another workgroup
     static constexpr size_t PER = NRT * (D / 16) * 1024 + NRT * 512;      // bytes of a wave's
     static constexpr size_t merge_bytes() { return (AT_ONCE ? NW : NW / 2) * PER; }
     static constexpr size_t smem(bool append) {
