@@ -12,6 +12,8 @@
 // a tile (with softmax and values beside it), or, for the append, rows of the identity: then S is a row of every key of the tile
 // carried to the chunk's END, and what is left of X at the chunk's start are the rows of H_{m-1} .. H_0.
 // A wave has 16 rows; results stay in registers and are the next product's operand.  Bound by the fp32 matrix rate and, for few tiles, by the chain.
+#include <type_traits>
+
 #include "paged_decl.h"
 
 namespace path {
@@ -20,7 +22,7 @@ constexpr int LDT = 68;      // row length of a 64 x 64 matrix in LDS
 template <int D> constexpr size_t chunk_smem() { return (size_t)(3 * 64 * (D + 4) + 3 * 64 * LDT + 64 + 256) * 4; }
 
 template <int D>
-__global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
+__global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     constexpr int LD = D + 4;
     extern __shared__ __attribute__((aligned(16))) float sm[];
     float* const W = sm;
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
     const float* const wg = reinterpret_cast<const float*>(a.w);
     const float* const qg = reinterpret_cast<const float*>(a.q);
     auto stage = [&](float* dst, const float* src, int heads, int head) {
-        for (int i = tid; i < 64 * D / 4; i += 256) {
+        for (int i = tid; i < 64 * D / 4; i += 512) {
             const int t = i / (D / 4), e = (i % (D / 4)) * 4;
             float x[4] = {0.f, 0.f, 0.f, 0.f};
             if (t < m) load_f32<4>(src + ((long long)(tok0 + t) * heads + head) * D + e, x);
@@ -59,9 +61,11 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
     if (tid < 64) beta[tid] = tid < m ? reinterpret_cast<const float*>(a.beta)[(long long)(tok0 + tid) * a.H + h] : 0.f;
     if (a.cpages) {      // gate sums: c of the last cached token, the earlier tiles' gates, then one by one
         const float* const fg = reinterpret_cast<const float*>(a.log_f);
-        float x = 0.f;
-        for (int t = tid; t < 64 * c; t += 256) x += fg[(long long)(q.t0 + t) * a.H + h];
-        red[tid] = x;
+        if (tid < 256) {
+            float x = 0.f;
+            for (int t = tid; t < 64 * c; t += 256) x += fg[(long long)(q.t0 + t) * a.H + h];
+            red[tid] = x;
+        }
         __syncthreads();
         if (wv == 0) {
             float y = red[lane] + red[64 + lane] + red[128 + lane] + red[192 + lane];
@@ -84,20 +88,21 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
     float* const vt = reinterpret_cast<float*>(a.vt) + th * 64 * D;
     __syncthreads();
 
-    for (int i = tid; i < 64 * D; i += 256) wt[(i / D) * D + (i % D)] = W[(i / D) * LD + i % D];
+    for (int i = tid; i < 64 * D; i += 512) wt[(i / D) * D + (i % D)] = W[(i / D) * LD + i % D];
     if (a.attn)
-        for (int i = tid; i < 64 * D; i += 256) {
+        for (int i = tid; i < 64 * D; i += 512) {
             const int t = i / D, e = i % D;
             vt[e * 64 + (t)] = t < m ? vg[((long long)(tok0 + t) * a.H + h) * D + e] : 0.f;
         }
     if (a.append)
-        for (int i = tid; i < 64 * (D / 4); i += 256) {
+        for (int i = tid; i < 64 * (D / 4); i += 512) {
             const int t = i / (D / 4), e = (i % (D / 4)) * 4;
             const long long r = t < m ? paged_row(a, s, h, q.n + 64 * c + t) : -1;
             if (r >= 0) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.vpages) + r * D + e) = *reinterpret_cast<const f32x4*>(vg + ((long long)(tok0 + t) * a.H + h) * D + e);
         }
 
-    const int rb = wv >> 1, cb = wv & 1;      // this wave's 32 x 32 block of a 64 x 64 matrix
+    const bool low = wv < 4;                              // which of two 64 x 64 matrices
+    const int rb = (wv >> 1) & 1, cb = wv & 1;            // this wave's 32 x 32 block of it
     auto put64 = [&](float* dst, const f32x16& v, auto f) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -105,15 +110,19 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
             dst[r * LDT + cc] = f(r, cc, v[j]);
         }
     };
-    {   // N = diag(beta) strictLower(W W^T)
+    {   // N = diag(beta) strictLower(W W^T); D = strictLower(W K^T)
         f32x16 v = zero16();
-        mm<float, D, false, false>(v, W, LD, 32 * rb, W, LD, 32 * cb, l32, hh);
-        put64(B1, v, [&](int r, int cc, float x) { return cc < r ? beta[r] * x : 0.f; });
+        mm<float, D, false, false>(v, W, LD, 32 * rb, low ? W : K, LD, 32 * cb, l32, hh);
+        if (low) {
+            put64(B1, v, [&](int r, int cc, float x) { return cc < r ? beta[r] * x : 0.f; });
+            put64(B2, v, [&](int, int, float) { return 0.f; });
+        } else {
+            put64(B3, v, [&](int r, int cc, float x) { return cc < r ? x : 0.f; });
+        }
     }
     __syncthreads();
-    // (I + N)^{-1} by blocks: 16 x 16 on the diagonal by substitution, a column per thread; then twice the lower left quarter, -T22 N21 T11
-    for (int i = tid; i < 64 * 64; i += 256) B2[(i >> 6) * LDT + (i & 63)] = 0.f;
-    __syncthreads();
+    // (I + N)^{-1} by blocks: 16 x 16 on the diagonal by substitution, a column per thread; then twice the lower left quarter, -T22 (N21 T11), by 16 x 16
+    // blocks, a product's result the next one's right operand as it stands
     if (tid < 64) {
         const int b = tid & ~15, j = tid & 15;
         float x[16];
@@ -127,54 +136,55 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
         }
     }
     __syncthreads();
+    const int g = lane >> 4, c16 = lane & 15;
+    auto quarter = [&](auto half, int b, int rq, int cq) {
+        constexpr int HB = decltype(half)::value, NB = HB / 16;
+        f32x4 tmp[NB];
 #pragma unroll
-    for (int half = 16; half <= 32; half *= 2) {
-        const int blocks = 32 / half, per = half * half;
-        float* const tmp = B3;
-        for (int i = tid; i < blocks * per; i += 256) {
-            const int b = i / per * 2 * half, r = i % per / half, cc = i % half;
-            float y = 0.f;
-            for (int t = cc; t < half; ++t) y += B1[(b + half + r) * LDT + b + t] * B2[(b + t) * LDT + b + cc];
-            tmp[(b + r) * LDT + cc] = y;
+        for (int r = 0; r < NB; ++r) {
+            tmp[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < HB; k += 4)
+                tmp[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(B1[(b + HB + 16 * r + c16) * LDT + b + k + g], B2[(b + k + g) * LDT + b + 16 * cq + c16], tmp[r], 0, 0, 0);
         }
-        __syncthreads();
-        for (int i = tid; i < blocks * per; i += 256) {
-            const int b = i / per * 2 * half, r = i % per / half, cc = i % half;
-            float y = 0.f;
-            for (int t = 0; t <= r; ++t) y -= B2[(b + half + r) * LDT + b + half + t] * tmp[(b + t) * LDT + cc];
-            B2[(b + half + r) * LDT + b + cc] = y;
-        }
-        __syncthreads();
-    }
-    for (int i = tid; i < 64 * 64; i += 256) B2[(i >> 6) * LDT + (i & 63)] *= beta[i & 63];      // T
-    {   // D = strictLower(W K^T)
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < NB; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                y = __builtin_amdgcn_mfma_f32_16x16x4f32(B2[(b + HB + 16 * rq + c16) * LDT + b + HB + 16 * r + 4 * g + i], tmp[r][i], y, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) B2[(b + HB + 16 * rq + 4 * g + i) * LDT + b + 16 * cq + c16] = -y[i];
+    };
+    if (wv < 2) quarter(std::integral_constant<int, 16>(), 32 * wv, 0, 0);
+    __syncthreads();
+    if (wv < 4) quarter(std::integral_constant<int, 32>(), 0, wv >> 1, wv & 1);
+    __syncthreads();
+    for (int i = tid; i < 64 * 64; i += 512) B2[(i >> 6) * LDT + (i & 63)] *= beta[i & 63];      // T
+    __syncthreads();
+    if (low) {   // T D
         f32x16 v = zero16();
-        mm<float, D, false, false>(v, W, LD, 32 * rb, K, LD, 32 * cb, l32, hh);
-        put64(B1, v, [&](int r, int cc, float x) { return cc < r ? x : 0.f; });
+        mm<float, 64, false, true>(v, B2, LDT, 32 * rb, B3, LDT, 32 * cb, l32, hh);
+        put64(B1, v, [&](int, int, float x) { return x; });
+    } else {
+        // -Z^T: rows of d, so computed with T W's factors exchanged
+        for (int b = wv - 4; b < D / 32 * 2; b += 4) {
+            const int r0 = 32 * (b >> 1), c0 = 32 * (b & 1);
+            f32x16 v = zero16();
+            mm<float, 64, true, false>(v, W, LD, r0, B2, LDT, c0, l32, hh);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) zt[(r0 + acc_row(j, hh)) * 64 + c0 + l32] = -v[j];
+        }
     }
     __syncthreads();
-    {   // T D
-        f32x16 v = zero16();
-        mm<float, 64, false, true>(v, B2, LDT, 32 * rb, B1, LDT, 32 * cb, l32, hh);
-        put64(B3, v, [&](int, int, float x) { return x; });
-    }
-    // -Z^T: rows of d, so computed with T W's factors exchanged
-    for (int b = wv; b < D / 32 * 2; b += 4) {
-        const int r0 = 32 * (b >> 1), c0 = 32 * (b & 1);
-        f32x16 v = zero16();
-        mm<float, 64, true, false>(v, W, LD, r0, B2, LDT, c0, l32, hh);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) zt[(r0 + acc_row(j, hh)) * 64 + (c0 + l32)] = -v[j];
-    }
-    __syncthreads();
-    for (int b = wv; b < D / 32 * 2; b += 4) {      // kt = K - (T D)^T W
+    for (int b = wv; b < D / 32 * 2; b += 8) {      // kt = K - (T D)^T W
         const int r0 = 32 * (b & 1), c0 = 32 * (b >> 1);
         f32x16 v = zero16();
-        mm<float, 64, true, true>(v, B3, LDT, r0, W, LD, c0, l32, hh);
+        mm<float, 64, true, true>(v, B1, LDT, r0, W, LD, c0, l32, hh);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const int r = r0 + acc_row(j, hh);
-            kt[r * D + (c0 + l32)] = (K[r * LD + c0 + l32] - v[j]);
+            kt[r * D + c0 + l32] = K[r * LD + c0 + l32] - v[j];
         }
     }
     if (!a.attn) return;
@@ -183,29 +193,30 @@ __global__ __launch_bounds__(256, 1) void paged_chunk_kernel(PagedArgs a) {
         __syncthreads();
         stage(Q, qg, Hq, hq);
         __syncthreads();
-        {   // L = lower(Q W^T)
+        if (low) {   // L = lower(Q W^T)
             f32x16 v = zero16();
             mm<float, D, false, false>(v, Q, LD, 32 * rb, W, LD, 32 * cb, l32, hh);
-            put64(B1, v, [&](int r, int cc, float x) { return cc <= r ? x : 0.f; });
+            put64(B3, v, [&](int r, int cc, float x) { return cc <= r ? x : 0.f; });
         }
         __syncthreads();
         f32x16 lt = zero16();
-        {
+        if (low) {
             f32x16 v = zero16(), u = zero16();
             mm<float, D, false, false>(v, Q, LD, 32 * rb, K, LD, 32 * cb, l32, hh);
-            mm<float, 64, false, true>(u, B1, LDT, 32 * rb, B3, LDT, 32 * cb, l32, hh);
-            mm<float, 64, false, true>(lt, B1, LDT, 32 * rb, B2, LDT, 32 * cb, l32, hh);
+            mm<float, 64, false, true>(u, B3, LDT, 32 * rb, B1, LDT, 32 * cb, l32, hh);
             float* const sd = a.sd + ((size_t)tile * Hq + hq) * 4096;
 #pragma unroll
             for (int j = 0; j < 16; ++j) sd[(32 * rb + acc_row(j, hh)) * 64 + 32 * cb + l32] = v[j] - u[j];
+        } else {
+            mm<float, 64, false, true>(lt, B3, LDT, 32 * rb, B2, LDT, 32 * cb, l32, hh);
         }
         __syncthreads();
-        put64(B1, lt, [&](int, int, float x) { return x; });
+        if (!low) put64(B3, lt, [&](int, int, float x) { return x; });
         __syncthreads();
-        for (int b = wv; b < D / 32 * 2; b += 4) {      // X = Q - (L T) W
+        for (int b = wv; b < D / 32 * 2; b += 8) {      // X = Q - (L T) W
             const int r0 = 32 * (b & 1), c0 = 32 * (b >> 1);
             f32x16 v = zero16();
-            mm<float, 64, false, true>(v, B1, LDT, r0, W, LD, c0, l32, hh);
+            mm<float, 64, false, true>(v, B3, LDT, r0, W, LD, c0, l32, hh);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const int r = r0 + acc_row(j, hh);
@@ -379,7 +390,7 @@ static hipError_t launch_chunk_t(const PagedArgs& a, hipStream_t st) {
     static_assert(bytes <= 160 * 1024, "LDS");
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_chunk_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((paged_chunk_kernel<D>), dim3((unsigned)(a.tiles * a.H)), dim3(256), bytes, st, a);
+    hipLaunchKernelGGL((paged_chunk_kernel<D>), dim3((unsigned)(a.tiles * a.H)), dim3(512), bytes, st, a);
     return hipGetLastError();
 }
 hipError_t launch_paged_chunk(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_chunk_t<64>(a, st) : launch_chunk_t<128>(a, st); }
