@@ -995,7 +995,7 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
     p.tiles = T / 64 + nseq;
     p.row_blocks = (int)((long long)T * group / 128) + nseq;
     const long long blocks = (long long)T * group / 128;
-    p.many_splits = pieces((blocks > 1 ? blocks : 1) * H, 512, 512, p.many_len);
+    p.many_splits = pieces((blocks > 1 ? blocks : 1) * H, 512, es == 4 ? 128 : 512, p.many_len);      // (fp32: bound by its matrix rate on any number of CUs)
     pieces((long long)nseq * H, 256, 128, p.refresh_len);      // (each loads the d x d matrix: 16 heads of 8192 tokens, 256 workgroups 56 us with the rest of the call, 512 60, 1024 65)
     if (p.refresh_len > 4096) p.refresh_len = 4096;
 
