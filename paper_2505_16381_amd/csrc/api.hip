@@ -1055,10 +1055,7 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     a.kt = ws + p.kt; a.wt = ws + p.wt; a.zt = ws + p.zt; a.vt = ws + p.vt; a.sd = f(p.sd); a.pt = ws + p.pt;
     const int bf = dt == PATH_BF16 ? 1 : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.few) {
-        if (!hip_ok(launch_paged_rows(a, d, bf, st), "paged cache, few new tokens")) return PATH_ERR_HIP;
-        if (a.attn && p.few_splits > 1 && !hip_ok(launch_paged_merge_few(a, d, bf, st), "paged cache, pieces joined")) return PATH_ERR_HIP;
-    }
+    if (p.few && !hip_ok(launch_paged_rows(a, d, bf, st), "paged cache, few new tokens")) return PATH_ERR_HIP;
     if (p.many) {
         if (bf) {
             if (!hip_ok(launch_paged_chunk16(a, d, st), "paged cache, chunk transform")) return PATH_ERR_HIP;
@@ -1070,9 +1067,10 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
             if (a.attn && p.many_splits > 0 && !hip_ok(launch_paged_rows_many(a, d, st), "paged cache, attention of a chunk")) return PATH_ERR_HIP;
             if (a.append && !hip_ok(launch_paged_scan(a, d, st), "paged cache, scan over the new tokens")) return PATH_ERR_HIP;
         }
-        if (a.attn && p.many_splits > a.joined && !hip_ok(launch_paged_merge_many(a, d, bf, st), "paged cache, pieces of a chunk joined")) return PATH_ERR_HIP;
-        if (a.append && a.max_cached > 0 && !hip_ok(launch_paged_refresh(a, d, bf, st), "paged cache, keys carried on")) return PATH_ERR_HIP;
     }
+    const bool few = p.few && p.few_splits > 1, many = p.many && p.many_splits > a.joined;
+    if (a.attn && (few || many) && !hip_ok(launch_paged_merge(a, few, many, d, bf, st), "paged cache, pieces joined")) return PATH_ERR_HIP;
+    if (p.many && a.append && a.max_cached > 0 && !hip_ok(launch_paged_refresh(a, d, bf, st), "paged cache, keys carried on")) return PATH_ERR_HIP;
     return PATH_OK;
 }
 

@@ -126,8 +126,7 @@ template <int E, typename T> __device__ __forceinline__ void load_f32(const T* p
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int is_bf16, hipStream_t st);       // few new tokens: everything; d = 64, 128
 hipError_t launch_paged_rows_many(const PagedArgs& a, int d, hipStream_t st);               // X rows from the workspace, fp32
 hipError_t launch_paged_attn(const PagedArgs& a, int d, hipStream_t st);                    // the same, bf16
-hipError_t launch_paged_merge_few(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
-hipError_t launch_paged_merge_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st);
+hipError_t launch_paged_merge(const PagedArgs& a, bool few, bool many, int d, int is_bf16, hipStream_t st);      // records joined, of either way or both
 hipError_t launch_paged_chunk(const PagedArgs& a, int d, hipStream_t st);                   // tiles of the new tokens, fp32
 hipError_t launch_paged_sweep(const PagedArgs& a, int d, hipStream_t st);                   // attention among the new tokens, X
 hipError_t launch_paged_scan(const PagedArgs& a, int d, hipStream_t st);                    // the new keys, H_{m-1} .. H_0

@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 &&
                 W.carry(st.k[u], Z.times_keys(st.k[u], f32x4{0.f, 0.f, 0.f, 0.f}));
                 const __amdgpu_buffer_rsrc_t rk = paged_rsrc(a.kpages, st.row[u], st.valid[u], ROWB);
 #pragma unroll
-                for (int r = 0; r < KR; ++r) __builtin_amdgcn_raw_buffer_store_b128(st.k[u][r], rk, koff + 64 * r, 0, 2);
+                for (int r = 0; r < KR; ++r) __builtin_amdgcn_raw_buffer_store_b128(st.k[u][r], rk, koff + 64 * r, 0, 0);
             }
         }
     };
@@ -593,9 +593,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 &&
 // The records of a row joined, one wave per row; FEW: the pieces of the cache (the last has the new tokens in it), else the new tokens'
 // record and the pieces'.
 template <typename T, int D, bool FEW>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
+__device__ __forceinline__ void merge_row(const PagedArgs& a, long long row) {
     const int Hq = a.H * a.G, lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     int s, tok, used;
     long long at, slot;
     if constexpr (FEW) {
@@ -642,6 +641,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     if (lane == 0) a.lse[at] = (mx + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+// Both kinds of sequences in one launch: workgroups of four rows, the first few_blocks for those of few new tokens.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, unsigned few_blocks) {
+    const unsigned wv = threadIdx.x >> 6;
+    if (blockIdx.x < few_blocks) merge_row<T, D, true>(a, (long long)blockIdx.x * 4 + wv);
+    else merge_row<T, D, false>(a, (long long)(blockIdx.x - few_blocks) * 4 + wv);
+}
+
 template <typename T, int D, int NRT, bool WALK, bool ATTN, bool APPEND, int NW = 4>
 static hipError_t launch_rows_t(const PagedArgs& a, long long grid, hipStream_t st) {
     constexpr size_t bytes = RowsCfg<T, D, NRT, ATTN && APPEND, NW>::smem(APPEND);
@@ -670,18 +677,15 @@ static hipError_t launch_rows_many_d(const PagedArgs& a, hipStream_t st) {
     return launch_rows_t<float, D, 4, false, true, false>(a, (long long)a.tiles * a.G * a.H * a.many_splits, st);
 }
 hipError_t launch_paged_rows_many(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_rows_many_d<64>(a, st) : launch_rows_many_d<128>(a, st); }
-template <typename T, int D, bool FEW>
-static hipError_t launch_merge_t(const PagedArgs& a, hipStream_t st) {
-    const long long rows = FEW ? (long long)a.nseq * a.few_m * a.H * a.G : (long long)a.T * a.H * a.G;
-    hipLaunchKernelGGL((paged_merge_kernel<T, D, FEW>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+template <typename T, int D>
+static hipError_t launch_merge_t(const PagedArgs& a, bool few, bool many, hipStream_t st) {
+    const long long fb = few ? ((long long)a.nseq * a.few_m * a.H * a.G + 3) / 4 : 0, mb = many ? ((long long)a.T * a.H * a.G + 3) / 4 : 0;
+    hipLaunchKernelGGL((paged_merge_kernel<T, D>), dim3((unsigned)(fb + mb)), dim3(256), 0, st, a, (unsigned)fb);
     return hipGetLastError();
 }
-template <bool FEW>
-static hipError_t launch_merge(const PagedArgs& a, int d, int is_bf16, hipStream_t st) {
-    if (is_bf16) return d == 64 ? launch_merge_t<bf16_t, 64, FEW>(a, st) : launch_merge_t<bf16_t, 128, FEW>(a, st);
-    return d == 64 ? launch_merge_t<float, 64, FEW>(a, st) : launch_merge_t<float, 128, FEW>(a, st);
+hipError_t launch_paged_merge(const PagedArgs& a, bool few, bool many, int d, int is_bf16, hipStream_t st) {
+    if (is_bf16) return d == 64 ? launch_merge_t<bf16_t, 64>(a, few, many, st) : launch_merge_t<bf16_t, 128>(a, few, many, st);
+    return d == 64 ? launch_merge_t<float, 64>(a, few, many, st) : launch_merge_t<float, 128>(a, few, many, st);
 }
-hipError_t launch_paged_merge_few(const PagedArgs& a, int d, int is_bf16, hipStream_t st) { return launch_merge<true>(a, d, is_bf16, st); }
-hipError_t launch_paged_merge_many(const PagedArgs& a, int d, int is_bf16, hipStream_t st) { return launch_merge<false>(a, d, is_bf16, st); }
 
 }  // namespace path
