@@ -349,7 +349,8 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
  *   brings the new tokens cu_new[s] .. cu_new[s+1]-1 of q, k, v, w, beta, log_f, o, lse, packed along the token axis.  No new tokens, none cached: allowed.
  * Host arguments bound them: T tokens in the packed tensors, at most max_new new and max_cached cached tokens a sequence (both choose the
  * grids and how the cache is split; close bounds are fast).  Values past the bounds are held to them; rows of o and lse that belong to no sequence are left
- * as they are.  A page_table entry outside [0, num_pages) is a hole: its tokens take no part, nothing is read or written there.
+ * as they are.  A page_table entry outside [0, num_pages) is a hole: its tokens take no part, nothing is read or written
+ * there (a gate sum that would have been read there counts as 0).
  *
  * Shapes: q, o [T, H * group, d], lse [T, H * group] (fp32); k, v, w [T, H, d]; beta, log_f [T, H]; all contiguous.  Query heads
  * h * group .. h * group + group - 1 share key head h with its w, beta and gates (group 1: as everywhere else).

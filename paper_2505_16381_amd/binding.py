@@ -569,15 +569,17 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
     num_pages, pH, page_size, pd = kpages.shape
     nseq, per_seq = page_table.shape
     dt = PATH_BF16 if td is torch.bfloat16 else _dt_of(k)
-    group, n, pool = 1, T * H * d, num_pages * H * page_size * d
+    group, n, pool, made = 1, T * H * d, num_pages * H * page_size * d, []
     if q is not None:
         if q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
             raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
         group = q.shape[1] // H
         if o is None:
             o = torch.empty_like(q)
+            made.append(o)
         if lse is None:
             lse = q.new_empty((T, H * group), dtype=f32)
+            made.append(lse)
     if (log_f is None) != (cpages is None):
         raise ValueError("log_f and cpages go together")
     looked = [(k, n, td), (v, n, td), (w, n, td), (beta, T * H, td), (kpages, pool, td), (vpages, pool, td), (page_table, nseq * per_seq, i32), (cached, nseq, i32),
@@ -598,6 +600,7 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
     max_new, max_cached = int(max_new), int(max_cached)
     if workspace is None:
         workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
+        made.append(workspace)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the GPU that k is on")
     if T == 0:
@@ -617,6 +620,9 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
             code = call(*args, _stream_handle(stream))
     if code:
         _check(code)
+    if isinstance(stream, torch.cuda.Stream):      # (allocated for the current stream, used on this one)
+        for t in made:
+            t.record_stream(stream)
     return o, lse
 
 

@@ -386,8 +386,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 &&
     unsigned char* const myv = sv + wv * (U * 16 * ROWB);
 
     auto process = [&](Step& st) {
+        f32x4 S[U][NRT];
         if constexpr (ATTN) {
-            f32x4 S[U][NRT];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -398,6 +398,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 &&
 #pragma unroll
                 for (int t = 0; t < NRT; ++t) S[u][t] = X[t].keys_times(st.k[u], f32x4{0.f, 0.f, 0.f, 0.f});
             }
+        }
+        if constexpr (APPEND) {      // (before the softmax: the stores are on their way, and the keys' registers free)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                W.carry(st.k[u], Z.times_keys(st.k[u], f32x4{0.f, 0.f, 0.f, 0.f}));
+                const __amdgpu_buffer_rsrc_t rk = paged_rsrc(a.kpages, st.row[u], st.valid[u], ROWB);
+#pragma unroll
+                for (int r = 0; r < KR; ++r) __builtin_amdgcn_raw_buffer_store_b128(st.k[u][r], rk, koff + 64 * r, 0, 0);
+            }
+        }
+        if constexpr (ATTN) {
             v4s P16[U][NRT];
 #pragma unroll
             for (int t = 0; t < NRT; ++t) {
@@ -448,15 +459,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && NRT == 1 && !(sizeof(T) == 4 &&
                         }
                     }
                 }
-            }
-        }
-        if constexpr (APPEND) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                W.carry(st.k[u], Z.times_keys(st.k[u], f32x4{0.f, 0.f, 0.f, 0.f}));
-                const __amdgpu_buffer_rsrc_t rk = paged_rsrc(a.kpages, st.row[u], st.valid[u], ROWB);
-#pragma unroll
-                for (int r = 0; r < KR; ++r) __builtin_amdgcn_raw_buffer_store_b128(st.k[u][r], rk, koff + 64 * r, 0, 0);
             }
         }
     };

@@ -369,3 +369,50 @@ def test_binding_refuses_tensors_of_another_kind(gpu):
     with pytest.raises(pa.PathAttnError) as e:
         run(workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
     assert e.value.code in (1, 5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("op", ["attn", "extend"])
+@pytest.mark.parametrize("old,new", [([33], [1]), ([1100], [3]), ([500], [1]), ([700], [90])])
+def test_infinite_values_stay_in_their_component(gpu, op, dtype, old, new):
+    """An infinite value in the cache makes its own component infinite and leaves the others' bits alone."""
+    torch, pa = gpu
+    x = pm.batch(old, new, 2, 1, 64, 32, dtype, seed=12)
+    y, z = to_gpu(torch, x), to_gpu(torch, x)
+    n = old[0]
+    for comp, row in ((5, n - 1), (9, n // 2), (11, 0)):
+        z["vpages"][z["page_table"][0, row // 32].long(), :, row % 32, comp] = math.inf
+    want, want_l = call(pa, op, y, new[0], n, 0.125)
+    got, got_l = call(pa, op, z, new[0], n, 0.125)
+    torch.cuda.synchronize()
+    assert torch.equal(got_l, want_l) and torch.isfinite(want).all()
+    rest = [i for i in range(64) if i not in (5, 9, 11)]
+    assert torch.equal(got[..., rest], want[..., rest])
+    assert (got[..., [5, 9, 11]] == math.inf).all()
+
+
+def test_the_same_call_from_two_threads(gpu):
+    """Two host threads, each with its own stream, workspace and cache."""
+    import threading
+    torch, pa = gpu
+    x = pm.batch([300, 40], [70, 2], 2, 1, 64, 16, "bf16", True, seed=13)
+    want_y = to_gpu(torch, x)
+    want = call(pa, "extend", want_y, 70, 300, 0.1)
+    torch.cuda.synchronize()
+    got = [None, None]
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            y = to_gpu(torch, x)
+            out = call(pa, "extend", y, 70, 300, 0.1)
+        stream.synchronize()
+        got[i] = (*out, y["kpages"])
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for o, lse, kp in got:
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(kp.view(torch.uint8), want_y["kpages"].view(torch.uint8))
