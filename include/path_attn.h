@@ -366,8 +366,9 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
  * Attention uses the cached keys as they stand: the logit is formed from x = H_{n} .. H_{n+a} q with the stored key, where path_decode_step
  * rounds the refreshed key first.  A server may put appends off: the new tokens of path_paged_attn are then all tokens since the
  * last append (keys are read and written back, and rounded, once per append instead of once per token).
- * Arithmetic with PATH_BF16: up to 16 new tokens, X and the transitions as sums of two bf16 operands (no range rule); longer chunks
- * carry queries, keys and transitions as fp16 operands under the range rule above (the logits inside a tile of 64 new tokens in fp32).
+ * Arithmetic with PATH_BF16: what is computed from the inputs -- X, the carried keys, the transitions -- is multiplied as the sum of two bf16 numbers, with
+ * bf16's range (log-sum-exp good to 1e-6 of itself), probabilities as one.  The one exception: the product of a chunk's transitions that its append applies to
+ * the cached keys is an fp16 operand, and so are the keys there: their elements must stay below 65504.
  * workspace: path_paged_workspace_bytes(...) bytes (0 for arguments that the calls reject), 256-byte aligned; contents undefined before and after.
  * Errors: PATH_ERR_SHAPE for nseq, H, group or max_new < 1, group > 64, T or max_cached < 0, a page size that is not allowed, or max_cached >
  * pages_per_seq * page_size; PATH_ERR_NULL also if only one of log_f and cpages is given.  T = 0 does nothing.
