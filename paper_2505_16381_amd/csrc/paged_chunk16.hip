@@ -239,19 +239,18 @@ __global__ __launch_bounds__(C16_THREADS, 1) void paged_chunk16_kernel(PagedArgs
 
 // ---- the way through the tiles ----
 //
-// 64 rows per workgroup, and four waves for each 16 of them, which share a step's work:
+// 32 or 64 rows per workgroup, and four waves for each 16 of them, which share a step's work:
 //     waves a   S = kt X^T (32 of the tile's 64 tokens each), softmax, O^T += V^T P^T: two online softmaxes, joined at the end.  scan: S are rows of keys, stored
 //     waves b   Y = W X^T (32 tokens each), exchanged; X^T -= Z^T Y (half of d each), and X as operands to LDS for the next step
 // The tile's operands come to LDS in two sets, each while the other is worked on: carried keys (hi, lo) and W; -Z (hi, lo) and V.
-// Bound by the chain of steps, about 3 us each at d = 128 and 1.8 at 64: products of 1.0 us a SIMD, LDS of 0.9, 0.7 of waiting for the copies, and between them
-// the latency of reads, packing and two barriers.  Per workgroup 144 KB of LDS, so one on a CU.  16 heads, d = 128: 1000 tokens with the scan 52 us, 512 without 24, the
-// scan alone 25; 2048 tokens of 16 query heads 123.  One wave for all of a row's work took 4.2 us a step, two 3.3; whole tiles from L2 to registers, without LDS, 7.5.
+// Bound by the chain of steps, with 64 rows about 3 us each at d = 128 and 1.8 at 64: products of 1.0 us a SIMD, LDS of 0.9, 0.7 of waiting for the copies, and between
+// them the latency of reads, packing and two barriers.  Per workgroup up to 144 KB of LDS, so one on a CU.  One wave for all of a row's work took 4.2 us a step, two
+// 3.3; whole tiles from L2 to registers, without LDS, 7.5.
 // The first workgroups are those of the append's scan, whose way is the longest: rows of the identity, of which S are rows of the
 // keys carried to the chunk's end, and what is left of X the rows of H_{m-1} .. H_0.
 // As an operand a lane holds elements 32 s + 4 g + 0..3 and 16 further on, as results have them; two eight-byte reads of the keys and of W, which like the
 // transposing reads take whole sixteen-byte pieces off the banks (eight elements in a row cost the latter twice their time).
-constexpr int S16_THREADS = 1024;
-template <int D> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)4 * (D / 32) * 2 * 64 * 16 + 4 * 2 * 2 * 64 * 16; }
+template <int D, int RS> constexpr size_t sweep16_smem() { return (size_t)6 * 64 * D * 2 + (size_t)RS * (D / 32) * 2 * 64 * 16 + RS * 2 * 2 * 64 * 16; }
 
 // Place of an element in a tile of 64 rows: sixteen-byte pieces of a row exchanged by its turn, such that 32 lanes' eight bytes fall on all banks
 // once, both of one piece's two halves in 16 rows (fragments along the row) and of 32 bytes in 8 rows (transposing reads).
@@ -333,13 +332,13 @@ template <int N> __device__ __forceinline__ void pack_pairs(const f32x4* x, bf16
 }
 __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-template <int D, bool SCAN>
+template <int D, bool SCAN, int RS>
 __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem, int s, int h, int hq, int ct, int r0) {
     typedef Turned16<D> L;
     constexpr int ROWB = D * 2, TILE = 64 * ROWB, DT = D / 16, DS = D / 32, HT = DT / 2, HS = DS / 2, PPR = D / 8, RPI = 64 / PPR;
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, Hq = a.H * a.G;
-    const int rw = wv & 3, part = (wv >> 2) & 1;      // its 16 rows, and which half of the work on them
-    const bool carries = wv >= 8;                     // waves b
+    const int rw = wv & (RS - 1), part = (wv / RS) & 1;      // its 16 rows, and which half of the work on them
+    const bool carries = wv >= 2 * RS;                       // waves b
     const PagedSeq q = paged_seq(a, s);
     const int first = first_tile(a, s), row = r0 + 16 * rw + c;
     const int tok = SCAN ? 0 : q.t0 + 64 * ct + row;
@@ -349,15 +348,18 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
     const bf16_t* const kt = reinterpret_cast<const bf16_t*>(a.kt);
     const bf16_t* const zt = reinterpret_cast<const bf16_t*>(a.zt);
     bf16x8* const sx = reinterpret_cast<bf16x8*>(smem + 6 * TILE) + rw * DS * 2 * 64 + lane;                            // X of the 16 rows: [slab][hi, lo][lane]
-    bf16x8* const sy = reinterpret_cast<bf16x8*>(smem + 6 * TILE + 4 * DS * 2 * 64 * 16) + rw * 2 * 2 * 64 + lane;      // Y: the same, two slabs
+    bf16x8* const sy = reinterpret_cast<bf16x8*>(smem + 6 * TILE + RS * DS * 2 * 64 * 16) + rw * 2 * 2 * 64 + lane;      // Y: the same, two slabs
 
     // copies: the waves share a tile's rows, a row's pieces exchanged by its turn; rows of w and v past the last token: that token's
-    const int copied = RPI * wv + lane / PPR;
     auto copy = [&](int slot, const bf16_t* src, long long stride, int last) {
-        if (RPI * wv < 64) {
-            const bf16_t* const p = src + min(copied, last) * stride + ((lane % PPR) ^ L::turn(copied)) * 8;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                             (__attribute__((address_space(3))) void*)(smem + slot * TILE + RPI * wv * ROWB), 16, 0, 0);
+#pragma unroll
+        for (int i0 = 0; i0 < 64 / RPI; i0 += 4 * RS) {
+            const int i = i0 + wv, r = RPI * i + lane / PPR;
+            if (i < 64 / RPI) {
+                const bf16_t* const p = src + min(r, last) * stride + ((lane % PPR) ^ L::turn(r)) * 8;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                                 (__attribute__((address_space(3))) void*)(smem + slot * TILE + RPI * i * ROWB), 16, 0, 0);
+            }
         }
     };
     auto tile_at = [&](int j) { return ((size_t)(first + j) * a.H + h) * 64 * D; };
@@ -623,26 +625,28 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
     }
 }
 
-template <int D>
-__global__ __launch_bounds__(S16_THREADS, 1) void paged_sweep16_kernel(PagedArgs a) {
+template <int D, int RS>
+__global__ __launch_bounds__(256 * RS, 1) void paged_sweep16_kernel(PagedArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
-    const int lane = threadIdx.x & 63, Hq = a.H * a.G, scans = a.append ? a.nseq * a.H * (D / 64) : 0;
+    constexpr int BLOCKS = D / (16 * RS), HALVES = 4 / RS;      // workgroups for the identity's rows, for a tile's
+    const int lane = threadIdx.x & 63, Hq = a.H * a.G, scans = a.append ? a.nseq * a.H * BLOCKS : 0;
     int x = blockIdx.x;
     if (x < scans) {
-        const int r0 = 64 * (x % (D / 64)); x /= D / 64;
+        const int r0 = 16 * RS * (x % BLOCKS); x /= BLOCKS;
         const int s = x / a.H, m = paged_seq(a, s).m;
         if (m <= a.few_limit) return;
-        sweep16<D, true>(a, smem, s, x % a.H, 0, (m + 63) >> 6, r0);
+        sweep16<D, true, RS>(a, smem, s, x % a.H, 0, (m + 63) >> 6, r0);
         return;
     }
     x -= scans;
-    const int tile = a.tiles - 1 - x / Hq, hq = x % Hq;      // (the last tiles have the longest way)
+    const int hq = x % Hq; x /= Hq;
+    const int tile = a.tiles - 1 - x / HALVES, r0 = 16 * RS * (x % HALVES);      // (the last tiles have the longest way)
     int s = 0;
     for (int i = 0; i < a.nseq; i += 64) s += __popcll(__ballot(i + lane < a.nseq && first_tile(a, min(i + lane, a.nseq - 1)) <= tile));
     s = __builtin_amdgcn_readfirstlane(max(0, s - 1));
     const int m = paged_seq(a, s).m, ct = tile - first_tile(a, s);
-    if (m <= a.few_limit || ct < 0 || 64 * ct >= m) return;
-    sweep16<D, false>(a, smem, s, hq / a.G, hq, __builtin_amdgcn_readfirstlane(ct), 0);
+    if (m <= a.few_limit || ct < 0 || 64 * ct + r0 >= m) return;
+    sweep16<D, false, RS>(a, smem, s, hq / a.G, hq, __builtin_amdgcn_readfirstlane(ct), r0);
 }
 
 template <int D>
@@ -655,15 +659,22 @@ static hipError_t launch_chunk16_t(const PagedArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 hipError_t launch_paged_chunk16(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_chunk16_t<64>(a, st) : launch_chunk16_t<128>(a, st); }
-template <int D>
+template <int D, int RS>
 static hipError_t launch_sweep16_t(const PagedArgs& a, hipStream_t st) {
-    constexpr size_t bytes = sweep16_smem<D>();
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_sweep16_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    constexpr size_t bytes = sweep16_smem<D, RS>();
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_sweep16_kernel<D, RS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
-    const unsigned grid = (unsigned)((a.append ? a.nseq * a.H * (D / 64) : 0) + (a.attn ? a.tiles * a.H * a.G : 0));
-    hipLaunchKernelGGL((paged_sweep16_kernel<D>), dim3(grid), dim3(S16_THREADS), bytes, st, a);
+    const unsigned grid = (unsigned)((a.append ? a.nseq * a.H * (D / (16 * RS)) : 0) + (a.attn ? a.tiles * a.H * a.G * (4 / RS) : 0));
+    hipLaunchKernelGGL((paged_sweep16_kernel<D, RS>), dim3(grid), dim3(256 * RS), bytes, st, a);
     return hipGetLastError();
 }
-hipError_t launch_paged_sweep16(const PagedArgs& a, int d, hipStream_t st) { return d == 64 ? launch_sweep16_t<64>(a, st) : launch_sweep16_t<128>(a, st); }
+// 32 rows per workgroup shorten the chain (two waves a SIMD instead of four) as long as there is a CU for nearly each of them; then 64, which bring the tiles for
+// twice as many.  us a call, 32 / 64 rows, d = 128, 16 heads over nothing: 256 tokens 29.9 / 31.2, 512 38.7 / 45.0, 1000 66.3 / 67.4, 1500 123 / 103,
+// 2048 182 / 147, 32 heads of 1000 125 / 102; append alone 512 33.8 / 38.3, 2048 91 / 113, to 8 sequences 111 / 89.
+hipError_t launch_paged_sweep16(const PagedArgs& a, int d, hipStream_t st) {
+    const bool narrow = a.attn ? (a.T / 64 + 1) * a.H * a.G <= 272 : a.nseq * a.H * d <= 8192;
+    if (narrow) return d == 64 ? launch_sweep16_t<64, 2>(a, st) : launch_sweep16_t<128, 2>(a, st);
+    return d == 64 ? launch_sweep16_t<64, 4>(a, st) : launch_sweep16_t<128, 4>(a, st);
+}
 
 }  // namespace path

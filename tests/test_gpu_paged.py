@@ -1,15 +1,13 @@
 """Paged caches on the GPU against the definition in 64 bits (paged_model.py).
 
-Bars, derived before the first run (e = half a step of bf16 = 2^-8, h = half a step of fp16 = 2^-11; inputs are standard normal, scale
-d^-1/2, so norms of q and k are below 1.6 sqrt(d) and scale |q| |k| below 2.6 sqrt(d)):
+Bars (e = half a step of bf16 = 2^-8, h = half a step of fp16 = 2^-11; inputs are standard normal, scale d^-1/2, so norms of q and k are below
+1.6 sqrt(d) and scale |q| |k| below 2.6 sqrt(d)):
   o     bf16: every weight is rounded once (e of a mean of |v| <= 4.5) and the result once: 2 e max|v|.
         fp32: sums of up to 4000 terms of size one, of logits good to 1e-5: 1e-4.
-  lse   one pass, bf16: x is a sum of two bf16 numbers, its rest 2^-16 of it: 2^-16 * 2.6 sqrt(d) and as much for fp32 sums: 1e-3 at worst.
-        chunks, bf16: x and keys in fp16: an element's error is uniform, a logit's deviation h sqrt(2/3) scale |x| |k| / sqrt(d) <= 1e-3 / sqrt(2)
-        at the largest norms, carried through up to four tiles: 2e-3.
-        fp32: 1e-4 (as above).
-  keys  bf16: the result is rounded once, e |k'|, and formed with operands good to h (chunks: of up to four tiles, |k| <= 1.6 sqrt(d) spread over d
-        elements, |k| h 4 < 4e-2 at worst, 4e-3 in one element): e |k'| + 4e-2 h sqrt(d) ... stated as e |k'| + 8e-3.  fp32: 1e-4.
+  lse   bf16: x is a sum of two bf16 numbers, its rest 2^-16 of it: 2^-16 * 2.6 sqrt(d) = 4.5e-4, and as much for fp32 sums: 1e-3; chunks carry x and the keys
+        through up to four tiles so: 2e-3.  fp32: 1e-4 (as above).
+  keys  bf16: the result is rounded once, e |k'|; a chunk's cached keys meet a matrix of fp16 elements, rows of norm <= 2: an element is off by a
+        deviation of 2 h / sqrt(3) = 6e-4, five of them 3e-3, and as much for the carried operands: e |k'| + 8e-3.  fp32: 1e-4.
   values and untouched slots: the bits."""
 import math
 
@@ -416,3 +414,26 @@ def test_the_same_call_from_two_threads(gpu):
         t.join()
     for o, lse, kp in got:
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(kp.view(torch.uint8), want_y["kpages"].view(torch.uint8))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(gpu, seed):
+    """Batches of up to nine sequences with lengths from nothing to several tiles, pages, groups, widths, types and gates at random."""
+    import random
+    r = random.Random(seed)
+    S = r.choice([1, 1, 2, 3, 5, 9])
+    old = [r.choice([0, 1, r.randint(2, 40), r.randint(41, 900)]) for _ in range(S)]
+    new = [r.choice([0, 1, 1, r.randint(2, 16), r.randint(17, 64), r.randint(65, 200)]) for _ in range(S)]
+    if not any(new):
+        new[0] = 1
+    G = r.choice([1, 1, 2, 3, 4, 7, 16])
+    check(gpu, r.choice(["attn", "append", "extend", "extend"]), old, new, r.choice([1, 2, 3]), G, r.choice([64, 128]), r.choice([16, 32, 64, 128, 1024]),
+          r.choice(["bf16", "bf16", "fp32"]), r.random() < 0.5, seed=100 + seed)
+
+
+def test_many_short_sequences(gpu):
+    """More sequences than a wave has lanes, some without new tokens, few and many new tokens mixed."""
+    old = [(7 * i) % 90 for i in range(150)]
+    new = [0 if i % 5 == 3 else 40 if i % 29 == 7 else 1 + i % 3 for i in range(150)]
+    check(gpu, "extend", old, new, 2, 1, 64, 16, "bf16", True, seed=21)
+    check(gpu, "attn", old, new, 1, 2, 64, 16, "fp32", False, seed=22)
