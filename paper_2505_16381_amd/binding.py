@@ -547,7 +547,7 @@ def path_attn_varlen_bwd(q, k, v, w, beta, o, lse, d_o, cu_seqlens, log_f=None, 
 
 
 def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) -> int:
-    """Bytes of scratch that the path_paged_* calls need for these bounds (more of any of them: not less)."""
+    """Bytes of scratch that the path_paged_* calls need for these bounds (it grows with every one of them: the largest call's serves all smaller ones)."""
     return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
 
 

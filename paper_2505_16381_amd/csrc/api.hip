@@ -1002,8 +1002,14 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
     const size_t Hq = (size_t)H * group;
-    if (p.few) {
-        const size_t slots = attn && p.few_splits > 1 ? (size_t)p.few_splits * nseq * p.few_m * Hq : 0;
+    // Records of the pieces, reserved by bounds that grow with every argument, so that a workspace of larger bounds serves all smaller calls.  With u units
+    // (sequences and heads) there are fewer than want / u + 1 pieces, so fewer than 512 + u records a row, and none from u = 512 on; at most 64 rows.
+    // A chunk's r = T * H * group rows are u = max(1, T * group / 128) * H units: fewer than r + 512 r / u records, where r / u is at most T * group and below 256.
+    auto most = [&](int least) { return (size_t)((max_cached + least - 1) / least); };
+    auto least_of = [](size_t x, size_t y) { return x < y ? x : y; };
+    {
+        const size_t rows = least_of((size_t)mn * group, PAGED_FEW_ROWS);
+        const size_t slots = attn && p.few_waves == 4 && most(128) > 1 ? least_of(1024, most(128) * nseq * H) * rows : 0;
         take(p.few_o, slots * d * 4);
         take(p.few_ml, slots * 2 * 4);
     }
@@ -1012,8 +1018,9 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
         const size_t rows = attn ? (size_t)T * Hq : 0;
         take(p.x, rows * d * 4);
         take(p.crow, (size_t)T * H * 4);
-        take(p.many_o, (size_t)(1 + p.many_splits) * rows * d * 4);
-        take(p.many_ml, (size_t)(1 + p.many_splits) * rows * 2 * 4);
+        const size_t records = rows + (attn ? least_of(most(es == 4 ? 128 : 512) * rows, rows + 512 * least_of((size_t)T * group, 256)) : 0);
+        take(p.many_o, records * d * 4);
+        take(p.many_ml, records * 2 * 4);
         // kt, zt: fp32, or pairs of bf16 tiles; w and v are taken as they are with bf16
         for (size_t* f : {&p.kt, &p.zt}) take(*f, th * CHUNK * d * 4);
         for (size_t* f : {&p.wt, &p.vt}) take(*f, es == 4 ? th * CHUNK * d * 4 : 0);

@@ -1,6 +1,7 @@
 """Paged caches without a GPU: refusals come before anything is launched, the workspace covers every smaller problem, and the 64-bit model of the
 GPU tests agrees with the decode oracle, with which it shares nothing."""
 import ctypes
+import random
 
 import numpy as np
 import pytest
@@ -72,6 +73,19 @@ def test_workspace_bytes():
         n = pa.path_paged_workspace_bytes(3, T, max_new, max_cached, 2, 1, 64, 0)
         assert attn(nseq=3, T=T, max_new=max_new, max_cached=max_cached, per=400, dt=0, wsb=n - 1) == 5
         assert append(nseq=3, T=T, max_new=max_new, max_cached=max_cached, per=400, dt=0, wsb=64 if n > 64 else 0) == 5
+
+
+def test_workspace_of_larger_bounds_serves_smaller_calls():
+    """A server keeps one workspace, made for its largest call."""
+    rng = random.Random(5)
+    for case in range(20000):
+        big = [rng.choice(r) for r in ((1, 2, 5, 16, 64, 300), (1, 16, 17, 100, 255, 256, 700, 5000), (1, 4, 16, 17, 600, 5000),
+                                       (0, 100, 700, 5000, 70000, 1 << 20), (1, 2, 7, 16, 40, 128), (1, 2, 3, 4, 16, 17, 64), (64, 128))]
+        small = [x if rng.random() < .5 else rng.randint(min(x, low), x) for x, low in zip(big, (1, 0, 1, 0, 1, 1, 64))]
+        small[6] = 64 if small[6] < 128 else 128
+        dt = rng.randrange(2)
+        need, have = pa.path_paged_workspace_bytes(*small, dt), pa.path_paged_workspace_bytes(*big, dt)
+        assert need <= have or have == 0, (small, big, dt)      # (0: the larger bounds are rejected)
 
 
 def test_binding_refuses_what_the_kernels_would_misread():
