@@ -551,25 +551,26 @@ def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) ->
     return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
 
 
-def _paged_refuse(named, dev):
-    for name, t, shape, dtype in named:
-        if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+def _paged_refuse(looked, dev):
+    for name, t, shape, dtype in looked:
+        if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
             raise ValueError(f"{name} is {tuple(shape)}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
-        if t is not None and (t.get_device() != dev or dev < 0 or not t.is_contiguous()):
+    for name, t, _, _ in looked:
+        if t.get_device() != dev or dev < 0 or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
 
 
 def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream):
-    """Checks that every tensor is what the kernels take it for, and calls.  A call of short kernels is bound by this function, so sizes, types and places
-    are looked at in one go, and by name only where something is wrong."""
+    """Checks that every tensor is what the kernels take it for, and calls.  A call of short kernels is bound by this function, so it passes once over shapes, types
+    and places, and says what is wrong only where something is."""
     import torch
     if k.dim() != 3 or kpages.dim() != 4 or page_table.dim() != 2 or (q is not None and q.dim() != 3):
         raise ValueError("q, k are [T,heads,d], kpages [num_pages,H,page_size,d], page_table [nseq,pages_per_seq]")
     (T, H, d), td, f32, i32, dev = k.shape, k.dtype, torch.float32, torch.int32, k.get_device()
-    num_pages, pH, page_size, pd = kpages.shape
+    num_pages, _, page_size, _ = kpages.shape
     nseq, per_seq = page_table.shape
     dt = PATH_BF16 if td is torch.bfloat16 else _dt_of(k)
-    group, n, pool, made = 1, T * H * d, num_pages * H * page_size * d, []
+    group, made = 1, []
     if q is not None:
         if q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
             raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
@@ -582,21 +583,17 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
             made.append(lse)
     if (log_f is None) != (cpages is None):
         raise ValueError("log_f and cpages go together")
-    looked = [(k, n, td), (v, n, td), (w, n, td), (beta, T * H, td), (kpages, pool, td), (vpages, pool, td), (page_table, nseq * per_seq, i32), (cached, nseq, i32),
-              (cu_new, nseq + 1, i32)]
+    tokens, pool = (T, H, d), (num_pages, H, page_size, d)
+    looked = [("k", k, tokens, td), ("v", v, tokens, td), ("w", w, tokens, td), ("beta", beta, (T, H), td), ("kpages", kpages, pool, td), ("vpages", vpages, pool, td),
+              ("page_table", page_table, (nseq, per_seq), i32), ("cached", cached, (nseq,), i32), ("cu_new", cu_new, (nseq + 1,), i32)]
     if log_f is not None:
-        looked += [(log_f, T * H, td), (cpages, num_pages * H * page_size, f32)]
+        looked += [("log_f", log_f, (T, H), td), ("cpages", cpages, pool[:3], f32)]
     if q is not None:
-        looked += [(q, n * group, td), (o, n * group, td), (lse, T * H * group, f32)]
-    fine = pH == H and pd == d and dev >= 0 and v.shape == k.shape and vpages.shape == kpages.shape
-    for t, size, dtype in looked:
-        if t.numel() != size or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-            fine = False
-    if not fine:
-        _paged_refuse([("k", k, (T, H, d), td), ("v", v, (T, H, d), td), ("w", w, (T, H, d), td), ("beta", beta, (T, H), td), ("log_f", log_f, (T, H), td),
-                       ("kpages", kpages, (num_pages, H, page_size, d), td), ("vpages", vpages, (num_pages, H, page_size, d), td),
-                       ("cpages", cpages, (num_pages, H, page_size), f32), ("page_table", page_table, (nseq, per_seq), i32), ("cached", cached, (nseq,), i32),
-                       ("cu_new", cu_new, (nseq + 1,), i32), ("q", q, (T, H * group, d), td), ("o", o, (T, H * group, d), td), ("lse", lse, (T, H * group), f32)], dev)
+        rows = (T, H * group, d)
+        looked += [("q", q, rows, td), ("o", o, rows, td), ("lse", lse, rows[:2], f32)]
+    for _, t, shape, dtype in looked:
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+            _paged_refuse(looked, dev)
     max_new, max_cached = int(max_new), int(max_cached)
     if workspace is None:
         workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
