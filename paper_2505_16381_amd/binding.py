@@ -547,7 +547,10 @@ def path_attn_varlen_bwd(q, k, v, w, beta, o, lse, d_o, cu_seqlens, log_f=None, 
 
 
 def path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt) -> int:
-    """Bytes of scratch that the path_paged_* calls need for these bounds (it grows with every one of them: the largest call's serves all smaller ones)."""
+    """Bytes of scratch that the path_paged_* calls need for these bounds (it grows with every one of them: the largest call's serves all smaller ones); 0 for
+    bounds that they refuse."""
+    if any(not 0 <= x < 1 << 31 for x in (nseq, T, max_new, max_cached, H, group, d)):      # (ctypes keeps the low 32 bits)
+        return 0
     return int(load_library().path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt))
 
 
@@ -595,6 +598,8 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
         if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous():
             _paged_refuse(looked, dev)
     max_new, max_cached = int(max_new), int(max_cached)
+    if not -(1 << 31) <= min(max_new, max_cached) <= max(max_new, max_cached) < 1 << 31:      # (ctypes keeps the low 32 bits)
+        raise ValueError(f"max_new and max_cached are 32-bit bounds: got {max_new}, {max_cached}")
     if workspace is None:
         workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
         made.append(workspace)
