@@ -563,6 +563,24 @@ def _paged_refuse(looked, dev):
             raise ValueError(f"{name} must be contiguous and on the GPU that k is on")
 
 
+def _paged_made(like, shape, dtype, stream, returned):
+    """A tensor that a call on `stream` writes, from that stream's memory: a block of another stream's may still be in use there, and would go back to it when
+    the call returns.  What the caller gets is also noted as used on the caller's stream."""
+    import torch
+    dev = like.get_device()
+    if stream is None or dev < 0:
+        return like.new_empty(shape, dtype=dtype)
+    handle = _stream_handle(stream)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+    mine = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+    if returned and mine.cuda_stream != handle:
+        t.record_stream(mine)
+    return t
+
+
 def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream):
     """Checks that every tensor is what the kernels take it for, and calls.  A call of short kernels is bound by this function, so it passes once over shapes, types
     and places, and says what is wrong only where something is."""
@@ -573,17 +591,15 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
     num_pages, _, page_size, _ = kpages.shape
     nseq, per_seq = page_table.shape
     dt = PATH_BF16 if td is torch.bfloat16 else _dt_of(k)
-    group, made = 1, []
+    group = 1
     if q is not None:
         if q.shape[0] != T or q.shape[2] != d or H == 0 or q.shape[1] % H:
             raise ValueError(f"q is [T,H*group,d] with T={T}, H={H}, d={d}: got {tuple(q.shape)}")
         group = q.shape[1] // H
         if o is None:
-            o = torch.empty_like(q)
-            made.append(o)
+            o = torch.empty_like(q) if stream is None else _paged_made(q, q.shape, td, stream, True)
         if lse is None:
-            lse = q.new_empty((T, H * group), dtype=f32)
-            made.append(lse)
+            lse = q.new_empty((T, H * group), dtype=f32) if stream is None else _paged_made(q, (T, H * group), f32, stream, True)
     if (log_f is None) != (cpages is None):
         raise ValueError("log_f and cpages go together")
     tokens, pool = (T, H, d), (num_pages, H, page_size, d)
@@ -594,15 +610,13 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
     if q is not None:
         rows = (T, H * group, d)
         looked += [("q", q, rows, td), ("o", o, rows, td), ("lse", lse, rows[:2], f32)]
-    for _, t, shape, dtype in looked:
-        if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous():
-            _paged_refuse(looked, dev)
+    if dev < 0 or any([t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() for _, t, shape, dtype in looked]):
+        _paged_refuse(looked, dev)
     max_new, max_cached = int(max_new), int(max_cached)
     if not -(1 << 31) <= min(max_new, max_cached) <= max(max_new, max_cached) < 1 << 31:      # (ctypes keeps the low 32 bits)
         raise ValueError(f"max_new and max_cached are 32-bit bounds: got {max_new}, {max_cached}")
     if workspace is None:
-        workspace = torch.empty(max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)), dtype=torch.uint8, device=k.device)
-        made.append(workspace)
+        workspace = _paged_made(k, (max(256, path_paged_workspace_bytes(nseq, T, max_new, max_cached, H, group, d, dt)),), torch.uint8, stream, False)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the GPU that k is on")
     if T == 0:
@@ -622,9 +636,6 @@ def _paged_call(name, q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
             code = call(*args, _stream_handle(stream))
     if code:
         _check(code)
-    if isinstance(stream, torch.cuda.Stream):      # (allocated for the current stream, used on this one)
-        for t in made:
-            t.record_stream(stream)
     return o, lse
 
 
@@ -632,7 +643,9 @@ def path_paged_attn(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new
                     scale=None, o=None, lse=None, workspace=None, stream=None):
     """Attention of packed new tokens over paged caches, which are only read: q [T,H*group,d], k, v, w [T,H,d], beta (and log_f) [T,H];
     kpages, vpages [num_pages,H,page_size,d] (cpages [num_pages,H,page_size] fp32); page_table [nseq,pages_per_seq], cached [nseq], cu_new [nseq+1]
-    int32 on the GPU.  Returns (o [T,H*group,d], lse [T,H*group]); rows of no sequence are left as they are."""
+    int32 on the GPU.  Returns (o [T,H*group,d], lse [T,H*group]); rows of no sequence are left as they are.
+    ``stream`` (a torch stream or a handle; None: the current one): what the call makes itself -- o, lse, workspace -- comes from that stream's memory, ready there
+    and nowhere else."""
     return _paged_call("path_paged_attn", q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream)
 
 
