@@ -2,9 +2,10 @@
 //
 // The d x d matrix comes from the scan over the chunk's tiles (paged_chunk16.hip, fp32 paged_chunk.hip).  As products of 16 keys at a time, K'^T = K^T + M K^T
 // with M's rows numbered so that a lane's results are the elements that it loaded: from memory to registers to memory.  16-bit: a wave
-// holds all of M (128 registers at d = 128) and takes every fourth group of 16 keys; keys are bf16 numbers, which fp16
-// holds exactly within its range.  fp32: M lies in LDS.
-// Bound by memory: every key read and written once, three groups of a wave on their way (16 heads of 8192, d = 128: 16 us, 4.2 TB/s; one group 22).
+// holds all of M (128 registers at d = 128) and takes every fourth group of 16 keys.  M's elements are at most 2, transitions being contractions, and one fp16 number
+// each; a key is brought to [1, 2) by a power of two before it is made fp16 numbers and back after the product, so that keys of any size are carried alike
+// (as they stood, those from 65520 on became infinite and those below 2^-25 were not carried).  fp32: M lies in LDS.
+// Bound by memory: every key read and written once, three groups of a wave on their way (16 heads of 8192, d = 128: 17.6 us, 3.8 TB/s, of which the scaling is 1; with one group on its way 6 more).
 #include "paged_decl.h"
 
 namespace path {
@@ -46,21 +47,32 @@ __global__ __launch_bounds__(256, 2) void paged_refresh_kernel(PagedArgs a) {
         auto carry = [&](const PagedGroup& p, const u32x4* k) {
             halfx8 kh[KR];
             union { u32x4 u; bf16x8 b; } x[KR];
+            // the key's exponent: that of its largest element, in the four lanes that have it (as an integer, which orders bf16 numbers without their sign)
+            unsigned even = 0, odd = 0;
 #pragma unroll
             for (int j = 0; j < KR; ++j) {
                 x[j].u = k[j];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) kh[j][e] = (half_t)(float)x[j].b[e];
+                for (int e = 0; e < 4; ++e) {
+                    even = max(even, k[j][e] << 16 & 0x7f800000u);
+                    odd = max(odd, k[j][e] & 0x7f800000u);
+                }
             }
+            const unsigned top = __float_as_uint(max_rows(__uint_as_float(max(even, odd))));
+            const unsigned expo = min(max(top, 1u << 23), 253u << 23);
+            const float down = __uint_as_float((254u << 23) - expo), up = __uint_as_float(expo);      // 2^(127 - e), 2^(e - 127)
+#pragma unroll
+            for (int j = 0; j < KR; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) kh[j][e] = (half_t)((float)x[j].b[e] * down);
+            __builtin_amdgcn_sched_barrier(0);      // (products between the conversions would need more registers than there are)
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) {
-                f32x4 y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = (float)x[t >> 1].b[4 * (t & 1) + e];
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) y = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][j], kh[j], y, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[t >> 1].b[4 * (t & 1) + e] = (bf16_t)y[e];
+                for (int e = 0; e < 4; ++e) x[t >> 1].b[4 * (t & 1) + e] = (bf16_t)((float)x[t >> 1].b[4 * (t & 1) + e] + y[e] * up);
             }
             const __amdgpu_buffer_rsrc_t r = paged_rsrc(a.kpages, p.row, p.valid, ROWB);
 #pragma unroll
