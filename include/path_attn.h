@@ -369,6 +369,8 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
  * Arithmetic with PATH_BF16: what is computed from the inputs -- X, the carried keys, the transitions -- is multiplied as the sum of two bf16 numbers, with
  * bf16's range (log-sum-exp good to 1e-6 of itself), probabilities as one.  The one exception: the product of a chunk's transitions that its append applies to
  * the cached keys is an fp16 operand, beta and w being held to the range rule above; the keys there are scaled by powers of two and may have any size.
+ * Infinities and NaN: a token's key and value show in no row before it, a cached one's in its own sequence and head only.  w, beta, log_f and c have to be
+ * finite: one that is not may spoil all rows and keys of its sequence and head.
  * workspace: path_paged_workspace_bytes(...) bytes (0 for arguments that the calls reject; grows with every bound, so that one for the largest call serves
  * all smaller ones; path_paged_append as with group 1), 256-byte aligned; contents undefined before and after.
  * Errors: PATH_ERR_SHAPE for nseq, H, group or max_new < 1, group > 64, T or max_cached < 0, a page size that is not allowed, or max_cached >

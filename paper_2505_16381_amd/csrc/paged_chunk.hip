@@ -321,6 +321,24 @@ __global__ __launch_bounds__(256, 2) void paged_sweep_kernel(PagedArgs a) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) S[b] = *reinterpret_cast<const f32x4*>(sd + 16 * b + 4 * g);
         attend(ct, S, true);
+        if (__any(not_finite<DT>(O))) {      // a later token's infinity or NaN shows in the product with its weight 0: the values up to each row's own token again
+#pragma unroll
+            for (int t = 0; t < DT; ++t) O[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                for (int from = 0; from < 4; ++from) {
+                    const int key = 16 * (k >> 2) + 4 * from + (k & 3);
+                    const float p = __shfl(S[k >> 2][k & 3], 16 * from + c);
+                    if (!there || key > row) continue;
+                    const float* const v = reinterpret_cast<const float*>(a.v) + ((long long)(q.t0 + 64 * ct + key) * a.H + h) * D + 4 * g;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(v + 16 * t);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) O[t][i] += p * x[i];
+                    }
+                }
+        }
     }
     for (int j = ct - 1; j >= 0; --j) {
         const size_t th = ((size_t)(first + j) * a.H + h) * 64 * D;

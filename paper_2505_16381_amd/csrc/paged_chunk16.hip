@@ -428,6 +428,26 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
                 for (int k = 0; k < 4; ++k) O[t + k] = mfma32(v[k], P, O[t + k]);
             }
         };
+        // The own tile's values again, each row with no token behind it: what a later one holds would show in the product with its weight 0 if it is an infinity or
+        // NaN.  Then this takes the product's place (and where a row's own are such: it gives what the product gave).
+        auto own_values = [&]() {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) O[t] = zero;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                for (int from = 0; from < 4; ++from) {
+                    const int key = 32 * part + 16 * (k >> 2) + 4 * from + (k & 3);
+                    const float p = __shfl((float)P[k], 16 * from + c);
+                    if (!there || key > row) continue;
+                    const bf16_t* const v = user(a.v, ct) + (long long)key * a.H * D + 4 * g;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        const bf16x4 x = *reinterpret_cast<const bf16x4*>(v + 16 * t);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) O[t][i] += p * (float)x[i];
+                    }
+                }
+        };
         long long place[2];      // SCAN: where this lane's key of each block goes
         auto places = [&](int j) {
 #pragma unroll
@@ -450,6 +470,7 @@ __device__ __forceinline__ void sweep16(const PagedArgs& a, unsigned char* smem,
             softmax(ct, true);
             wait_async_and_sync();
             values();
+            if (__any(not_finite<DT>(O))) own_values();
             lds_barrier();
             if (ct > 0) bring1(ct - 1);
         }

@@ -115,6 +115,15 @@ __device__ __forceinline__ float sum_lanes16(float x) {
     x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, true));
     return x;
 }
+// Whether one of N registers of four is an infinity or NaN (by the bits: comparisons take NaN for absent)
+template <int N> __device__ __forceinline__ bool not_finite(const f32x4* x) {
+    unsigned top = 0;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[t][i]) & 0x7fffffffu);
+    return top >= 0x7f800000u;
+}
 // E consecutive elements as fp32
 template <int E, typename T> __device__ __forceinline__ void load_f32(const T* p, float* x) {
     typedef T V __attribute__((ext_vector_type(E)));
