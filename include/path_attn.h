@@ -374,7 +374,8 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
  * workspace: path_paged_workspace_bytes(...) bytes (0 for arguments that the calls reject; grows with every bound, so that one for the largest call serves
  * all smaller ones; path_paged_append as with group 1), 256-byte aligned; contents undefined before and after.
  * Errors: PATH_ERR_SHAPE for nseq, H, group or max_new < 1, group > 64, T or max_cached < 0, a page size that is not allowed, or max_cached >
- * pages_per_seq * page_size, or more than 65535 of nseq * H or H * group; PATH_ERR_NULL also if only one of log_f and cpages is given.  T = 0 does nothing.
+ * pages_per_seq * page_size, more than 65535 of nseq * H or H * group, or bounds for which a kernel would need 2^32 threads (fp32: T * H * group of 2^26;
+ * bf16: 2^28; thousands of sequences times heads with bounds of millions of cached tokens); PATH_ERR_NULL also if only one of log_f and cpages is given.  T = 0 does nothing.
  */
 size_t path_paged_workspace_bytes(int nseq, int T, int max_new, int max_cached, int H, int group, int d, path_dtype_t dt);
 path_status_t path_paged_attn(const void* q, const void* k, const void* v, const void* w, const void* beta, const void* log_f,

@@ -1031,10 +1031,26 @@ static PagedPlan paged_plan(int nseq, int T, int max_new, int max_cached, int H,
     return p;
 }
 
+// HIP takes launches of fewer than 2^32 threads.  Looked at before the first one, for all that attention and append of these bounds launch: a call that fails at its
+// last launch has already written new keys.
+static bool paged_launches_ok(const PagedPlan& p, int nseq, int T, int max_cached, int H, int group, int d, size_t es) {
+    const long long units = (long long)nseq * H, Hq = (long long)H * group, limit = 1LL << 32;
+    if (p.few && units * p.few_splits * 64 * p.few_waves >= limit) return false;
+    const bool few = p.few && p.few_splits > 1, many = p.many && p.many_splits > (es == 2);
+    if ((few ? nseq * p.few_m * Hq : 0) * 64 + (many ? T * Hq : 0) * 64 + 512 >= limit) return false;      // records joined
+    if (!p.many) return true;
+    if (p.tiles * (long long)H * 512 >= limit) return false;                                               // chunk transform
+    if ((units * d + p.tiles * Hq * 64) * 16 >= limit) return false;                                       // sweep, scan (bf16; fp32: a quarter)
+    if (es == 2 ? (H * (long long)p.many_splits + 7) * p.row_blocks * 256 >= limit : p.tiles * Hq * p.many_splits * 256 >= limit) return false;
+    return units * ((max_cached + p.refresh_len - 1LL) / p.refresh_len) * 256 < limit;
+}
+
 extern "C" size_t path_paged_workspace_bytes(int nseq, int T, int max_new, int max_cached, int H, int group, int d, path_dtype_t dt) {
     if (dt != PATH_F32 && dt != PATH_BF16) return 0;
     if (!paged_shape_ok(nseq, T, max_new, max_cached, H, group, d)) return 0;
-    return paged_plan(nseq, T, max_new, max_cached, H, group, d, dt == PATH_F32 ? 4 : 2, true).total;      // (the append needs no records)
+    const size_t es = dt == PATH_F32 ? 4 : 2;
+    const PagedPlan p = paged_plan(nseq, T, max_new, max_cached, H, group, d, es, true);      // (the append needs no records)
+    return paged_launches_ok(p, nseq, T, max_cached, H, group, d, es) ? p.total : 0;
 }
 
 static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1047,7 +1063,9 @@ static path_status_t paged_call(PagedArgs a, int page_size, int d, path_dtype_t 
     if (a.max_cached > (long long)a.per_seq * page_size) return PATH_ERR_SHAPE;
     if (a.attn && !(a.scale > 0.f)) return PATH_ERR_UNSUPPORTED;
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
-    const PagedPlan p = paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, dt == PATH_F32 ? 4 : 2, a.attn);
+    const size_t es = dt == PATH_F32 ? 4 : 2;
+    if (!paged_launches_ok(paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, es, true), a.nseq, a.T, a.max_cached, a.H, a.G, d, es)) return PATH_ERR_SHAPE;
+    const PagedPlan p = paged_plan(a.nseq, a.T, a.max_new, a.max_cached, a.H, a.G, d, es, a.attn);
     if (workspace_bytes < p.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
     const void* al[] = {a.q, a.k, a.v, a.w, a.kpages, a.vpages, a.cpages, a.o};
     for (const void* ptr : al) if (misaligned(ptr)) return PATH_ERR_ALIGN;
