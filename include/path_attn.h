@@ -367,7 +367,7 @@ path_status_t path_decode_step_fox(const void* q, const void* k, const void* v, 
  * rounds the refreshed key first.  A server may put appends off: the new tokens of path_paged_attn are then all tokens since the
  * last append (keys are read and written back, and rounded, once per append instead of once per token).
  * Arithmetic with PATH_BF16: what is computed from the inputs -- X, the carried keys, the transitions -- is multiplied as the sum of two bf16 numbers, with
- * bf16's range (log-sum-exp good to 1e-6 of itself), probabilities as one.  The one exception: the product of a chunk's transitions that its append applies to
+ * bf16's range (log-sum-exp 5e-7 off in the mean, single rows up to 6e-6), probabilities as one.  The one exception: the product of a chunk's transitions that its append applies to
  * the cached keys is an fp16 operand, beta and w being held to the range rule above; the keys there are scaled by powers of two and may have any size.
  * Infinities and NaN: a token's key and value show in no row before it, a cached one's in its own sequence and head only.  w, beta, log_f and c have to be
  * finite: one that is not may spoil all rows and keys of its sequence and head.

@@ -12,7 +12,7 @@
 // A piece of 16 rows in LDS is 16-byte pieces exchanged as in lds_tile.h, such that neither fragments along a row nor transposing reads
 // meet on a bank; the copies fetch them in that order.  Past the end of the sequence and in holes they bring zeros (the buffer's bounds).
 // Two workgroups share a CU (64 KB of LDS, 256 registers): the softmax of one runs under the products of the other.  512 rows over 8192 tokens and 2048 over
-// 16384, 16 query heads, d = 128: 61 and 380 us, 730 TFLOP/s of logits and P V or 1.1 PFLOP/s of products; bound by the matrix units at the clock that
+// 16384, 16 query heads, d = 128: 60 and 405 us (medians under a profiler; 372 at best), 680 TFLOP/s of logits and P V or 1.0 PFLOP/s of products; bound by the matrix units at the clock that
 // power leaves them (half of their cycles): without X's second part 82 us less, with a stage's exponentials put between the next one's products, by hand or in a
 // pipeline of half stages, the same.  The
 // accumulator is rescaled only when a row's maximum has grown by more than 8 (2^8 in P and its sum is exact enough: both are floating).

@@ -689,9 +689,11 @@ static hipError_t launch_sweep16_t(const PagedArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((paged_sweep16_kernel<D, RS>), dim3(grid), dim3(256 * RS), bytes, st, a);
     return hipGetLastError();
 }
-// 32 rows per workgroup shorten the chain (two waves a SIMD instead of four) as long as there is a CU for nearly each of them; then 64, which bring the tiles for
-// twice as many.  us a call, 32 / 64 rows, d = 128, 16 heads over nothing: 256 tokens 29.9 / 31.2, 512 38.7 / 45.0, 1000 66.3 / 67.4, 1500 123 / 103,
-// 2048 182 / 147, 32 heads of 1000 125 / 102; append alone 512 33.8 / 38.3, 2048 91 / 113, to 8 sequences 111 / 89.
+// 32 rows per workgroup shorten a step (two waves a SIMD instead of four), 64 bring the tiles for twice as many rows.  A CU holds one workgroup, and those with the
+// longest ways start first, so that 32 rows, two workgroups for every tile and head, win up to about two for each CU: the last tiles' fill the chip, the first ones' short
+// ways run behind them.  us a call over nothing, 32 / 64 rows, 16 heads, d = 128: 512 tokens 36.0 / 40.4, 1000 (256 tiles and heads) 56.2 / 61.2, 1080 (272) 72.8 / 74.3,
+// 1150 (288) 78.6 / 77.3, 1500 (384) 111 / 93.5; with the append, whose scan's workgroups come on top, 1000 66.7 / 67.4, 1080 84.7 / 81.5; d = 64: 1080 48.8 / 50.9, 1300
+// 54.7 / 56.2, 1500 61.8 / 60.4.  The append alone, 512 tokens, d = 128: 32 heads 53.5 / 59.1, 64 (8192) 72.2 / 69.5, 96 102 / 83.7; d = 64: 8192 64.7 / 66.0.
 hipError_t launch_paged_sweep16(const PagedArgs& a, int d, hipStream_t st) {
     const bool narrow = a.attn ? (a.T / 64 + 1) * a.H * a.G <= 272 : a.nseq * a.H * d <= 8192;
     if (narrow) return d == 64 ? launch_sweep16_t<64, 2>(a, st) : launch_sweep16_t<128, 2>(a, st);

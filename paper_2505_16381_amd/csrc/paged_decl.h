@@ -44,7 +44,7 @@ struct PagedArgs {
     float *many_o, *many_ml;                       // [1 + split][T * H * G][d], [..][2]; record 0: the new tokens' own
     void *kt, *wt, *zt, *vt;                       // [tiles][H]: operand tiles of the new tokens, see paged_chunk.hip (bf16: kt, zt only, [hi, lo][tiles][H])
     float* sd;                                     // [tiles][H*G][64][64] logits inside a tile
-    void* pt;                                      // [nseq][H][d][d]: H_{m-1} .. H_0 - I of all new tokens (fp32, fp16)
+    void* pt;                                      // [nseq][H][d][d]: H_{m-1} .. H_0 - I of all new tokens (fp32; with bf16 fp16)
 };
 
 struct PagedSeq { int n, t0, m; };

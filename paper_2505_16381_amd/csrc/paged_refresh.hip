@@ -5,7 +5,7 @@
 // holds all of M (128 registers at d = 128) and takes every fourth group of 16 keys.  M's elements are at most 2, transitions being contractions, and one fp16 number
 // each; a key is brought to [1, 2) by a power of two before it is made fp16 numbers and back after the product, so that keys of any size are carried alike
 // (as they stood, those from 65520 on became infinite and those below 2^-25 were not carried).  fp32: M lies in LDS.
-// Bound by memory: every key read and written once, three groups of a wave on their way (16 heads of 8192, d = 128: 17.6 us, 3.8 TB/s, of which the scaling is 1; with one group on its way 6 more).
+// Bound by memory: every key read and written once, three groups of a wave on their way (16 heads of 8192, d = 128: 18 us, 3.7 TB/s, of which scaling takes 1; with one group on its way 6 more).
 #include "paged_decl.h"
 
 namespace path {
