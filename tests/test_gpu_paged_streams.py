@@ -71,3 +71,27 @@ def test_given_tensors_stay_the_callers(gpu):
         got = attn(pa, y, o=o, stream=stream)
         torch.cuda.synchronize()
         assert got[0] is o and torch.equal(o, want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("kind", ["stream", "handle", "forked"])
+def test_made_tensors_in_a_captured_call(gpu, kind):
+    """The call given its stream while that is being captured, or another one forked from it, with everything made by the call: replayed between eager calls."""
+    torch, pa = gpu
+    y = {n: t.cuda() if t is not None else None for n, t in pm.batch([300, 40], [40, 2], 2, 1, 64, 16, "bf16", seed=3).items()}
+    z = {n: t.cuda() if t is not None else None for n, t in pm.batch([300, 40], [40, 2], 2, 1, 64, 16, "bf16", seed=3).items()}
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    attn(pa, z)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        if kind == "forked":
+            other.wait_stream(s)
+        o, lse = attn(pa, y, stream={"stream": s, "handle": s.cuda_stream, "forked": other}[kind])
+        if kind == "forked":
+            s.wait_stream(other)
+    for step in range(3):
+        y["q"].copy_(torch.roll(z["q"], step, 0))
+        graph.replay()
+        want = attn(pa, {**z, "q": torch.roll(z["q"], step, 0)})
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]), step
