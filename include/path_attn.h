@@ -395,6 +395,69 @@ path_status_t path_paged_extend(const void* q, const void* k, const void* v, con
                                 path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Page tables of the path_paged_* calls, made to fit the requests' lengths on the GPU (lengths, tables and the stack of free pages are DEVICE int32 arrays; nothing is
+ * read back, so a captured call follows them through its replays).  For every sequence, cached [nseq] is how many tokens stay and new_tokens [nseq] how many the coming call
+ * brings (0 and 0: the sequence has ended; a smaller `cached` than before: drafts were dropped; negative counts as 0):
+ *   1. entries of page_table [nseq, pages_per_seq] behind the ceil((cached + new) / page_size) pages that its tokens want go back: entries that are pages (0 .. num_pages - 1) are
+ *      put on the stack free_pages [num_pages], whose first free_count [1] entries are free; all of them become -1.
+ *   2. entries of new tokens' pages -- from ceil(cached / page_size) on -- that are no page get the one on top of the stack; if it is empty they become -1 (a hole) and are
+ *      counted in missing [nseq].  Entries of pages that already hold cached tokens are left as they are.
+ *   3. cu_new [nseq + 1] = offsets of the packed new tokens; slots [T] (64 bits) = page * page_size + place in it of every new token; -1 where there is no page, and for t behind
+ *      the last new token.  T bounds the new tokens: offsets end at it, and tokens behind it take no part.  Tokens past pages_per_seq * page_size get no slot.
+ * Pages go back before any is taken, both in the order of the table (sequence after sequence): the result is always the same.  A page is in one entry only (a page in two
+ * entries goes back twice); what finds no room on the stack is dropped.  free_count outside 0 .. num_pages is held to it.
+ * workspace: path_paged_plan_workspace_bytes(...) bytes (0 for sizes that are refused), 256-byte aligned.
+ * Errors: PATH_ERR_SHAPE for nseq, num_pages or pages_per_seq < 1, T < 0, more than 2^22 sequences, or a page size that the path_paged_* calls do not take.  slots may be NULL if T = 0.
+ */
+size_t path_paged_plan_workspace_bytes(int nseq, int pages_per_seq, int T);
+path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* page_table, int* free_pages, int* free_count, int* cu_new, long long* slots, int* missing, int nseq,
+                              int T, int num_pages, int page_size, int pages_per_seq, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gated delta rule: the recurrence whose transitions PaTH attention takes into the softmax, as layers beside it use it.  A value head's state S [d, d] (rows: key index,
+ * columns: value index; always fp32) follows
+ *     S' = f_t S,   u_t = beta_t (v_t - S'^T k_t),   S = S' + k_t u_t^T,   o_t = scale S^T q_t,        f_t = exp(log_f_t),
+ * evaluated by chunks of 64 tokens (served sequences of up to 8 new tokens: token by token).  H key heads, V = H * group value heads: value heads h * group .. h * group + group - 1
+ * share q and k of head h.  log_f NULL: no gates.  q, k as given (unit vectors keep the recurrence from growing), beta as given.
+ * Shapes: q, k, dq, dk [B,H,L,d], v, o, d_o, dv [B,V,L,d], beta, log_f, dbeta, dlog_f [B,V,L] (PATH_LAYOUT_BHLD), or the same with the token axis before the heads
+ * (PATH_LAYOUT_BLHD), with nseq = B, max_len = L, T = B * L, cu_seqlens NULL; or packed: [T,H,d], [T,V,d], [T,V] (PATH_LAYOUT_BLHD), sequence s being the tokens
+ * cu_seqlens[s] .. cu_seqlens[s+1]-1 (DEVICE int32 [nseq + 1], not decreasing), none longer than max_len; offsets and lengths past T and max_len are held to them.  Rows that belong to no sequence are left
+ * as they are.  Sequences of no tokens: allowed.
+ *   path_delta_fwd        o; state_in [nseq,V,d,d] = first states (NULL: zeros), state_out = last ones (NULL: not wanted; may be state_in).
+ *   path_delta_train_fwd  the same, leaving in `workspace` what the gradients need.
+ *   path_delta_train_bwd  gradients of sum(d_o * o) + sum(d_state_out * state_out) (d_state_out NULL: zeros), from the workspace of path_delta_train_fwd on the same
+ *                         tensors and sizes (state_in given to both or neither), as often as wanted; dlog_f is NULL exactly if log_f is, d_state_in if state_in is.  What a step
+ *                         does not want to keep it recomputes by calling path_delta_train_fwd again.
+ *   path_delta_extend     serving: packed new tokens (as cu_new of the path_paged_* calls, at most max_new a sequence) for states in a pool [num_slots,V,d,d], carried on in place.
+ *                         slots [nseq] (DEVICE int32): the sequence's state; outside 0 .. num_slots - 1: starts from zeros and is not kept.  cached [nseq] (DEVICE int32, as in the
+ *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
+ *                         have different slots (the state of one that is named twice is undefined; no fault).
+ * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16 accumulates in fp32; q, k, v are operands as they are, what is computed is multiplied as the sum of two bf16 numbers, of
+ * three where states are handed out (bf16's range; states 1e-6 of their norm from exact ones, o and gradients that are rounded to bf16 once).  dq, dk, dbeta, dlog_f are computed from fp16 operands over powers of two taken
+ * from their largest values (q and k themselves: below 65504).  log_f below -200 counts as -200; log_f > 0 is carried as it is.
+ * Infinities and NaN: values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
+ * sequence and head; token by token, no row before them.
+ * No atomics: the same bits every time.
+ * workspace: path_delta_workspace_bytes(...) bytes (0 for sizes that are refused; training != 0 for the path_delta_train_* pair), 256-byte aligned; grows with every argument, so that one for the
+ * largest call serves all smaller ones.
+ * Errors: PATH_ERR_SHAPE for nseq, max_len, H or group < 1, T < 0, T != nseq * max_len without cu_seqlens, nseq * V >= 2^21, (T / 64 + nseq) * V >= 2^23, V > 65535;
+ * PATH_ERR_UNSUPPORTED for scale <= 0 or a packed batch that is not PATH_LAYOUT_BLHD; PATH_ERR_ALIGN for q, k, v, o, states or gradients of these off 16 bytes.
+ */
+size_t path_delta_workspace_bytes(int nseq, int T, int max_len, int H, int group, int d, path_dtype_t dt, int training);
+path_status_t path_delta_fwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in, void* o,
+                             float* state_out, int nseq, int T, int max_len, int H, int group, int d, int layout, float scale, path_dtype_t dt, void* workspace,
+                             size_t workspace_bytes, void* stream);
+path_status_t path_delta_train_fwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in, void* o,
+                                   float* state_out, int nseq, int T, int max_len, int H, int group, int d, int layout, float scale, path_dtype_t dt, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+path_status_t path_delta_train_bwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in, const void* d_o,
+                                   const float* d_state_out, void* dq, void* dk, void* dv, void* dbeta, void* dlog_f, float* d_state_in, int nseq, int T, int max_len,
+                                   int H, int group, int d, int layout, float scale, path_dtype_t dt, void* workspace, size_t workspace_bytes, void* stream);
+path_status_t path_delta_extend(const void* q, const void* k, const void* v, const void* beta, const void* log_f, float* states, const int* slots, const int* cached,
+                                const int* cu_new, void* o, int nseq, int T, int max_new, int num_slots, int H, int group, int d, float scale, path_dtype_t dt, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
  * Sequence-parallel forward: ONE device's share of the ring of paper Sec. 3.5 ("context parallelism": the
  * sequence is split into contiguous segments, one per device; a device attends its own segment, then the
  * segments to its left one hop at a time, applying one d x d product per super-block it has passed).  The three

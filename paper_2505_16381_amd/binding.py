@@ -127,6 +127,19 @@ def load_library():
     lib.path_paged_append.argtypes = [vp] * 11 + [ci] * 10 + [vp, sz, vp]
     lib.path_paged_extend.restype = ci
     lib.path_paged_extend.argtypes = [vp] * 14 + [ci] * 10 + [cf, ci, vp, sz, vp]
+    lib.path_paged_plan_workspace_bytes.restype = sz
+    lib.path_paged_plan_workspace_bytes.argtypes = [ci] * 3
+    lib.path_paged_plan.restype = ci
+    lib.path_paged_plan.argtypes = [vp] * 8 + [ci] * 5 + [vp, sz, vp]
+    lib.path_delta_workspace_bytes.restype = sz
+    lib.path_delta_workspace_bytes.argtypes = [ci] * 8
+    for name in ("path_delta_fwd", "path_delta_train_fwd"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [vp] * 9 + [ci] * 7 + [cf, ci, vp, sz, vp]
+    lib.path_delta_train_bwd.restype = ci
+    lib.path_delta_train_bwd.argtypes = [vp] * 15 + [ci] * 7 + [cf, ci, vp, sz, vp]
+    lib.path_delta_extend.restype = ci
+    lib.path_delta_extend.argtypes = [vp] * 10 + [ci] * 7 + [cf, ci, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -660,3 +673,192 @@ def path_paged_extend(q, k, v, w, beta, kpages, vpages, page_table, cached, cu_n
                       scale=None, o=None, lse=None, workspace=None, stream=None):
     """path_paged_attn, then path_paged_append; few new tokens a sequence (one, or drafts) in one pass over its cache."""
     return _paged_call("path_paged_extend", q, k, v, w, beta, kpages, vpages, page_table, cached, cu_new, max_new, max_cached, log_f, cpages, scale, o, lse, workspace, stream)
+
+
+def _look(looked, dev, whose):
+    """Checks tensors' shapes, types and places, in one pass; what is wrong is said only where something is."""
+    if dev < 0 or any([t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() for _, t, shape, dtype in looked]):
+        for name, t, shape, dtype in looked:
+            if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+                raise ValueError(f"{name} is {tuple(shape)}, {dtype}: got {tuple(t.shape)}, {t.dtype}")
+        for name, t, _, _ in looked:
+            if t.get_device() != dev or dev < 0 or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous and on the GPU that {whose} is on")
+
+
+def _scratch(workspace, nbytes, like, stream, whose):
+    import torch
+    if workspace is None:
+        return _paged_made(like, (max(256, nbytes),), torch.uint8, stream, False)
+    if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on the GPU that {whose} is on")
+    return workspace
+
+
+def _call_on(dev, name, args, stream):
+    """One call of the library, launched on GPU `dev`."""
+    import torch
+    call = getattr(load_library(), name)
+    if torch.cuda.current_device() == dev:
+        code = call(*args, _stream_handle(stream))
+    else:
+        with torch.cuda.device(dev):
+            code = call(*args, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def path_paged_plan_workspace_bytes(nseq, pages_per_seq, T) -> int:
+    """Bytes of scratch that path_paged_plan needs; 0 for sizes that it refuses."""
+    if any(not 0 <= x < 1 << 31 for x in (nseq, pages_per_seq, T)):      # (ctypes keeps the low 32 bits)
+        return 0
+    return int(load_library().path_paged_plan_workspace_bytes(nseq, pages_per_seq, T))
+
+
+def path_paged_plan(cached, new, page_table, free_pages, free_count, T, page_size, cu_new=None, slots=None, missing=None, workspace=None, stream=None):
+    """Makes the page tables of the path_paged_* calls fit the requests' lengths, on the GPU: cached, new [nseq] tokens that stay and that come, page_table
+    [nseq,pages_per_seq], the stack free_pages [num_pages] with free_count [1] pages on it (all int32; the last three are updated), at most T new tokens.  Returns
+    (cu_new [nseq+1] int32, slots [T] int64, missing [nseq] int32)."""
+    import torch
+    if cached.dim() != 1 or page_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("cached is [nseq], page_table [nseq,pages_per_seq], free_pages [num_pages]")
+    (nseq,), per_seq, pool, dev, i32 = cached.shape, page_table.shape[1], free_pages.shape[0], cached.get_device(), torch.int32
+    T, page_size = int(T), int(page_size)
+    if not 0 <= T < 1 << 31 or not 0 <= page_size < 1 << 31:
+        raise ValueError(f"T and page_size are 32-bit sizes: got {T}, {page_size}")
+    if cu_new is None:
+        cu_new = _paged_made(cached, (nseq + 1,), i32, stream, True)
+    if slots is None:
+        slots = _paged_made(cached, (T,), torch.int64, stream, True)
+    if missing is None:
+        missing = _paged_made(cached, (nseq,), i32, stream, True)
+    _look([("cached", cached, (nseq,), i32), ("new", new, (nseq,), i32), ("page_table", page_table, (nseq, per_seq), i32), ("free_pages", free_pages, (pool,), i32),
+           ("free_count", free_count, (1,), i32), ("cu_new", cu_new, (nseq + 1,), i32), ("slots", slots, (T,), torch.int64), ("missing", missing, (nseq,), i32)], dev, "cached")
+    workspace = _scratch(workspace, path_paged_plan_workspace_bytes(nseq, per_seq, T), cached, stream, "cached")
+    _call_on(dev, "path_paged_plan", (cached.data_ptr(), new.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), cu_new.data_ptr(), slots.data_ptr(),
+                                      missing.data_ptr(), nseq, T, pool, page_size, per_seq, workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
+    return cu_new, slots, missing
+
+
+def path_delta_workspace_bytes(nseq, T, max_len, H, group, d, dt, training=False) -> int:
+    """Bytes of scratch of the path_delta_* calls (training: of the path_delta_train_* pair); 0 for sizes that they refuse."""
+    if any(not 0 <= x < 1 << 31 for x in (nseq, T, max_len, H, group, d)):      # (ctypes keeps the low 32 bits)
+        return 0
+    return int(load_library().path_delta_workspace_bytes(nseq, T, max_len, H, group, d, dt, int(bool(training))))
+
+
+def _delta_sizes(q, v, cu_seqlens, max_len, layout):
+    """nseq, T, max_len, H, group, d, layout, and the shapes of tensors with the key heads, the value heads and of per-token numbers."""
+    if cu_seqlens is not None:
+        if q.dim() != 3 or v.dim() != 3 or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
+            raise ValueError("packed: q is [T,H,d], v [T,H*group,d], cu_seqlens [nseq+1]")
+        if max_len is None:
+            raise ValueError("packed: max_len, a bound on the sequences' lengths, has to be given")
+        (T, H, d), V, nseq, L = q.shape, v.shape[1], cu_seqlens.shape[0] - 1, int(max_len)
+        if not -(1 << 31) <= L < 1 << 31:      # (ctypes keeps the low 32 bits)
+            raise ValueError(f"max_len is a 32-bit bound: got {L}")
+        shapes, layout = ((T, H, d), (T, V, d), (T, V)), PATH_LAYOUT_BLHD
+    else:
+        if q.dim() != 4 or v.dim() != 4:
+            raise ValueError("q is [B,H,L,d] or [B,L,H,d], v the same with H*group heads")
+        if layout not in (PATH_LAYOUT_BHLD, PATH_LAYOUT_BLHD):
+            raise ValueError(f"layout {layout}")
+        at = 1 if layout == PATH_LAYOUT_BHLD else 2
+        nseq, H, L, d, V = q.shape[0], q.shape[at], q.shape[3 - at], q.shape[3], v.shape[at]
+        T = nseq * L
+        if T >= 1 << 31:
+            raise ValueError(f"{T} tokens: at most 2^31 - 1")
+        dims = lambda heads: (nseq, heads, L) if at == 1 else (nseq, L, heads)
+        shapes = ((*dims(H), d), (*dims(V), d), dims(V))
+    if H == 0 or V % H:
+        raise ValueError(f"v has a multiple of q's {H} heads: got {V}")
+    return nseq, T, L, H, V // H, d, layout, shapes
+
+
+def _delta_look(q, k, v, beta, log_f, cu_seqlens, states, more, shapes):
+    import torch
+    td, dev = q.dtype, q.get_device()
+    looked = [("q", q, shapes[0], td), ("k", k, shapes[0], td), ("v", v, shapes[1], td), ("beta", beta, shapes[2], td)]
+    if log_f is not None:
+        looked.append(("log_f", log_f, shapes[2], td))
+    if cu_seqlens is not None:
+        looked.append(("cu_seqlens", cu_seqlens, cu_seqlens.shape, torch.int32))
+    looked += [(name, t, shape, torch.float32) for name, t, shape in states if t is not None]
+    _look(looked + [(name, t, shape, td) for name, t, shape in more], dev, "q")
+    return dev
+
+
+def _delta_fwd(name, q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, state_in, final_state, o, state_out, workspace, stream):
+    import torch
+    nseq, T, L, H, G, d, layout, shapes = _delta_sizes(q, v, cu_seqlens, max_len, layout)
+    dt, st = _dt_of(q), (nseq, H * G, d, d)
+    if o is None:
+        o = _paged_made(v, v.shape, v.dtype, stream, True)
+    if state_out is None and final_state:
+        state_out = _paged_made(v, st, torch.float32, stream, True)
+    dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("state_out", state_out, st)], [("o", o, shapes[1])], shapes)
+    workspace = _scratch(workspace, path_delta_workspace_bytes(nseq, T, L, H, G, d, dt, name == "path_delta_train_fwd"), q, stream, "q")
+    if T > 0 or state_out is not None:
+        _call_on(dev, name, (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), _opt(cu_seqlens), _opt(state_in), o.data_ptr(), _opt(state_out), nseq, T, L, H, G, d,
+                             layout, float(d ** -0.5 if scale is None else scale), dt, workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
+    return (o, state_out) if state_out is not None else o
+
+
+def path_delta_fwd(q, k, v, beta, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, final_state=False, o=None, state_out=None,
+                   workspace=None, stream=None):
+    """Gated delta rule: q, k [B,H,L,d], v [B,H*group,L,d], beta (and log_f) [B,H*group,L], or with the tokens before the heads (``layout``), or packed [T,heads,d] with
+    cu_seqlens [nseq+1] (int32, on the GPU) and max_len, a bound on the lengths.  Returns o, and the last states [nseq,H*group,d,d] (fp32) with ``final_state`` or ``state_out``."""
+    return _delta_fwd("path_delta_fwd", q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, state_in, final_state, o, state_out, workspace, stream)
+
+
+def path_delta_train_fwd(q, k, v, beta, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, final_state=False, o=None, state_out=None,
+                         workspace=None, stream=None):
+    """path_delta_fwd, which leaves in ``workspace`` (path_delta_workspace_bytes(.., training=True) bytes, needed) what path_delta_train_bwd takes from it."""
+    if workspace is None:
+        raise ValueError("the workspace is what the backward starts from: it has to be given")
+    return _delta_fwd("path_delta_train_fwd", q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, state_in, final_state, o, state_out, workspace, stream)
+
+
+def path_delta_train_bwd(q, k, v, beta, d_o, workspace, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, d_state_out=None, stream=None):
+    """(dq, dk, dv, dbeta[, dlog_f][, d_state_in]) from the workspace of path_delta_train_fwd on the same tensors; d_state_out: gradient of the last states."""
+    import torch
+    nseq, T, L, H, G, d, layout, shapes = _delta_sizes(q, v, cu_seqlens, max_len, layout)
+    dt, st = _dt_of(q), (nseq, H * G, d, d)
+    dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("d_state_out", d_state_out, st)], [("d_o", d_o, shapes[1])], shapes)
+    _scratch(workspace, 0, q, stream, "q")
+    made = lambda like: _paged_made(like, like.shape, like.dtype, stream, True)
+    out = [made(q), made(k), made(v), made(beta)]
+    dlog_f = made(log_f) if log_f is not None else None
+    d_state_in = made(state_in) if state_in is not None else None
+    if T > 0 or d_state_in is not None:
+        _call_on(dev, "path_delta_train_bwd", (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), _opt(cu_seqlens), _opt(state_in), d_o.data_ptr(), _opt(d_state_out),
+                                               *[x.data_ptr() for x in out], _opt(dlog_f), _opt(d_state_in), nseq, T, L, H, G, d, layout, float(d ** -0.5 if scale is None else scale), dt,
+                                               workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
+    return (*out, *[x for x in (dlog_f, d_state_in) if x is not None])
+
+
+def path_delta_extend(q, k, v, beta, states, slots, cached, cu_new, max_new, log_f=None, scale=None, o=None, workspace=None, stream=None):
+    """Gated delta rule for packed new tokens (q, k [T,H,d], v [T,H*group,d], beta and log_f [T,H*group], cu_new [nseq+1], at most max_new a sequence) and states in a pool
+    [num_slots,H*group,d,d] (fp32), which are carried on in place: slots [nseq] names them, cached [nseq] is 0 for sequences that start.  Returns o; rows of no sequence are
+    left as they are."""
+    import torch
+    nseq, T, L, H, G, d, layout, shapes = _delta_sizes(q, v, cu_new, max_new, PATH_LAYOUT_BLHD)
+    if states.dim() != 4 or slots.dim() != 1:
+        raise ValueError("states is [num_slots,H*group,d,d], slots [nseq]")
+    dt, i32 = _dt_of(q), torch.int32
+    if o is None:
+        o = torch.empty_like(v) if stream is None else _paged_made(v, v.shape, v.dtype, stream, True)
+    td = q.dtype
+    looked = [("q", q, shapes[0], td), ("k", k, shapes[0], td), ("v", v, shapes[1], td), ("beta", beta, shapes[2], td), ("o", o, shapes[1], td),
+              ("states", states, (states.shape[0], H * G, d, d), torch.float32), ("slots", slots, (nseq,), i32), ("cached", cached, (nseq,), i32), ("cu_new", cu_new, (nseq + 1,), i32)]
+    if log_f is not None:
+        looked.append(("log_f", log_f, shapes[2], td))
+    dev = q.get_device()
+    _look(looked, dev, "q")
+    workspace = _scratch(workspace, path_delta_workspace_bytes(nseq, T, L, H, G, d, dt), q, stream, "q")
+    if T == 0:
+        return o
+    _call_on(dev, "path_delta_extend", (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), states.data_ptr(), slots.data_ptr(), cached.data_ptr(), cu_new.data_ptr(),
+                                        o.data_ptr(), nseq, T, L, states.shape[0], H, G, d, float(d ** -0.5 if scale is None else scale), dt, workspace.data_ptr(),
+                                        workspace.numel() * workspace.element_size()), stream)
+    return o

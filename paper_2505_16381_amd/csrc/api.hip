@@ -19,6 +19,8 @@ hipError_t launch_attn_states(const FwdParams& p, int d, int is_bf16, hipStream_
 #include "decode_decl.h"
 #include "fox_decl.h"
 #include "paged_decl.h"
+#include "plan_decl.h"
+#include "delta_decl.h"
 namespace path {
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -1125,4 +1127,162 @@ extern "C" path_status_t path_paged_extend(const void* q, const void* k, const v
     PagedArgs a{q, k, v, w, beta, log_f, kpages, vpages, cpages, page_table, cached, cu_new,
                 o, lse, nseq, T, max_new, max_cached, num_pages, 0, pages_per_seq, H, group, scale, 1, 1};
     return paged_call(a, page_size, d, dt, workspace, workspace_bytes, stream);
+}
+
+// ---- page tables ----
+static bool plan_shape_ok(int nseq, int per_seq, int T) {
+    return nseq >= 1 && per_seq >= 1 && T >= 0 && nseq <= (1 << 22);      // 32-bit launches of a wave per sequence
+}
+extern "C" size_t path_paged_plan_workspace_bytes(int nseq, int pages_per_seq, int T) {
+    return plan_shape_ok(nseq, pages_per_seq, T) ? align256((size_t)(1 + 2 * (size_t)nseq) * 4) : 0;
+}
+extern "C" path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* page_table, int* free_pages, int* free_count, int* cu_new, long long* slots,
+                                         int* missing, int nseq, int T, int num_pages, int page_size, int pages_per_seq, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!cached || !new_tokens || !page_table || !free_pages || !free_count || !cu_new || !missing || !workspace || (!slots && T > 0)) return PATH_ERR_NULL;
+    if (!plan_shape_ok(nseq, pages_per_seq, T) || num_pages < 1) return PATH_ERR_SHAPE;
+    if (page_size < PAGED_GROUP || page_size > 4096 || (page_size & (page_size - 1))) return PATH_ERR_SHAPE;
+    if (workspace_bytes < path_paged_plan_workspace_bytes(nseq, pages_per_seq, T) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
+    clear_inherited_error();
+    PlanArgs a{cached, new_tokens, page_table, free_pages, free_count, cu_new, slots, missing, nseq, pages_per_seq, num_pages, 0, T, static_cast<int*>(workspace)};
+    while ((1 << a.shift) < page_size) ++a.shift;
+    return hip_ok(launch_plan(a, static_cast<hipStream_t>(stream)), "page tables") ? PATH_OK : PATH_ERR_HIP;
+}
+
+// ---- gated delta rule ----
+namespace {
+struct DeltaPlan { long long tiles; size_t a, m, rows, at, mt, sm, gm, um, ym, ex, total; };
+}  // namespace
+
+// Launches of fewer than 2^32 threads: 512 per tile and key head, 256 per tile and value head, 1024 per sequence and value head.
+static bool delta_shape_ok(int nseq, int T, int L, int H, int group, int d) {
+    if (nseq < 1 || T < 0 || L < 1 || H < 1 || group < 1 || (d != 64 && d != 128)) return false;
+    const long long V = (long long)H * group, tiles = (long long)T / CHUNK + nseq;
+    return V <= 65535 && nseq * V < (1 << 21) && tiles * V < (1 << 23);
+}
+// tiles: a packed batch's; sequences of one length need no more (n ceil(L / 64) <= n L / 64 + n)
+static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool training) {
+    DeltaPlan p{};
+    p.tiles = (long long)T / CHUNK + nseq;
+    size_t off = 0;
+    auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
+    const size_t units = (size_t)p.tiles * V, tri = es == 4 ? 10 * 1024 : 3 * 6 * 1024;
+    take(p.a, units * tri);
+    take(p.m, units * tri);
+    take(p.rows, units * DELTA_ROWS * 64 * 4);
+    if (training) {
+        take(p.at, units * tri);
+        take(p.mt, units * tri);
+        take(p.sm, units * d * d * es);
+        take(p.gm, units * d * d * es);
+        take(p.um, units * d * 64 * es);
+        take(p.ym, units * d * 64 * es);
+        take(p.ex, es == 4 ? 0 : units * 32 * 4);
+    }
+    p.total = off;
+    return p;
+}
+extern "C" size_t path_delta_workspace_bytes(int nseq, int T, int max_len, int H, int group, int d, path_dtype_t dt, int training) {
+    if ((dt != PATH_F32 && dt != PATH_BF16) || !delta_shape_ok(nseq, T, max_len, H, group, d)) return 0;
+    return delta_plan(nseq, T, H * group, d, dt == PATH_F32 ? 4 : 2, training != 0).total;
+}
+
+// The arguments' checks and everything in DeltaArgs that follows from sizes and workspace.
+static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt, bool training, void* workspace, size_t workspace_bytes) {
+    if (!a.q || !a.k || !a.v || !a.beta || !workspace) return PATH_ERR_NULL;
+    if (dt != PATH_F32 && dt != PATH_BF16) return PATH_ERR_DTYPE;
+    if (!delta_shape_ok(a.nseq, a.T, a.L, a.H, a.G, d)) return PATH_ERR_SHAPE;
+    if (!layout_ok(layout) || !(a.scale > 0.f) || (a.cu && layout != PATH_LAYOUT_BLHD)) return PATH_ERR_UNSUPPORTED;
+    if (!a.cu && (long long)a.nseq * a.L != a.T) return PATH_ERR_SHAPE;
+    a.V = a.H * a.G;
+    a.NC = (int)(((long long)a.L + CHUNK - 1) / CHUNK);
+    const size_t es = dt == PATH_F32 ? 4 : 2;
+    const DeltaPlan p = delta_plan(a.nseq, a.T, a.V, d, es, training);
+    if (workspace_bytes < p.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
+    a.tiles = a.cu ? (int)p.tiles : a.nseq * a.NC;
+    const long long L = a.L, H = a.H, V = a.V;
+    if (layout == PATH_LAYOUT_BHLD) {
+        a.ks = H * L * d; a.kt = d; a.kh = L * d;
+        a.vs = V * L * d; a.vt = d; a.vh = L * d;
+        a.ss = V * L; a.st = 1; a.sh = L;
+    } else {
+        a.ks = L * H * d; a.kt = H * d; a.kh = d;
+        a.vs = L * V * d; a.vt = V * d; a.vh = d;
+        a.ss = L * V; a.st = V; a.sh = 1;
+    }
+    char* const ws = static_cast<char*>(workspace);
+    a.a = ws + p.a; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
+    a.at = ws + p.at; a.mt = ws + p.mt;
+    a.sm = ws + p.sm; a.gm = ws + p.gm; a.um = ws + p.um; a.ym = ws + p.ym; a.ex = reinterpret_cast<int*>(ws + p.ex);
+    a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 3 : 2;      // (delta_parts.h)
+    a.np_b = dt == PATH_F32 ? 1 : a.state_in ? 3 : 2;
+    return PATH_OK;
+}
+
+static path_status_t delta_forward(DeltaArgs a, int d, int layout, path_dtype_t dt, bool training, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!a.o) return PATH_ERR_NULL;
+    if (const path_status_t e = delta_args(a, d, layout, dt, training, workspace, workspace_bytes)) return e;
+    for (const void* ptr : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.state_in, (const void*)a.state_out}) if (misaligned(ptr)) return PATH_ERR_ALIGN;
+    clear_inherited_error();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int bf = dt == PATH_BF16;
+    if (a.T > 0 && !hip_ok(launch_delta_prep(a, d, bf, training, st), "delta rule, matrices of the chunks")) return PATH_ERR_HIP;
+    if (a.T == 0 && !a.state_out) return PATH_OK;
+    return hip_ok(launch_delta_scan(a, d, bf, training ? 1 : 0, st), "delta rule, states") ? PATH_OK : PATH_ERR_HIP;
+}
+
+extern "C" path_status_t path_delta_fwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in, void* o,
+                                        float* state_out, int nseq, int T, int max_len, int H, int group, int d, int layout, float scale, path_dtype_t dt, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+    DeltaArgs a{};
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_seqlens; a.state_in = state_in; a.o = o; a.state_out = state_out;
+    a.nseq = nseq; a.T = T; a.L = max_len; a.H = H; a.G = group; a.scale = scale;
+    return delta_forward(a, d, layout, dt, false, workspace, workspace_bytes, stream);
+}
+extern "C" path_status_t path_delta_train_fwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in, void* o,
+                                              float* state_out, int nseq, int T, int max_len, int H, int group, int d, int layout, float scale, path_dtype_t dt,
+                                              void* workspace, size_t workspace_bytes, void* stream) {
+    DeltaArgs a{};
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_seqlens; a.state_in = state_in; a.o = o; a.state_out = state_out;
+    a.nseq = nseq; a.T = T; a.L = max_len; a.H = H; a.G = group; a.scale = scale;
+    return delta_forward(a, d, layout, dt, true, workspace, workspace_bytes, stream);
+}
+extern "C" path_status_t path_delta_train_bwd(const void* q, const void* k, const void* v, const void* beta, const void* log_f, const int* cu_seqlens, const float* state_in,
+                                              const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv, void* dbeta, void* dlog_f, float* d_state_in,
+                                              int nseq, int T, int max_len, int H, int group, int d, int layout, float scale, path_dtype_t dt, void* workspace,
+                                              size_t workspace_bytes, void* stream) {
+    DeltaArgs a{};
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_seqlens; a.state_in = state_in;
+    a.d_o = d_o; a.d_state = d_state_out; a.dq = dq; a.dk = dk; a.dv = dv; a.dbeta = dbeta; a.dlog_f = dlog_f; a.d_state_in = d_state_in;
+    a.nseq = nseq; a.T = T; a.L = max_len; a.H = H; a.G = group; a.scale = scale;
+    if (!d_o || !dq || !dk || !dv || !dbeta || !log_f != !dlog_f || !state_in != !d_state_in) return PATH_ERR_NULL;
+    if (const path_status_t e = delta_args(a, d, layout, dt, true, workspace, workspace_bytes)) return e;
+    for (const void* ptr : {q, k, v, d_o, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)state_in, (const void*)d_state_out, (const void*)d_state_in})
+        if (misaligned(ptr)) return PATH_ERR_ALIGN;
+    clear_inherited_error();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int bf = dt == PATH_BF16;
+    if (T == 0 && !d_state_in) return PATH_OK;
+    if (!hip_ok(launch_delta_scan(a, d, bf, 2, st), "delta rule, gradients of the states")) return PATH_ERR_HIP;
+    return T == 0 || hip_ok(launch_delta_grad(a, d, bf, st), "delta rule, gradients of the chunks") ? PATH_OK : PATH_ERR_HIP;
+}
+extern "C" path_status_t path_delta_extend(const void* q, const void* k, const void* v, const void* beta, const void* log_f, float* states, const int* slots, const int* cached,
+                                           const int* cu_new, void* o, int nseq, int T, int max_new, int num_slots, int H, int group, int d, float scale, path_dtype_t dt,
+                                           void* workspace, size_t workspace_bytes, void* stream) {
+    DeltaArgs a{};
+    a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_new; a.o = o; a.states = states; a.slots = slots; a.cached = cached; a.num_slots = num_slots;
+    a.nseq = nseq; a.T = T; a.L = max_new; a.H = H; a.G = group; a.scale = scale;
+    a.few = DELTA_FEW;
+    if (!states || !slots || !cached || !cu_new || !o) return PATH_ERR_NULL;
+    if (const path_status_t e = delta_args(a, d, PATH_LAYOUT_BLHD, dt, false, workspace, workspace_bytes)) return e;
+    if (num_slots < 1) return PATH_ERR_SHAPE;
+    for (const void* ptr : {q, k, v, (const void*)o, (const void*)states}) if (misaligned(ptr)) return PATH_ERR_ALIGN;
+    if (T == 0) return PATH_OK;
+    clear_inherited_error();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int bf = dt == PATH_BF16, longest = max_new < T ? max_new : T;
+    if ((nseq > 1 || longest <= DELTA_FEW) && !hip_ok(launch_delta_step(a, d, bf, st), "delta rule, tokens")) return PATH_ERR_HIP;
+    if (longest <= DELTA_FEW) return PATH_OK;
+    if (nseq == 1) a.few = 0;      // (one sequence that may be long is taken for long)
+    if (!hip_ok(launch_delta_prep(a, d, bf, false, st), "delta rule, matrices of the chunks")) return PATH_ERR_HIP;
+    return hip_ok(launch_delta_scan(a, d, bf, 0, st), "delta rule, states") ? PATH_OK : PATH_ERR_HIP;
 }
