@@ -58,6 +58,27 @@ template <typename T, int NP> __device__ __forceinline__ void delta_split(const 
         }
     }
 }
+// four numbers as sums of NP bf16 numbers each, two to a register
+template <int NP> struct DeltaSplit4 {
+    uint2 p[NP];
+    __device__ __forceinline__ explicit DeltaSplit4(const f32x4& v) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        float r[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            unsigned w[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const f32x2 x = {r[2 * j], r[2 * j + 1]};
+                w[j] = __builtin_bit_cast(unsigned, __builtin_convertvector(x, bf16x2));
+                r[2 * j] -= __uint_as_float(w[j] << 16);
+                r[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
+            }
+            p[i] = uint2{w[0], w[1]};
+        }
+    }
+};
 // slab s of a column of result tiles, each value times f[...] of its tile and register, as a B operand
 template <typename T, int NP> __device__ __forceinline__ void delta_pack(const f32x4* tile, int s, DeltaParts<T, NP>& o) {
     constexpr int FE = DeltaOps<T>::FE, TPS = DeltaOps<T>::TPS;

@@ -1,80 +1,60 @@
 // Gated delta rule: the states, chunk after chunk, and backwards their gradients (delta_decl.h has the formulas).
 //
-// A wave keeps 16 columns (value indices) of a head's state in registers, all d rows: what it computes needs no other wave.  The chunk's K, Q, A and M come
-// through LDS, copied while the chunk before is worked on and shared by the workgroup's NW waves.
+// A workgroup of four waves has CT * 16 columns (value indices) of a head's state, which stays in registers: each wave a quarter of its rows (key indices), and of a chunk's
+// products with it the 16 tokens of one result tile.  What a wave needs of K, Q, A and M nobody else needs, so it comes from memory straight into its
+// registers, a chunk ahead; what all need -- the state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
 #include "delta_parts.h"
 
 namespace path {
 
 enum { DELTA_O = 0, DELTA_KEEP = 1, DELTA_BACK = 2 };      // forward; forward that keeps what the backward needs; backwards
 
-template <typename T, int D, int NP, int NW>
+template <typename T, int D, int NP, int CT, int MODE>
 struct ScanLds {
     typedef DeltaOps<T> P;
-    static constexpr int TILE = DeltaTile<T, D>::BYTES, TRI = NP * P::NLOW * 1024, ROWS = DELTA_ROWS * 256;
-    static constexpr int K = 0, Q = TILE, A = 2 * TILE, M = A + TRI, R = M + TRI, BUF = (R + ROWS + 255) / 256 * 256;
-    static constexpr int NB = 2 * BUF <= 160 * 1024 ? 2 : 1, BYTES = NB * BUF;
+    static constexpr int NS = D / P::SL, CS = 64 / P::SL;                      // slabs of the state's rows, of a chunk
+    static constexpr int TW = D / 64;                                          // state tiles of a wave
+    static constexpr int SW = sizeof(T) == 2 ? 32 : 16 * TW, SROW = sizeof(T) == 2 ? 64 : (SW + 4) * 4;      // a wave's columns of K: elements, bytes of a row in LDS
+    static constexpr int SLICE = 64 * SROW, NSL = MODE == DELTA_BACK ? 2 : 1;
+    static constexpr int S = 0, Y = S + NS * NP * CT * 1024, U = Y + CS * NP * CT * 1024, V = U + CS * NP * CT * 1024, O = V + CS * NP * CT * 1024;
+    static constexpr int X = O + (MODE == DELTA_BACK ? CS * CT * 1024 : 0), KT = X + 256, BYTES = KT + 4 * NSL * SLICE;
 };
 
-__device__ __forceinline__ void delta_copy16(const void* g, unsigned char* s, unsigned lane_offset) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)scalar_base(g, lane_offset), (__attribute__((address_space(3))) void*)s, 16, 0, 0);
-}
-
-// largest |x| of the wave's values as an exponent that leaves fp16 numbers below 2^11
-template <int N> __device__ __forceinline__ int delta_exponent(const f32x4* x) {
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m = fmaxf(m, fabsf(x[i][j]));
+// largest |x| of a wave's values; the exponent that leaves fp16 numbers below 2^11
+__device__ __forceinline__ float delta_most(float m) {
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+    return m;
+}
+__device__ __forceinline__ int delta_exponent(float m) {
     const int e = (int)(__float_as_uint(m) >> 23) - 127 - 10;
     return e < -126 ? -126 : e;
 }
 
-// tile column -> memory, lane n's row of the transposed matrix, as fp32 or as fp16 over 2^ex
-template <typename T, int NT> __device__ __forceinline__ void delta_keep(const f32x4* x, void* out, size_t row, int ld, int g, int ex) {
-    if constexpr (sizeof(T) == 4) {
-        float* const p = static_cast<float*>(out) + row * ld + 4 * g;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(p + 16 * t) = x[t];
-    } else {
-        half_t* const p = static_cast<half_t*>(out) + row * ld + 8 * g;
-#pragma unroll
-        for (int s = 0; s < NT / 2; ++s) {
-            halfx8 h;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = (half_t)ldexpf(x[2 * s + e / 4][e % 4], -ex);
-            *reinterpret_cast<halfx8*>(p + 32 * s) = h;
-        }
-    }
-}
-
-template <typename T, int D, int NP, int NW, int MODE>
-__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a) {
+template <typename T, int D, int NP, int CT, int MODE>
+__global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaArgs a) {
     typedef DeltaOps<T> P;
     typedef typename P::Frag Frag;
-    typedef ScanLds<T, D, NP, NW> L;
-    typedef DeltaTile<T, D> Tile;
-    constexpr int NS = D / P::SL, NR = D / 16, CS = 64 / P::SL, VEC = 16 / (int)sizeof(T);      // slabs of d, tiles of d, slabs of a chunk
+    typedef ScanLds<T, D, NP, CT, MODE> L;
+    constexpr int NS = L::NS, CS = L::CS, TW = L::TW;
+    constexpr bool BACK = MODE == DELTA_BACK;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     int unit, part;
-    if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, NR / NW, a.nseq * a.V, unit, part)) return;
+    if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, D / 16 / CT, a.nseq * a.V, unit, part)) return;
     const int s = __builtin_amdgcn_readfirstlane(unit / a.V), hv = unit - s * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
     const DeltaSeq sq = delta_seq(a, s);
     const int len = __builtin_amdgcn_readfirstlane(sq.len), tile0 = __builtin_amdgcn_readfirstlane(sq.tile0);
     if (a.slots && len <= a.few) return;
     const int NC = (len + CHUNK - 1) / CHUNK;
-    const int col = 16 * (part * NW + wv) + n;      // the lane's value index
+    const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
 
-    // the first state: of a pool's slot, given, or zeros.  Rows of tile t: delta_row(t, 4 g + j)
-    f32x4 S[NR];
+    // the first state: of a pool's slot, given, or zeros
+    f32x4 S[TW][CT];
     const size_t head = ((size_t)s * a.V + hv) * D * D;
     const float* from = nullptr;
     float* to = nullptr;
-    if (MODE == DELTA_BACK) {
+    if (BACK) {
         from = a.d_state ? a.d_state + head : nullptr;
         to = a.d_state_in ? a.d_state_in + head : nullptr;
     } else if (a.slots) {
@@ -88,270 +68,398 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a) {
         to = a.state_out ? a.state_out + head : nullptr;
     }
 #pragma unroll
-    for (int t = 0; t < NR; ++t)
+    for (int t = 0; t < TW; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) S[t][j] = from ? from[(size_t)P::row(t, 4 * g + j) * D + col] : 0.f;
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[t][x][j] = from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
 
-    const T* const kp = static_cast<const T*>(a.k) + delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh;
-    const T* const qp = static_cast<const T*>(a.q) + delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh;
-    const long long vat = delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + col;
-    const T* const vp = static_cast<const T*>(MODE == DELTA_BACK ? a.d_o : a.v) + vat;
-    T* const op = static_cast<T*>(MODE == DELTA_BACK ? a.dv : a.o) + vat;
-    const char *const ga = static_cast<const char*>(MODE == DELTA_BACK ? a.at : a.a), *const gm = static_cast<const char*>(MODE == DELTA_BACK ? a.mt : a.m);
-
-    // Copies of a chunk to LDS, 1 KB each, dealt to the waves.  Rows behind the sequence's end are its last one again: their beta is 0.
-    auto copies = [&](int c, unsigned char* buf) {
-        const size_t u = (size_t)(tile0 + c) * a.V + hv;
-        const int last = len - 1 - c * CHUNK;
-        constexpr int RPI = 1024 / Tile::ROWB;      // rows of an instruction
-        const int r = lane / Tile::PPR, x = lane % Tile::PPR;
-        for (int i = wv; i < 64 / RPI; i += NW) {
-            const int row = i * RPI + r, held = row < last ? row : last;
-            const unsigned off = (unsigned)((x ^ Tile::turn(row)) * 16);
-            const T* const k0 = kp + (long long)(c * CHUNK + held) * a.kt;
-            const T* const q0 = qp + (long long)(c * CHUNK + held) * a.kt;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(k0) + off),
-                                             (__attribute__((address_space(3))) void*)(buf + L::K + i * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(q0) + off),
-                                             (__attribute__((address_space(3))) void*)(buf + L::Q + i * 1024), 16, 0, 0);
-        }
-        for (int i = wv; i < L::TRI / 1024; i += NW) {
-            delta_copy16(ga + u * L::TRI + i * 1024, buf + L::A + i * 1024, lane * 16);
-            delta_copy16(gm + u * L::TRI + i * 1024, buf + L::M + i * 1024, lane * 16);
-        }
-        const char* const rows = reinterpret_cast<const char*>(a.rows + u * DELTA_ROWS * 64);
-        if (wv == 0) delta_copy16(rows, buf + L::R, lane * 16);
-        if (wv == NW - 1 && lane < 16) delta_copy16(rows + 1024, buf + L::R + 1024, lane * 16);
+    // an exchange area's fragment, and one tile of a slab as operands into it
+    auto frag = [&](int area, int sl, int x) {
+        DeltaParts<T, NP> f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) f.p[p] = *reinterpret_cast<const Frag*>(smem + area + ((sl * CT + x) * NP + p) * 1024 + lane * 16);
+        return f;
     };
-    auto values = [&](int c, T (&v)[4][4]) {      // the lane's column of V (backwards: dO)
+    auto put = [&](int area, int tile, int x, const f32x4& v) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4*>(smem + area + (tile * CT + x) * 1024 + lane * 16) = v;
+        } else {
+            DeltaSplit4<NP> r(v);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+            for (int p = 0; p < NP; ++p)
+                *reinterpret_cast<uint2*>(smem + area + (((tile >> 1) * CT + x) * NP + p) * 1024 + lane * 16 + (tile & 1) * 8) = r.p[p];
+        }
+    };
+
+    // Addresses: a chunk's place in scalar registers, the lane's in 32 bits of bytes, made anew only where a chunk has fewer than 64 tokens: rows behind the sequence's end are
+    // its last one again (their beta is 0).
+    constexpr int ES = sizeof(T), PPR = L::SW * ES / 16, NK = PPR;      // 16-byte pieces of a slice's row; of a slice per lane
+    const char* const kb = static_cast<const char*>(a.k) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
+    const char* const qb = static_cast<const char*>(a.q) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
+    const long long vat = (delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + 16 * part * CT) * ES;
+    const char* const vb = static_cast<const char*>(BACK ? a.d_o : a.v) + vat;
+    char* const ob = static_cast<char*>(BACK ? a.dv : a.o) + vat;
+    const long long kstep = a.kt * ES * CHUNK, vstep = a.vt * ES * CHUNK;
+    unsigned row_at, slice_at[NK], value_at[4];
+    auto place = [&](int c) {
+        const int last = len - 1 - c * CHUNK;
+        const unsigned kt = (unsigned)a.kt * ES, vt = (unsigned)a.vt * ES;
+        auto held = [&](int r) { return (unsigned)(r < last ? r : last); };
+        row_at = held(P::row(wv, n)) * kt + 16 * g;
+        const int c0 = sizeof(T) == 2 ? 32 * (TW * wv >> 1) : 16 * TW * wv;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = c * CHUNK + P::row(t, 4 * g + j), held = r < len ? r : len - 1;
-                v[t][j] = vp[held * a.vt];
+        for (int i = 0; i < NK; ++i) slice_at[i] = held((i * 64 + lane) / PPR) * kt + c0 * ES + (lane % PPR) * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) value_at[j] = held(P::row(wv, 4 * g + j)) * vt + n * ES;
+    };
+    auto partial = [&](int c) { return len - c * CHUNK < CHUNK; };
+
+    // What a chunk brings, loaded again as soon as it has been used.
+    Frag K[NS], Q[BACK ? 1 : NS], kt[L::NSL][NK];
+    DeltaParts<T, NP> A[CS], M[CS];
+    T v[CT][4];
+    f32x4 be, ga4, rh;
+    float g63;
+    typedef const __attribute__((address_space(1))) Frag GlobalFrag;
+    auto load_rows = [&](const char* base, int c, Frag* f) {
+        const GlobalBytes p = scalar_base(base + c * kstep, row_at);
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) f[sl] = *(GlobalFrag*)(p + sl * P::SL * ES);
+    };
+    auto load_slice = [&](const char* base, int c, Frag* f) {      // all rows of the wave's columns
+#pragma unroll
+        for (int i = 0; i < NK; ++i) f[i] = *(GlobalFrag*)scalar_base(base + c * kstep, slice_at[i]);
+    };
+    auto store_slice = [&](const Frag* f, int at) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) *reinterpret_cast<Frag*>(smem + at + (i * 64 + lane) / PPR * L::SROW + (lane % PPR) * 16) = f[i];
+    };
+    auto used = [&](int sl) { return BACK ? P::up(wv, sl) : P::low(wv, sl); };
+    auto load_tri = [&](const void* base, int c, DeltaParts<T, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
+        const char* const p = static_cast<const char*>(base) + ((size_t)(tile0 + c) * a.V + hv) * NP * P::NLOW * 1024;
+#pragma unroll
+        for (int sl = 0; sl < CS; ++sl) {
+            const int at = BACK ? P::up_at(wv, used(sl) ? sl : CS - 1) : P::low_at(wv, used(sl) ? sl : 0);
+#pragma unroll
+            for (int z = 0; z < NP; ++z) f[sl].p[z] = *(GlobalFrag*)scalar_base(p + (z * P::NLOW + at) * 1024, lane * 16);
+        }
+    };
+    auto load_values = [&](int c) {      // the lane's tokens and columns of V (backwards: dO)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) v[x][j] = *(const __attribute__((address_space(1))) T*)(scalar_base(vb + c * vstep, value_at[j]) + 16 * x * ES);
+    };
+    auto load_numbers = [&](int c) {
+        const float* const p = a.rows + ((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS * 64;
+        typedef const __attribute__((address_space(1))) f32x4 Global4;
+        const GlobalBytes r = scalar_base(p, P::row(wv, 4 * g) * 4);
+        be = *(Global4*)r;
+        ga4 = *(Global4*)(r + 256);
+        rh = *(Global4*)(r + 512);
+        g63 = p[64 + 63];
+    };
+    unsigned out_at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out_at[j] = P::row(wv, 4 * g + j) * ((unsigned)a.vt * ES) + n * ES;
+    const void *const ga = BACK ? a.at : a.a, *const gm = BACK ? a.mt : a.m;
+    const int slice = L::KT + wv * L::NSL * L::SLICE;
+    // state tiles += (the wave's columns of K or Q)^T y
+    auto into_state = [&](int at, const DeltaParts<T, NP> (&y)[CS][CT]) {
+        if constexpr (sizeof(T) == 2) {
+            const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(smem + at) + (8 * g + (n >> 2)) * 64 + (n & 3) * 16;
+            bf16x8 f[2][2];
+            delta_ld_tr<32>(base, f);
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) {
+                        DeltaParts<T, 1> k;
+                        k.p[0] = TW == 2 ? f[t][sl] : (wv & 1) ? f[1][sl] : f[0][sl];
+                        S[t][x] = delta_mma(k, y[sl][x], S[t][x]);
+                    }
+        } else {
+#pragma unroll
+            for (int sl = 0; sl < CS; ++sl)
+#pragma unroll
+                for (int t = 0; t < TW; ++t) {
+                    DeltaParts<T, 1> k;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) k.p[0][e] = *reinterpret_cast<const float*>(smem + at + (16 * sl + 4 * g + e) * L::SROW + (16 * t + n) * 4);
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) S[t][x] = delta_mma(k, y[sl][x], S[t][x]);
+                }
+        }
+    };
+    // an exchange area's slabs, requested together: left to itself the compiler waits for each on its own
+    auto frags = [&](int area, DeltaParts<T, NP> (&f)[CS][CT]) {
+#pragma unroll
+        for (int sl = 0; sl < CS; ++sl)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) f[sl][x] = frag(area, sl, x);
+    };
+    float* const xs = reinterpret_cast<float*>(smem + L::X);      // largest values: [2][CT][wave]
+    auto put_state = [&]() {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            float m = 0.f;
+#pragma unroll
+            for (int t = 0; t < TW; ++t) {
+                put(L::S, TW * wv + t, x, S[t][x]);
+                if (MODE != DELTA_O && sizeof(T) == 2)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) m = fmaxf(m, fabsf(S[t][x][j]));
+            }
+            if (MODE != DELTA_O && sizeof(T) == 2) {
+                m = delta_most(m);
+                if (lane == 0) xs[x * 4 + wv] = m;
+            }
+        }
+    };
+    auto put_most = [&](const f32x4* w) {      // of a token tile
+        if (MODE != DELTA_O && sizeof(T) == 2)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                const float m = delta_most(fmaxf(fmaxf(fabsf(w[x][0]), fabsf(w[x][1])), fmaxf(fabsf(w[x][2]), fabsf(w[x][3]))));
+                if (lane == 0) xs[16 + x * 4 + wv] = m;
             }
     };
-
-    const int step = MODE == DELTA_BACK ? -1 : 1, first = MODE == DELTA_BACK ? NC - 1 : 0;
-    T vn[4][4];
-    if (NC > 0) {
-        copies(first, smem);
-        values(first, vn);
-    }
-    unsigned char* buf = smem;
-    for (int i = 0; i < NC; ++i) {
-        const int c = first + i * step;
-        __builtin_amdgcn_s_waitcnt(0x0000);      // this wave's copies have landed; then everybody's, and the other buffer is free
-        __syncthreads();
-        f32x4 V[4];
+    // a tile to memory for the chunk's gradients, the lane's row of the transposed matrix: fp32, or fp16 over a power of two of the 16 columns
+    auto keep = [&](void* out, int which, int at, int x, size_t u, int ld, int tile, const f32x4& w) {
+        const size_t row = (u * D + col + 16 * x) * ld + P::row(tile, 4 * g);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(out) + row) = w;
+        } else {
+            const f32x4 m = *reinterpret_cast<const f32x4*>(xs + at + x * 4);
+            const int ex = delta_exponent(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+            if (tid == 0) a.ex[u * 32 + which * 8 + part * CT + x] = ex;
+            halfx4 h;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) V[t][j] = c * CHUNK + P::row(t, 4 * g + j) < len ? (float)vn[t][j] : 0.f;
-        if (i + 1 < NC) {
-            if (L::NB == 2) copies(c + step, buf == smem ? smem + L::BUF : smem);
-            values(c + step, vn);
+            for (int j = 0; j < 4; ++j) h[j] = (half_t)ldexpf(w[j], -ex);
+            *reinterpret_cast<halfx4*>(static_cast<half_t*>(out) + row) = h;
         }
-        const float* const rows = reinterpret_cast<const float*>(buf + L::R);
-        auto of_row = [&](int which, int t) { return *reinterpret_cast<const f32x4*>(rows + which * 64 + P::row(t, 4 * g)); };      // of the lane's four tokens of tile t
-        const unsigned nat = Tile::nat(n, g);
-        auto along = [&](int tile, int t, int sl) { DeltaParts<T, 1> f; f.p[0] = *reinterpret_cast<const Frag*>(buf + tile + ((nat ^ (64 * sl)) + Tile::tile_off(t))); return f; };
-        auto tri = [&](int mat, int at) {
-            DeltaParts<T, NP> f;
+    };
+
+    const int step = BACK ? -1 : 1;
+    int c = BACK ? NC - 1 : 0;
+    if (NC > 0) {
+        place(c);
+        load_rows(kb, c, K);
+        if (!BACK) load_rows(qb, c, Q);
+        load_numbers(c);
+        load_values(c);
+        load_tri(ga, c, A);
+        load_tri(gm, c, M);
+        load_slice(kb, c, kt[0]);
+        if (BACK) load_slice(qb, c, kt[L::NSL - 1]);
+    }
+    put_state();
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NC; ++i, c += step) {
+        const int next = i + 1 < NC ? c + step : c;      // (the last chunk's loads are its own again)
+        const size_t u = (size_t)(tile0 + c) * a.V + hv;
+        f32x4 V[CT], ys[CT], os[CT];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) f.p[p] = reinterpret_cast<const Frag*>(buf + mat)[(p * P::NLOW + at) * 64 + lane];
-            return f;
-        };
-        // tiles of the state += (tile in LDS)^T x, x in slabs of the chunk
-        auto into_state = [&](int tile, const DeltaParts<T, NP>* x) {
-            if constexpr (sizeof(T) == 2) {
-                const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(buf + tile);
+        for (int x = 0; x < CT; ++x)
 #pragma unroll
-                for (int tp = 0; tp < NR / 2; ++tp) {
-                    bf16x8 f[2][2];
-                    delta_ld_tr<D>(base + (delta_tr<D>(lane) ^ (64 * tp)), f);
+            for (int j = 0; j < 4; ++j) V[x][j] = c * CHUNK + P::row(wv, 4 * g + j) < len ? (float)v[x][j] : 0.f;
+        if (partial(next) != partial(c)) place(next);
+        load_values(next);
+        store_slice(kt[0], slice);
+        if (BACK) {
+            store_slice(kt[L::NSL - 1], slice + L::SLICE);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+            for (int x = 0; x < CT; ++x) {      // dO is an operand as it is
+                if constexpr (sizeof(T) == 4) {
+                    *reinterpret_cast<f32x4*>(smem + L::O + (wv * CT + x) * 1024 + lane * 16) = V[x];
+                } else {
+                    bf16x4 b;
 #pragma unroll
-                        for (int sl = 0; sl < 2; ++sl) {
-                            DeltaParts<T, 1> y;
-                            y.p[0] = f[b][sl];
-                            S[2 * tp + b] = delta_mma(y, x[sl], S[2 * tp + b]);
-                        }
+                    for (int j = 0; j < 4; ++j) b[j] = (bf16_t)V[x][j];
+                    *reinterpret_cast<bf16x4*>(smem + L::O + ((wv >> 1) * CT + x) * 1024 + lane * 16 + (wv & 1) * 8) = b;
                 }
-            } else {
+            }
+        }
+        load_slice(kb, next, kt[0]);
+        if (BACK) load_slice(qb, next, kt[L::NSL - 1]);
+        lds_barrier();
+
+        // K S and Q S of the wave's tokens
 #pragma unroll
-                for (int t = 0; t < NR; ++t)
+        for (int x = 0; x < CT; ++x) ys[x] = os[x] = zero;
+        {
+            constexpr int HS = NS * NP * CT > 16 ? NS / 2 : NS;      // slabs requested together: up to 64 registers
 #pragma unroll
-                    for (int sl = 0; sl < CS; ++sl) {
-                        DeltaParts<T, 1> y;
+            for (int s0 = 0; s0 < NS; s0 += HS) {
+                DeltaParts<T, NP> f[HS][CT];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int row = 16 * sl + 4 * g + e, cc = 16 * t + n;
-                            y.p[0][e] = *reinterpret_cast<const float*>(buf + tile + row * Tile::ROWB + (((cc >> 2) ^ Tile::turn(row)) << 4) + (cc & 3) * 4);
+                for (int sl = 0; sl < HS; ++sl)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) f[sl][x] = frag(L::S, s0 + sl, x);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int sl = 0; sl < HS; ++sl)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) {
+                        DeltaParts<T, 1> k;
+                        k.p[0] = K[s0 + sl];
+                        ys[x] = delta_mma(k, f[sl][x], ys[x]);
+                        if (!BACK) {
+                            k.p[0] = Q[s0 + sl];
+                            os[x] = delta_mma(k, f[sl][x], os[x]);
                         }
-                        S[t] = delta_mma(y, x[sl], S[t]);
                     }
             }
-        };
-        const size_t u = (size_t)(tile0 + c) * a.V + hv;
-        const float g63 = rows[64 + 63];
-
-        if (MODE == DELTA_KEEP || MODE == DELTA_BACK) {
-            int ex = 0;
-            if constexpr (sizeof(T) == 2) {
-                ex = delta_exponent<NR>(S);
-                if (lane == 0) a.ex[u * 32 + (MODE == DELTA_BACK ? 8 : 0) + part * NW + wv] = ex;
-            }
-            delta_keep<T, NR>(S, MODE == DELTA_BACK ? a.gm : a.sm, u * D + col, D, g, ex);
         }
-        DeltaParts<T, NP> Sp[NS];
+        load_rows(kb, next, K);
+        if (!BACK) load_rows(qb, next, Q);
+        if (MODE != DELTA_O)
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) delta_pack<T, NP>(S, sl, Sp[sl]);
-        f32x4 x[4];      // K S
+            for (int x = 0; x < CT; ++x)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < TW; ++t) keep(BACK ? a.gm : a.sm, BACK ? 1 : 0, 0, x, u, D, TW * wv + t, S[t][x]);
+        if (!BACK) {
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl) x[t] = delta_mma(along(L::K, t, sl), Sp[sl], x[t]);
-        }
-        if (MODE != DELTA_BACK) {
-            f32x4 o[4];      // scale diag(gamma) Q S
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int sl = 0; sl < NS; ++sl) o[t] = delta_mma(along(L::Q, t, sl), Sp[sl], o[t]);
-                const f32x4 be = of_row(0, t), ga4 = of_row(1, t);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[t][j] = be[j] * (V[t][j] - ga4[j] * x[t][j]);
-                    o[t][j] *= a.scale * ga4[j];
-                }
+            for (int x = 0; x < CT; ++x) {
+                put(L::Y, wv, x, be * (V[x] - ga4 * ys[x]));
+                os[x] = os[x] * (ga4 * a.scale);
             }
-            DeltaParts<T, NP> y[CS];
+            lds_barrier();
+            DeltaParts<T, NP> f[CS][CT];
+            frags(L::Y, f);
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 U[CT];
 #pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(x, sl, y[sl]);
-            f32x4 U[4];
+            for (int x = 0; x < CT; ++x) U[x] = zero;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                U[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int sl = 0; sl < CS; ++sl)
+                if (used(sl))
 #pragma unroll
-                for (int sl = 0; sl < CS; ++sl)
-                    if (P::low(t, sl)) U[t] = delta_mma(tri(L::A, P::low_at(t, sl)), y[sl], U[t]);
+                    for (int x = 0; x < CT; ++x) U[x] = delta_mma(A[sl], f[sl][x], U[x]);
+            load_tri(ga, next, A);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                put(L::U, wv, x, U[x] * rh);
+                put(L::V, wv, x, U[x]);
             }
-            if (MODE == DELTA_KEEP) {
-                int ex = 0;
-                if constexpr (sizeof(T) == 2) {
-                    ex = delta_exponent<4>(U);
-                    if (lane == 0) a.ex[u * 32 + 16 + part * NW + wv] = ex;
-                }
-                delta_keep<T, 4>(U, a.um, u * D + col, 64, g, ex);
+            put_most(U);
+            lds_barrier();
+            DeltaParts<T, NP> f2[CS][CT];
+            frags(L::U, f);
+            frags(L::V, f2);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int x = 0; x < CT; ++x) S[t][x] = S[t][x] * g63;
+            load_numbers(next);
+            into_state(slice, f);
+#pragma unroll
+            for (int sl = 0; sl < CS; ++sl)
+                if (used(sl))
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) os[x] = delta_mma(M[sl], f2[sl][x], os[x]);
+            load_tri(gm, next, M);
+            if (MODE == DELTA_KEEP)
+#pragma unroll
+                for (int x = 0; x < CT; ++x) keep(a.um, 2, 16, x, u, 64, wv, U[x]);
+            put_state();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = c * CHUNK + P::row(wv, 4 * g + j);
+                if (r < len)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) *(__attribute__((address_space(1))) T*)(scalar_base(ob + c * vstep, out_at[j]) + 16 * x * ES) = (T)os[x][j];
             }
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(U, sl, y[sl]);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int sl = 0; sl < CS; ++sl)
-                    if (P::low(t, sl)) o[t] = delta_mma(tri(L::M, P::low_at(t, sl)), y[sl], o[t]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = c * CHUNK + P::row(t, 4 * g + j);
-                    if (r < len) op[r * a.vt] = (T)o[t][j];
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) U[t] = U[t] * of_row(2, t);
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(U, sl, y[sl]);
-#pragma unroll
-            for (int t = 0; t < NR; ++t) S[t] = S[t] * g63;
-            into_state(L::K, y);
         } else {
-            DeltaParts<T, 1> dO[CS];
+            // dU = diag(rho) K G + M^T dO
 #pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, 1>(V, sl, dO[sl]);
+            for (int x = 0; x < CT; ++x) ys[x] = ys[x] * rh;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {      // dU = diag(rho) K G + M^T dO
-                x[t] = x[t] * of_row(2, t);
+            for (int sl = 0; sl < CS; ++sl)
+                if (used(sl))
 #pragma unroll
-                for (int sl = 0; sl < CS; ++sl)
-                    if (P::up(t, sl)) x[t] = delta_mma(tri(L::M, P::up_at(t, sl)), dO[sl], x[t]);
+                    for (int x = 0; x < CT; ++x) {
+                        DeltaParts<T, 1> f;
+                        f.p[0] = *reinterpret_cast<const Frag*>(smem + L::O + (sl * CT + x) * 1024 + lane * 16);
+                        ys[x] = delta_mma(M[sl], f, ys[x]);
+                    }
+            load_tri(gm, next, M);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) put(L::Y, wv, x, ys[x]);
+            lds_barrier();
+            DeltaParts<T, NP> f[CS][CT];
+            frags(L::Y, f);
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 Y[CT];
+#pragma unroll
+            for (int x = 0; x < CT; ++x) Y[x] = zero;
+#pragma unroll
+            for (int sl = 0; sl < CS; ++sl)
+                if (used(sl))
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) Y[x] = delta_mma(A[sl], f[sl][x], Y[x]);
+            load_tri(ga, next, A);
+            put_most(Y);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                os[x] = be * Y[x];
+                put(L::U, wv, x, -(ga4 * os[x]));
+                put(L::V, wv, x, V[x] * (ga4 * a.scale));
             }
-            DeltaParts<T, NP> y[CS];
+            lds_barrier();
+            DeltaParts<T, NP> f2[CS][CT];
+            frags(L::U, f);
+            frags(L::V, f2);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(x, sl, y[sl]);
-            f32x4 Y[4];
+            for (int t = 0; t < TW; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                Y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < CT; ++x) S[t][x] = S[t][x] * g63;
+            load_numbers(next);
+            into_state(slice, f);
+            into_state(slice + L::SLICE, f2);
 #pragma unroll
-                for (int sl = 0; sl < CS; ++sl)
-                    if (P::up(t, sl)) Y[t] = delta_mma(tri(L::A, P::up_at(t, sl)), y[sl], Y[t]);
+            for (int x = 0; x < CT; ++x) keep(a.ym, 3, 16, x, u, 64, wv, Y[x]);
+            put_state();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = c * CHUNK + P::row(wv, 4 * g + j);
+                if (r < len)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) *(__attribute__((address_space(1))) T*)(scalar_base(ob + c * vstep, out_at[j]) + 16 * x * ES) = (T)os[x][j];
             }
-            int ex = 0;
-            if constexpr (sizeof(T) == 2) {
-                ex = delta_exponent<4>(Y);
-                if (lane == 0) a.ex[u * 32 + 24 + part * NW + wv] = ex;
-            }
-            delta_keep<T, 4>(Y, a.ym, u * D + col, 64, g, ex);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const f32x4 be = of_row(0, t), ga4 = of_row(1, t);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = c * CHUNK + P::row(t, 4 * g + j);
-                    const float z = be[j] * Y[t][j];
-                    if (r < len) op[r * a.vt] = (T)z;
-                    Y[t][j] = -ga4[j] * z;
-                    V[t][j] *= a.scale * ga4[j];
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < NR; ++t) S[t] = S[t] * g63;
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(Y, sl, y[sl]);
-            into_state(L::K, y);
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl) delta_pack<T, NP>(V, sl, y[sl]);
-            into_state(L::Q, y);
-        }
-        if (L::NB == 2) {
-            buf = buf == smem ? smem + L::BUF : smem;
-        } else if (i + 1 < NC) {
-            __syncthreads();
-            copies(c + step, buf);
         }
     }
     if (to) {
 #pragma unroll
-        for (int t = 0; t < NR; ++t)
+        for (int t = 0; t < TW; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) to[(size_t)P::row(t, 4 * g + j) * D + col] = S[t][j];
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] = S[t][x][j];
     }
 }
 
-template <typename T, int D, int NP, int NW, int MODE>
+template <typename T, int D, int NP, int CT, int MODE>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    typedef ScanLds<T, D, NP, NW> L;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, NP, NW, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+    typedef ScanLds<T, D, NP, CT, MODE> L;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, NP, CT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
     if (attr != hipSuccess) return attr;
-    delta_scan_kernel<T, D, NP, NW, MODE><<<dim3(xcd_deal_grid(D / 16 / NW, a.nseq * a.V)), dim3(64 * NW), L::BYTES, stream>>>(a);
+    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(D / 16 / CT, a.nseq * a.V)), dim3(256), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D, int NP, int MODE>
-static hipError_t launch_nw(const DeltaArgs& a, hipStream_t stream) {
-    const long long blocks = (long long)a.nseq * a.V * (D / 16);
-    if (D == 128 && sizeof(T) == 2 && blocks >= 8 * 256) return launch<T, D, NP, sizeof(T) == 2 ? D / 16 : 4, MODE>(a, stream);
-    if (blocks >= 4 * 256) return launch<T, D, NP, 4, MODE>(a, stream);
-    return launch<T, D, NP, 2, MODE>(a, stream);
+static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
+    return (long long)a.nseq * a.V * (D / 32) >= 256 ? launch<T, D, NP, 2, MODE>(a, stream) : launch<T, D, NP, 1, MODE>(a, stream);
 }
 template <int D, int MODE>
 static hipError_t launch_np(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
-    if (!is_bf16) return launch_nw<float, D, 1, MODE>(a, stream);
-    return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 3 ? launch_nw<bf16_t, D, 3, MODE>(a, stream) : launch_nw<bf16_t, D, 2, MODE>(a, stream);
+    if (!is_bf16) return launch_ct<float, D, 1, MODE>(a, stream);
+    return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 3 ? launch_ct<bf16_t, D, 3, MODE>(a, stream) : launch_ct<bf16_t, D, 2, MODE>(a, stream);
 }
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream) {
     if (d == 64) return mode == DELTA_O ? launch_np<64, DELTA_O>(a, is_bf16, stream) : mode == DELTA_KEEP ? launch_np<64, DELTA_KEEP>(a, is_bf16, stream) : launch_np<64, DELTA_BACK>(a, is_bf16, stream);
