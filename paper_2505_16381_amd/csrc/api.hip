@@ -1150,7 +1150,7 @@ extern "C" path_status_t path_paged_plan(const int* cached, const int* new_token
 
 // ---- gated delta rule ----
 namespace {
-struct DeltaPlan { long long tiles; size_t a, m, rows, at, mt, sm, gm, um, ym, ex, total; };
+struct DeltaPlan { long long tiles; size_t a, m, rows, vmost, at, mt, sm, gm, um, ym, gmost, vex, gex, total; };
 }  // namespace
 
 // Launches of fewer than 2^32 threads: 512 per tile and key head, 256 per tile and value head, 1024 per sequence and value head.
@@ -1165,10 +1165,11 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
     p.tiles = (long long)T / CHUNK + nseq;
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
-    const size_t units = (size_t)p.tiles * V, tri = es == 4 ? 10 * 1024 : 3 * 6 * 1024;
+    const size_t units = (size_t)p.tiles * V, tri = es == 4 ? 10 * 1024 : 2 * 6 * 1024, half = es == 2;
     take(p.a, units * tri);
     take(p.m, units * tri);
     take(p.rows, units * DELTA_ROWS * 64 * 4);
+    take(p.vmost, half * units * 8 * 4);
     if (training) {
         take(p.at, units * tri);
         take(p.mt, units * tri);
@@ -1176,7 +1177,9 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
         take(p.gm, units * d * d * es);
         take(p.um, units * d * 64 * es);
         take(p.ym, units * d * 64 * es);
-        take(p.ex, es == 4 ? 0 : units * 32 * 4);
+        take(p.gmost, half * units * 8 * 4);
+        take(p.vex, half * nseq * V * 8 * 4);
+        take(p.gex, half * nseq * V * 8 * 4);
     }
     p.total = off;
     return p;
@@ -1212,9 +1215,11 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     char* const ws = static_cast<char*>(workspace);
     a.a = ws + p.a; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
     a.at = ws + p.at; a.mt = ws + p.mt;
-    a.sm = ws + p.sm; a.gm = ws + p.gm; a.um = ws + p.um; a.ym = ws + p.ym; a.ex = reinterpret_cast<int*>(ws + p.ex);
-    a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 3 : 2;      // (delta_parts.h)
-    a.np_b = dt == PATH_F32 ? 1 : a.state_in ? 3 : 2;
+    a.sm = ws + p.sm; a.gm = ws + p.gm; a.um = ws + p.um; a.ym = ws + p.ym;
+    a.vmost = reinterpret_cast<float*>(ws + p.vmost); a.gmost = reinterpret_cast<float*>(ws + p.gmost);
+    a.vex = reinterpret_cast<int*>(ws + p.vex); a.gex = reinterpret_cast<int*>(ws + p.gex);
+    a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 2 : 1;      // (delta_parts.h)
+    a.np_b = dt == PATH_F32 ? 1 : a.state_in ? 2 : 1;
     return PATH_OK;
 }
 
@@ -1262,6 +1267,7 @@ extern "C" path_status_t path_delta_train_bwd(const void* q, const void* k, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int bf = dt == PATH_BF16;
     if (T == 0 && !d_state_in) return PATH_OK;
+    if (bf && T > 0 && !hip_ok(launch_delta_most(a, d, st), "delta rule, size of the gradient")) return PATH_ERR_HIP;
     if (!hip_ok(launch_delta_scan(a, d, bf, 2, st), "delta rule, gradients of the states")) return PATH_ERR_HIP;
     return T == 0 || hip_ok(launch_delta_grad(a, d, bf, st), "delta rule, gradients of the chunks") ? PATH_OK : PATH_ERR_HIP;
 }

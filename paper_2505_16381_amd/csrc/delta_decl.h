@@ -34,12 +34,13 @@ struct DeltaArgs {
     long long ks, kt, kh, vs, vt, vh, ss, st, sh;      // element strides of sequence, token and head: q, k; v, o; beta, log_f
     float scale;
     int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
+    float *vmost, *gmost;                      // per (tile, head) [8]: largest finite |v|, |d_o| of the chunk, of each 16 value indices
     void *a, *m, *at, *mt;                     // per (tile, head): A and M as operand fragments, and their transposes (training)
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
-    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], U and Y, [value index][token]: fp32, or fp16 with
-    // an exponent per block of 16 value indices, ex [4][8] (S, G, U, Y)
+    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], U and Y, [value index][token]: fp32, or fp16 over
+    // the powers of two that the scans chose, per (sequence, head) and 16 value indices
     void *sm, *gm, *um, *ym;
-    int* ex;
+    int *vex, *gex;                            // [nseq * V][8]: of S and U, of G and Y
     const void* d_o;
     const float* d_state;                      // gradient of the last states; NULL: zeros
     void *dq, *dk, *dv, *dbeta, *dlog_f;
@@ -77,6 +78,7 @@ __device__ __forceinline__ bool delta_tile(const DeltaArgs& a, int tile, int lan
 }
 
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream);
+hipError_t launch_delta_most(const DeltaArgs& a, int d, hipStream_t stream);      // gmost of d_o (bf16)
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream);      // 0: o; 1: o, and what the backward needs; 2: backwards
 hipError_t launch_delta_grad(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);

@@ -253,48 +253,33 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
             sf[i] = *reinterpret_cast<const halfx8*>(sg + (tid + i * NT) * 8);
             gf[i] = *reinterpret_cast<const halfx8*>(gg + (tid + i * NT) * 8);
         }
-        int exs[4];      // the largest exponents of S, G, U, Y
-        const int* const ex = a.ex + u * 32;
+        const int *const vex = a.vex + ((size_t)s * a.V + hv) * 8, *const gex = a.gex + ((size_t)s * a.V + hv) * 8;
+        int ev = vex[0], eg = gex[0];      // the largest exponents: of S and U, of G, Y and dO
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            exs[m] = ex[8 * m];
-#pragma unroll
-            for (int b = 1; b < D / 16; ++b) exs[m] = ex[8 * m + b] > exs[m] ? ex[8 * m + b] : exs[m];
+        for (int b = 1; b < D / 16; ++b) {
+            ev = vex[b] > ev ? vex[b] : ev;
+            eg = gex[b] > eg ? gex[b] : eg;
         }
         __syncthreads();      // (the head before has been read out)
         for (int i = tid; i < DELTA_ROWS * 64; i += NT) rows[i] = a.rows[u * DELTA_ROWS * 64 + i];
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)of[i][e]));
-#pragma unroll
-        for (int i = 1; i < 64; i *= 2) most = fmaxf(most, __shfl_xor(most, i));
-        if (lane == 0) wred[wv] = most;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int p = tid + i * NT, r = p >> 3, y = (p & 7) * 8;
-            const half_t wu = half_power(ex[16 + (r >> 4)] - exs[2]), wy = half_power(ex[24 + (r >> 4)] - exs[3]);
+            const half_t wu = half_power(vex[r >> 4] - ev), wy = half_power(gex[r >> 4] - eg);
             *reinterpret_cast<halfx8*>(U + r * LU + y) = uf[i] * wu;
             *reinterpret_cast<halfx8*>(Y + r * LU + y) = yf[i] * wy;
         }
-        float sum = 0.f;      // <S, G>, over 2^(exs[0] + exs[1])
+        float sum = 0.f;      // <S, G>, over 2^(ev + eg)
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             const int p = tid + i * NT, r = p / PPR, y = p % PPR * 8;
-            sf[i] = sf[i] * half_power(ex[r >> 4] - exs[0]);
-            gf[i] = gf[i] * half_power(ex[8 + (r >> 4)] - exs[1]);
+            sf[i] = sf[i] * half_power(vex[r >> 4] - ev);
+            gf[i] = gf[i] * half_power(gex[r >> 4] - eg);
             *reinterpret_cast<halfx8*>(S + r * LD + y) = sf[i];
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += (float)sf[i][e] * (float)gf[i][e];
         }
-        __syncthreads();
-        most = wred[0];
-#pragma unroll
-        for (int i = 1; i < NWV; ++i) most = fmaxf(most, wred[i]);
-        int eo = (int)(__float_as_uint(most) >> 23) - 127 - 10;
-        eo = eo < -126 ? -126 : eo;
-        const float wo = ldexpf(1.f, -eo);
+        const float wo = delta_power(-eg);
 #pragma unroll
         for (int i = 0; i < NP; ++i) put(O, of[i], i, wo);
         __syncthreads();
@@ -318,7 +303,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
                     const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il));
                     const bool in = i < r;
                     part[j] = in ? acc[j] * w * kk[j] : 0.f;
-                    Gk[r * LU + i] = (half_t)(in ? -rows[r] * w * acc[j] * 0x1p-14f : 0.f);
+                    Gk[r * LU + i] = (half_t)(in ? -rows[r] * w * acc[j] * 0x1p-12f : 0.f);
                 }
                 if (b == 1)
 #pragma unroll
@@ -334,7 +319,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
                 for (int j = 0; j < 16; ++j) {
                     const int r = 32 * br + acc_row(j, h);
                     const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il));
-                    Gq[r * LU + i] = (half_t)(i <= r ? w * acc[j] * 0x1p-14f : 0.f);
+                    Gq[r * LU + i] = (half_t)(i <= r ? w * acc[j] * 0x1p-12f : 0.f);
                 }
                 if (b == 1)
 #pragma unroll
@@ -368,7 +353,8 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
         }
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
-        const int eou = 14 + eo + exs[2], eyu = 14 + exs[3] + exs[2], eys = exs[3] + exs[0], eos = eo + exs[0], eug = exs[2] + exs[1];
+        const float up = ldexpf(1.f, ev + eg);      // of every product of two of them
+        const float up12 = up * 4096.f;              // ... of Gq and Gk, which are 2^12 below theirs: sums of 128 products stay far from fp16's end
         asm volatile("" : "+v"(l32), "+v"(h));
         // one product after the other, so that no more than three are held beside dq and dk
         float pk[16], pl[16], kug = 0.f;
@@ -379,7 +365,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
         mm<half_t, 64, false, true>(acc, Gq, LU, 32 * rb, K, LD, 32 * cb, l32, h);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float v = a.scale * (ldexpf(acc[j], eou) + rz[64 + row(j)] * ldexpf(os[j], eos));
+            const float v = a.scale * (acc[j] * up12 + rz[64 + row(j)] * os[j] * up);
             dq[j] += v;
             pl[j] = (float)qz[row(j) * LD] * v;
         }
@@ -388,7 +374,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
         mm<half_t, 64, false, true>(acc, Gk, LU, 32 * rb, K, LD, 32 * cb, l32, h);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float kv = (float)kz[row(j) * LD], y = rz[64 + row(j)] * ldexpf(ys[j], eys), v = ldexpf(acc[j], eyu) - rz[row(j)] * y;
+            const float kv = (float)kz[row(j) * LD], y = rz[64 + row(j)] * ys[j] * up, v = acc[j] * up12 - rz[row(j)] * y;
             pk[j] = kv * y;
             pl[j] += kv * v;
             dk[j] += v;
@@ -398,7 +384,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
         mm<half_t, D, true, true>(acc, U, LU, 32 * rb, S, LD, 32 * cb, l32, h);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float v = rz[128 + row(j)] * ldexpf(acc[j], eug), kv = (float)kz[row(j) * LD];
+            const float v = rz[128 + row(j)] * acc[j] * up, kv = (float)kz[row(j) * LD];
             kug += kv * v;
             pl[j] -= kv * v;
             dk[j] += v;
@@ -410,12 +396,12 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
         mm<half_t, 64, true, true>(os, Gq, LU, 32 * rb, Q, LD, 32 * cb, l32, h);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float v = ldexpf(acc[j], eyu) + a.scale * ldexpf(os[j], eou);
+            const float v = (acc[j] + a.scale * os[j]) * up12;
             pl[j] -= (float)kz[row(j) * LD] * v;
             dk[j] += v;
         }
         __builtin_amdgcn_sched_barrier(0);
-        kug += rows[64 + 63] * ldexpf(sum, exs[0] + exs[1]);
+        kug += rows[64 + 63] * sum * up;
         const float pks = sum16(pk, l32), pls = sum16(pl, l32);
         if (!(l32 & 1)) {
             kys[cb * 64 + 32 * rb + acc_row(l32 >> 1, h)] = pks;
@@ -437,7 +423,7 @@ __global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArg
                 if (lane + z < 64) l += t;
             }
             if (lane < left) {
-                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)(ldexpf(y, exs[3]) - ky - ldexpf(xl[lane] + xl[64 + lane], exs[3] + exs[2]));
+                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)(ldexpf(y, eg) - ky - (xl[lane] + xl[64 + lane]) * up);
                 if (a.dlog_f) static_cast<bf16_t*>(a.dlog_f)[sat + lane * a.st] = (bf16_t)(l + all);
             }
         }

@@ -1,24 +1,27 @@
-// Operands of the gated delta rule's kernels: 16x16 products of a wave, and their operands as sums of bf16 numbers.
+// Operands of the gated delta rule's kernels: 16x16 products of a wave, and their operands.
 //
 // A product D [16 x 16] += A [16 x SL] B [SL x 16] has, lane l = 16 g + n: D rows 4 g + j in register j, column n; A row n and B column n, contraction indices
-// FE g + e in element e (bf16: SL = 32, eight elements; fp32: SL = 16, four elements, one instruction each).  Results become the B operand of the next product in
-// place: rows along the registers are its contraction index.  For bf16 that takes two tiles for a slab of 32, and their rows are chosen such that a lane's eight
+// FE g + e in element e (fp16: SL = 32, eight elements; fp32: SL = 16, four elements, one instruction each).  Results become the B operand of the next product in
+// place: rows along the registers are its contraction index.  For fp16 that takes two tiles for a slab of 32, and their rows are chosen such that a lane's eight
 // registers are eight successive indices: row m of tile t is index
 //     delta_row(t, m) = 32 (t / 2) + 8 (m / 4) + 4 (t % 2) + m % 4          (fp32: 16 t + m).
-// What is computed -- states, predictions, the chunk's matrices -- is multiplied as a sum of NP bf16 numbers, each the rounding of what the ones before it leave;
-// inputs are one.  Of the products of the parts those below the last part's size are left out.  NP = 2 (relative steps of 2^-17) is enough for results that are rounded to
-// bf16; NP = 3 (2^-25) where states are handed out in 32 bits: with two, states came out 4e-6 (of their norm) from 64 bits, ten times what sums in 32 bits cost.
+//
+// With bf16 tensors the operands are fp16: q, k and what is computed from them as they are, and what hangs on v (states, U; backwards d_o, their gradients) over a power of two that
+// puts the largest finite value of the sequence, head and 16 columns between 32 and 64, so that values of any size have fp16's eleven bits (down to 2^-19 of the largest;
+// less below).  What is computed is multiplied as the sum of NP fp16 numbers, each the rounding of what the one before leaves.  NP = 1 (relative steps of 2^-12; o and gradients 4e-4 of their norm
+// from 64 bits before they are rounded to bf16, which is 1.7e-3) where nothing but bf16 is handed out, NP = 2 (2^-23; 2e-7) where states are.  (Sums of bf16 numbers need two and three for
+// less, 5e-6 and 7e-8: forward of 4 x 16 heads, 8192 tokens, states 331 us.)
 #pragma once
 #include "delta_decl.h"
 
 namespace path {
 
 template <typename T> struct DeltaOps;
-template <> struct DeltaOps<bf16_t> {
+template <> struct DeltaOps<half_t> {
     static constexpr int SL = 32, FE = 8, TPS = 2;      // contraction indices of a slab, elements of a fragment, result tiles that make a slab
     static constexpr int NLOW = 6;                      // fragments of a 64 x 64 lower (or upper) triangular operand
-    typedef bf16x8 Frag;
-    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    typedef halfx8 Frag;
+    static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ int row(int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); }
     static constexpr __device__ __forceinline__ bool low(int t, int s) { return s <= t >> 1; }
     static constexpr __device__ __forceinline__ int low_at(int t, int s) { return t < 2 ? t : 2 * (t - 1) + s; }              // t >= 2: slabs 0, 1
@@ -58,35 +61,25 @@ template <typename T, int NP> __device__ __forceinline__ void delta_split(const 
         }
     }
 }
-// four numbers as sums of NP bf16 numbers each, two to a register
+// four numbers as sums of NP fp16 numbers each, two to a register
 template <int NP> struct DeltaSplit4 {
     uint2 p[NP];
     __device__ __forceinline__ explicit DeltaSplit4(const f32x4& v) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        float r[4] = {v[0], v[1], v[2], v[3]};
+        f32x4 r = v;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            unsigned w[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const f32x2 x = {r[2 * j], r[2 * j + 1]};
-                w[j] = __builtin_bit_cast(unsigned, __builtin_convertvector(x, bf16x2));
-                r[2 * j] -= __uint_as_float(w[j] << 16);
-                r[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
-            }
-            p[i] = uint2{w[0], w[1]};
+            const halfx4 h = __builtin_convertvector(r, halfx4);
+            p[i] = __builtin_bit_cast(uint2, h);
+            if (i + 1 < NP) r = r - __builtin_convertvector(h, f32x4);
         }
     }
 };
-// slab s of a column of result tiles, each value times f[...] of its tile and register, as a B operand
-template <typename T, int NP> __device__ __forceinline__ void delta_pack(const f32x4* tile, int s, DeltaParts<T, NP>& o) {
-    constexpr int FE = DeltaOps<T>::FE, TPS = DeltaOps<T>::TPS;
-    float x[FE];
-#pragma unroll
-    for (int e = 0; e < FE; ++e) x[e] = tile[TPS * s + e / 4][e % 4];
-    delta_split<T, NP>(x, o);
+// eight values of the caller's type as an operand
+__device__ __forceinline__ halfx8 delta_operand(const bf16x8& f) {
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    return __builtin_convertvector(__builtin_convertvector(f, f32x8), halfx8);
 }
+__device__ __forceinline__ f32x4 delta_operand(const f32x4& f) { return f; }
 // c += a b, products of parts that together are below the last one left out
 template <typename T, int NA, int NB> __device__ __forceinline__ f32x4 delta_mma(const DeltaParts<T, NA>& a, const DeltaParts<T, NB>& b, f32x4 c) {
     constexpr int NP = NA > NB ? NA : NB;
@@ -98,30 +91,11 @@ template <typename T, int NA, int NB> __device__ __forceinline__ f32x4 delta_mma
     return c;
 }
 
-// Tiles of K and Q in LDS: rows of d elements without padding, the 16-byte pieces of a row permuted by an exclusive or with a number made of the row, so that
-// neither a fragment along the row (sixteen rows' pieces of one column) nor, 16 bits, a transposing read (four rows, four pieces) meets itself on a bank.
-template <typename T, int D> struct DeltaTile {
-    static constexpr int ROWB = D * (int)sizeof(T), PPR = ROWB / 16, BYTES = 64 * ROWB;
-    static __device__ __forceinline__ int turn(int row) {
-        return sizeof(T) == 4 ? row & 15 : D == 128 ? ((row & 3) << 2) | ((row >> 3) & 3) : (((row >> 1) & 1) << 2) | ((row >> 3) & 3);
-    }
-    // bytes: the lane's place in the fragment (tile 0, slab 0) along the rows; slab s: xor 64 s; tile t: + tile_off(t)
-    static __device__ __forceinline__ unsigned nat(int n, int g) {
-        const int row = DeltaOps<T>::row(0, n);
-        return row * ROWB + ((g ^ turn(row)) << 4);
-    }
-    static constexpr __device__ __forceinline__ unsigned tile_off(int t) { return sizeof(T) == 4 ? 16 * t * ROWB : (32 * (t >> 1) + 4 * (t & 1)) * ROWB; }
-};
-
-// The transposed tile as an A operand: rows of result tiles 2 tp, 2 tp + 1 (bf16) are the tile's columns, the contraction its 64 rows: fragments [tile % 2][slab] of
-// one tp.  base: LDS address of the tile plus the lane's share tr(); xor 64 tp.
-template <int D> __device__ __forceinline__ unsigned delta_tr(int lane) {
-    const int g = lane >> 4, j = lane & 15, row = 8 * g + (j >> 2);
-    return row * D * 2 + (((j & 3) ^ DeltaTile<bf16_t, D>::turn(row)) << 4);
-}
-template <int D> __device__ __forceinline__ void delta_ld_tr(unsigned at, bf16x8 (&f)[2][2]) {
-    union U { unsigned long long v[2]; bf16x8 f; } u[4];
-    constexpr int R4 = 4 * D * 2, R32 = 32 * D * 2;
+// A matrix in LDS, 64 rows of W 16-bit elements, transposed as an A operand: rows of result tiles 2 t, 2 t + 1 are 32 of its columns, the contraction its rows: fragments
+// [tile % 2][slab].  at: LDS address of row 8 g + n / 4, column 8 (n % 4) of the 32.
+template <int W> __device__ __forceinline__ void delta_ld_tr(unsigned at, halfx8 (&f)[2][2]) {
+    union U { unsigned long long v[2]; halfx8 f; } u[4];
+    constexpr int R4 = 4 * W * 2, R32 = 32 * W * 2;
     asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%9\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
                  "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
                  "ds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %8 offset:%14\n\t"
@@ -135,5 +109,13 @@ template <int D> __device__ __forceinline__ void delta_ld_tr(unsigned at, bf16x8
 #pragma unroll
         for (int s = 0; s < 2; ++s) f[b][s] = u[2 * b + s].f;
 }
+
+// the exponent that puts numbers up to m between 32 and 64 (2^100 and 2^-100 are the ends)
+__device__ __forceinline__ int delta_exponent(float m) {
+    const int e = (int)(__float_as_uint(m) >> 23) - 127 - 5;
+    return e < -100 ? -100 : e > 100 ? 100 : e;
+}
+__device__ __forceinline__ float delta_power(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
+__device__ __forceinline__ float delta_finite(float x) { const float y = fabsf(x); return __float_as_uint(y) < 0x7f800000u ? y : 0.f; }
 
 }  // namespace path

@@ -1,4 +1,6 @@
 // Gated delta rule: the matrices of a chunk, all chunks at once (delta_decl.h has the formulas).
+#include <type_traits>
+
 #include "delta_parts.h"
 
 namespace path {
@@ -16,6 +18,40 @@ __device__ __forceinline__ f32x4 block_mma(const float* A, int bi, int bk, const
 // the same with B in registers, as a product left it
 __device__ __forceinline__ f32x4 block_mma(const float* A, int bi, int bk, f32x4 y, int n, int g, f32x4 c) {
     return DeltaOps<float>::mma(*reinterpret_cast<const f32x4*>(A + (16 * bi + n) * DP_LF + 16 * bk + 4 * g), y, c);
+}
+
+// K K^T and Q K^T take the caller's numbers as they are
+__device__ __forceinline__ f32x4 mma_user(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma_user(f32x4 a, f32x4 b, f32x4 c) { return DeltaOps<float>::mma(a, b, c); }
+
+// largest finite |x| of 64 rows of d values, of each 16 columns, by 256 threads
+template <int D> __device__ __forceinline__ void most_of(const bf16_t* x, long long ld, int rows, float* out, float (*red)[8], int tid) {
+    constexpr int PPR = D / 8;      // pieces of 8 columns; a thread's are all in one place
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 64 * PPR / 256; ++i) {
+        const int r = (tid + 256 * i) / PPR;
+        if (r < rows) {
+            const bf16x8 f = *reinterpret_cast<const bf16x8*>(x + r * ld + tid % PPR * 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, delta_finite((float)f[e]));
+        }
+    }
+    m = fmaxf(m, __shfl_xor(m, 1));
+#pragma unroll
+    for (int i = PPR; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+    if ((tid & 63) < PPR && !(tid & 1)) red[tid >> 6][(tid & 63) >> 1] = m;
+    __syncthreads();
+    if (tid < D / 16) out[tid] = fmaxf(fmaxf(red[0][tid], red[1][tid]), fmaxf(red[2][tid], red[3][tid]));
+}
+
+template <int D> __global__ __launch_bounds__(256) void delta_most_kernel(DeltaArgs a) {
+    __shared__ float red[4][8];
+    const int tid = threadIdx.x, tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.V), hv = blockIdx.x - tile * a.V;
+    int s, c;
+    DeltaSeq sq;
+    if (!delta_tile(a, tile, tid & 63, s, c, sq)) return;
+    most_of<D>(static_cast<const bf16_t*>(a.d_o) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + (long long)c * CHUNK * a.vt, a.vt, sq.len - c * CHUNK, a.gmost + ((size_t)tile * a.V + hv) * 8, red, tid);
 }
 
 template <typename T, int NP>
@@ -44,13 +80,15 @@ __device__ __forceinline__ void store_frags(const float* X, bool transposed, voi
 
 template <typename T, int D, int NPF, int NPB>      // NPB = 0: no transposes
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
-    typedef DeltaOps<T> P;
+    typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept
+    typedef typename Tr<T>::Frag Frag;
+    constexpr int SL = sizeof(T) == 2 ? 32 : 16, FE = 16 / (int)sizeof(T);
     constexpr int LD = D + 16 / (int)sizeof(T), VEC = 16 / (int)sizeof(T);
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* const N = reinterpret_cast<float*>(smem);
     float* const M = N + 64 * DP_LF;
     float* const rows = M + 64 * DP_LF;
-    T* const K = reinterpret_cast<T*>(rows + DELTA_ROWS * 64);
+    T* const K = reinterpret_cast<T*>(rows + DELTA_ROWS * 64 + 32);
     T* const Q = K + 64 * LD;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = lane & 15, g = lane >> 4;
     const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.V), hv = blockIdx.x - tile * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
@@ -63,12 +101,11 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     const long long kat = delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh + t0 * a.kt, sat = delta_at(a, sq, s, a.ss, a.st) + hv * a.sh + t0 * a.st;
     {
         const T *kp = static_cast<const T*>(a.k) + kat, *qp = static_cast<const T*>(a.q) + kat;
-        typedef typename P::Frag Frag;
         for (int i = tid; i < 64 * D / VEC; i += 256) {
             const int r = i / (D / VEC), x = i % (D / VEC) * VEC;
             Frag fk, fq;
 #pragma unroll
-            for (int e = 0; e < P::FE; ++e) { fk[e] = (T)0.f; fq[e] = (T)0.f; }
+            for (int e = 0; e < FE; ++e) { fk[e] = (T)0.f; fq[e] = (T)0.f; }
             if (r < left) {
                 fk = *reinterpret_cast<const Frag*>(kp + r * a.kt + x);
                 fq = *reinterpret_cast<const Frag*>(qp + r * a.kt + x);
@@ -77,6 +114,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
             *reinterpret_cast<Frag*>(Q + r * LD + x) = fq;
         }
     }
+    if constexpr (sizeof(T) == 2)
+        most_of<D>(static_cast<const bf16_t*>(a.v) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, a.vt, left, a.vmost + unit * 8, reinterpret_cast<float(*)[8]>(rows + DELTA_ROWS * 64), tid);
     if (wv == 0) {
         // Running sums in 64 bits: 64 gates of -20 each add up to 1e3, whose rounding to 32 bits would be 6e-5 of a neighbour's weight.  Gates below exp(-200) count as
         // that: it is nothing beside any number of 32 bits, and sums stay small enough for differences between the tokens behind a gate that forgets everything.
@@ -102,21 +141,21 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     float be[4], bh[4], bl[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) { const int r = 16 * wv + 4 * g + j; be[j] = rows[r]; bh[j] = rows[3 * 64 + r]; bl[j] = rows[4 * 64 + r]; }
-    typename P::Frag fk[D / P::SL], fq[D / P::SL];
+    Frag fk[D / SL], fq[D / SL];
 #pragma unroll
-    for (int x = 0; x < D / P::SL; ++x) {
-        fk[x] = *reinterpret_cast<const typename P::Frag*>(K + (16 * wv + n) * LD + x * P::SL + P::FE * g);
-        fq[x] = *reinterpret_cast<const typename P::Frag*>(Q + (16 * wv + n) * LD + x * P::SL + P::FE * g);
+    for (int x = 0; x < D / SL; ++x) {
+        fk[x] = *reinterpret_cast<const Frag*>(K + (16 * wv + n) * LD + x * SL + FE * g);
+        fq[x] = *reinterpret_cast<const Frag*>(Q + (16 * wv + n) * LD + x * SL + FE * g);
     }
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
         if (ib <= wv) {
 #pragma unroll
-            for (int z = 0; z < D / P::SL; ++z) {
-                const typename P::Frag f = *reinterpret_cast<const typename P::Frag*>(K + (16 * ib + n) * LD + z * P::SL + P::FE * g);
-                x = P::mma(fk[z], f, x);
-                y = P::mma(fq[z], f, y);
+            for (int z = 0; z < D / SL; ++z) {
+                const Frag f = *reinterpret_cast<const Frag*>(K + (16 * ib + n) * LD + z * SL + FE * g);
+                x = mma_user(fk[z], f, x);
+                y = mma_user(fq[z], f, y);
             }
         }
         const int i = 16 * ib + n;
@@ -174,17 +213,17 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         for (int j = 0; j < 4; ++j) N[(16 * bi + 4 * g + j) * DP_LF + 16 * bj + n] = -x[j];
     }
     __syncthreads();
-    store_frags<T, NPF>(N, false, a.a, unit, tid);
-    store_frags<T, NPF>(M, false, a.m, unit, tid);
+    store_frags<C, NPF>(N, false, a.a, unit, tid);
+    store_frags<C, NPF>(M, false, a.m, unit, tid);
     if constexpr (NPB > 0) {
-        store_frags<T, NPB>(N, true, a.at, unit, tid);
-        store_frags<T, NPB>(M, true, a.mt, unit, tid);
+        store_frags<C, NPB>(N, true, a.at, unit, tid);
+        store_frags<C, NPB>(M, true, a.mt, unit, tid);
     }
 }
 
 template <typename T, int D, int NPF, int NPB>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    constexpr size_t bytes = (size_t)(2 * 64 * DP_LF + DELTA_ROWS * 64) * 4 + (size_t)2 * 64 * (D * sizeof(T) + 16);
+    constexpr size_t bytes = (size_t)(2 * 64 * DP_LF + DELTA_ROWS * 64 + 32) * 4 + (size_t)2 * 64 * (D * sizeof(T) + 16);
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_prep_kernel<T, D, NPF, NPB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
     delta_prep_kernel<T, D, NPF, NPB><<<dim3((unsigned)a.tiles * a.V), dim3(256), bytes, stream>>>(a);
@@ -193,12 +232,19 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
 template <int D>
 static hipError_t launch_d(const DeltaArgs& a, int is_bf16, bool training, hipStream_t stream) {
     if (!is_bf16) return training ? launch<float, D, 1, 1>(a, stream) : launch<float, D, 1, 0>(a, stream);
-    if (!training) return a.np_f == 3 ? launch<bf16_t, D, 3, 0>(a, stream) : launch<bf16_t, D, 2, 0>(a, stream);
-    if (a.np_f == 3) return a.np_b == 3 ? launch<bf16_t, D, 3, 3>(a, stream) : launch<bf16_t, D, 3, 2>(a, stream);
-    return a.np_b == 3 ? launch<bf16_t, D, 2, 3>(a, stream) : launch<bf16_t, D, 2, 2>(a, stream);
+    if (!training) return a.np_f == 2 ? launch<bf16_t, D, 2, 0>(a, stream) : launch<bf16_t, D, 1, 0>(a, stream);
+    if (a.np_f == 2) return a.np_b == 2 ? launch<bf16_t, D, 2, 2>(a, stream) : launch<bf16_t, D, 2, 1>(a, stream);
+    return a.np_b == 2 ? launch<bf16_t, D, 1, 2>(a, stream) : launch<bf16_t, D, 1, 1>(a, stream);
 }
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream) {
     return d == 64 ? launch_d<64>(a, is_bf16, training, stream) : launch_d<128>(a, is_bf16, training, stream);
+}
+
+hipError_t launch_delta_most(const DeltaArgs& a, int d, hipStream_t stream) {
+    const dim3 grid((unsigned)a.tiles * a.V);
+    if (d == 64) delta_most_kernel<64><<<grid, dim3(256), 0, stream>>>(a);
+    else delta_most_kernel<128><<<grid, dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace path

@@ -1,45 +1,63 @@
 // Gated delta rule: the states, chunk after chunk, and backwards their gradients (delta_decl.h has the formulas).
 //
-// A workgroup of four waves has CT * 16 columns (value indices) of a head's state, which stays in registers: each wave a quarter of its rows (key indices), and of a chunk's
-// products with it the 16 tokens of one result tile.  What a wave needs of K, Q, A and M nobody else needs, so it comes from memory straight into its
-// registers, a chunk ahead; what all need -- the state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
+// A workgroup has CT * 16 columns (value indices) of a head's state.  Four waves carry it on, each a quarter of its rows (key indices), in registers, and of a chunk's products
+// with it the 16 tokens of one result tile; four more do what the chain of chunks does not wait for: the outputs (forward), and what d_o adds to dU and to the state's
+// gradient (backwards, a chunk ahead).  What one wave alone needs of K, Q, A and M comes from memory straight into its registers, a chunk ahead; what others need -- the
+// state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
+#include <type_traits>
+
 #include "delta_parts.h"
 
 namespace path {
 
 enum { DELTA_O = 0, DELTA_KEEP = 1, DELTA_BACK = 2 };      // forward; forward that keeps what the backward needs; backwards
 
+template <typename T> struct DeltaOperand { typedef T type; };
+template <> struct DeltaOperand<bf16_t> { typedef half_t type; };
+
 template <typename T, int D, int NP, int CT, int MODE>
 struct ScanLds {
-    typedef DeltaOps<T> P;
+    typedef DeltaOps<typename DeltaOperand<T>::type> P;
     static constexpr int NS = D / P::SL, CS = 64 / P::SL;                      // slabs of the state's rows, of a chunk
     static constexpr int TW = D / 64;                                          // state tiles of a wave
     static constexpr int SW = sizeof(T) == 2 ? 32 : 16 * TW, SROW = sizeof(T) == 2 ? 64 : (SW + 4) * 4;      // a wave's columns of K: elements, bytes of a row in LDS
-    static constexpr int SLICE = 64 * SROW, NSL = MODE == DELTA_BACK ? 2 : 1;
-    static constexpr int S = 0, Y = S + NS * NP * CT * 1024, U = Y + CS * NP * CT * 1024, V = U + CS * NP * CT * 1024, O = V + CS * NP * CT * 1024;
-    static constexpr int X = O + (MODE == DELTA_BACK ? CS * CT * 1024 : 0), KT = X + 256, BYTES = KT + 4 * NSL * SLICE;
+    static constexpr bool BACK = MODE == DELTA_BACK;
+    // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the two operands of the gradient's update: that of Y, and Y to be kept); backwards d_o
+    // and diag(gamma) d_o as operands, and what they add up to, in fp32
+    static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (BACK ? CS * CT * 1024 : 0);
+    static constexpr int DU = OG + (BACK ? AREA : 0), DG = DU + (BACK ? 4 * CT * 1024 : 0), X = DG + (BACK ? 4 * TW * CT * 1024 : 0), KT = X + 256;
+    static constexpr int BYTES = KT + (BACK ? 8 : 4) * 64 * SROW;
 };
 
-// largest |x| of a wave's values; the exponent that leaves fp16 numbers below 2^11
-__device__ __forceinline__ float delta_most(float m) {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
-    return m;
+// `rows` rows of `row` bytes as a buffer, and what a lane loads from and stores to it
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t delta_buffer(const char* base, int rows, unsigned row) {
+    const unsigned long long p = reinterpret_cast<unsigned long long>(base);
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)p), hi = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane((rows < CHUNK ? rows : CHUNK) * row), 0x00020000);
 }
-__device__ __forceinline__ int delta_exponent(float m) {
-    const int e = (int)(__float_as_uint(m) >> 23) - 127 - 10;
-    return e < -126 ? -126 : e;
+template <typename F> __device__ __forceinline__ F delta_load16(__amdgpu_buffer_rsrc_t r, unsigned at) { return __builtin_bit_cast(F, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0)); }
+template <typename T> __device__ __forceinline__ T delta_load1(__amdgpu_buffer_rsrc_t r, unsigned at) {
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
+    else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+}
+template <typename T> __device__ __forceinline__ void delta_store1(__amdgpu_buffer_rsrc_t r, unsigned at, T x) {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), r, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), r, at, 0, 0);
 }
 
 template <typename T, int D, int NP, int CT, int MODE>
-__global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaArgs a) {
-    typedef DeltaOps<T> P;
+__global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
+    typedef typename DeltaOperand<T>::type C;
+    typedef DeltaOps<C> P;
     typedef typename P::Frag Frag;
+    typedef decltype(delta_operand(typename Tr<T>::Frag())) Operand;
+    typedef typename Tr<T>::Frag UserFrag;
     typedef ScanLds<T, D, NP, CT, MODE> L;
-    constexpr int NS = L::NS, CS = L::CS, TW = L::TW;
-    constexpr bool BACK = MODE == DELTA_BACK;
+    constexpr int NS = L::NS, CS = L::CS, TW = L::TW, ES = sizeof(T);
+    constexpr bool BACK = MODE == DELTA_BACK, HALF = ES == 2;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 3, n = lane & 15, g = lane >> 4;
+    const bool chain = wave < 4;
     int unit, part;
     if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, D / 16 / CT, a.nseq * a.V, unit, part)) return;
     const int s = __builtin_amdgcn_readfirstlane(unit / a.V), hv = unit - s * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
@@ -48,6 +66,7 @@ __global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaA
     if (a.slots && len <= a.few) return;
     const int NC = (len + CHUNK - 1) / CHUNK;
     const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     // the first state: of a pool's slot, given, or zeros
     f32x4 S[TW][CT];
@@ -72,71 +91,96 @@ __global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaA
 #pragma unroll
         for (int x = 0; x < CT; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[t][x][j] = from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
+            for (int j = 0; j < 4; ++j) S[t][x][j] = chain && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
 
-    // an exchange area's fragment, and one tile of a slab as operands into it
-    auto frag = [&](int area, int sl, int x) {
-        DeltaParts<T, NP> f;
+    // the powers of two of the columns: down for what comes in, up for what goes out
+    float down[CT], up[CT];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) f.p[p] = *reinterpret_cast<const Frag*>(smem + area + ((sl * CT + x) * NP + p) * 1024 + lane * 16);
-        return f;
+    for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
+    if constexpr (HALF) {
+        float* const xs = reinterpret_cast<float*>(smem + L::X);
+        const float* const most = (BACK ? a.gmost : a.vmost) + ((size_t)tile0 * a.V + hv) * 8 + part * CT;
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            float m = 0.f;
+            for (int i = tid; i < NC; i += 512) m = fmaxf(m, most[(size_t)i * a.V * 8 + x]);
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = fmaxf(m, delta_finite(S[t][x][j]));
+#pragma unroll
+            for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+            if (lane == 0) xs[x * 8 + wave] = m;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            float m = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, xs[x * 8 + i]);
+            const int e = __builtin_amdgcn_readfirstlane(delta_exponent(m));
+            down[x] = delta_power(-e);
+            up[x] = delta_power(e);
+            if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
+#pragma unroll
+            for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
+        }
+    }
+
+    // an exchange area's fragment, slabs of one requested together (left to itself the compiler waits for each on its own), and one tile of a slab as operands into it
+    auto frags = [&](int area, DeltaParts<C, NP> (&f)[CS][CT]) {
+#pragma unroll
+        for (int sl = 0; sl < CS; ++sl)
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) f[sl][x].p[p] = *reinterpret_cast<const Frag*>(smem + area + ((sl * CT + x) * NP + p) * 1024 + lane * 16);
     };
-    auto put = [&](int area, int tile, int x, const f32x4& v) {
-        if constexpr (sizeof(T) == 4) {
+    auto frag1 = [&](int area, int sl, int x, int np) { return *reinterpret_cast<const Frag*>(smem + area + (sl * CT + x) * np * 1024 + lane * 16); };
+    auto put = [&](auto parts, int area, int tile, int x, const f32x4& v) {
+        constexpr int N = decltype(parts)::value;
+        if constexpr (!HALF) {
             *reinterpret_cast<f32x4*>(smem + area + (tile * CT + x) * 1024 + lane * 16) = v;
         } else {
-            DeltaSplit4<NP> r(v);
+            const DeltaSplit4<N> r(v);
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                *reinterpret_cast<uint2*>(smem + area + (((tile >> 1) * CT + x) * NP + p) * 1024 + lane * 16 + (tile & 1) * 8) = r.p[p];
+            for (int p = 0; p < N; ++p)
+                *reinterpret_cast<uint2*>(smem + area + (((tile >> 1) * CT + x) * N + p) * 1024 + lane * 16 + (tile & 1) * 8) = r.p[p];
         }
     };
+    const std::integral_constant<int, NP> all_parts{};
+    const std::integral_constant<int, 1> one_part{};
 
-    // Addresses: a chunk's place in scalar registers, the lane's in 32 bits of bytes, made anew only where a chunk has fewer than 64 tokens: rows behind the sequence's end are
-    // its last one again (their beta is 0).
-    constexpr int ES = sizeof(T), PPR = L::SW * ES / 16, NK = PPR;      // 16-byte pieces of a slice's row; of a slice per lane
-    const char* const kb = static_cast<const char*>(a.k) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
-    const char* const qb = static_cast<const char*>(a.q) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
+    // A chunk's rows of the caller's tensors as a buffer that ends behind the sequence's last one: rows behind it come in as zeros, and nothing is stored there.
+    // (A store under a condition would have every later wait for a load wait for the store as well.)
+    constexpr int PPR = L::SW * ES / 16, NK = PPR;      // 16-byte pieces of a slice's row; of a slice per lane
+    const char* const kb = static_cast<const char*>(chain ? a.k : a.q) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
     const long long vat = (delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + 16 * part * CT) * ES;
     const char* const vb = static_cast<const char*>(BACK ? a.d_o : a.v) + vat;
     char* const ob = static_cast<char*>(BACK ? a.dv : a.o) + vat;
-    const long long kstep = a.kt * ES * CHUNK, vstep = a.vt * ES * CHUNK;
-    unsigned row_at, slice_at[NK], value_at[4];
-    auto place = [&](int c) {
-        const int last = len - 1 - c * CHUNK;
-        const unsigned kt = (unsigned)a.kt * ES, vt = (unsigned)a.vt * ES;
-        auto held = [&](int r) { return (unsigned)(r < last ? r : last); };
-        row_at = held(P::row(wv, n)) * kt + 16 * g;
-        const int c0 = sizeof(T) == 2 ? 32 * (TW * wv >> 1) : 16 * TW * wv;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) slice_at[i] = held((i * 64 + lane) / PPR) * kt + c0 * ES + (lane % PPR) * 16;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) value_at[j] = held(P::row(wv, 4 * g + j)) * vt + n * ES;
-    };
-    auto partial = [&](int c) { return len - c * CHUNK < CHUNK; };
-
-    // What a chunk brings, loaded again as soon as it has been used.
-    Frag K[NS], Q[BACK ? 1 : NS], kt[L::NSL][NK];
-    DeltaParts<T, NP> A[CS], M[CS];
-    T v[CT][4];
-    f32x4 be, ga4, rh;
-    float g63;
+    const unsigned krow = (unsigned)a.kt * ES, vrow = (unsigned)a.vt * ES;
+    auto buffer = [&](const char* base, unsigned row, int c) { return delta_buffer(base + (long long)c * CHUNK * row, len - c * CHUNK, row); };
+    const unsigned row_at = P::row(wv, n) * krow + 16 * g, value_at = P::row(wv, 4 * g) * vrow + n * ES;
+    const unsigned slice_at = lane / PPR * krow + (HALF ? 32 * (TW * wv >> 1) : 16 * TW * wv) * ES + lane % PPR * 16;
     typedef const __attribute__((address_space(1))) Frag GlobalFrag;
-    auto load_rows = [&](const char* base, int c, Frag* f) {
-        const GlobalBytes p = scalar_base(base + c * kstep, row_at);
+    constexpr int RS = D * ES / 64;      // 64-byte pieces of a row: a fragment of one each
+    auto load_rows = [&](int c, UserFrag* f) {
+        const auto r = buffer(kb, krow, c);
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) f[sl] = *(GlobalFrag*)(p + sl * P::SL * ES);
+        for (int sl = 0; sl < RS; ++sl) f[sl] = delta_load16<UserFrag>(r, row_at + sl * 64);
     };
-    auto load_slice = [&](const char* base, int c, Frag* f) {      // all rows of the wave's columns
+    auto load_slice = [&](int c, UserFrag* f) {      // all rows of the wave's columns
+        const auto r = buffer(kb, krow, c);
 #pragma unroll
-        for (int i = 0; i < NK; ++i) f[i] = *(GlobalFrag*)scalar_base(base + c * kstep, slice_at[i]);
+        for (int i = 0; i < NK; ++i) f[i] = delta_load16<UserFrag>(r, slice_at + i * (64 / PPR) * krow);
     };
-    auto store_slice = [&](const Frag* f, int at) {
+    const int slice = L::KT + wave * 64 * L::SROW;
+    auto store_slice = [&](const UserFrag* f) {
 #pragma unroll
-        for (int i = 0; i < NK; ++i) *reinterpret_cast<Frag*>(smem + at + (i * 64 + lane) / PPR * L::SROW + (lane % PPR) * 16) = f[i];
+        for (int i = 0; i < NK; ++i) *reinterpret_cast<Operand*>(smem + slice + (i * 64 + lane) / PPR * L::SROW + (lane % PPR) * 16) = delta_operand(f[i]);
     };
     auto used = [&](int sl) { return BACK ? P::up(wv, sl) : P::low(wv, sl); };
-    auto load_tri = [&](const void* base, int c, DeltaParts<T, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
+    auto load_tri = [&](const void* base, int c, DeltaParts<C, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
         const char* const p = static_cast<const char*>(base) + ((size_t)(tile0 + c) * a.V + hv) * NP * P::NLOW * 1024;
 #pragma unroll
         for (int sl = 0; sl < CS; ++sl) {
@@ -145,31 +189,36 @@ __global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaA
             for (int z = 0; z < NP; ++z) f[sl].p[z] = *(GlobalFrag*)scalar_base(p + (z * P::NLOW + at) * 1024, lane * 16);
         }
     };
-    auto load_values = [&](int c) {      // the lane's tokens and columns of V (backwards: dO)
+    auto load_values = [&](int c, T (&v)[CT][4]) {      // the lane's tokens and columns of V (backwards: dO)
+        const auto r = buffer(vb, vrow, c);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int x = 0; x < CT; ++x) v[x][j] = *(const __attribute__((address_space(1))) T*)(scalar_base(vb + c * vstep, value_at[j]) + 16 * x * ES);
+            for (int x = 0; x < CT; ++x) v[x][j] = delta_load1<T>(r, value_at + j * vrow + 16 * x * ES);
     };
-    auto load_numbers = [&](int c) {
-        const float* const p = a.rows + ((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS * 64;
-        typedef const __attribute__((address_space(1))) f32x4 Global4;
-        const GlobalBytes r = scalar_base(p, P::row(wv, 4 * g) * 4);
-        be = *(Global4*)r;
-        ga4 = *(Global4*)(r + 256);
-        rh = *(Global4*)(r + 512);
-        g63 = p[64 + 63];
-    };
-    unsigned out_at[4];
+    auto values = [&](const T (&v)[CT][4], f32x4* V) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) out_at[j] = P::row(wv, 4 * g + j) * ((unsigned)a.vt * ES) + n * ES;
-    const void *const ga = BACK ? a.at : a.a, *const gm = BACK ? a.mt : a.m;
-    const int slice = L::KT + wv * L::NSL * L::SLICE;
-    // state tiles += (the wave's columns of K or Q)^T y
-    auto into_state = [&](int at, const DeltaParts<T, NP> (&y)[CS][CT]) {
-        if constexpr (sizeof(T) == 2) {
-            const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(smem + at) + (8 * g + (n >> 2)) * 64 + (n & 3) * 16;
-            bf16x8 f[2][2];
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) V[x][j] = (float)v[x][j] * down[x];
+    };
+    auto store_values = [&](int c, const f32x4* o) {
+        const auto r = buffer(ob, vrow, c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) delta_store1<T>(r, value_at + j * vrow + 16 * x * ES, (T)(o[x][j] * up[x]));
+    };
+    auto number = [&](int c, int which) {      // of the lane's four tokens
+        typedef const __attribute__((address_space(1))) f32x4 Global4;
+        return *(Global4*)scalar_base(a.rows + (((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + which) * 64, P::row(wv, 4 * g) * 4);
+    };
+    auto last_gamma = [&](int c) { return a.rows[(((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64 + 63]; };
+    // tiles [TW][CT] += (the wave's columns of K or Q)^T y
+    auto into = [&](f32x4 (&z)[TW][CT], const DeltaParts<C, NP> (&y)[CS][CT]) {
+        if constexpr (HALF) {
+            const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(smem + slice) + (8 * g + (n >> 2)) * 64 + (n & 3) * 16;
+            halfx8 f[2][2];
             delta_ld_tr<32>(base, f);
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl)
@@ -177,270 +226,239 @@ __global__ __launch_bounds__(256, CT == 2 ? 1 : 2) void delta_scan_kernel(DeltaA
                 for (int t = 0; t < TW; ++t)
 #pragma unroll
                     for (int x = 0; x < CT; ++x) {
-                        DeltaParts<T, 1> k;
+                        DeltaParts<C, 1> k;
                         k.p[0] = TW == 2 ? f[t][sl] : (wv & 1) ? f[1][sl] : f[0][sl];
-                        S[t][x] = delta_mma(k, y[sl][x], S[t][x]);
+                        z[t][x] = delta_mma(k, y[sl][x], z[t][x]);
                     }
         } else {
 #pragma unroll
             for (int sl = 0; sl < CS; ++sl)
 #pragma unroll
                 for (int t = 0; t < TW; ++t) {
-                    DeltaParts<T, 1> k;
+                    DeltaParts<C, 1> k;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) k.p[0][e] = *reinterpret_cast<const float*>(smem + at + (16 * sl + 4 * g + e) * L::SROW + (16 * t + n) * 4);
+                    for (int e = 0; e < 4; ++e) k.p[0][e] = *reinterpret_cast<const float*>(smem + slice + (16 * sl + 4 * g + e) * L::SROW + (16 * t + n) * 4);
 #pragma unroll
-                    for (int x = 0; x < CT; ++x) S[t][x] = delta_mma(k, y[sl][x], S[t][x]);
+                    for (int x = 0; x < CT; ++x) z[t][x] = delta_mma(k, y[sl][x], z[t][x]);
                 }
         }
     };
-    // an exchange area's slabs, requested together: left to itself the compiler waits for each on its own
-    auto frags = [&](int area, DeltaParts<T, NP> (&f)[CS][CT]) {
+    // the wave's tokens' rows of K or Q times the state
+    auto times_state = [&](const UserFrag* k, f32x4* y) {
+        constexpr int HS = NS * NP * CT > 16 ? NS / 2 : NS;      // slabs requested together: up to 64 registers
+#pragma unroll
+        for (int x = 0; x < CT; ++x) y[x] = zero;
+#pragma unroll
+        for (int s0 = 0; s0 < NS; s0 += HS) {
+            DeltaParts<C, NP> f[HS][CT];
+#pragma unroll
+            for (int sl = 0; sl < HS; ++sl)
+#pragma unroll
+                for (int x = 0; x < CT; ++x)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) f[sl][x].p[p] = *reinterpret_cast<const Frag*>(smem + L::S + (((s0 + sl) * CT + x) * NP + p) * 1024 + lane * 16);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int sl = 0; sl < HS; ++sl) {
+                DeltaParts<C, 1> q;
+                q.p[0] = delta_operand(k[s0 + sl]);
+#pragma unroll
+                for (int x = 0; x < CT; ++x) y[x] = delta_mma(q, f[sl][x], y[x]);
+            }
+        }
+    };
+    // the wave's tokens' rows of A or M (transposed: of A^T or M^T) times y
+    auto times = [&](const DeltaParts<C, NP>* m, const DeltaParts<C, NP> (&y)[CS][CT], f32x4* o) {
 #pragma unroll
         for (int sl = 0; sl < CS; ++sl)
+            if (used(sl))
 #pragma unroll
-            for (int x = 0; x < CT; ++x) f[sl][x] = frag(area, sl, x);
+                for (int x = 0; x < CT; ++x) o[x] = delta_mma(m[sl], y[sl][x], o[x]);
     };
-    float* const xs = reinterpret_cast<float*>(smem + L::X);      // largest values: [2][CT][wave]
+    // a state's or token matrix's slabs to memory for the chunk's gradients, the lane's row of the transposed matrix; the waves take turns
+    auto keep = [&](void* out, int area, size_t u, int np, int slabs) {
+        const int ld = slabs * P::SL;
+        for (int sl = wv; sl < slabs; sl += 4)
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+                *reinterpret_cast<Frag*>(static_cast<C*>(out) + (u * D + col + 16 * x) * ld + P::SL * sl + P::FE * g) = frag1(area, sl, x, np);
+    };
     auto put_state = [&]() {
-#pragma unroll
-        for (int x = 0; x < CT; ++x) {
-            float m = 0.f;
-#pragma unroll
-            for (int t = 0; t < TW; ++t) {
-                put(L::S, TW * wv + t, x, S[t][x]);
-                if (MODE != DELTA_O && sizeof(T) == 2)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) m = fmaxf(m, fabsf(S[t][x][j]));
-            }
-            if (MODE != DELTA_O && sizeof(T) == 2) {
-                m = delta_most(m);
-                if (lane == 0) xs[x * 4 + wv] = m;
-            }
-        }
-    };
-    auto put_most = [&](const f32x4* w) {      // of a token tile
-        if (MODE != DELTA_O && sizeof(T) == 2)
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {
-                const float m = delta_most(fmaxf(fmaxf(fabsf(w[x][0]), fabsf(w[x][1])), fmaxf(fabsf(w[x][2]), fabsf(w[x][3]))));
-                if (lane == 0) xs[16 + x * 4 + wv] = m;
-            }
-    };
-    // a tile to memory for the chunk's gradients, the lane's row of the transposed matrix: fp32, or fp16 over a power of two of the 16 columns
-    auto keep = [&](void* out, int which, int at, int x, size_t u, int ld, int tile, const f32x4& w) {
-        const size_t row = (u * D + col + 16 * x) * ld + P::row(tile, 4 * g);
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(out) + row) = w;
-        } else {
-            const f32x4 m = *reinterpret_cast<const f32x4*>(xs + at + x * 4);
-            const int ex = delta_exponent(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-            if (tid == 0) a.ex[u * 32 + which * 8 + part * CT + x] = ex;
-            halfx4 h;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = (half_t)ldexpf(w[j], -ex);
-            *reinterpret_cast<halfx4*>(static_cast<half_t*>(out) + row) = h;
-        }
-    };
-
-    const int step = BACK ? -1 : 1;
-    int c = BACK ? NC - 1 : 0;
-    if (NC > 0) {
-        place(c);
-        load_rows(kb, c, K);
-        if (!BACK) load_rows(qb, c, Q);
-        load_numbers(c);
-        load_values(c);
-        load_tri(ga, c, A);
-        load_tri(gm, c, M);
-        load_slice(kb, c, kt[0]);
-        if (BACK) load_slice(qb, c, kt[L::NSL - 1]);
-    }
-    put_state();
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < NC; ++i, c += step) {
-        const int next = i + 1 < NC ? c + step : c;      // (the last chunk's loads are its own again)
-        const size_t u = (size_t)(tile0 + c) * a.V + hv;
-        f32x4 V[CT], ys[CT], os[CT];
 #pragma unroll
         for (int x = 0; x < CT; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) V[x][j] = c * CHUNK + P::row(wv, 4 * g + j) < len ? (float)v[x][j] : 0.f;
-        if (partial(next) != partial(c)) place(next);
-        load_values(next);
-        store_slice(kt[0], slice);
-        if (BACK) {
-            store_slice(kt[L::NSL - 1], slice + L::SLICE);
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {      // dO is an operand as it is
-                if constexpr (sizeof(T) == 4) {
-                    *reinterpret_cast<f32x4*>(smem + L::O + (wv * CT + x) * 1024 + lane * 16) = V[x];
-                } else {
-                    bf16x4 b;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) b[j] = (bf16_t)V[x][j];
-                    *reinterpret_cast<bf16x4*>(smem + L::O + ((wv >> 1) * CT + x) * 1024 + lane * 16 + (wv & 1) * 8) = b;
-                }
-            }
-        }
-        load_slice(kb, next, kt[0]);
-        if (BACK) load_slice(qb, next, kt[L::NSL - 1]);
-        lds_barrier();
+            for (int t = 0; t < TW; ++t) put(all_parts, L::S, TW * wv + t, x, S[t][x]);
+    };
 
-        // K S and Q S of the wave's tokens
-#pragma unroll
-        for (int x = 0; x < CT; ++x) ys[x] = os[x] = zero;
-        {
-            constexpr int HS = NS * NP * CT > 16 ? NS / 2 : NS;      // slabs requested together: up to 64 registers
-#pragma unroll
-            for (int s0 = 0; s0 < NS; s0 += HS) {
-                DeltaParts<T, NP> f[HS][CT];
-#pragma unroll
-                for (int sl = 0; sl < HS; ++sl)
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) f[sl][x] = frag(L::S, s0 + sl, x);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int sl = 0; sl < HS; ++sl)
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) {
-                        DeltaParts<T, 1> k;
-                        k.p[0] = K[s0 + sl];
-                        ys[x] = delta_mma(k, f[sl][x], ys[x]);
-                        if (!BACK) {
-                            k.p[0] = Q[s0 + sl];
-                            os[x] = delta_mma(k, f[sl][x], os[x]);
-                        }
-                    }
-            }
+    const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
+    const void *const ga = BACK ? a.at : a.a, *const gm = BACK ? a.mt : a.m;
+    auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
+    if (chain) {
+        UserFrag K[RS], kt[NK];
+        DeltaParts<C, NP> A[CS];
+        T v[CT][4];
+        f32x4 be, ga4, rh;
+        float g63 = 0.f;
+        if (NC > 0) {
+            load_rows(first, K);
+            be = number(first, 0); ga4 = number(first, 1); rh = number(first, 2);
+            g63 = last_gamma(first);
+            if (!BACK) load_values(first, v);
+            load_tri(ga, first, A);
+            load_slice(first, kt);
         }
-        load_rows(kb, next, K);
-        if (!BACK) load_rows(qb, next, Q);
-        if (MODE != DELTA_O)
+        put_state();
+        if (BACK && NC > 0) { lds_barrier(); lds_barrier(); lds_barrier(); }      // (the other waves' first chunk)
+        for (int i = 0, c = first; i < NC; ++i, c += step) {
+            const int next = after(c);
+            f32x4 V[CT], y[CT];
+            if (!BACK) values(v, V);
+            if (!BACK) load_values(next, v);
+            store_slice(kt);
+            load_slice(next, kt);
+            lds_barrier();
+            times_state(K, y);
+            load_rows(next, K);
+            if (!BACK) {
 #pragma unroll
-            for (int x = 0; x < CT; ++x)
+                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, be * (V[x] - ga4 * y[x]));
+            } else {      // dU = diag(rho) K G + M^T dO
 #pragma unroll
-                for (int t = 0; t < TW; ++t) keep(BACK ? a.gm : a.sm, BACK ? 1 : 0, 0, x, u, D, TW * wv + t, S[t][x]);
-        if (!BACK) {
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {
-                put(L::Y, wv, x, be * (V[x] - ga4 * ys[x]));
-                os[x] = os[x] * (ga4 * a.scale);
+                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, y[x] * rh + *reinterpret_cast<const f32x4*>(smem + L::DU + (wv * CT + x) * 1024 + lane * 16));
             }
             lds_barrier();
-            DeltaParts<T, NP> f[CS][CT];
+            DeltaParts<C, NP> f[CS][CT];
             frags(L::Y, f);
             __builtin_amdgcn_sched_barrier(0);
             f32x4 U[CT];
 #pragma unroll
             for (int x = 0; x < CT; ++x) U[x] = zero;
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl)
-                if (used(sl))
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) U[x] = delta_mma(A[sl], f[sl][x], U[x]);
+            times(A, f, U);
             load_tri(ga, next, A);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
-                put(L::U, wv, x, U[x] * rh);
-                put(L::V, wv, x, U[x]);
+                if (!BACK) {
+                    put(all_parts, L::U, wv, x, U[x] * rh);
+                    put(all_parts, L::V, wv, x, U[x]);
+                } else {      // (U: the gradient's Y)
+                    put(one_part, L::V, wv, x, U[x]);
+                    U[x] = be * U[x];
+                    put(all_parts, L::U, wv, x, -(ga4 * U[x]));
+                }
             }
-            put_most(U);
+            if (BACK) store_values(c, U);
+            be = number(next, 0);
+            ga4 = number(next, 1);
+            rh = number(next, 2);
             lds_barrier();
-            DeltaParts<T, NP> f2[CS][CT];
             frags(L::U, f);
-            frags(L::V, f2);
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TW; ++t)
 #pragma unroll
-                for (int x = 0; x < CT; ++x) S[t][x] = S[t][x] * g63;
-            load_numbers(next);
-            into_state(slice, f);
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl)
-                if (used(sl))
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) os[x] = delta_mma(M[sl], f2[sl][x], os[x]);
-            load_tri(gm, next, M);
-            if (MODE == DELTA_KEEP)
-#pragma unroll
-                for (int x = 0; x < CT; ++x) keep(a.um, 2, 16, x, u, 64, wv, U[x]);
+                for (int x = 0; x < CT; ++x) {
+                    S[t][x] = S[t][x] * g63;
+                    if (BACK) S[t][x] = S[t][x] + *reinterpret_cast<const f32x4*>(smem + L::DG + ((TW * wv + t) * CT + x) * 1024 + lane * 16);
+                }
+            g63 = last_gamma(next);
+            into(S, f);
             put_state();
+        }
+        if (to) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = c * CHUNK + P::row(wv, 4 * g + j);
-                if (r < len)
+            for (int t = 0; t < TW; ++t)
 #pragma unroll
-                    for (int x = 0; x < CT; ++x) *(__attribute__((address_space(1))) T*)(scalar_base(ob + c * vstep, out_at[j]) + 16 * x * ES) = (T)os[x][j];
+                for (int x = 0; x < CT; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] = S[t][x][j] * up[x];
+        }
+    } else if (!BACK) {
+        UserFrag Q[RS];
+        DeltaParts<C, NP> M[CS];
+        f32x4 ga4;
+        if (NC > 0) {
+            load_rows(first, Q);
+            load_tri(gm, first, M);
+            ga4 = number(first, 1);
+        }
+        for (int i = 0, c = first; i < NC; ++i, c += step) {
+            const int next = after(c);
+            const size_t u = (size_t)(tile0 + c) * a.V + hv;
+            f32x4 o[CT];
+            lds_barrier();
+            times_state(Q, o);
+            load_rows(next, Q);
+            if (MODE == DELTA_KEEP) keep(a.sm, L::S, u, NP, NS);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) o[x] = o[x] * (ga4 * a.scale);
+            ga4 = number(next, 1);
+            lds_barrier();
+            lds_barrier();
+            DeltaParts<C, NP> f[CS][CT];
+            frags(L::V, f);
+            __builtin_amdgcn_sched_barrier(0);
+            times(M, f, o);
+            load_tri(gm, next, M);
+            if (MODE == DELTA_KEEP) keep(a.um, L::V, u, NP, CS);
+            store_values(c, o);
+        }
+    } else if (NC > 0) {
+        // Of the chunk that the first four waves come to next: M^T dO and Q^T diag(scale gamma) dO, in fp32.  The first goes out behind the second barrier (they have read
+        // the one before), the second, held back, behind the first barrier of the next round.
+        UserFrag qt[NK];
+        DeltaParts<C, NP> M[CS];
+        T v[CT][4];
+        f32x4 ga4 = number(first, 1), V[CT], du[CT], dg[TW][CT];
+        load_slice(first, qt);
+        load_tri(gm, first, M);
+        load_values(first, v);
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) dg[t][x] = zero;
+        for (int i = -1, c = first; i < NC; ++i) {      // round i: they are at chunk i of theirs, this is the one behind it
+            const int next = after(c);
+            values(v, V);
+            load_values(next, v);
+            store_slice(qt);
+            load_slice(next, qt);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                put(one_part, L::O, wv, x, V[x]);
+                put(all_parts, L::OG, wv, x, V[x] * (ga4 * a.scale));
             }
-        } else {
-            // dU = diag(rho) K G + M^T dO
+            ga4 = number(next, 1);
+            lds_barrier();
 #pragma unroll
-            for (int x = 0; x < CT; ++x) ys[x] = ys[x] * rh;
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int x = 0; x < CT; ++x) *reinterpret_cast<f32x4*>(smem + L::DG + ((TW * wv + t) * CT + x) * 1024 + lane * 16) = dg[t][x];
+            if (i >= 0) keep(a.gm, L::S, (size_t)(tile0 + first + i * step) * a.V + hv, NP, NS);
+            DeltaParts<C, NP> f[CS][CT];
+            frags(L::OG, f);
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int x = 0; x < CT; ++x) dg[t][x] = zero;
+            into(dg, f);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) du[x] = zero;
 #pragma unroll
             for (int sl = 0; sl < CS; ++sl)
                 if (used(sl))
 #pragma unroll
                     for (int x = 0; x < CT; ++x) {
-                        DeltaParts<T, 1> f;
-                        f.p[0] = *reinterpret_cast<const Frag*>(smem + L::O + (sl * CT + x) * 1024 + lane * 16);
-                        ys[x] = delta_mma(M[sl], f, ys[x]);
+                        DeltaParts<C, 1> y;
+                        y.p[0] = frag1(L::O, sl, x, 1);
+                        du[x] = delta_mma(M[sl], y, du[x]);
                     }
             load_tri(gm, next, M);
-#pragma unroll
-            for (int x = 0; x < CT; ++x) put(L::Y, wv, x, ys[x]);
             lds_barrier();
-            DeltaParts<T, NP> f[CS][CT];
-            frags(L::Y, f);
-            __builtin_amdgcn_sched_barrier(0);
-            f32x4 Y[CT];
 #pragma unroll
-            for (int x = 0; x < CT; ++x) Y[x] = zero;
-#pragma unroll
-            for (int sl = 0; sl < CS; ++sl)
-                if (used(sl))
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) Y[x] = delta_mma(A[sl], f[sl][x], Y[x]);
-            load_tri(ga, next, A);
-            put_most(Y);
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {
-                os[x] = be * Y[x];
-                put(L::U, wv, x, -(ga4 * os[x]));
-                put(L::V, wv, x, V[x] * (ga4 * a.scale));
-            }
+            for (int x = 0; x < CT; ++x) *reinterpret_cast<f32x4*>(smem + L::DU + (wv * CT + x) * 1024 + lane * 16) = du[x];
             lds_barrier();
-            DeltaParts<T, NP> f2[CS][CT];
-            frags(L::U, f);
-            frags(L::V, f2);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int t = 0; t < TW; ++t)
-#pragma unroll
-                for (int x = 0; x < CT; ++x) S[t][x] = S[t][x] * g63;
-            load_numbers(next);
-            into_state(slice, f);
-            into_state(slice + L::SLICE, f2);
-#pragma unroll
-            for (int x = 0; x < CT; ++x) keep(a.ym, 3, 16, x, u, 64, wv, Y[x]);
-            put_state();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = c * CHUNK + P::row(wv, 4 * g + j);
-                if (r < len)
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) *(__attribute__((address_space(1))) T*)(scalar_base(ob + c * vstep, out_at[j]) + 16 * x * ES) = (T)os[x][j];
-            }
+            if (i >= 0) keep(a.ym, L::V, (size_t)(tile0 + first + i * step) * a.V + hv, 1, CS);
+            c = next;
         }
-    }
-    if (to) {
-#pragma unroll
-        for (int t = 0; t < TW; ++t)
-#pragma unroll
-            for (int x = 0; x < CT; ++x)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) to[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] = S[t][x][j];
     }
 }
 
@@ -449,7 +467,7 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
     typedef ScanLds<T, D, NP, CT, MODE> L;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, NP, CT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
     if (attr != hipSuccess) return attr;
-    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(D / 16 / CT, a.nseq * a.V)), dim3(256), L::BYTES, stream>>>(a);
+    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(D / 16 / CT, a.nseq * a.V)), dim3(512), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D, int NP, int MODE>
@@ -459,7 +477,7 @@ static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
 template <int D, int MODE>
 static hipError_t launch_np(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
     if (!is_bf16) return launch_ct<float, D, 1, MODE>(a, stream);
-    return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 3 ? launch_ct<bf16_t, D, 3, MODE>(a, stream) : launch_ct<bf16_t, D, 2, MODE>(a, stream);
+    return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 2 ? launch_ct<bf16_t, D, 2, MODE>(a, stream) : launch_ct<bf16_t, D, 1, MODE>(a, stream);
 }
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream) {
     if (d == 64) return mode == DELTA_O ? launch_np<64, DELTA_O>(a, is_bf16, stream) : mode == DELTA_KEEP ? launch_np<64, DELTA_KEEP>(a, is_bf16, stream) : launch_np<64, DELTA_BACK>(a, is_bf16, stream);
