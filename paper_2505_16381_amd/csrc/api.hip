@@ -1150,7 +1150,7 @@ extern "C" path_status_t path_paged_plan(const int* cached, const int* new_token
 
 // ---- gated delta rule ----
 namespace {
-struct DeltaPlan { long long tiles; size_t a, m, rows, vmost, at, mt, sm, gm, um, ym, gmost, vex, gex, total; };
+struct DeltaPlan { long long tiles; size_t p, m, rows, vmost, at, mt, sm, gm, em, ym, gmost, vex, gex, total; };
 }  // namespace
 
 // Launches of fewer than 2^32 threads: 512 per tile and key head, 256 per tile and value head, 1024 per sequence and value head.
@@ -1166,7 +1166,7 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
     size_t off = 0;
     auto take = [&](size_t& field, size_t bytes) { field = off; off = align256(off + bytes); };
     const size_t units = (size_t)p.tiles * V, tri = es == 4 ? 10 * 1024 : 2 * 6 * 1024, half = es == 2;
-    take(p.a, units * tri);
+    take(p.p, units * tri);
     take(p.m, units * tri);
     take(p.rows, units * DELTA_ROWS * 64 * 4);
     take(p.vmost, half * units * 8 * 4);
@@ -1175,7 +1175,7 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
         take(p.mt, units * tri);
         take(p.sm, units * d * d * es);
         take(p.gm, units * d * d * es);
-        take(p.um, units * d * 64 * es);
+        take(p.em, units * d * 64 * es);
         take(p.ym, units * d * 64 * es);
         take(p.gmost, half * units * 8 * 4);
         take(p.vex, half * nseq * V * 8 * 4);
@@ -1213,9 +1213,9 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
         a.ss = L * V; a.st = V; a.sh = 1;
     }
     char* const ws = static_cast<char*>(workspace);
-    a.a = ws + p.a; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
+    a.p = ws + p.p; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
     a.at = ws + p.at; a.mt = ws + p.mt;
-    a.sm = ws + p.sm; a.gm = ws + p.gm; a.um = ws + p.um; a.ym = ws + p.ym;
+    a.sm = ws + p.sm; a.gm = ws + p.gm; a.em = ws + p.em; a.ym = ws + p.ym;
     a.vmost = reinterpret_cast<float*>(ws + p.vmost); a.gmost = reinterpret_cast<float*>(ws + p.gmost);
     a.vex = reinterpret_cast<int*>(ws + p.vex); a.gex = reinterpret_cast<int*>(ws + p.gex);
     a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 2 : 1;      // (delta_parts.h)

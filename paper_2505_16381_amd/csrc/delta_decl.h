@@ -4,14 +4,14 @@
 //   S' = f_t S,  u_t = beta_t (v_t - S'^T k_t),  S = S' + k_t u_t^T,  o_t = scale S^T q_t,   f_t = exp(log_f_t).
 // By chunks of 64 tokens, b the running sums of log f inside the chunk, gamma = exp(b), rho_i = exp(b_63 - b_i), D_ri = exp(b_r - b_i) for i <= r (every
 // exponent that is formed is that of a difference, at most 0 for gates that forget):
-//   L = strictLower(D o K K^T),  M = scale lower(D o Q K^T),  A = (I + diag(beta) L)^-1                       (delta_prep.hip, all chunks at once)
-//   U = A diag(beta) (V - diag(gamma) K S),  O = scale diag(gamma) Q S + M U,  S <- gamma_63 S + K^T diag(rho) U          (delta_scan.hip, chunk after chunk)
+//   L = strictLower(D o K K^T),  M = scale lower(D o Q K^T),  P = (I + L diag(beta))^-1,  A = (I + diag(beta) L)^-1 = I - diag(beta) P L        (delta_prep.hip, all chunks at once)
+//   E = P (V - diag(gamma) K S),  U = diag(beta) E,  O = scale diag(gamma) Q S + M U,  S <- gamma_63 S + K^T diag(rho) U          (delta_scan.hip, chunk after chunk)
 // and the gradients, G that of the state behind the chunk:
 //   dU = M^T dO + diag(rho) K G,  Y = A^T dU,  dV = diag(beta) Y,  G <- gamma_63 G + Q^T diag(scale gamma) dO - K^T diag(gamma beta) Y     (delta_scan.hip, backwards)
-//   X = Y U^T,  N = dO U^T,  Gq = scale lower(N o D),  Gk = -strictLower(diag(beta) X o D)
+//   dbeta_r = Y_r.E_r,  X = Y U^T,  N = dO U^T,  Gq = scale lower(N o D),  Gk = -strictLower(diag(beta) X o D)
 //   dQ = Gq K + scale diag(gamma) dO S^T,   dK = Gk K - diag(gamma beta) Y S^T  +  Gk^T K + Gq^T Q + diag(rho) U G^T     ("read" and "written" part)
-//   dbeta_r = Y_r.v_r - gamma_r (Y S^T)_r.k_r - sum_i X_ri L_ri
 //   dlog_f_t = sum_{r >= t} (q_r.dq_r + k_r.dk_r(read) - k_r.dk_r(written)) + gamma_63 <S, G> + sum_i rho_i k_i.(U G^T)_i                      (delta_grad.hip)
+// (E: what a token's prediction is off.  U = A diag(beta) (..) is the same, but leaves no E, which dbeta needs, where beta is 0.)
 #pragma once
 #include "path_common.h"
 
@@ -35,12 +35,12 @@ struct DeltaArgs {
     float scale;
     int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
     float *vmost, *gmost;                      // per (tile, head) [8]: largest finite |v|, |d_o| of the chunk, of each 16 value indices
-    void *a, *m, *at, *mt;                     // per (tile, head): A and M as operand fragments, and their transposes (training)
+    void *p, *m, *at, *mt;                     // per (tile, head): P and M as operand fragments; training: the transposes of A and M
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
-    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], U and Y, [value index][token]: fp32, or fp16 over
+    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], E and Y, [value index][token]: fp32, or fp16 over
     // the powers of two that the scans chose, per (sequence, head) and 16 value indices
-    void *sm, *gm, *um, *ym;
-    int *vex, *gex;                            // [nseq * V][8]: of S and U, of G and Y
+    void *sm, *gm, *em, *ym;
+    int *vex, *gex;                            // [nseq * V][8]: of S and E, of G and Y
     const void* d_o;
     const float* d_state;                      // gradient of the last states; NULL: zeros
     void *dq, *dk, *dv, *dbeta, *dlog_f;

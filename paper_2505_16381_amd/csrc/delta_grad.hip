@@ -1,6 +1,7 @@
 // Gated delta rule: gradients of q, k, beta and log f from the states, their gradients, U and Y of a chunk, all chunks at once (delta_decl.h has the formulas).
 // A workgroup takes a chunk of a key head and adds up its value heads one after the other, in registers.
 #include "delta_parts.h"
+#include "lds_tile.h"
 
 namespace path {
 
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
         const size_t u = (size_t)tile * a.V + hv;
         const long long vat = delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, sat = delta_at(a, sq, s, a.ss, a.st) + hv * a.sh + t0 * a.st;
         const float *const S = static_cast<const float*>(a.sm) + u * D * D, *const G = static_cast<const float*>(a.gm) + u * D * D;
-        const float *const U = static_cast<const float*>(a.um) + u * D * 64, *const Y = static_cast<const float*>(a.ym) + u * D * 64;
+        const float *const E = static_cast<const float*>(a.em) + u * D * 64, *const Y = static_cast<const float*>(a.ym) + u * D * 64;
         __syncthreads();
         fill(O, static_cast<const float*>(a.d_o) + vat, a.vt);
         for (int i = tid; i < DELTA_ROWS * 64; i += 256) rows[i] = a.rows[u * DELTA_ROWS * 64 + i];
@@ -66,14 +67,13 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
         }
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) {
-            f32x4 X = zero, N = zero, KK = zero;
+            f32x4 X = zero, N = zero;
             if (ib <= wv)
 #pragma unroll 1
                 for (int z = 0; z < D; z += 16) {
-                    const f32x4 uf = tr(U, 64, 16 * ib, z);
+                    const f32x4 uf = tr(E, 64, 16 * ib, z) * rows[16 * ib + n];
                     X = P::mma(tr(Y, 64, r0, z), uf, X);
                     N = P::mma(nat(O, LD, r0, z), uf, N);
-                    KK = P::mma(nat(K, LD, r0, z), nat(K, LD, 16 * ib, z), KK);
                 }
             const int i = 16 * ib + n;
             const float ih = rows[192 + i], il = rows[256 + i];
@@ -83,17 +83,13 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
                 const float w = expf((bh[j] - ih) + (bl[j] - il));
                 Gq[r * DG_LF + i] = i <= r ? a.scale * w * N[j] : 0.f;
                 Gk[r * DG_LF + i] = i < r ? -be[j] * w * X[j] : 0.f;
-                if (i < r) db[j] -= X[j] * w * KK[j];
             }
         }
-        // Y.v, value indices n, n + 16, ..
-        const float* const vp = static_cast<const float*>(a.v) + vat;
+        // Y.E, value indices n, n + 16, ..
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = r0 + 4 * g + j;
-            if (r < left)
-                for (int z = n; z < D; z += 16) db[j] += Y[z * 64 + r] * vp[r * a.vt + z];
-        }
+        for (int j = 0; j < 4; ++j)
+#pragma unroll 1
+            for (int z = n; z < D; z += 16) db[j] += Y[z * 64 + r0 + 4 * g + j] * E[z * 64 + r0 + 4 * g + j];
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
@@ -103,7 +99,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
                 const f32x4 sf = tr(S, D, 16 * t, z);
                 ys = P::mma(tr(Y, 64, r0, z), sf, ys);
                 os = P::mma(nat(O, LD, r0, z), sf, os);
-                ug = P::mma(tr(U, 64, r0, z), tr(G, D, 16 * t, z), ug);
+                ug = P::mma(tr(E, 64, r0, z) * rows[r0 + n], tr(G, D, 16 * t, z), ug);
             }
 #pragma unroll 1
             for (int z = 0; z < 64; z += 16) {
@@ -118,7 +114,6 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
                 const int r = r0 + 4 * g + j;
                 const float kv = K[r * LD + 16 * t + n], qv = Q[r * LD + 16 * t + n];
                 const float dqv = q1[j] + a.scale * ga[j] * os[j], rdv = rd[j] - ga[j] * be[j] * ys[j], u4 = rh[j] * ug[j], wrv = wr[j] + u4;
-                db[j] -= ga[j] * ys[j] * kv;
                 dl[j] += qv * dqv + kv * (rdv - wrv);
                 kug += kv * u4;
                 dq[t][j] += dqv;
@@ -163,10 +158,11 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
         }
 }
 
-// ---- bf16: 32x32 products of fp16 operands, each matrix over a power of two of its own ----
+// ---- bf16: 32x32 products of fp16 operands of one part, over the powers of two of the scans ----
 //
-// Operands of one part: the states, U, Y and dO with the exponents of their largest values taken out (numbers down to 2^-24 of those keep eleven bits), so that gradients of any
-// size are as exact: results come out 2e-4 (of their norm) off before they are rounded to bf16, 2e-3.  bf16 operands of one part: dk 2.5e-3, dlog_f 2.2e-3 off.
+// A wave has 32 key indices of dq and dk, of all 64 tokens (d = 64: of 32).  E (as U), Y and dO are in LDS for everybody; the wave's columns of S, G, K and Q pass through
+// 4 KB of its own, half a state at a time, the next piece on its way in registers meanwhile: no barrier from the first product to the last but the two around Gq and Gk, and two
+// workgroups on a CU.  Factors of a token (gamma, beta, rho) are multiplied into the operand whose rows the tokens are.
 
 // sums over the 32 lanes of a half-wave of each of 16 values; lane l32 gets the value l32 / 2
 __device__ __forceinline__ float sum16(float (&v)[16], int l32) {
@@ -184,268 +180,336 @@ __device__ __forceinline__ float sum16(float (&v)[16], int l32) {
 __device__ __forceinline__ half_t half_power(int e) { return e < -24 ? (half_t)0.f : (half_t)ldexpf(1.f, e); }
 
 template <int D> struct Grad16 {
-    static constexpr int NT = 4 * D, NWV = NT / 64, LD = D + 8, LU = 72, CB = D / 32;
-    static constexpr int K = 0, Q = K + 64 * LD, O = Q + 64 * LD, U = O + 64 * LD, Y = U + D * LU, S = Y + D * LU, GQ = S + D * LD, GK = GQ + 64 * LU, HALVES = GK + 64 * LU;
-    static constexpr size_t bytes = (size_t)HALVES * 2 + (DELTA_ROWS * 64 + 32 + 64 * (2 * CB + 2 + NWV)) * 4;
+    static constexpr int RB = D / 64, CB = D / 32;                     // blocks of 32 tokens of a wave, of 32 key indices of a head
+    static constexpr int TOK = 64 * D * 2, G2 = 64 * 64 * 2;            // bytes of a tokens' matrix, of Gq
+    static constexpr int U = 0, Y = TOK, O = 2 * TOK, SLOT = O + (TOK > 2 * G2 ? TOK : 2 * G2), ROWS = SLOT + 4 * 4096, RED = ROWS + DELTA_ROWS * 256;
+    static constexpr int BYTES = RED + (4 * 64 + CB * 64 + 16) * 4;
 };
 
-template <int D>
-__global__ __launch_bounds__(Grad16<D>::NT, 1) void delta_grad16_kernel(DeltaArgs a) {
+template <int D, bool GROUP>
+__global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     typedef Grad16<D> C;
-    constexpr int NT = C::NT, LD = C::LD, LU = C::LU, CB = C::CB, NWV = C::NWV;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    half_t* const H = reinterpret_cast<half_t*>(smem);
-    half_t *const K = H + C::K, *const Q = H + C::Q, *const O = H + C::O, *const U = H + C::U, *const Y = H + C::Y, *const S = H + C::S, *const Gq = H + C::GQ, *const Gk = H + C::GK;
-    float* const rows = reinterpret_cast<float*>(H + C::HALVES);
-    float *const wred = rows + DELTA_ROWS * 64;      // [2][16] of the waves
-    float *const kys = wred + 32, *const dls = kys + 64 * CB, *const xl = dls + 64 * CB, *const yv = xl + 128;      // [column block][64], the same, [2][64], [wave][64]
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    typedef TurnedLane<64> Lane;      // of U, Y, Gq, Gk
+    constexpr int RB = C::RB, CB = C::CB, NP = 64 * D / 8 / 256;      // 16-byte pieces of a tokens' matrix per thread
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    float* const rows = reinterpret_cast<float*>(smem + C::ROWS);
+    float *const dbs = reinterpret_cast<float*>(smem + C::RED), *const dls = dbs + 256, *const kus = dls + CB * 64;      // [wave][64], [column block][64], [wave]
+    int tid = threadIdx.x, lane = tid & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.H), hk = blockIdx.x - tile * a.H;
     int s, c;
     DeltaSeq sq;
     if (!delta_tile(a, tile, lane, s, c, sq)) return;
     const int t0 = c * CHUNK, left = sq.len - t0;
+    const int cb = wv % CB, rb0 = RB == 2 ? 0 : wv / CB;      // the wave's column block, its first block of tokens
     const long long kat = delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh + t0 * a.kt;
-    constexpr int PPR = D / 8, NP = 64 * PPR / NT, NU = D * 8 / NT, NS = D * PPR / NT;      // pieces of 8 in a row; of a thread: tokens' matrices, U and Y, states
-    auto rows_in = [&](const void* base, long long ld, int i) {      // piece i of the thread of a tokens' matrix
-        const int p = tid + i * NT, r = p / PPR, x = p % PPR * 8;
-        bf16x8 f;
+    const bf16_t *const kp = static_cast<const bf16_t*>(a.k) + kat + 32 * cb, *const qp = static_cast<const bf16_t*>(a.q) + kat + 32 * cb;
+    half_t* const slot = reinterpret_cast<half_t*>(smem + C::SLOT + wv * 4096);      // [64][32]
+    f32x16 dq[RB], dk[RB];
+    if (GROUP)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (bf16_t)0.f;
-        if (r < left) f = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(base) + r * ld + x);
-        return f;
+        for (int b = 0; b < RB; ++b) dq[b] = dk[b] = zero16();
+    // the wave's 32 columns of 64 rows: 16 bytes a lane, rows lane / 4 + 16 i
+    auto slice_rows = [&](const half_t* x, halfx8 (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + (size_t)(lane / 4 + 16 * i) * D + lane % 4 * 8);
     };
-    auto put = [&](half_t* to, const bf16x8& f, int i, float w) {
-        const int p = tid + i * NT, r = p / PPR, x = p % PPR * 8;
-        halfx8 y;
+    auto slice_tokens = [&](const bf16_t* x, float w, halfx8 (&f)[4]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (half_t)((float)f[e] * w);
-        *reinterpret_cast<halfx8*>(to + r * LD + x) = y;
+        for (int i = 0; i < 4; ++i) {
+            const int r = lane / 4 + 16 * i;
+            bf16x8 y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = (bf16_t)0.f;
+            if (r < left) y = *reinterpret_cast<const bf16x8*>(x + r * a.kt + lane % 4 * 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = (half_t)((float)y[e] * w);
+        }
     };
+    auto to_slot = [&](const halfx8 (&f)[4]) {
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        put(K, rows_in(static_cast<const bf16_t*>(a.k) + kat, a.kt, i), i, 1.f);
-        put(Q, rows_in(static_cast<const bf16_t*>(a.q) + kat, a.kt, i), i, 1.f);
-    }
-    const int rb = wv / CB, cb = wv % CB;      // the wave's 32 tokens and 32 key indices of dq, dk
-    f32x16 dq = zero16(), dk = zero16();
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<halfx8*>(slot + (lane / 4 + 16 * i) * 32 + lane % 4 * 8) = f[i];
+        __builtin_amdgcn_wave_barrier();
+    };
 #pragma unroll 1
-    for (int x = 0; x < a.G; ++x) {
+    for (int x = 0; x < (GROUP ? a.G : 1); ++x) {
         const int hv = hk * a.G + x;
-        // (the lane's place, made anew: LDS addresses of all products kept across the loop over heads would not fit the registers)
-        int l32 = lane & 31, h = lane >> 5;
-        asm volatile("" : "+v"(l32), "+v"(h));
+        // (the lane's place, made anew: addresses of all products kept across the loop over heads would not fit the registers)
+        if (GROUP) asm volatile("" : "+v"(tid), "+v"(lane));
+        const int l32 = lane & 31, h = lane >> 5;
         const size_t u = (size_t)tile * a.V + hv;
         const long long vat = delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, sat = delta_at(a, sq, s, a.ss, a.st) + hv * a.sh + t0 * a.st;
-        const half_t *const sg = static_cast<const half_t*>(a.sm) + u * D * D, *const gg = static_cast<const half_t*>(a.gm) + u * D * D;
-        const half_t *const ug = static_cast<const half_t*>(a.um) + u * D * 64, *const yg = static_cast<const half_t*>(a.ym) + u * D * 64;
-        bf16x8 of[NP];
-        halfx8 sf[NS], gf[NS], uf[NU], yf[NU];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) of[i] = rows_in(static_cast<const bf16_t*>(a.d_o) + vat, a.vt, i);
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            uf[i] = *reinterpret_cast<const halfx8*>(ug + (tid + i * NT) * 8);
-            yf[i] = *reinterpret_cast<const halfx8*>(yg + (tid + i * NT) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            sf[i] = *reinterpret_cast<const halfx8*>(sg + (tid + i * NT) * 8);
-            gf[i] = *reinterpret_cast<const halfx8*>(gg + (tid + i * NT) * 8);
-        }
+        const half_t *const sg = static_cast<const half_t*>(a.sm) + u * D * D + 32 * cb, *const gg = static_cast<const half_t*>(a.gm) + u * D * D + 32 * cb;
+        const half_t *const eg = static_cast<const half_t*>(a.em) + u * D * 64, *const yg = static_cast<const half_t*>(a.ym) + u * D * 64;
         const int *const vex = a.vex + ((size_t)s * a.V + hv) * 8, *const gex = a.gex + ((size_t)s * a.V + hv) * 8;
-        int ev = vex[0], eg = gex[0];      // the largest exponents: of S and U, of G, Y and dO
+        int ev = vex[0], eq = gex[0];      // the largest exponents: of S and E, of G, Y and dO
 #pragma unroll
         for (int b = 1; b < D / 16; ++b) {
             ev = vex[b] > ev ? vex[b] : ev;
-            eg = gex[b] > eg ? gex[b] : eg;
+            eq = gex[b] > eq ? gex[b] : eq;
         }
         __syncthreads();      // (the head before has been read out)
-        for (int i = tid; i < DELTA_ROWS * 64; i += NT) rows[i] = a.rows[u * DELTA_ROWS * 64 + i];
+        {
+            halfx8 ef[NP], yf[NP];
+            bf16x8 of[NP];
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int p = tid + i * NT, r = p >> 3, y = (p & 7) * 8;
-            const half_t wu = half_power(vex[r >> 4] - ev), wy = half_power(gex[r >> 4] - eg);
-            *reinterpret_cast<halfx8*>(U + r * LU + y) = uf[i] * wu;
-            *reinterpret_cast<halfx8*>(Y + r * LU + y) = yf[i] * wy;
+            for (int i = 0; i < NP; ++i) {
+                const int p = tid + i * 256, r = p / (D / 8);
+                ef[i] = *reinterpret_cast<const halfx8*>(eg + p * 8);
+                yf[i] = *reinterpret_cast<const halfx8*>(yg + p * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) of[i][e] = (bf16_t)0.f;
+                if (r < left) of[i] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.d_o) + vat + r * a.vt + p % (D / 8) * 8);
+            }
+            const f32x4 b0 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8), b1 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8 + 4);
+            halfx8 be;      // of the eight tokens of the thread's pieces
+#pragma unroll
+            for (int e = 0; e < 8; ++e) be[e] = (half_t)(e < 4 ? b0[e & 3] : b1[e & 3]);
+            for (int i = tid; i < DELTA_ROWS * 64; i += 256) rows[i] = a.rows[u * DELTA_ROWS * 64 + i];
+            const float wo = delta_power(-eq);
+            float db[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int p = tid + i * 256, r = p >> 3, y = (p & 7) * 8, ro = p / (D / 8), xo = p % (D / 8) * 8;
+                const halfx8 e1 = ef[i] * half_power(vex[r >> 4] - ev), y1 = yf[i] * half_power(gex[r >> 4] - eq);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) db[e] += (float)e1[e] * (float)y1[e];
+                *reinterpret_cast<halfx8*>(smem + C::U + 2 * TurnedTile<64>::at(r, y)) = e1 * be;
+                *reinterpret_cast<halfx8*>(smem + C::Y + 2 * TurnedTile<64>::at(r, y)) = y1;
+                halfx8 o1;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o1[e] = (half_t)((float)of[i][e] * wo);
+                *reinterpret_cast<halfx8*>(smem + C::O + 2 * TurnedTile<D>::at(ro, xo)) = o1;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int z = 8; z < 64; z *= 2) db[e] += __shfl_xor(db[e], z);
+            if (lane < 8)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dbs[wv * 64 + lane * 8 + e] = db[e];
         }
-        float sum = 0.f;      // <S, G>, over 2^(ev + eg)
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int p = tid + i * NT, r = p / PPR, y = p % PPR * 8;
-            sf[i] = sf[i] * half_power(vex[r >> 4] - ev);
-            gf[i] = gf[i] * half_power(gex[r >> 4] - eg);
-            *reinterpret_cast<halfx8*>(S + r * LD + y) = sf[i];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)sf[i][e] * (float)gf[i][e];
-        }
-        const float wo = delta_power(-eg);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) put(O, of[i], i, wo);
+        halfx8 sf[4], gf[4];
+        slice_rows(sg, sf);
+        slice_rows(gg, gf);
         __syncthreads();
 
-        // X, N, K K^T of the lower 32x32 blocks -> Gk, Gq, sum_i X_ri L_ri
+        const Lane at(lane);
+        const TurnedLane<D> ato(lane);
+        auto u_frag = [&](int mat, int b, int sl) {      // tokens 32 b .. along the lanes, value indices 16 sl .. as the contraction
+            typedef short v4s __attribute__((ext_vector_type(4)));
+            union { v4s v[2]; halfx8 f; } w;
+            w.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(smem + mat + at.tr_at(16 * sl, 32 * b, 0)));
+            w.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(smem + mat + at.tr_at(16 * sl, 32 * b, 1)));
+            return w.f;
+        };
+        auto o_frag = [&](int b, int sl) { return *reinterpret_cast<const halfx8*>(smem + C::O + ato.nat_at(32 * b, 16 * sl)); };
+        auto slot_frag = [&](int sl) { return ld_frag_tr<half_t>(slot, 32, 16 * sl, 0, l32, h); };
+        f32x16 q1[RB], rd[RB], wr[RB];
+        float sum = 0.f;      // <S, G>, over 2^(ev + eq)
+        {
+            half_t wg[RB], wy[RB], wu[RB];      // of the lane's tokens
+            float bt[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int r = 32 * (rb0 + b) + l32;
+                bt[b] = rows[r];
+                wg[b] = (half_t)rows[64 + r];
+                wy[b] = (half_t)(-rows[64 + r] * rows[r]);
+                wu[b] = (half_t)rows[128 + r];
+                q1[b] = rd[b] = wr[b] = zero16();
+            }
+            const float wdv = delta_power(eq);
+            bf16_t* const dvp = static_cast<bf16_t*>(a.dv) + vat;
 #pragma unroll 1
-        for (int job = wv; job < 6; job += NWV) {
-            const int b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
-            f32x16 acc = zero16();
-            if (job < 3) {
-                mm<half_t, D, true, true>(acc, Y, LU, 32 * br, U, LU, 32 * bi, l32, h);
-                __builtin_amdgcn_sched_barrier(0);
-                f32x16 kk = zero16();
-                mm<half_t, D, false, false>(kk, K, LD, 32 * br, K, LD, 32 * bi, l32, h);
-                float part[16];
+            for (int half = 0; half < D / 64; ++half) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 64 * half + lane / 4 + 16 * i;
+                    sf[i] = sf[i] * half_power(vex[r >> 4] - ev);
+                    gf[i] = gf[i] * half_power(gex[r >> 4] - eq);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += (float)sf[i][e] * (float)gf[i][e];
+                }
+                to_slot(sf);
+                if (half + 1 < D / 64) slice_rows(sg + (size_t)64 * D, sf);
+#pragma unroll
+                for (int sl = 0; sl < 4; ++sl) {
+                    const halfx8 f = slot_frag(sl);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        const halfx8 y = u_frag(C::Y, rb0 + b, 4 * half + sl);
+                        q1[b] = Tr<half_t>::mma(o_frag(rb0 + b, 4 * half + sl) * wg[b], f, q1[b]);
+                        rd[b] = Tr<half_t>::mma(y * wy[b], f, rd[b]);
+                        if ((RB == 2 ? sl : sl & 1) == cb) {      // dv = beta Y: 8 value indices of the lane's token; the waves take turns
+                            const int r = 32 * (rb0 + b) + l32;
+                            bf16x8 v;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = (bf16_t)((float)y[e] * (bt[b] * wdv));
+                            if (r < left) *reinterpret_cast<bf16x8*>(dvp + r * a.vt + 16 * (4 * half + sl) + 8 * h) = v;
+                        }
+                    }
+                }
+                to_slot(gf);
+                if (half + 1 < D / 64) slice_rows(gg + (size_t)64 * D, gf);
+#pragma unroll
+                for (int sl = 0; sl < 4; ++sl) {
+                    const halfx8 f = slot_frag(sl);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) wr[b] = Tr<half_t>::mma(u_frag(C::U, rb0 + b, 4 * half + sl) * wu[b], f, wr[b]);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        halfx8 kf[4];
+        slice_tokens(kp, 1.f, kf);
+        // X and N of the lower 32x32 blocks
+        halfx8 res[2][2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
+            if (job < 6) {
+                f32x16 acc = zero16();
+#pragma unroll
+                for (int sl = 0; sl < D / 16; ++sl) {
+                    const halfx8 f = u_frag(C::U, bi, sl);
+                    acc = Tr<half_t>::mma(job < 3 ? u_frag(C::Y, br, sl) : o_frag(br, sl), f, acc);
+                }
                 const int i = 32 * bi + l32;
                 const float ih = rows[192 + i], il = rows[256 + i];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int r = 32 * br + acc_row(j, h);
-                    const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il));
-                    const bool in = i < r;
-                    part[j] = in ? acc[j] * w * kk[j] : 0.f;
-                    Gk[r * LU + i] = (half_t)(in ? -rows[r] * w * acc[j] * 0x1p-12f : 0.f);
-                }
-                if (b == 1)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) Gk[acc_row(j, h) * LU + 32 + l32] = (half_t)0.f;
-                const float y = sum16(part, l32);
-                if (!(l32 & 1)) xl[bi * 64 + 32 * br + acc_row(l32 >> 1, h)] = y;
-                if (b == 0 && lane < 32) xl[64 + lane] = 0.f;
-            } else {
-                mm<half_t, D, false, true>(acc, O, LD, 32 * br, U, LU, 32 * bi, l32, h);
-                const int i = 32 * bi + l32;
-                const float ih = rows[192 + i], il = rows[256 + i];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int r = 32 * br + acc_row(j, h);
-                    const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il));
-                    Gq[r * LU + i] = (half_t)(i <= r ? w * acc[j] * 0x1p-12f : 0.f);
-                }
-                if (b == 1)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) Gq[acc_row(j, h) * LU + 32 + l32] = (half_t)0.f;
-            }
-        }
-        {      // Y.v of token `lane`, the wave's share of the value indices
-            float y = 0.f;
-            if (lane < left) {
-                constexpr int W = D / NWV;
-                const bf16_t* const vp = static_cast<const bf16_t*>(a.v) + vat + lane * a.vt + wv * W;
-#pragma unroll
-                for (int z = 0; z < W; z += 8) {
-                    const bf16x8 f = *reinterpret_cast<const bf16x8*>(vp + z);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y += (float)f[e] * (float)Y[(wv * W + z + e) * LU + lane];
+                    const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il)) * 0x1p-12f;      // (sums of 128 products stay far from fp16's end)
+                    const float y = job < 3 ? (i < r ? -rows[r] * w * acc[j] : 0.f) : (i <= r ? w * acc[j] : 0.f);
+                    res[n][j / 8][j % 8] = (half_t)y;
                 }
             }
-            yv[wv * 64 + lane] = y;
         }
-        f32x16 ys = zero16(), os = zero16();
+        __syncthreads();      // (dO has been read: Gq and Gk take its place)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
+            if (job < 6) {
+                half_t* const to = reinterpret_cast<half_t*>(smem + C::O + (job < 3 ? C::G2 : 0));
+#pragma unroll
+                for (int j = 0; j < 16; ++j) to[TurnedTile<64>::at(32 * br + acc_row(j, h), 32 * bi + l32)] = res[n][j / 8][j % 8];
+                if (b == 1)      // the upper block
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) to[TurnedTile<64>::at(acc_row(j, h), 32 + l32)] = (half_t)0.f;
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
-        mm<half_t, D, true, true>(ys, Y, LU, 32 * rb, S, LD, 32 * cb, l32, h);
-        __builtin_amdgcn_sched_barrier(0);
-        mm<half_t, D, false, true>(os, O, LD, 32 * rb, S, LD, 32 * cb, l32, h);
+        to_slot(kf);
+        halfx8 qf[4];
+        slice_tokens(qp, a.scale, qf);
         __syncthreads();
+        const float up = ldexpf(1.f, ev + eq), up12 = up * 4096.f;      // of every product of two of them, of Gq and Gk, which are 2^12 below theirs
+        auto nat = [&](int mat, int b, int sl) { return *reinterpret_cast<const halfx8*>(smem + mat + at.nat_at(32 * b, 16 * sl)); };
+        float kug = 0.f;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int p = tid + i * NT, r = p / PPR, y = p % PPR * 8;
-            *reinterpret_cast<halfx8*>(S + r * LD + y) = gf[i];
-        }
-        __syncthreads();
-        __builtin_amdgcn_sched_barrier(0);
-        const float up = ldexpf(1.f, ev + eg);      // of every product of two of them
-        const float up12 = up * 4096.f;              // ... of Gq and Gk, which are 2^12 below theirs: sums of 128 products stay far from fp16's end
-        asm volatile("" : "+v"(l32), "+v"(h));
-        // one product after the other, so that no more than three are held beside dq and dk
-        float pk[16], pl[16], kug = 0.f;
-        const half_t *const kz = K + (32 * rb + 4 * h) * LD + 32 * cb + l32, *const qz = Q + (32 * rb + 4 * h) * LD + 32 * cb + l32;
-        const float* const rz = rows + 32 * rb + 4 * h;
-        auto row = [](int j) { return acc_row(j, 0); };
-        f32x16 acc = zero16();
-        mm<half_t, 64, false, true>(acc, Gq, LU, 32 * rb, K, LD, 32 * cb, l32, h);
+        for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = a.scale * (acc[j] * up12 + rz[64 + row(j)] * os[j] * up);
-            dq[j] += v;
-            pl[j] = (float)qz[row(j) * LD] * v;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        acc = zero16();
-        mm<half_t, 64, false, true>(acc, Gk, LU, 32 * rb, K, LD, 32 * cb, l32, h);
+            for (int j = 0; j < 16; ++j) {
+                kug += (float)slot[(32 * (rb0 + b) + acc_row(j, h)) * 32 + l32] * wr[b][j];
+                q1[b][j] *= 0x1p-12f;
+                rd[b][j] *= 0x1p-12f;
+                wr[b][j] *= 0x1p-12f;
+            }
+        kug = (kug + (rb0 == 0 ? rows[64 + 63] * sum : 0.f)) * up;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float kv = (float)kz[row(j) * LD], y = rz[64 + row(j)] * ys[j] * up, v = acc[j] * up12 - rz[row(j)] * y;
-            pk[j] = kv * y;
-            pl[j] += kv * v;
-            dk[j] += v;
+        for (int sl = 0; sl < 4; ++sl) {
+            const halfx8 f = slot_frag(sl);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int br = rb0 + b;
+                // (Gq and Gk are lower triangular: 32 tokens are before or behind the others)
+                if (br == 1 || sl < 2) {
+                    q1[b] = Tr<half_t>::mma(nat(C::O, br, sl), f, q1[b]);
+                    rd[b] = Tr<half_t>::mma(nat(C::O + C::G2, br, sl), f, rd[b]);
+                }
+                if (br == 0 || sl >= 2) wr[b] = Tr<half_t>::mma(u_frag(C::O + C::G2, br, sl), f, wr[b]);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
-        acc = zero16();
-        mm<half_t, D, true, true>(acc, U, LU, 32 * rb, S, LD, 32 * cb, l32, h);
+        // k.dk before Q takes K's place; then q.dq
+        halfx8 kl[RB][2];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = rz[128 + row(j)] * acc[j] * up, kv = (float)kz[row(j) * LD];
-            kug += kv * v;
-            pl[j] -= kv * v;
-            dk[j] += v;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        acc = zero16();
-        mm<half_t, 64, true, true>(acc, Gk, LU, 32 * rb, K, LD, 32 * cb, l32, h);
-        os = zero16();
-        mm<half_t, 64, true, true>(os, Gq, LU, 32 * rb, Q, LD, 32 * cb, l32, h);
+        for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = (acc[j] + a.scale * os[j]) * up12;
-            pl[j] -= (float)kz[row(j) * LD] * v;
-            dk[j] += v;
+            for (int j = 0; j < 16; ++j) kl[b][j / 8][j % 8] = slot[(32 * (rb0 + b) + acc_row(j, h)) * 32 + l32];
+        to_slot(qf);
+#pragma unroll
+        for (int sl = 0; sl < 4; ++sl) {
+            const halfx8 f = slot_frag(sl);
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+                if (rb0 + b == 0 || sl >= 2) wr[b] = Tr<half_t>::mma(u_frag(C::O, rb0 + b, sl), f, wr[b]);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        kug += rows[64 + 63] * sum * up;
-        const float pks = sum16(pk, l32), pls = sum16(pl, l32);
-        if (!(l32 & 1)) {
-            kys[cb * 64 + 32 * rb + acc_row(l32 >> 1, h)] = pks;
-            dls[cb * 64 + 32 * rb + acc_row(l32 >> 1, h)] = pls;
+        bf16_t *const dqp = static_cast<bf16_t*>(a.dq) + kat + 32 * cb + l32, *const dkp = static_cast<bf16_t*>(a.dk) + kat + 32 * cb + l32;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            float pl[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int r = 32 * (rb0 + b) + acc_row(j, h);
+                const float d1 = q1[b][j] * up12, d2 = rd[b][j] * up12, d3 = wr[b][j] * up12;      // (dq without scale: so is Q with it)
+                pl[j] = (float)slot[r * 32 + l32] * d1 + (float)kl[b][j / 8][j % 8] * (d2 - d3);
+                if (GROUP) {
+                    dq[b][j] += a.scale * d1;
+                    dk[b][j] += d2 + d3;
+                } else if (r < left) {
+                    dqp[r * a.kt] = (bf16_t)(a.scale * d1);
+                    dkp[r * a.kt] = (bf16_t)(d2 + d3);
+                }
+            }
+            const float y = sum16(pl, l32);
+            if (!(l32 & 1)) dls[cb * 64 + 32 * (rb0 + b) + acc_row(l32 >> 1, h)] = y;
         }
 #pragma unroll
         for (int z = 1; z < 64; z *= 2) kug += __shfl_xor(kug, z);
-        if (lane == 0) wred[16 + wv] = kug;
+        if (lane == 0) kus[wv] = kug;
         __syncthreads();
         if (wv == 0) {
-            float l = 0.f, ky = 0.f, y = 0.f, all = 0.f;
+            float l = 0.f;
 #pragma unroll
-            for (int i = 0; i < CB; ++i) { l += dls[i * 64 + lane]; ky += kys[i * 64 + lane]; }
-#pragma unroll
-            for (int i = 0; i < NWV; ++i) { y += yv[i * 64 + lane]; all += wred[16 + i]; }
+            for (int i = 0; i < CB; ++i) l += dls[i * 64 + lane];
 #pragma unroll
             for (int z = 1; z < 64; z *= 2) {
-                const float t = __shfl_down(l, z);
-                if (lane + z < 64) l += t;
+                const float y = __shfl_down(l, z);
+                if (lane + z < 64) l += y;
             }
             if (lane < left) {
-                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)(ldexpf(y, eg) - ky - (xl[lane] + xl[64 + lane]) * up);
-                if (a.dlog_f) static_cast<bf16_t*>(a.dlog_f)[sat + lane * a.st] = (bf16_t)(l + all);
+                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)(((dbs[lane] + dbs[64 + lane]) + (dbs[128 + lane] + dbs[192 + lane])) * up);
+                if (a.dlog_f) static_cast<bf16_t*>(a.dlog_f)[sat + lane * a.st] = (bf16_t)(l + ((kus[0] + kus[1]) + (kus[2] + kus[3])));
             }
         }
-    }
-    const int l32 = lane & 31, h = lane >> 5;
-    bf16_t *const dqp = static_cast<bf16_t*>(a.dq) + kat, *const dkp = static_cast<bf16_t*>(a.dk) + kat;
+        if (GROUP && x + 1 == a.G) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const int r = 32 * rb + acc_row(j, h), z = 32 * cb + l32;
-        if (r < left) {
-            dqp[r * a.kt + z] = (bf16_t)dq[j];
-            dkp[r * a.kt + z] = (bf16_t)dk[j];
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int r = 32 * (rb0 + b) + acc_row(j, h);
+                    if (r < left) {
+                        dqp[r * a.kt] = (bf16_t)dq[b][j];
+                        dkp[r * a.kt] = (bf16_t)dk[b][j];
+                    }
+                }
         }
     }
 }
 
+template <int D, bool GROUP> static hipError_t launch16(const DeltaArgs& a, hipStream_t stream) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_grad16_kernel<D, GROUP>), hipFuncAttributeMaxDynamicSharedMemorySize, Grad16<D>::BYTES);
+    if (attr != hipSuccess) return attr;
+    delta_grad16_kernel<D, GROUP><<<dim3((unsigned)a.tiles * a.H), dim3(256), Grad16<D>::BYTES, stream>>>(a);
+    return hipGetLastError();
+}
 template <int D> static hipError_t launch(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
     const dim3 grid((unsigned)a.tiles * a.H);
     if (is_bf16) {
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_grad16_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Grad16<D>::bytes);
-        if (attr != hipSuccess) return attr;
-        delta_grad16_kernel<D><<<grid, dim3(Grad16<D>::NT), Grad16<D>::bytes, stream>>>(a);
+        return a.G > 1 ? launch16<D, true>(a, stream) : launch16<D, false>(a, stream);
     } else {
         constexpr size_t bytes = (size_t)(3 * 64 * (D + 4) + 2 * 64 * DG_LF + DELTA_ROWS * 64 + 192) * 4;
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_grad_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);

@@ -78,44 +78,43 @@ __device__ __forceinline__ void store_frags(const float* X, bool transposed, voi
     }
 }
 
+// 16 bytes of row r of a tokens' matrix, zeros behind the last one
+template <typename F, typename T> __device__ __forceinline__ F row_frag(const T* p, long long ld, int r, int left, int x) {
+    F f;
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) f[e] = (T)0.f;
+    return r < left ? *reinterpret_cast<const F*>(p + r * ld + x) : f;
+}
+
+// Four waves to a chunk, 16 rows each; K and Q come from memory as operands (a wave's four tiles of K overlap the others' in L1).  Bound by the chain of its phases,
+// so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone.
 template <typename T, int D, int NPF, int NPB>      // NPB = 0: no transposes
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept
     typedef typename Tr<T>::Frag Frag;
     constexpr int SL = sizeof(T) == 2 ? 32 : 16, FE = 16 / (int)sizeof(T);
-    constexpr int LD = D + 16 / (int)sizeof(T), VEC = 16 / (int)sizeof(T);
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* const N = reinterpret_cast<float*>(smem);
     float* const M = N + 64 * DP_LF;
     float* const rows = M + 64 * DP_LF;
-    T* const K = reinterpret_cast<T*>(rows + DELTA_ROWS * 64 + 32);
-    T* const Q = K + 64 * LD;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = lane & 15, g = lane >> 4;
+    float(*const red)[8] = reinterpret_cast<float(*)[8]>(rows + DELTA_ROWS * 64);
+    float* const Lm = rows + DELTA_ROWS * 64 + 32;      // training only
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.V), hv = blockIdx.x - tile * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
     int s, c;
     DeltaSeq sq;
     if (!delta_tile(a, tile, lane, s, c, sq)) return;
     const int t0 = c * CHUNK, left = sq.len - t0;      // tokens of this chunk: min(64, left)
     const size_t unit = (size_t)tile * a.V + hv;
-
     const long long kat = delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh + t0 * a.kt, sat = delta_at(a, sq, s, a.ss, a.st) + hv * a.sh + t0 * a.st;
-    {
-        const T *kp = static_cast<const T*>(a.k) + kat, *qp = static_cast<const T*>(a.q) + kat;
-        for (int i = tid; i < 64 * D / VEC; i += 256) {
-            const int r = i / (D / VEC), x = i % (D / VEC) * VEC;
-            Frag fk, fq;
+    const T *const kp = static_cast<const T*>(a.k) + kat, *const qp = static_cast<const T*>(a.q) + kat;
+
+    // rows 16 wv .. of K K^T and Q K^T
+    Frag fk[D / SL], fq[D / SL];
 #pragma unroll
-            for (int e = 0; e < FE; ++e) { fk[e] = (T)0.f; fq[e] = (T)0.f; }
-            if (r < left) {
-                fk = *reinterpret_cast<const Frag*>(kp + r * a.kt + x);
-                fq = *reinterpret_cast<const Frag*>(qp + r * a.kt + x);
-            }
-            *reinterpret_cast<Frag*>(K + r * LD + x) = fk;
-            *reinterpret_cast<Frag*>(Q + r * LD + x) = fq;
-        }
-    }
-    if constexpr (sizeof(T) == 2)
-        most_of<D>(static_cast<const bf16_t*>(a.v) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, a.vt, left, a.vmost + unit * 8, reinterpret_cast<float(*)[8]>(rows + DELTA_ROWS * 64), tid);
+    for (int x = 0; x < D / SL; ++x) fk[x] = row_frag<Frag>(kp, a.kt, 16 * wv + n, left, x * SL + FE * g);
+#pragma unroll
+    for (int x = 0; x < D / SL; ++x) fq[x] = row_frag<Frag>(qp, a.kt, 16 * wv + n, left, x * SL + FE * g);
     if (wv == 0) {
         // Running sums in 64 bits: 64 gates of -20 each add up to 1e3, whose rounding to 32 bits would be 6e-5 of a neighbour's weight.  Gates below exp(-200) count as
         // that: it is nothing beside any number of 32 bits, and sums stay small enough for differences between the tokens behind a gate that forgets everything.
@@ -135,42 +134,46 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < DELTA_ROWS; ++i) { rows[i * 64 + lane] = vals[i]; out[i * 64 + lane] = vals[i]; }
     }
-    __syncthreads();
-
-    // rows 16 wv .. of K K^T and Q K^T, weighted
-    float be[4], bh[4], bl[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { const int r = 16 * wv + 4 * g + j; be[j] = rows[r]; bh[j] = rows[3 * 64 + r]; bl[j] = rows[4 * 64 + r]; }
-    Frag fk[D / SL], fq[D / SL];
-#pragma unroll
-    for (int x = 0; x < D / SL; ++x) {
-        fk[x] = *reinterpret_cast<const Frag*>(K + (16 * wv + n) * LD + x * SL + FE * g);
-        fq[x] = *reinterpret_cast<const Frag*>(Q + (16 * wv + n) * LD + x * SL + FE * g);
-    }
+    f32x4 kk[4], qk[4];
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+        kk[ib] = qk[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (ib <= wv) {
+            Frag f[D / SL];
+#pragma unroll
+            for (int z = 0; z < D / SL; ++z) f[z] = ib == wv ? fk[z] : row_frag<Frag>(kp, a.kt, 16 * ib + n, left, z * SL + FE * g);
 #pragma unroll
             for (int z = 0; z < D / SL; ++z) {
-                const Frag f = *reinterpret_cast<const Frag*>(K + (16 * ib + n) * LD + z * SL + FE * g);
-                x = mma_user(fk[z], f, x);
-                y = mma_user(fq[z], f, y);
+                kk[ib] = mma_user(fk[z], f[z], kk[ib]);
+                qk[ib] = mma_user(fq[z], f[z], qk[ib]);
             }
         }
-        const int i = 16 * ib + n;
-        const float ih = rows[3 * 64 + i], il = rows[4 * 64 + i];
+    }
+    if constexpr (sizeof(T) == 2)
+        most_of<D>(static_cast<const bf16_t*>(a.v) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, a.vt, left, a.vmost + unit * 8, red, tid);
+    else
+        __syncthreads();
+    {
+        float bh[4], bl[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = 16 * wv + 4 * g + j;
-            const float w = expf((bh[j] - ih) + (bl[j] - il));
-            N[r * DP_LF + i] = i < r ? be[j] * w * x[j] : 0.f;
-            M[r * DP_LF + i] = i <= r ? a.scale * w * y[j] : 0.f;
+        for (int j = 0; j < 4; ++j) { const int r = 16 * wv + 4 * g + j; bh[j] = rows[3 * 64 + r]; bl[j] = rows[4 * 64 + r]; }
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) {
+            const int i = 16 * ib + n;
+            const float ih = rows[3 * 64 + i], il = rows[4 * 64 + i], be = rows[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 16 * wv + 4 * g + j;
+                const float w = ib <= wv ? expf((bh[j] - ih) + (bl[j] - il)) : 0.f, l = i < r ? w * kk[ib][j] : 0.f;
+                N[r * DP_LF + i] = l * be;
+                M[r * DP_LF + i] = i <= r ? a.scale * w * qk[ib][j] : 0.f;
+                if (NPB > 0) Lm[r * DP_LF + i] = l;
+            }
         }
     }
     __syncthreads();
 
-    // A = (I + N)^-1: 16x16 diagonal blocks by substitution, a column per lane, then -X22 N21 X11, of 16 and of 32 rows, all in 32 bits
+    // P = (I + N)^-1: 16x16 diagonal blocks by substitution, a column per lane, then -X22 N21 X11, of 16 and of 32 rows, all in 32 bits
     {
         float x[16];
         const float* const B = N + 16 * wv * DP_LF + 16 * wv;
@@ -213,17 +216,35 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         for (int j = 0; j < 4; ++j) N[(16 * bi + 4 * g + j) * DP_LF + 16 * bj + n] = -x[j];
     }
     __syncthreads();
-    store_frags<C, NPF>(N, false, a.a, unit, tid);
+    store_frags<C, NPF>(N, false, a.p, unit, tid);
     store_frags<C, NPF>(M, false, a.m, unit, tid);
     if constexpr (NPB > 0) {
-        store_frags<C, NPB>(N, true, a.at, unit, tid);
         store_frags<C, NPB>(M, true, a.mt, unit, tid);
+        // A = I - diag(beta) P L, rows 16 wv ..
+        f32x4 x[4];
+#pragma unroll
+        for (int bj = 0; bj < 4; ++bj) {
+            x[bj] = zero;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k >= bj && k <= wv) x[bj] = block_mma(N, wv, k, Lm, bj, n, g, x[bj]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int bj = 0; bj < 4; ++bj)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 16 * wv + 4 * g + j, i = 16 * bj + n;
+                N[r * DP_LF + i] = (r == i ? 1.f : 0.f) - rows[r] * x[bj][j];
+            }
+        __syncthreads();
+        store_frags<C, NPB>(N, true, a.at, unit, tid);
     }
 }
 
 template <typename T, int D, int NPF, int NPB>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    constexpr size_t bytes = (size_t)(2 * 64 * DP_LF + DELTA_ROWS * 64 + 32) * 4 + (size_t)2 * 64 * (D * sizeof(T) + 16);
+    constexpr size_t bytes = (size_t)((NPB > 0 ? 3 : 2) * 64 * DP_LF + DELTA_ROWS * 64 + 32) * 4;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_prep_kernel<T, D, NPF, NPB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
     delta_prep_kernel<T, D, NPF, NPB><<<dim3((unsigned)a.tiles * a.V), dim3(256), bytes, stream>>>(a);
@@ -239,7 +260,6 @@ static hipError_t launch_d(const DeltaArgs& a, int is_bf16, bool training, hipSt
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream) {
     return d == 64 ? launch_d<64>(a, is_bf16, training, stream) : launch_d<128>(a, is_bf16, training, stream);
 }
-
 hipError_t launch_delta_most(const DeltaArgs& a, int d, hipStream_t stream) {
     const dim3 grid((unsigned)a.tiles * a.V);
     if (d == 64) delta_most_kernel<64><<<grid, dim3(256), 0, stream>>>(a);

@@ -24,7 +24,8 @@ struct ScanLds {
     static constexpr bool BACK = MODE == DELTA_BACK;
     // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the two operands of the gradient's update: that of Y, and Y to be kept); backwards d_o
     // and diag(gamma) d_o as operands, and what they add up to, in fp32
-    static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (BACK ? CS * CT * 1024 : 0);
+    // (E: to be kept, in place of O)
+    static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (MODE != DELTA_O ? CS * CT * 1024 : 0);
     static constexpr int DU = OG + (BACK ? AREA : 0), DG = DU + (BACK ? 4 * CT * 1024 : 0), X = DG + (BACK ? 4 * TW * CT * 1024 : 0), KT = X + 256;
     static constexpr int BYTES = KT + (BACK ? 8 : 4) * 64 * SROW;
 };
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     };
 
     const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
-    const void *const ga = BACK ? a.at : a.a, *const gm = BACK ? a.mt : a.m;
+    const void *const ga = BACK ? a.at : a.p, *const gm = BACK ? a.mt : a.m;
     auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
     if (chain) {
         UserFrag K[RS], kt[NK];
@@ -299,13 +300,13 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         T v[CT][4];
         f32x4 be, ga4, rh;
         float g63 = 0.f;
-        if (NC > 0) {
+        if (NC > 0) {      // (in the order of the loop: waits for loads go by how many came after them)
+            if (!BACK) load_values(first, v);
+            load_slice(first, kt);
             load_rows(first, K);
+            load_tri(ga, first, A);
             be = number(first, 0); ga4 = number(first, 1); rh = number(first, 2);
             g63 = last_gamma(first);
-            if (!BACK) load_values(first, v);
-            load_tri(ga, first, A);
-            load_slice(first, kt);
         }
         put_state();
         if (BACK && NC > 0) { lds_barrier(); lds_barrier(); lds_barrier(); }      // (the other waves' first chunk)
@@ -321,7 +322,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             load_rows(next, K);
             if (!BACK) {
 #pragma unroll
-                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, be * (V[x] - ga4 * y[x]));
+                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, V[x] - ga4 * y[x]);
             } else {      // dU = diag(rho) K G + M^T dO
 #pragma unroll
                 for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, y[x] * rh + *reinterpret_cast<const f32x4*>(smem + L::DU + (wv * CT + x) * 1024 + lane * 16));
@@ -337,7 +338,9 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             load_tri(ga, next, A);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
-                if (!BACK) {
+                if (!BACK) {      // (U: E at first)
+                    if (MODE == DELTA_KEEP) put(one_part, L::O, wv, x, U[x]);
+                    U[x] = be * U[x];
                     put(all_parts, L::U, wv, x, U[x] * rh);
                     put(all_parts, L::V, wv, x, U[x]);
                 } else {      // (U: the gradient's Y)
@@ -377,8 +380,8 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         f32x4 ga4;
         if (NC > 0) {
             load_rows(first, Q);
-            load_tri(gm, first, M);
             ga4 = number(first, 1);
+            load_tri(gm, first, M);
         }
         for (int i = 0, c = first; i < NC; ++i, c += step) {
             const int next = after(c);
@@ -398,7 +401,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             __builtin_amdgcn_sched_barrier(0);
             times(M, f, o);
             load_tri(gm, next, M);
-            if (MODE == DELTA_KEEP) keep(a.um, L::V, u, NP, CS);
+            if (MODE == DELTA_KEEP) keep(a.em, L::O, u, 1, CS);
             store_values(c, o);
         }
     } else if (NC > 0) {
@@ -407,10 +410,11 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         UserFrag qt[NK];
         DeltaParts<C, NP> M[CS];
         T v[CT][4];
-        f32x4 ga4 = number(first, 1), V[CT], du[CT], dg[TW][CT];
-        load_slice(first, qt);
-        load_tri(gm, first, M);
+        f32x4 ga4, V[CT], du[CT], dg[TW][CT];
         load_values(first, v);
+        load_slice(first, qt);
+        ga4 = number(first, 1);
+        load_tri(gm, first, M);
 #pragma unroll
         for (int t = 0; t < TW; ++t)
 #pragma unroll
