@@ -91,23 +91,19 @@ template <typename T, int NA, int NB> __device__ __forceinline__ f32x4 delta_mma
     return c;
 }
 
-// A matrix in LDS, 64 rows of W 16-bit elements, transposed as an A operand: rows of result tiles 2 t, 2 t + 1 are 32 of its columns, the contraction its rows: fragments
-// [tile % 2][slab].  at: LDS address of row 8 g + n / 4, column 8 (n % 4) of the 32.
-template <int W> __device__ __forceinline__ void delta_ld_tr(unsigned at, halfx8 (&f)[2][2]) {
-    union U { unsigned long long v[2]; halfx8 f; } u[4];
-    constexpr int R4 = 4 * W * 2, R32 = 32 * W * 2;
-    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%9\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
-                 "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %8 offset:%14\n\t"
-                 "ds_read_b64_tr_b16 %6, %8 offset:%15\n\tds_read_b64_tr_b16 %7, %8 offset:%16\n\t"
-                 "s_waitcnt lgkmcnt(0)"
-                 : "=&v"(u[0].v[0]), "=&v"(u[0].v[1]), "=&v"(u[1].v[0]), "=&v"(u[1].v[1]), "=&v"(u[2].v[0]), "=&v"(u[2].v[1]), "=&v"(u[3].v[0]), "=&v"(u[3].v[1])
-                 : "v"(at), "n"(0), "n"(R4), "n"(R32), "n"(R32 + R4), "n"(8), "n"(R4 + 8), "n"(R32 + 8), "n"(R32 + R4 + 8)
-                 : "memory");
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) f[b][s] = u[2 * b + s].f;
+// K in LDS: 64 rows of D elements without padding, the 16-byte pieces of a row permuted by an exclusive or with a number made of the row, so that neither a fragment along the
+// rows (sixteen rows' pieces of one column) nor a transposing read (four rows, four pieces) meets itself on a bank.
+template <typename C, int D> struct DeltaTile {
+    static constexpr int ROWB = D * (int)sizeof(C), PPR = ROWB / 16, BYTES = 64 * ROWB;
+    static __device__ __forceinline__ int turn(int row) {
+        return sizeof(C) == 4 ? row & 15 : D == 128 ? ((row & 3) << 2) | ((row >> 3) & 3) : (((row >> 1) & 1) << 2) | ((row >> 3) & 3);
+    }
+    static __device__ __forceinline__ int piece(int row, int p) { return row * ROWB + ((p ^ turn(row)) << 4); }
+};
+// four rows of a column, as a transposing read gives them to the lane that asks for the row and the four columns of its number
+__device__ __forceinline__ halfx4 delta_ld_tr(const unsigned char* p) {
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(halfx4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
 }
 
 // the exponent that puts numbers up to m between 32 and 64 (2^100 and 2^-100 are the ends)

@@ -17,17 +17,19 @@ template <> struct DeltaOperand<bf16_t> { typedef half_t type; };
 
 template <typename T, int D, int NP, int CT, int MODE>
 struct ScanLds {
-    typedef DeltaOps<typename DeltaOperand<T>::type> P;
+    typedef typename DeltaOperand<T>::type C;
+    typedef DeltaOps<C> P;
     static constexpr int NS = D / P::SL, CS = 64 / P::SL;                      // slabs of the state's rows, of a chunk
     static constexpr int TW = D / 64;                                          // state tiles of a wave
-    static constexpr int SW = sizeof(T) == 2 ? 32 : 16 * TW, SROW = sizeof(T) == 2 ? 64 : (SW + 4) * 4;      // a wave's columns of K: elements, bytes of a row in LDS
-    static constexpr bool BACK = MODE == DELTA_BACK;
-    // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the two operands of the gradient's update: that of Y, and Y to be kept); backwards d_o
+    static constexpr bool BACK = MODE == DELTA_BACK, HALF = sizeof(T) == 2;
+    // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the operand of the gradient's update, and Y to be kept); forward E, to be kept; backwards d_o
     // and diag(gamma) d_o as operands, and what they add up to, in fp32
-    // (E: to be kept, in place of O)
     static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (MODE != DELTA_O ? CS * CT * 1024 : 0);
-    static constexpr int DU = OG + (BACK ? AREA : 0), DG = DU + (BACK ? 4 * CT * 1024 : 0), X = DG + (BACK ? 4 * TW * CT * 1024 : 0), KT = X + 256;
-    static constexpr int BYTES = KT + (BACK ? 8 : 4) * 64 * SROW;
+    static constexpr int DU = OG + (BACK ? AREA : 0), DG = DU + (BACK ? 4 * CT * 1024 : 0), X = DG + (BACK ? 4 * TW * CT * 1024 : 0);
+    // K and the tokens' numbers, two chunks; a wave's own tokens of V (16-bit), its own columns of Q (backwards)
+    static constexpr int KT = X + 256, NUM = KT + 2 * DeltaTile<C, D>::BYTES, VT = NUM + 2 * 768, QT = VT + (HALF ? (BACK ? 8 : 4) * CT * 512 : 0);
+    static constexpr int SW = HALF ? 32 : 16 * TW, SROW = HALF ? 64 : (SW + 4) * 4;      // columns of Q: elements, bytes of a row
+    static constexpr int BYTES = QT + (BACK ? 4 * 64 * SROW : 0);
 };
 
 // `rows` rows of `row` bytes as a buffer, and what a lane loads from and stores to it
@@ -41,9 +43,11 @@ template <typename T> __device__ __forceinline__ T delta_load1(__amdgpu_buffer_r
     if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
     else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
 }
-template <typename T> __device__ __forceinline__ void delta_store1(__amdgpu_buffer_rsrc_t r, unsigned at, T x) {
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), r, at, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), r, at, 0, 0);
+template <typename T> __device__ __forceinline__ void delta_store4(__amdgpu_buffer_rsrc_t r, unsigned at, f32x4 x) {
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, __builtin_convertvector(x, bf16x4)), r, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), r, at, 0, 0);
 }
 
 template <typename T, int D, int NP, int CT, int MODE>
@@ -161,25 +165,42 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     char* const ob = static_cast<char*>(BACK ? a.dv : a.o) + vat;
     const unsigned krow = (unsigned)a.kt * ES, vrow = (unsigned)a.vt * ES;
     auto buffer = [&](const char* base, unsigned row, int c) { return delta_buffer(base + (long long)c * CHUNK * row, len - c * CHUNK, row); };
-    const unsigned row_at = P::row(wv, n) * krow + 16 * g, value_at = P::row(wv, 4 * g) * vrow + n * ES;
+    const unsigned row_at = P::row(wv, n) * krow + 16 * g;
     const unsigned slice_at = lane / PPR * krow + (HALF ? 32 * (TW * wv >> 1) : 16 * TW * wv) * ES + lane % PPR * 16;
+    typedef DeltaTile<C, D> Tile;
     typedef const __attribute__((address_space(1))) Frag GlobalFrag;
-    constexpr int RS = D * ES / 64;      // 64-byte pieces of a row: a fragment of one each
-    auto load_rows = [&](int c, UserFrag* f) {
+    constexpr int RS = D * ES / 64;                       // 64-byte pieces of a row: a fragment of one each; 16-byte pieces of 16 rows per lane
+    constexpr int UPR = D * ES / 16;                      // 16-byte pieces of a row
+    auto load_rows = [&](int c, UserFrag* f) {            // fragments of the wave's tokens
         const auto r = buffer(kb, krow, c);
 #pragma unroll
         for (int sl = 0; sl < RS; ++sl) f[sl] = delta_load16<UserFrag>(r, row_at + sl * 64);
     };
-    auto load_slice = [&](int c, UserFrag* f) {      // all rows of the wave's columns
+    auto load_slice = [&](int c, UserFrag* f) {           // all rows of the wave's columns
         const auto r = buffer(kb, krow, c);
 #pragma unroll
         for (int i = 0; i < NK; ++i) f[i] = delta_load16<UserFrag>(r, slice_at + i * (64 / PPR) * krow);
     };
-    const int slice = L::KT + wave * 64 * L::SROW;
+    const int slice = L::QT + wv * 64 * L::SROW;
     auto store_slice = [&](const UserFrag* f) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) *reinterpret_cast<Operand*>(smem + slice + (i * 64 + lane) / PPR * L::SROW + (lane % PPR) * 16) = delta_operand(f[i]);
     };
+    // a quarter of a chunk's K for everybody, and the tokens' beta, gamma and rho
+    auto load_tile = [&](int c, UserFrag* f, f32x4& w) {
+        const auto r = buffer(kb, krow, c);
+#pragma unroll
+        for (int i = 0; i < RS; ++i) f[i] = delta_load16<UserFrag>(r, (16 * wv + (i * 64 + lane) / UPR) * krow + lane % UPR * 16);
+        typedef const __attribute__((address_space(1))) f32x4 Global4;
+        if (wv == 0) w = *(Global4*)scalar_base(a.rows + ((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS * 64, (lane < 48 ? lane : 47) * 16);
+    };
+    auto store_tile = [&](int c, const UserFrag* f, const f32x4& w) {
+        const int at = L::KT + (c & 1) * Tile::BYTES;
+#pragma unroll
+        for (int i = 0; i < RS; ++i) *reinterpret_cast<Operand*>(smem + at + Tile::piece(16 * wv + (i * 64 + lane) / UPR, lane % UPR)) = delta_operand(f[i]);
+        if (wv == 0 && lane < 48) *reinterpret_cast<f32x4*>(smem + L::NUM + (c & 1) * 768 + lane * 16) = w;
+    };
+    auto numbers = [&](int c, int which) { return *reinterpret_cast<const f32x4*>(smem + L::NUM + (c & 1) * 768 + (which * 64 + P::row(wv, 4 * g)) * 4); };      // of the lane's four tokens
     auto used = [&](int sl) { return BACK ? P::up(wv, sl) : P::low(wv, sl); };
     auto load_tri = [&](const void* base, int c, DeltaParts<C, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
         const char* const p = static_cast<const char*>(base) + ((size_t)(tile0 + c) * a.V + hv) * NP * P::NLOW * 1024;
@@ -190,91 +211,87 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             for (int z = 0; z < NP; ++z) f[sl].p[z] = *(GlobalFrag*)scalar_base(p + (z * P::NLOW + at) * 1024, lane * 16);
         }
     };
-    auto load_values = [&](int c, T (&v)[CT][4]) {      // the lane's tokens and columns of V (backwards: dO)
+    // The wave's tokens and columns of V (backwards: dO): 16-bit numbers by whole pieces, to the lane that takes four tokens of a column by way of LDS
+    constexpr int VN = HALF ? 1 : 4 * CT;
+    typedef typename std::conditional<HALF, UserFrag, float>::type Value;
+    const int vt = L::VT + (BACK && !chain ? 4 * CT * 512 : 0) + wv * CT * 512;
+    auto load_values = [&](int c, Value (&v)[VN]) {
         const auto r = buffer(vb, vrow, c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int x = 0; x < CT; ++x) v[x][j] = delta_load1<T>(r, value_at + j * vrow + 16 * x * ES);
-    };
-    auto values = [&](const T (&v)[CT][4], f32x4* V) {
-#pragma unroll
-        for (int x = 0; x < CT; ++x)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) V[x][j] = (float)v[x][j] * down[x];
-    };
-    auto store_values = [&](int c, const f32x4* o) {
-        const auto r = buffer(ob, vrow, c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int x = 0; x < CT; ++x) delta_store1<T>(r, value_at + j * vrow + 16 * x * ES, (T)(o[x][j] * up[x]));
-    };
-    auto number = [&](int c, int which) {      // of the lane's four tokens
-        typedef const __attribute__((address_space(1))) f32x4 Global4;
-        return *(Global4*)scalar_base(a.rows + (((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + which) * 64, P::row(wv, 4 * g) * 4);
-    };
-    auto last_gamma = [&](int c) { return a.rows[(((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64 + 63]; };
-    // tiles [TW][CT] += (the wave's columns of K or Q)^T y
-    auto into = [&](f32x4 (&z)[TW][CT], const DeltaParts<C, NP> (&y)[CS][CT]) {
         if constexpr (HALF) {
-            const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(smem + slice) + (8 * g + (n >> 2)) * 64 + (n & 3) * 16;
-            halfx8 f[2][2];
-            delta_ld_tr<32>(base, f);
-#pragma unroll
-            for (int sl = 0; sl < 2; ++sl)
-#pragma unroll
-                for (int t = 0; t < TW; ++t)
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) {
-                        DeltaParts<C, 1> k;
-                        k.p[0] = TW == 2 ? f[t][sl] : (wv & 1) ? f[1][sl] : f[0][sl];
-                        z[t][x] = delta_mma(k, y[sl][x], z[t][x]);
-                    }
+            if (lane < 32 * CT) v[0] = delta_load16<UserFrag>(r, P::row(wv, lane / (2 * CT)) * vrow + lane % (2 * CT) * 16);
         } else {
 #pragma unroll
-            for (int sl = 0; sl < CS; ++sl)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int t = 0; t < TW; ++t) {
-                    DeltaParts<C, 1> k;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) k.p[0][e] = *reinterpret_cast<const float*>(smem + slice + (16 * sl + 4 * g + e) * L::SROW + (16 * t + n) * 4);
-#pragma unroll
-                    for (int x = 0; x < CT; ++x) z[t][x] = delta_mma(k, y[sl][x], z[t][x]);
-                }
+                for (int x = 0; x < CT; ++x) v[4 * x + j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, P::row(wv, 4 * g + j) * vrow + (n + 16 * x) * 4, 0, 0));
         }
     };
-    // the wave's tokens' rows of K or Q times the state
-    auto times_state = [&](const UserFrag* k, f32x4* y) {
+    auto store_values = [&](const Value (&v)[VN]) {
+        if constexpr (HALF)
+            if (lane < 32 * CT) *reinterpret_cast<UserFrag*>(smem + vt + lane * 16) = v[0];
+    };
+    auto values = [&](const Value (&v)[VN], f32x4* V) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            if constexpr (HALF) {
+                const uint2 w = __builtin_bit_cast(uint2, delta_ld_tr(smem + vt + (4 * g + (n >> 2)) * CT * 32 + 32 * x + (n & 3) * 8));
+                V[x] = f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)} * down[x];
+            } else {
+                V[x] = f32x4{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
+            }
+        }
+    };
+    auto last_gamma = [&](int c) { return a.rows[(((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64 + 63]; };
+    // tiles [TW][CT] += (the wave's columns of K, or of Q)^T y; at: of row r, piece p of the matrix in LDS
+    auto into = [&](f32x4 (&z)[TW][CT], const DeltaParts<C, NP> (&y)[CS][CT], auto at, int first_piece) {
+#pragma unroll
+        for (int sl = 0; sl < CS; ++sl)
+#pragma unroll
+            for (int t = 0; t < TW; ++t) {
+                DeltaParts<C, 1> k;
+                if constexpr (HALF) {
+                    const unsigned char* const p = smem + at(8 * g + (n >> 2) + 32 * sl, first_piece + (n & 3)) + 8 * (TW == 2 ? t : wv & 1);
+                    const halfx4 k0 = delta_ld_tr(p), k1 = delta_ld_tr(p + (at(4, 0) - at(0, 0)));
+                    k.p[0] = halfx8{k0[0], k0[1], k0[2], k0[3], k1[0], k1[1], k1[2], k1[3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) k.p[0][e] = *reinterpret_cast<const float*>(smem + at(16 * sl + 4 * g + e, first_piece + 4 * t + (n >> 2)) + (n & 3) * 4);
+                }
+#pragma unroll
+                for (int x = 0; x < CT; ++x) z[t][x] = delta_mma(k, y[sl][x], z[t][x]);
+            }
+    };
+    // the wave's tokens' rows of K times the state: tokens along the registers; of Q: tokens along the lanes
+    auto times_state = [&](auto row, auto turned, f32x4* y) {
         constexpr int HS = NS * NP * CT > 16 ? NS / 2 : NS;      // slabs requested together: up to 64 registers
 #pragma unroll
         for (int x = 0; x < CT; ++x) y[x] = zero;
 #pragma unroll
         for (int s0 = 0; s0 < NS; s0 += HS) {
             DeltaParts<C, NP> f[HS][CT];
+            DeltaParts<C, 1> q[HS];
 #pragma unroll
-            for (int sl = 0; sl < HS; ++sl)
+            for (int sl = 0; sl < HS; ++sl) {
+                q[sl].p[0] = row(s0 + sl);
 #pragma unroll
                 for (int x = 0; x < CT; ++x)
 #pragma unroll
                     for (int p = 0; p < NP; ++p) f[sl][x].p[p] = *reinterpret_cast<const Frag*>(smem + L::S + (((s0 + sl) * CT + x) * NP + p) * 1024 + lane * 16);
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int sl = 0; sl < HS; ++sl) {
-                DeltaParts<C, 1> q;
-                q.p[0] = delta_operand(k[s0 + sl]);
+            for (int sl = 0; sl < HS; ++sl)
 #pragma unroll
-                for (int x = 0; x < CT; ++x) y[x] = delta_mma(q, f[sl][x], y[x]);
-            }
+                for (int x = 0; x < CT; ++x) y[x] = decltype(turned)::value ? delta_mma(f[sl][x], q[sl], y[x]) : delta_mma(q[sl], f[sl][x], y[x]);
         }
     };
-    // the wave's tokens' rows of A or M (transposed: of A^T or M^T) times y
-    auto times = [&](const DeltaParts<C, NP>* m, const DeltaParts<C, NP> (&y)[CS][CT], f32x4* o) {
+    // the wave's tokens' rows of P or M (transposed: of A^T or M^T) times y
+    auto times = [&](const DeltaParts<C, NP>* m, const DeltaParts<C, NP> (&y)[CS][CT], auto turned, f32x4* o) {
 #pragma unroll
         for (int sl = 0; sl < CS; ++sl)
             if (used(sl))
 #pragma unroll
-                for (int x = 0; x < CT; ++x) o[x] = delta_mma(m[sl], y[sl][x], o[x]);
+                for (int x = 0; x < CT; ++x) o[x] = decltype(turned)::value ? delta_mma(y[sl][x], m[sl], o[x]) : delta_mma(m[sl], y[sl][x], o[x]);
     };
     // a state's or token matrix's slabs to memory for the chunk's gradients, the lane's row of the transposed matrix; the waves take turns
     auto keep = [&](void* out, int area, size_t u, int np, int slabs) {
@@ -294,18 +311,21 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
     const void *const ga = BACK ? a.at : a.p, *const gm = BACK ? a.mt : a.m;
     auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
+    const std::true_type turned{};
+    const std::false_type upright{};
     if (chain) {
-        UserFrag K[RS], kt[NK];
+        UserFrag kt[RS];
         DeltaParts<C, NP> A[CS];
-        T v[CT][4];
-        f32x4 be, ga4, rh;
+        Value v[VN];
+        f32x4 num = zero;
         float g63 = 0.f;
-        if (NC > 0) {      // (in the order of the loop: waits for loads go by how many came after them)
+        if (NC > 0) {
+            load_tile(first, kt, num);
+            store_tile(first, kt, num);
+            // (in the order of the loop: waits for loads go by how many came after them)
             if (!BACK) load_values(first, v);
-            load_slice(first, kt);
-            load_rows(first, K);
+            load_tile(after(first), kt, num);
             load_tri(ga, first, A);
-            be = number(first, 0); ga4 = number(first, 1); rh = number(first, 2);
             g63 = last_gamma(first);
         }
         put_state();
@@ -313,17 +333,20 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         for (int i = 0, c = first; i < NC; ++i, c += step) {
             const int next = after(c);
             f32x4 V[CT], y[CT];
-            if (!BACK) values(v, V);
-            if (!BACK) load_values(next, v);
-            store_slice(kt);
-            load_slice(next, kt);
-            lds_barrier();
-            times_state(K, y);
-            load_rows(next, K);
             if (!BACK) {
+                store_values(v);
+                values(v, V);
+                load_values(next, v);
+            }
+            lds_barrier();
+            const int tile = L::KT + (c & 1) * Tile::BYTES;
+            times_state([&](int sl) { return *reinterpret_cast<const Frag*>(smem + tile + Tile::piece(P::row(wv, n), 4 * sl + g)); }, upright, y);
+            if (!BACK) {
+                const f32x4 ga4 = numbers(c, 1);
 #pragma unroll
                 for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, V[x] - ga4 * y[x]);
             } else {      // dU = diag(rho) K G + M^T dO
+                const f32x4 rh = numbers(c, 2);
 #pragma unroll
                 for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, y[x] * rh + *reinterpret_cast<const f32x4*>(smem + L::DU + (wv * CT + x) * 1024 + lane * 16));
             }
@@ -334,25 +357,26 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             f32x4 U[CT];
 #pragma unroll
             for (int x = 0; x < CT; ++x) U[x] = zero;
-            times(A, f, U);
-            load_tri(ga, next, A);
+            const f32x4 be = numbers(c, 0), w = numbers(c, BACK ? 1 : 2);
+            times(A, f, upright, U);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 if (!BACK) {      // (U: E at first)
                     if (MODE == DELTA_KEEP) put(one_part, L::O, wv, x, U[x]);
                     U[x] = be * U[x];
-                    put(all_parts, L::U, wv, x, U[x] * rh);
+                    put(all_parts, L::U, wv, x, U[x] * w);
                     put(all_parts, L::V, wv, x, U[x]);
                 } else {      // (U: the gradient's Y)
                     put(one_part, L::V, wv, x, U[x]);
                     U[x] = be * U[x];
-                    put(all_parts, L::U, wv, x, -(ga4 * U[x]));
+                    put(all_parts, L::U, wv, x, -(w * U[x]));
+                    if constexpr (!HALF) {      // dv, which with 16 bits the kernel of the chunks' gradients makes from Y
+                        const auto r = buffer(ob, vrow, c);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(U[x][j]), r, P::row(wv, 4 * g + j) * vrow + (n + 16 * x) * 4, 0, 0);
+                    }
                 }
             }
-            if (BACK) store_values(c, U);
-            be = number(next, 0);
-            ga4 = number(next, 1);
-            rh = number(next, 2);
             lds_barrier();
             frags(L::U, f);
 #pragma unroll
@@ -362,8 +386,12 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     S[t][x] = S[t][x] * g63;
                     if (BACK) S[t][x] = S[t][x] + *reinterpret_cast<const f32x4*>(smem + L::DG + ((TW * wv + t) * CT + x) * 1024 + lane * 16);
                 }
+            into(S, f, [&](int r, int p) { return tile + Tile::piece(r, p); }, HALF ? 4 * (TW * wv >> 1) : 4 * TW * wv);
+            // The next chunk's K, into the other buffer, which nobody has read since the last chunk's third barrier; and what the one behind it brings
+            store_tile(next, kt, num);
+            load_tile(after(next), kt, num);
+            load_tri(ga, next, A);
             g63 = last_gamma(next);
-            into(S, f);
             put_state();
         }
         if (to) {
@@ -377,10 +405,8 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     } else if (!BACK) {
         UserFrag Q[RS];
         DeltaParts<C, NP> M[CS];
-        f32x4 ga4;
         if (NC > 0) {
             load_rows(first, Q);
-            ga4 = number(first, 1);
             load_tri(gm, first, M);
         }
         for (int i = 0, c = first; i < NC; ++i, c += step) {
@@ -388,32 +414,38 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             const size_t u = (size_t)(tile0 + c) * a.V + hv;
             f32x4 o[CT];
             lds_barrier();
-            times_state(Q, o);
+            times_state([&](int sl) { return delta_operand(Q[sl]); }, turned, o);
             load_rows(next, Q);
             if (MODE == DELTA_KEEP) keep(a.sm, L::S, u, NP, NS);
+            const float w = a.scale * *reinterpret_cast<const float*>(smem + L::NUM + (c & 1) * 768 + (64 + P::row(wv, n)) * 4);
 #pragma unroll
-            for (int x = 0; x < CT; ++x) o[x] = o[x] * (ga4 * a.scale);
-            ga4 = number(next, 1);
+            for (int x = 0; x < CT; ++x) o[x] = o[x] * w;
             lds_barrier();
             lds_barrier();
             DeltaParts<C, NP> f[CS][CT];
             frags(L::V, f);
             __builtin_amdgcn_sched_barrier(0);
-            times(M, f, o);
+            times(M, f, turned, o);
             load_tri(gm, next, M);
             if (MODE == DELTA_KEEP) keep(a.em, L::O, u, 1, CS);
-            store_values(c, o);
+            const auto r = buffer(ob, vrow, c);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) delta_store4<T>(r, P::row(wv, n) * vrow + (16 * x + 4 * g) * ES, o[x] * up[x]);
         }
     } else if (NC > 0) {
         // Of the chunk that the first four waves come to next: M^T dO and Q^T diag(scale gamma) dO, in fp32.  The first goes out behind the second barrier (they have read
         // the one before), the second, held back, behind the first barrier of the next round.
         UserFrag qt[NK];
         DeltaParts<C, NP> M[CS];
-        T v[CT][4];
-        f32x4 ga4, V[CT], du[CT], dg[TW][CT];
+        Value v[VN];
+        f32x4 V[CT], du[CT], dg[TW][CT], ga4;
+        auto gammas = [&](int c) {
+            typedef const __attribute__((address_space(1))) f32x4 Global4;
+            return *(Global4*)scalar_base(a.rows + (((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64, P::row(wv, 4 * g) * 4);
+        };
         load_values(first, v);
         load_slice(first, qt);
-        ga4 = number(first, 1);
+        ga4 = gammas(first);
         load_tri(gm, first, M);
 #pragma unroll
         for (int t = 0; t < TW; ++t)
@@ -421,6 +453,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             for (int x = 0; x < CT; ++x) dg[t][x] = zero;
         for (int i = -1, c = first; i < NC; ++i) {      // round i: they are at chunk i of theirs, this is the one behind it
             const int next = after(c);
+            store_values(v);
             values(v, V);
             load_values(next, v);
             store_slice(qt);
@@ -430,7 +463,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                 put(one_part, L::O, wv, x, V[x]);
                 put(all_parts, L::OG, wv, x, V[x] * (ga4 * a.scale));
             }
-            ga4 = number(next, 1);
+            ga4 = gammas(next);
             lds_barrier();
 #pragma unroll
             for (int t = 0; t < TW; ++t)
@@ -443,7 +476,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             for (int t = 0; t < TW; ++t)
 #pragma unroll
                 for (int x = 0; x < CT; ++x) dg[t][x] = zero;
-            into(dg, f);
+            into(dg, f, [&](int r, int p) { return slice + r * L::SROW + p * 16; }, 0);
 #pragma unroll
             for (int x = 0; x < CT; ++x) du[x] = zero;
 #pragma unroll
@@ -476,7 +509,9 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
 }
 template <typename T, int D, int NP, int MODE>
 static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
-    return (long long)a.nseq * a.V * (D / 32) >= 256 ? launch<T, D, NP, 2, MODE>(a, stream) : launch<T, D, NP, 1, MODE>(a, stream);
+    if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers)
+        if ((long long)a.nseq * a.V * (D / 32) >= 256) return launch<T, D, NP, 2, MODE>(a, stream);
+    return launch<T, D, NP, 1, MODE>(a, stream);
 }
 template <int D, int MODE>
 static hipError_t launch_np(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
