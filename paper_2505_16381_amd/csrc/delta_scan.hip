@@ -159,25 +159,40 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     // A chunk's rows of the caller's tensors as a buffer that ends behind the sequence's last one: rows behind it come in as zeros, and nothing is stored there.
     // (A store under a condition would have every later wait for a load wait for the store as well.)
     constexpr int PPR = L::SW * ES / 16, NK = PPR;      // 16-byte pieces of a slice's row; of a slice per lane
-    const char* const kb = static_cast<const char*>(chain ? a.k : a.q) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
+    const char* const kb = static_cast<const char*>(a.k) + (delta_at(a, sq, s, a.ks, a.kt) + hk * a.kh) * ES;
+    const char* const qb = static_cast<const char*>(a.q) + (kb - static_cast<const char*>(a.k));
     const long long vat = (delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + 16 * part * CT) * ES;
     const char* const vb = static_cast<const char*>(BACK ? a.d_o : a.v) + vat;
     char* const ob = static_cast<char*>(BACK ? a.dv : a.o) + vat;
     const unsigned krow = (unsigned)a.kt * ES, vrow = (unsigned)a.vt * ES;
-    auto buffer = [&](const char* base, unsigned row, int c) { return delta_buffer(base + (long long)c * CHUNK * row, len - c * CHUNK, row); };
+    // (Pointers to a chunk's rows and matrices move with the chunks: made anew by multiplications they took a fifth of a chunk's time.)
+    auto buffer = [&](const char* p, unsigned row, int c) { return delta_buffer(p, len - c * CHUNK, row); };
+    const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
+    auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
+    auto at_first = [&](const char* base, unsigned row) { return base + (long long)(first > 0 ? first : 0) * CHUNK * row; };
+    const size_t unit0 = (size_t)(tile0 + (first > 0 ? first : 0)) * a.V + hv;
+    constexpr int TRI = NP * P::NLOW * 1024;
+    auto moved = [&](const char* p, int c, int to, long long bytes) { return p + (to == c ? 0 : step * bytes); };      // from chunk c to `to`
+    // Loads are two chunks ahead, in two sets of registers that the chunks use in turn: memory under this load takes longer than a chunk.
+    auto in_turn = [&](auto&& body) {
+        for (int i = 0, c = first; i < NC; i += 2, c += 2 * step) {
+            body(std::integral_constant<int, 0>{}, i, c);
+            if (i + 1 < NC) body(std::integral_constant<int, 1>{}, i + 1, c + step);
+        }
+    };
     const unsigned row_at = P::row(wv, n) * krow + 16 * g;
     const unsigned slice_at = lane / PPR * krow + (HALF ? 32 * (TW * wv >> 1) : 16 * TW * wv) * ES + lane % PPR * 16;
     typedef DeltaTile<C, D> Tile;
     typedef const __attribute__((address_space(1))) Frag GlobalFrag;
     constexpr int RS = D * ES / 64;                       // 64-byte pieces of a row: a fragment of one each; 16-byte pieces of 16 rows per lane
     constexpr int UPR = D * ES / 16;                      // 16-byte pieces of a row
-    auto load_rows = [&](int c, UserFrag* f) {            // fragments of the wave's tokens
-        const auto r = buffer(kb, krow, c);
+    auto load_rows = [&](const char* p, int c, UserFrag* f) {            // fragments of the wave's tokens
+        const auto r = buffer(p, krow, c);
 #pragma unroll
         for (int sl = 0; sl < RS; ++sl) f[sl] = delta_load16<UserFrag>(r, row_at + sl * 64);
     };
-    auto load_slice = [&](int c, UserFrag* f) {           // all rows of the wave's columns
-        const auto r = buffer(kb, krow, c);
+    auto load_slice = [&](const char* p, int c, UserFrag* f) {           // all rows of the wave's columns
+        const auto r = buffer(p, krow, c);
 #pragma unroll
         for (int i = 0; i < NK; ++i) f[i] = delta_load16<UserFrag>(r, slice_at + i * (64 / PPR) * krow);
     };
@@ -187,12 +202,12 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         for (int i = 0; i < NK; ++i) *reinterpret_cast<Operand*>(smem + slice + (i * 64 + lane) / PPR * L::SROW + (lane % PPR) * 16) = delta_operand(f[i]);
     };
     // a quarter of a chunk's K for everybody, and the tokens' beta, gamma and rho
-    auto load_tile = [&](int c, UserFrag* f, f32x4& w) {
-        const auto r = buffer(kb, krow, c);
+    auto load_tile = [&](const char* p, const char* num, int c, UserFrag* f, f32x4& w) {
+        const auto r = buffer(p, krow, c);
 #pragma unroll
         for (int i = 0; i < RS; ++i) f[i] = delta_load16<UserFrag>(r, (16 * wv + (i * 64 + lane) / UPR) * krow + lane % UPR * 16);
         typedef const __attribute__((address_space(1))) f32x4 Global4;
-        if (wv == 0) w = *(Global4*)scalar_base(a.rows + ((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS * 64, (lane < 48 ? lane : 47) * 16);
+        if (wv == 0) w = *(Global4*)scalar_base(num, (lane < 48 ? lane : 47) * 16);
     };
     auto store_tile = [&](int c, const UserFrag* f, const f32x4& w) {
         const int at = L::KT + (c & 1) * Tile::BYTES;
@@ -202,8 +217,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     };
     auto numbers = [&](int c, int which) { return *reinterpret_cast<const f32x4*>(smem + L::NUM + (c & 1) * 768 + (which * 64 + P::row(wv, 4 * g)) * 4); };      // of the lane's four tokens
     auto used = [&](int sl) { return BACK ? P::up(wv, sl) : P::low(wv, sl); };
-    auto load_tri = [&](const void* base, int c, DeltaParts<C, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
-        const char* const p = static_cast<const char*>(base) + ((size_t)(tile0 + c) * a.V + hv) * NP * P::NLOW * 1024;
+    auto load_tri = [&](const char* p, DeltaParts<C, NP>* f) {      // (without branches: a slab that is not used is the wave's first or last one again)
 #pragma unroll
         for (int sl = 0; sl < CS; ++sl) {
             const int at = BACK ? P::up_at(wv, used(sl) ? sl : CS - 1) : P::low_at(wv, used(sl) ? sl : 0);
@@ -215,8 +229,8 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     constexpr int VN = HALF ? 1 : 4 * CT;
     typedef typename std::conditional<HALF, UserFrag, float>::type Value;
     const int vt = L::VT + (BACK && !chain ? 4 * CT * 512 : 0) + wv * CT * 512;
-    auto load_values = [&](int c, Value (&v)[VN]) {
-        const auto r = buffer(vb, vrow, c);
+    auto load_values = [&](const char* p, int c, Value (&v)[VN]) {
+        const auto r = buffer(p, vrow, c);
         if constexpr (HALF) {
             if (lane < 32 * CT) v[0] = delta_load16<UserFrag>(r, P::row(wv, lane / (2 * CT)) * vrow + lane % (2 * CT) * 16);
         } else {
@@ -241,7 +255,6 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             }
         }
     };
-    auto last_gamma = [&](int c) { return a.rows[(((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64 + 63]; };
     // tiles [TW][CT] += (the wave's columns of K, or of Q)^T y; at: of row r, piece p of the matrix in LDS
     auto into = [&](f32x4 (&z)[TW][CT], const DeltaParts<C, NP> (&y)[CS][CT], auto at, int first_piece) {
 #pragma unroll
@@ -308,35 +321,60 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             for (int t = 0; t < TW; ++t) put(all_parts, L::S, TW * wv + t, x, S[t][x]);
     };
 
-    const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
-    const void *const ga = BACK ? a.at : a.p, *const gm = BACK ? a.mt : a.m;
-    auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
+    const char *const ga = static_cast<const char*>(BACK ? a.at : a.p), *const gm = static_cast<const char*>(BACK ? a.mt : a.m);
+    const long long dk = (long long)CHUNK * krow, dv = (long long)CHUNK * vrow, dtri = (long long)a.V * TRI, dnum = (long long)a.V * DELTA_ROWS * 256;      // bytes from chunk to chunk
     const std::true_type turned{};
     const std::false_type upright{};
+    // Who brings K and the numbers: the waves that wait for the others
+    constexpr bool CHAIN_STAGES = BACK;
+    UserFrag kt[2][RS];
+    f32x4 num[2] = {zero, zero};
+    const char *kn = at_first(kb, krow), *nn = reinterpret_cast<const char*>(a.rows) + unit0 * DELTA_ROWS * 256;
+    int kc = first;      // the chunk that they are at
+    auto load_next = [&](UserFrag (&f)[RS], f32x4& w) {
+        const int then = after(kc);
+        kn = moved(kn, kc, then, dk);
+        nn = moved(nn, kc, then, dnum);
+        kc = then;
+        load_tile(kn, nn, kc, f, w);
+    };
+    auto stage = [&](auto other, int next) {      // the next chunk's K, into the buffer that nobody has read since the last chunk's third barrier
+        constexpr int O = decltype(other)::value;
+        store_tile(next, kt[O], num[O]);
+        load_next(kt[O], num[O]);
+    };
+    if (chain == CHAIN_STAGES && NC > 0) {
+        load_tile(kn, nn, first, kt[0], num[0]);
+        store_tile(first, kt[0], num[0]);
+        load_next(kt[1], num[1]);
+        load_next(kt[0], num[0]);
+    }
     if (chain) {
-        UserFrag kt[RS];
-        DeltaParts<C, NP> A[CS];
-        Value v[VN];
-        f32x4 num = zero;
-        float g63 = 0.f;
+        DeltaParts<C, NP> A[2][CS];
+        Value v[2][VN];
+        const char *vn = at_first(vb, vrow), *an = ga + unit0 * TRI;
+        int ahead = first;      // the chunk that they are at
         if (NC > 0) {
-            load_tile(first, kt, num);
-            store_tile(first, kt, num);
             // (in the order of the loop: waits for loads go by how many came after them)
-            if (!BACK) load_values(first, v);
-            load_tile(after(first), kt, num);
-            load_tri(ga, first, A);
-            g63 = last_gamma(first);
+            if (!BACK) load_values(vn, first, v[0]);
+            load_tri(an, A[0]);
+            ahead = after(first);
+            vn = moved(vn, first, ahead, dv);
+            an = moved(an, first, ahead, dtri);
+            if (!BACK) load_values(vn, ahead, v[1]);
+            load_tri(an, A[1]);
         }
         put_state();
         if (BACK && NC > 0) { lds_barrier(); lds_barrier(); lds_barrier(); }      // (the other waves' first chunk)
-        for (int i = 0, c = first; i < NC; ++i, c += step) {
-            const int next = after(c);
+        in_turn([&](auto turn, int i, int c) {
+            constexpr int T2 = decltype(turn)::value;
+            const int next = after(c), then = after(ahead);
             f32x4 V[CT], y[CT];
             if (!BACK) {
-                store_values(v);
-                values(v, V);
-                load_values(next, v);
+                store_values(v[T2]);
+                values(v[T2], V);
+                vn = moved(vn, ahead, then, dv);
+                load_values(vn, then, v[T2]);
             }
             lds_barrier();
             const int tile = L::KT + (c & 1) * Tile::BYTES;
@@ -353,12 +391,13 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             lds_barrier();
             DeltaParts<C, NP> f[CS][CT];
             frags(L::Y, f);
+            const f32x4 be = numbers(c, 0), w = numbers(c, BACK ? 1 : 2);
+            const float g63 = *reinterpret_cast<const float*>(smem + L::NUM + (c & 1) * 768 + (64 + 63) * 4);
             __builtin_amdgcn_sched_barrier(0);
             f32x4 U[CT];
 #pragma unroll
             for (int x = 0; x < CT; ++x) U[x] = zero;
-            const f32x4 be = numbers(c, 0), w = numbers(c, BACK ? 1 : 2);
-            times(A, f, upright, U);
+            times(A[T2], f, upright, U);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 if (!BACK) {      // (U: E at first)
@@ -371,7 +410,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     U[x] = be * U[x];
                     put(all_parts, L::U, wv, x, -(w * U[x]));
                     if constexpr (!HALF) {      // dv, which with 16 bits the kernel of the chunks' gradients makes from Y
-                        const auto r = buffer(ob, vrow, c);
+                        const auto r = buffer(ob + (long long)c * dv, vrow, c);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(U[x][j]), r, P::row(wv, 4 * g + j) * vrow + (n + 16 * x) * 4, 0, 0);
                     }
@@ -387,13 +426,12 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     if (BACK) S[t][x] = S[t][x] + *reinterpret_cast<const f32x4*>(smem + L::DG + ((TW * wv + t) * CT + x) * 1024 + lane * 16);
                 }
             into(S, f, [&](int r, int p) { return tile + Tile::piece(r, p); }, HALF ? 4 * (TW * wv >> 1) : 4 * TW * wv);
-            // The next chunk's K, into the other buffer, which nobody has read since the last chunk's third barrier; and what the one behind it brings
-            store_tile(next, kt, num);
-            load_tile(after(next), kt, num);
-            load_tri(ga, next, A);
-            g63 = last_gamma(next);
+            an = moved(an, ahead, then, dtri);
+            load_tri(an, A[T2]);
+            ahead = then;
             put_state();
-        }
+            if (CHAIN_STAGES) stage(std::integral_constant<int, 1 - T2>{}, next);
+        });
         if (to) {
 #pragma unroll
             for (int t = 0; t < TW; ++t)
@@ -403,73 +441,105 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     for (int j = 0; j < 4; ++j) to[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] = S[t][x][j] * up[x];
         }
     } else if (!BACK) {
-        UserFrag Q[RS];
-        DeltaParts<C, NP> M[CS];
+        UserFrag Q[2][RS];
+        Operand Qh[RS];
+        DeltaParts<C, NP> M[2][CS];
+        const char *qn = at_first(qb, krow), *mn = gm + unit0 * TRI;
+        char* on = ob;
+        int ahead = first;
         if (NC > 0) {
-            load_rows(first, Q);
-            load_tri(gm, first, M);
+            load_rows(qn, first, Q[0]);
+            load_tri(mn, M[0]);
+            ahead = after(first);
+            qn = moved(qn, first, ahead, dk);
+            mn = moved(mn, first, ahead, dtri);
+            load_rows(qn, ahead, Q[1]);
+            load_tri(mn, M[1]);
         }
-        for (int i = 0, c = first; i < NC; ++i, c += step) {
-            const int next = after(c);
+        in_turn([&](auto turn, int i, int c) {
+            constexpr int T2 = decltype(turn)::value;
+            const int next = after(c), then = after(ahead);
             const size_t u = (size_t)(tile0 + c) * a.V + hv;
             f32x4 o[CT];
+#pragma unroll
+            for (int sl = 0; sl < RS; ++sl) Qh[sl] = delta_operand(Q[T2][sl]);
+            qn = moved(qn, ahead, then, dk);
+            load_rows(qn, then, Q[T2]);
             lds_barrier();
-            times_state([&](int sl) { return delta_operand(Q[sl]); }, turned, o);
-            load_rows(next, Q);
-            if (MODE == DELTA_KEEP) keep(a.sm, L::S, u, NP, NS);
+            times_state([&](int sl) { return Qh[sl]; }, turned, o);
             const float w = a.scale * *reinterpret_cast<const float*>(smem + L::NUM + (c & 1) * 768 + (64 + P::row(wv, n)) * 4);
+            lds_barrier();
 #pragma unroll
             for (int x = 0; x < CT; ++x) o[x] = o[x] * w;
-            lds_barrier();
+            if (MODE == DELTA_KEEP) keep(a.sm, L::S, u, NP, NS);
             lds_barrier();
             DeltaParts<C, NP> f[CS][CT];
             frags(L::V, f);
             __builtin_amdgcn_sched_barrier(0);
-            times(M, f, turned, o);
-            load_tri(gm, next, M);
+            times(M[T2], f, turned, o);
+            mn = moved(mn, ahead, then, dtri);
+            load_tri(mn, M[T2]);
+            ahead = then;
             if (MODE == DELTA_KEEP) keep(a.em, L::O, u, 1, CS);
-            const auto r = buffer(ob, vrow, c);
+            const auto r = buffer(on, vrow, c);
 #pragma unroll
             for (int x = 0; x < CT; ++x) delta_store4<T>(r, P::row(wv, n) * vrow + (16 * x + 4 * g) * ES, o[x] * up[x]);
-        }
+            on += dv;
+            stage(std::integral_constant<int, 1 - T2>{}, next);
+        });
     } else if (NC > 0) {
         // Of the chunk that the first four waves come to next: M^T dO and Q^T diag(scale gamma) dO, in fp32.  The first goes out behind the second barrier (they have read
         // the one before), the second, held back, behind the first barrier of the next round.
-        UserFrag qt[NK];
-        DeltaParts<C, NP> M[CS];
-        Value v[VN];
-        f32x4 V[CT], du[CT], dg[TW][CT], ga4;
+        UserFrag qt[2][NK];
+        DeltaParts<C, NP> M[2][CS];
+        Value v[2][VN];
+        f32x4 V[CT], du[CT], dg[TW][CT], ga4[2];
         auto gammas = [&](int c) {
             typedef const __attribute__((address_space(1))) f32x4 Global4;
             return *(Global4*)scalar_base(a.rows + (((size_t)(tile0 + c) * a.V + hv) * DELTA_ROWS + 1) * 64, P::row(wv, 4 * g) * 4);
         };
-        load_values(first, v);
-        load_slice(first, qt);
-        ga4 = gammas(first);
-        load_tri(gm, first, M);
+        const char *vn = at_first(vb, vrow), *qn = at_first(qb, krow), *mn = gm + unit0 * TRI;
+        int ahead = first;
+        load_values(vn, first, v[0]);
+        load_slice(qn, first, qt[0]);
+        ga4[0] = gammas(first);
+        load_tri(mn, M[0]);
+        ahead = after(first);
+        vn = moved(vn, first, ahead, dv);
+        qn = moved(qn, first, ahead, dk);
+        mn = moved(mn, first, ahead, dtri);
+        load_values(vn, ahead, v[1]);
+        load_slice(qn, ahead, qt[1]);
+        ga4[1] = gammas(ahead);
+        load_tri(mn, M[1]);
 #pragma unroll
         for (int t = 0; t < TW; ++t)
 #pragma unroll
             for (int x = 0; x < CT; ++x) dg[t][x] = zero;
-        for (int i = -1, c = first; i < NC; ++i) {      // round i: they are at chunk i of theirs, this is the one behind it
-            const int next = after(c);
-            store_values(v);
-            values(v, V);
-            load_values(next, v);
-            store_slice(qt);
-            load_slice(next, qt);
+        // round i: this is at chunk i of theirs, they are at the one before
+        auto round = [&](auto turn, int i, int c) {
+            constexpr int T2 = decltype(turn)::value;
+            const int then = after(ahead);
+            const size_t u = (size_t)(tile0 + c - step) * a.V + hv;
+            store_values(v[T2]);
+            values(v[T2], V);
+            vn = moved(vn, ahead, then, dv);
+            load_values(vn, then, v[T2]);
+            store_slice(qt[T2]);
+            qn = moved(qn, ahead, then, dk);
+            load_slice(qn, then, qt[T2]);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 put(one_part, L::O, wv, x, V[x]);
-                put(all_parts, L::OG, wv, x, V[x] * (ga4 * a.scale));
+                put(all_parts, L::OG, wv, x, V[x] * (ga4[T2] * a.scale));
             }
-            ga4 = gammas(next);
+            ga4[T2] = gammas(then);
             lds_barrier();
 #pragma unroll
             for (int t = 0; t < TW; ++t)
 #pragma unroll
                 for (int x = 0; x < CT; ++x) *reinterpret_cast<f32x4*>(smem + L::DG + ((TW * wv + t) * CT + x) * 1024 + lane * 16) = dg[t][x];
-            if (i >= 0) keep(a.gm, L::S, (size_t)(tile0 + first + i * step) * a.V + hv, NP, NS);
+            if (i > 0) keep(a.gm, L::S, u, NP, NS);
             DeltaParts<C, NP> f[CS][CT];
             frags(L::OG, f);
 #pragma unroll
@@ -486,16 +556,21 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     for (int x = 0; x < CT; ++x) {
                         DeltaParts<C, 1> y;
                         y.p[0] = frag1(L::O, sl, x, 1);
-                        du[x] = delta_mma(M[sl], y, du[x]);
+                        du[x] = delta_mma(M[T2][sl], y, du[x]);
                     }
-            load_tri(gm, next, M);
+            mn = moved(mn, ahead, then, dtri);
+            load_tri(mn, M[T2]);
+            ahead = then;
             lds_barrier();
 #pragma unroll
             for (int x = 0; x < CT; ++x) *reinterpret_cast<f32x4*>(smem + L::DU + (wv * CT + x) * 1024 + lane * 16) = du[x];
             lds_barrier();
-            if (i >= 0) keep(a.ym, L::V, (size_t)(tile0 + first + i * step) * a.V + hv, 1, CS);
-            c = next;
-        }
+            if (i > 0) keep(a.ym, L::V, u, 1, CS);
+        };
+        in_turn(round);
+        // the last round, in which they are at the last chunk: nothing is left to bring (what it computes again nobody takes)
+        if (NC & 1) round(std::integral_constant<int, 1>{}, NC, first + NC * step);
+        else round(std::integral_constant<int, 0>{}, NC, first + NC * step);
     }
 }
 
