@@ -171,8 +171,9 @@ __device__ __forceinline__ float sum16(float (&v)[16], int l32) {
         const bool up = l32 & m;
 #pragma unroll
         for (int j = 0; j < w; ++j) {
-            const float keep = up ? v[j + w] : v[j], give = up ? v[j] : v[j + w];
-            v[j] = keep + __shfl_xor(give, m);
+            float x = v[j], y = v[j + w];
+            asm volatile("" : "+v"(x), "+v"(y));      // (two registers: left to itself the compiler makes it one index into sixteen, and that a chain of sixteen selections)
+            v[j] = (up ? y : x) + __shfl_xor(up ? x : y, m);
         }
     }
     return v[0] + __shfl_xor(v[0], 1);
@@ -224,6 +225,22 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             if (r < left) y = *reinterpret_cast<const bf16x8*>(x + r * a.kt + lane % 4 * 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[i][e] = (half_t)((float)y[e] * w);
+        }
+    };
+    // the wave's block of a gradient, by whole pieces: through its own LDS
+    auto out_rows = [&](void* base, const f32x16 (&x)[RB]) {
+        bf16_t* const to = reinterpret_cast<bf16_t*>(slot);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) to[(32 * b + acc_row(j, lane >> 5)) * 32 + (lane & 31)] = (bf16_t)x[b][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 2 * RB; ++i) {
+            const int r = lane / 4 + 16 * i;
+            const bf16x8 f = *reinterpret_cast<const bf16x8*>(to + r * 32 + lane % 4 * 8);
+            if (32 * rb0 + r < left) *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(base) + kat + (32 * rb0 + r) * a.kt + 32 * cb + lane % 4 * 8) = f;
         }
     };
     auto to_slot = [&](const halfx8 (&f)[4]) {
@@ -447,7 +464,6 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             for (int b = 0; b < RB; ++b)
                 if (rb0 + b == 0 || sl >= 2) wr[b] = Tr<half_t>::mma(u_frag(C::O, rb0 + b, sl), f, wr[b]);
         }
-        bf16_t *const dqp = static_cast<bf16_t*>(a.dq) + kat + 32 * cb + l32, *const dkp = static_cast<bf16_t*>(a.dk) + kat + 32 * cb + l32;
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             float pl[16];
@@ -456,12 +472,11 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 const int r = 32 * (rb0 + b) + acc_row(j, h);
                 const float d1 = q1[b][j] * up12, d2 = rd[b][j] * up12, d3 = wr[b][j] * up12;      // (dq without scale: so is Q with it)
                 pl[j] = (float)slot[r * 32 + l32] * d1 + (float)kl[b][j / 8][j % 8] * (d2 - d3);
+                q1[b][j] = a.scale * d1;
+                rd[b][j] = d2 + d3;
                 if (GROUP) {
-                    dq[b][j] += a.scale * d1;
-                    dk[b][j] += d2 + d3;
-                } else if (r < left) {
-                    dqp[r * a.kt] = (bf16_t)(a.scale * d1);
-                    dkp[r * a.kt] = (bf16_t)(d2 + d3);
+                    dq[b][j] += q1[b][j];
+                    dk[b][j] += rd[b][j];
                 }
             }
             const float y = sum16(pl, l32);
@@ -485,17 +500,12 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 if (a.dlog_f) static_cast<bf16_t*>(a.dlog_f)[sat + lane * a.st] = (bf16_t)(l + ((kus[0] + kus[1]) + (kus[2] + kus[3])));
             }
         }
-        if (GROUP && x + 1 == a.G) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int r = 32 * (rb0 + b) + acc_row(j, h);
-                    if (r < left) {
-                        dqp[r * a.kt] = (bf16_t)dq[b][j];
-                        dkp[r * a.kt] = (bf16_t)dk[b][j];
-                    }
-                }
+        if (!GROUP) {
+            out_rows(a.dq, q1);
+            out_rows(a.dk, rd);
+        } else if (x + 1 == a.G) {
+            out_rows(a.dq, dq);
+            out_rows(a.dk, dk);
         }
     }
 }
