@@ -432,15 +432,19 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  *                         slots [nseq] (DEVICE int32): the sequence's state; outside 0 .. num_slots - 1: starts from zeros and is not kept.  cached [nseq] (DEVICE int32, as in the
  *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
  *                         have different slots (the state of one that is named twice is undefined; no fault).
- * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16 accumulates in fp32; q, k, v are operands as they are, what is computed is multiplied as the sum of two bf16 numbers, of
- * three where states are handed out (bf16's range; states 1e-6 of their norm from exact ones, o and gradients that are rounded to bf16 once).  dq, dk, dbeta, dlog_f are computed from fp16 operands over powers of two taken
- * from their largest values (q and k themselves: below 65504).  log_f below -200 counts as -200; log_f > 0 is carried as it is.
- * Infinities and NaN: values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
+ * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16: states and sums in fp32, products of fp16 operands.  q and k are operands as they are (below 65504 in magnitude, as scale q.k has to
+ * be); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value that comes in, as one fp16 number, or, where
+ * fp32 states are handed out (forward: state_out or a pool; backward: state_in), as the sum of two: states are off by some 1e-6 of their size, o and the 16-bit gradients by
+ * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
+ * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A state may grow to 1000 times what comes in; a sequence whose operands
+ * outgrow fp16 is walked again with 2^8, then 2^16 times the room.  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
+ * log_f below -200 counts as -200; log_f > 0 is carried as it is.
+ * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.
  * No atomics: the same bits every time.
  * workspace: path_delta_workspace_bytes(...) bytes (0 for sizes that are refused; training != 0 for the path_delta_train_* pair), 256-byte aligned; grows with every argument, so that one for the
  * largest call serves all smaller ones.
- * Errors: PATH_ERR_SHAPE for nseq, max_len, H or group < 1, T < 0, T != nseq * max_len without cu_seqlens, nseq * V >= 2^21, (T / 64 + nseq) * V >= 2^23, V > 65535;
+ * Errors: PATH_ERR_SHAPE for nseq, max_len, H or group < 1, T < 0, T != nseq * max_len without cu_seqlens, nseq * V > 2^19, (T / 64 + nseq) * V >= 2^23, V > 65535;
  * PATH_ERR_UNSUPPORTED for scale <= 0 or a packed batch that is not PATH_LAYOUT_BLHD; PATH_ERR_ALIGN for q, k, v, o, states or gradients of these off 16 bytes.
  */
 size_t path_delta_workspace_bytes(int nseq, int T, int max_len, int H, int group, int d, path_dtype_t dt, int training);

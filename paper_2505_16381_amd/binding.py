@@ -686,10 +686,10 @@ def _look(looked, dev, whose):
                 raise ValueError(f"{name} must be contiguous and on the GPU that {whose} is on")
 
 
-def _scratch(workspace, nbytes, like, stream, whose):
-    import torch
+def _scratch(workspace, nbytes, sizes, like, stream, whose):
     if workspace is None:
-        return _paged_made(like, (max(256, nbytes),), torch.uint8, stream, False)
+        import torch
+        return _paged_made(like, (max(256, nbytes(*sizes)),), torch.uint8, stream, False)
     if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous and on the GPU that {whose} is on")
     return workspace
@@ -734,7 +734,7 @@ def path_paged_plan(cached, new, page_table, free_pages, free_count, T, page_siz
         missing = _paged_made(cached, (nseq,), i32, stream, True)
     _look([("cached", cached, (nseq,), i32), ("new", new, (nseq,), i32), ("page_table", page_table, (nseq, per_seq), i32), ("free_pages", free_pages, (pool,), i32),
            ("free_count", free_count, (1,), i32), ("cu_new", cu_new, (nseq + 1,), i32), ("slots", slots, (T,), torch.int64), ("missing", missing, (nseq,), i32)], dev, "cached")
-    workspace = _scratch(workspace, path_paged_plan_workspace_bytes(nseq, per_seq, T), cached, stream, "cached")
+    workspace = _scratch(workspace, path_paged_plan_workspace_bytes, (nseq, per_seq, T), cached, stream, "cached")
     _call_on(dev, "path_paged_plan", (cached.data_ptr(), new.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), cu_new.data_ptr(), slots.data_ptr(),
                                       missing.data_ptr(), nseq, T, pool, page_size, per_seq, workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
     return cu_new, slots, missing
@@ -797,7 +797,7 @@ def _delta_fwd(name, q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, s
     if state_out is None and final_state:
         state_out = _paged_made(v, st, torch.float32, stream, True)
     dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("state_out", state_out, st)], [("o", o, shapes[1])], shapes)
-    workspace = _scratch(workspace, path_delta_workspace_bytes(nseq, T, L, H, G, d, dt, name == "path_delta_train_fwd"), q, stream, "q")
+    workspace = _scratch(workspace, path_delta_workspace_bytes, (nseq, T, L, H, G, d, dt, name == "path_delta_train_fwd"), q, stream, "q")
     if T > 0 or state_out is not None:
         _call_on(dev, name, (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), _opt(cu_seqlens), _opt(state_in), o.data_ptr(), _opt(state_out), nseq, T, L, H, G, d,
                              layout, float(d ** -0.5 if scale is None else scale), dt, workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
@@ -825,7 +825,7 @@ def path_delta_train_bwd(q, k, v, beta, d_o, workspace, log_f=None, scale=None, 
     nseq, T, L, H, G, d, layout, shapes = _delta_sizes(q, v, cu_seqlens, max_len, layout)
     dt, st = _dt_of(q), (nseq, H * G, d, d)
     dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("d_state_out", d_state_out, st)], [("d_o", d_o, shapes[1])], shapes)
-    _scratch(workspace, 0, q, stream, "q")
+    _scratch(workspace, None, None, q, stream, "q")
     made = lambda like: _paged_made(like, like.shape, like.dtype, stream, True)
     out = [made(q), made(k), made(v), made(beta)]
     dlog_f = made(log_f) if log_f is not None else None
@@ -855,7 +855,7 @@ def path_delta_extend(q, k, v, beta, states, slots, cached, cu_new, max_new, log
         looked.append(("log_f", log_f, shapes[2], td))
     dev = q.get_device()
     _look(looked, dev, "q")
-    workspace = _scratch(workspace, path_delta_workspace_bytes(nseq, T, L, H, G, d, dt), q, stream, "q")
+    workspace = _scratch(workspace, path_delta_workspace_bytes, (nseq, T, L, H, G, d, dt), q, stream, "q")
     if T == 0:
         return o
     _call_on(dev, "path_delta_extend", (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), states.data_ptr(), slots.data_ptr(), cached.data_ptr(), cu_new.data_ptr(),

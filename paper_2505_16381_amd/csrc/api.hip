@@ -1153,11 +1153,11 @@ namespace {
 struct DeltaPlan { long long tiles; size_t p, m, rows, vmost, at, mt, sm, gm, em, ym, gmost, vex, gex, total; };
 }  // namespace
 
-// Launches of fewer than 2^32 threads: 512 per tile and key head, 256 per tile and value head, 1024 per sequence and value head.
+// Launches of fewer than 2^32 threads: 256 per tile and head, 4096 per sequence and value head (the states: 512 for each 16 columns).
 static bool delta_shape_ok(int nseq, int T, int L, int H, int group, int d) {
     if (nseq < 1 || T < 0 || L < 1 || H < 1 || group < 1 || (d != 64 && d != 128)) return false;
     const long long V = (long long)H * group, tiles = (long long)T / CHUNK + nseq;
-    return V <= 65535 && nseq * V < (1 << 21) && tiles * V < (1 << 23);
+    return V <= 65535 && nseq * V <= (1 << 19) && tiles * V < (1 << 23);
 }
 // tiles: a packed batch's; sequences of one length need no more (n ceil(L / 64) <= n L / 64 + n)
 static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool training) {

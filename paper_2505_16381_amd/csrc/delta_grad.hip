@@ -215,17 +215,20 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + (size_t)(lane / 4 + 16 * i) * D + lane % 4 * 8);
     };
-    auto slice_tokens = [&](const bf16_t* x, float w, halfx8 (&f)[4]) {
+    auto slice_tokens = [&](const bf16_t* x, bf16x8 (&f)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = lane / 4 + 16 * i;
-            bf16x8 y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = (bf16_t)0.f;
-            if (r < left) y = *reinterpret_cast<const bf16x8*>(x + r * a.kt + lane % 4 * 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[i][e] = (half_t)((float)y[e] * w);
+            for (int e = 0; e < 8; ++e) f[i][e] = (bf16_t)0.f;
+            if (r < left) f[i] = *reinterpret_cast<const bf16x8*>(x + r * a.kt + lane % 4 * 8);
         }
+    };
+    auto operands = [&](const bf16x8 (&x)[4], float w, halfx8 (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = (half_t)((float)x[i][e] * w);
     };
     // the wave's block of a gradient, by whole pieces: through its own LDS
     auto out_rows = [&](void* base, const f32x16 (&x)[RB]) {
@@ -267,6 +270,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             eq = gex[b] > eq ? gex[b] : eq;
         }
         __syncthreads();      // (the head before has been read out)
+        halfx8 sf[4], gf[4];
         {
             halfx8 ef[NP], yf[NP];
             bf16x8 of[NP];
@@ -279,6 +283,8 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 for (int e = 0; e < 8; ++e) of[i][e] = (bf16_t)0.f;
                 if (r < left) of[i] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.d_o) + vat + r * a.vt + p % (D / 8) * 8);
             }
+            slice_rows(sg, sf);
+            slice_rows(gg, gf);
             const f32x4 b0 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8), b1 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8 + 4);
             halfx8 be;      // of the eight tokens of the thread's pieces
 #pragma unroll
@@ -307,9 +313,6 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dbs[wv * 64 + lane * 8 + e] = db[e];
         }
-        halfx8 sf[4], gf[4];
-        slice_rows(sg, sf);
-        slice_rows(gg, gf);
         __syncthreads();
 
         const Lane at(lane);
@@ -379,8 +382,8 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        halfx8 kf[4];
-        slice_tokens(kp, 1.f, kf);
+        bf16x8 kr[4];
+        slice_tokens(kp, kr);
         // X and N of the lower 32x32 blocks
         halfx8 res[2][2];
 #pragma unroll
@@ -396,11 +399,16 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 const int i = 32 * bi + l32;
                 const float ih = rows[192 + i], il = rows[256 + i];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int r = 32 * br + acc_row(j, h);
-                    const float w = expf((rows[192 + r] - ih) + (rows[256 + r] - il)) * 0x1p-12f;      // (sums of 128 products stay far from fp16's end)
-                    const float y = job < 3 ? (i < r ? -rows[r] * w * acc[j] : 0.f) : (i <= r ? w * acc[j] : 0.f);
-                    res[n][j / 8][j % 8] = (half_t)y;
+                for (int j4 = 0; j4 < 16; j4 += 4) {
+                    const int r0 = 32 * br + acc_row(j4, h);
+                    const f32x4 rh = *reinterpret_cast<const f32x4*>(rows + 192 + r0), rl = *reinterpret_cast<const f32x4*>(rows + 256 + r0), rb = *reinterpret_cast<const f32x4*>(rows + r0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        // (a power of two: its rounding and that of the exponent, 1e-5, are nothing beside the operand's; 2^-16: sums of 128 products stay far from fp16's end, one factor's growth included)
+                        const float w = __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f - 16.f);
+                        const float y = job < 3 ? (i < r0 + j ? -rb[j] * w * acc[j4 + j] : 0.f) : (i <= r0 + j ? w * acc[j4 + j] : 0.f);
+                        res[n][j4 / 8][(j4 + j) % 8] = (half_t)y;
+                    }
                 }
             }
         }
@@ -418,11 +426,12 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+        halfx8 kf[4];
+        operands(kr, 1.f, kf);
         to_slot(kf);
-        halfx8 qf[4];
-        slice_tokens(qp, a.scale, qf);
+        slice_tokens(qp, kr);
         __syncthreads();
-        const float up = ldexpf(1.f, ev + eq), up12 = up * 4096.f;      // of every product of two of them, of Gq and Gk, which are 2^12 below theirs
+        const float up = ldexpf(1.f, ev + eq), up16 = up * 65536.f;      // of every product of two of them, of Gq and Gk, which are 2^16 below theirs
         auto nat = [&](int mat, int b, int sl) { return *reinterpret_cast<const halfx8*>(smem + mat + at.nat_at(32 * b, 16 * sl)); };
         float kug = 0.f;
 #pragma unroll
@@ -430,9 +439,9 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 kug += (float)slot[(32 * (rb0 + b) + acc_row(j, h)) * 32 + l32] * wr[b][j];
-                q1[b][j] *= 0x1p-12f;
-                rd[b][j] *= 0x1p-12f;
-                wr[b][j] *= 0x1p-12f;
+                q1[b][j] *= 0x1p-16f;
+                rd[b][j] *= 0x1p-16f;
+                wr[b][j] *= 0x1p-16f;
             }
         kug = (kug + (rb0 == 0 ? rows[64 + 63] * sum : 0.f)) * up;
 #pragma unroll
@@ -456,7 +465,8 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int j = 0; j < 16; ++j) kl[b][j / 8][j % 8] = slot[(32 * (rb0 + b) + acc_row(j, h)) * 32 + l32];
-        to_slot(qf);
+        operands(kr, a.scale, kf);
+        to_slot(kf);
 #pragma unroll
         for (int sl = 0; sl < 4; ++sl) {
             const halfx8 f = slot_frag(sl);
@@ -470,7 +480,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const int r = 32 * (rb0 + b) + acc_row(j, h);
-                const float d1 = q1[b][j] * up12, d2 = rd[b][j] * up12, d3 = wr[b][j] * up12;      // (dq without scale: so is Q with it)
+                const float d1 = q1[b][j] * up16, d2 = rd[b][j] * up16, d3 = wr[b][j] * up16;      // (dq without scale: so is Q with it)
                 pl[j] = (float)slot[r * 32 + l32] * d1 + (float)kl[b][j / 8][j % 8] * (d2 - d3);
                 q1[b][j] = a.scale * d1;
                 rd[b][j] = d2 + d3;

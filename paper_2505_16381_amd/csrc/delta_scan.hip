@@ -61,8 +61,6 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     constexpr int NS = L::NS, CS = L::CS, TW = L::TW, ES = sizeof(T);
     constexpr bool BACK = MODE == DELTA_BACK, HALF = ES == 2;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 3, n = lane & 15, g = lane >> 4;
-    const bool chain = wave < 4;
     int unit, part;
     if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, D / 16 / CT, a.nseq * a.V, unit, part)) return;
     const int s = __builtin_amdgcn_readfirstlane(unit / a.V), hv = unit - s * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
@@ -70,11 +68,9 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     const int len = __builtin_amdgcn_readfirstlane(sq.len), tile0 = __builtin_amdgcn_readfirstlane(sq.tile0);
     if (a.slots && len <= a.few) return;
     const int NC = (len + CHUNK - 1) / CHUNK;
-    const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     // the first state: of a pool's slot, given, or zeros
-    f32x4 S[TW][CT];
     const size_t head = ((size_t)s * a.V + hv) * D * D;
     const float* from = nullptr;
     float* to = nullptr;
@@ -91,46 +87,63 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         from = a.state_in ? a.state_in + head : nullptr;
         to = a.state_out ? a.state_out + head : nullptr;
     }
-#pragma unroll
-    for (int t = 0; t < TW; ++t)
-#pragma unroll
-        for (int x = 0; x < CT; ++x)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[t][x][j] = chain && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
-
-    // the powers of two of the columns: down for what comes in, up for what goes out
-    float down[CT], up[CT];
-#pragma unroll
-    for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
-    if constexpr (HALF) {
-        float* const xs = reinterpret_cast<float*>(smem + L::X);
-        const float* const most = (BACK ? a.gmost : a.vmost) + ((size_t)tile0 * a.V + hv) * 8 + part * CT;
-#pragma unroll
-        for (int x = 0; x < CT; ++x) {
-            float m = 0.f;
-            for (int i = tid; i < NC; i += 512) m = fmaxf(m, most[(size_t)i * a.V * 8 + x]);
-#pragma unroll
-            for (int t = 0; t < TW; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) m = fmaxf(m, delta_finite(S[t][x][j]));
-#pragma unroll
-            for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
-            if (lane == 0) xs[x * 8 + wave] = m;
-        }
+    // fp16's range leaves a state, its predictions' errors and U room to grow to 1000 times the largest value that comes in, ample for unit keys (whose steps change a state
+    // by no more than 2 |v|) unless thousands of tokens push the same way.  Where an operand went past its end all the same, the sequence is walked again with 2^8 or 2^16
+    // times the room; if neither helps, a value that came in was not finite, and the first powers stand.
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 3, n = lane & 15, g = lane >> 4;
+    const bool chain = wave < 4;
+    const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
+    int attempt = 0;
+    auto walk_again = [&]() {      // all waves ask, behind their last chunk
+        if constexpr (!HALF) return false;
         __syncthreads();
+        const int4 past = *reinterpret_cast<const int4*>(smem + L::X + 128);
+        return __builtin_amdgcn_readfirstlane(past.x | past.y | past.z | past.w) != 0 && attempt++ < 3;
+    };
+    f32x4 S[TW][CT];
+    float down[CT], up[CT];
+    auto begin = [&](bool holds) {      // (a wave of the first four holds a part of the state)
 #pragma unroll
-        for (int x = 0; x < CT; ++x) {
-            float m = 0.f;
+        for (int t = 0; t < TW; ++t)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, xs[x * 8 + i]);
-            const int e = __builtin_amdgcn_readfirstlane(delta_exponent(m));
-            down[x] = delta_power(-e);
-            up[x] = delta_power(e);
-            if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
+            for (int x = 0; x < CT; ++x)
 #pragma unroll
-            for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
+                for (int j = 0; j < 4; ++j) S[t][x][j] = holds && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
+
+        // the powers of two of the columns: down for what comes in, up for what goes out
+#pragma unroll
+        for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
+        if constexpr (HALF) {
+            float* const xs = reinterpret_cast<float*>(smem + L::X);
+            const float* const most = (BACK ? a.gmost : a.vmost) + ((size_t)tile0 * a.V + hv) * 8 + part * CT;
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                float m = 0.f;
+                for (int i = tid; i < NC; i += 512) m = fmaxf(m, most[(size_t)i * a.V * 8 + x]);
+                if (holds)
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) m = fmaxf(m, delta_finite(S[t][x][j]));
+#pragma unroll
+                for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+                if (lane == 0) xs[x * 8 + wave] = m;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                float m = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = fmaxf(m, xs[x * 8 + i]);
+                const int e = __builtin_amdgcn_readfirstlane(delta_exponent(m)) + (attempt < 3 ? 8 * attempt : 0);
+                down[x] = delta_power(-e);
+                up[x] = delta_power(e);
+                if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
+#pragma unroll
+                for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
+            }
         }
-    }
+    };
 
     // an exchange area's fragment, slabs of one requested together (left to itself the compiler waits for each on its own), and one tile of a slab as operands into it
     auto frags = [&](int area, DeltaParts<C, NP> (&f)[CS][CT]) {
@@ -328,9 +341,9 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     // Who brings K and the numbers: the waves that wait for the others
     constexpr bool CHAIN_STAGES = BACK;
     UserFrag kt[2][RS];
-    f32x4 num[2] = {zero, zero};
-    const char *kn = at_first(kb, krow), *nn = reinterpret_cast<const char*>(a.rows) + unit0 * DELTA_ROWS * 256;
-    int kc = first;      // the chunk that they are at
+    f32x4 num[2];
+    const char *kn, *nn;
+    int kc;      // the chunk that they are at
     auto load_next = [&](UserFrag (&f)[RS], f32x4& w) {
         const int then = after(kc);
         kn = moved(kn, kc, then, dk);
@@ -343,13 +356,21 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         store_tile(next, kt[O], num[O]);
         load_next(kt[O], num[O]);
     };
-    if (chain == CHAIN_STAGES && NC > 0) {
+    auto begin_tile = [&]() {
+        if (NC == 0) return;
+        kn = at_first(kb, krow);
+        nn = reinterpret_cast<const char*>(a.rows) + unit0 * DELTA_ROWS * 256;
+        kc = first;
+        num[0] = num[1] = zero;
         load_tile(kn, nn, first, kt[0], num[0]);
         store_tile(first, kt[0], num[0]);
         load_next(kt[1], num[1]);
         load_next(kt[0], num[0]);
-    }
-    if (chain) {
+    };
+    if (chain) for (;;) {
+        begin(true);
+        if (CHAIN_STAGES) begin_tile();
+        float most_out = 0.f;
         DeltaParts<C, NP> A[2][CS];
         Value v[2][VN];
         const char *vn = at_first(vb, vrow), *an = ga + unit0 * TRI;
@@ -400,6 +421,9 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             times(A[T2], f, upright, U);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
+                if (HALF)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) most_out = fmaxf(most_out, fmaxf(fabsf(U[x][j]), fabsf(be[j] * U[x][j])));
                 if (!BACK) {      // (U: E at first)
                     if (MODE == DELTA_KEEP) put(one_part, L::O, wv, x, U[x]);
                     U[x] = be * U[x];
@@ -432,6 +456,18 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             put_state();
             if (CHAIN_STAGES) stage(std::integral_constant<int, 1 - T2>{}, next);
         });
+        if (HALF) {
+            bool past = most_out > 65504.f;
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int x = 0; x < CT; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) past |= (__float_as_uint(S[t][x][j]) & 0x7f800000u) == 0x7f800000u;
+            const bool any = __ballot(past) != 0;
+            if (lane == 0) reinterpret_cast<int*>(smem + L::X)[32 + wv] = any;
+        }
+        if (walk_again()) continue;
         if (to) {
 #pragma unroll
             for (int t = 0; t < TW; ++t)
@@ -440,7 +476,11 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) to[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] = S[t][x][j] * up[x];
         }
-    } else if (!BACK) {
+        return;
+    }
+    if (!BACK) for (;;) {
+        begin(false);
+        begin_tile();
         UserFrag Q[2][RS];
         Operand Qh[RS];
         DeltaParts<C, NP> M[2][CS];
@@ -487,7 +527,11 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             on += dv;
             stage(std::integral_constant<int, 1 - T2>{}, next);
         });
-    } else if (NC > 0) {
+        if (!walk_again()) return;
+    }
+    if (BACK) for (;;) {
+        begin(false);
+        if (NC > 0) {
         // Of the chunk that the first four waves come to next: M^T dO and Q^T diag(scale gamma) dO, in fp32.  The first goes out behind the second barrier (they have read
         // the one before), the second, held back, behind the first barrier of the next round.
         UserFrag qt[2][NK];
@@ -571,6 +615,8 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         // the last round, in which they are at the last chunk: nothing is left to bring (what it computes again nobody takes)
         if (NC & 1) round(std::integral_constant<int, 1>{}, NC, first + NC * step);
         else round(std::integral_constant<int, 0>{}, NC, first + NC * step);
+        }
+        if (!walk_again()) return;
     }
 }
 
