@@ -433,11 +433,12 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
  *                         have different slots (the state of one that is named twice is undefined; no fault).
  * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16: states and sums in fp32, products of fp16 operands.  q and k are operands as they are (below 65504 in magnitude, as scale q.k has to
- * be); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value that comes in, as one fp16 number, or, where
+ * be); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as one fp16 number, or, where
  * fp32 states are handed out (forward: state_out or a pool; backward: state_in), as the sum of two: states are off by some 1e-6 of their size, o and the 16-bit gradients by
  * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
- * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A state may grow to 1000 times what comes in; a sequence whose operands
- * outgrow fp16 is walked again with 2^8, then 2^16 times the room.  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
+ * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A sequence in which
+ * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
+ * below 2^-30 of the largest are lost.  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
  * log_f below -200 counts as -200; log_f > 0 is carried as it is.
  * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.

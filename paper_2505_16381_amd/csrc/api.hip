@@ -1150,7 +1150,7 @@ extern "C" path_status_t path_paged_plan(const int* cached, const int* new_token
 
 // ---- gated delta rule ----
 namespace {
-struct DeltaPlan { long long tiles; size_t p, m, rows, vmost, at, mt, sm, gm, em, ym, gmost, vex, gex, total; };
+struct DeltaPlan { long long tiles; size_t p, m, rows, at, mt, sm, gm, em, ym, vex, gex, total; };
 }  // namespace
 
 // Launches of fewer than 2^32 threads: 256 per tile and head, 4096 per sequence and value head (the states: 512 for each 16 columns).
@@ -1169,7 +1169,6 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
     take(p.p, units * tri);
     take(p.m, units * tri);
     take(p.rows, units * DELTA_ROWS * 64 * 4);
-    take(p.vmost, half * units * 8 * 4);
     if (training) {
         take(p.at, units * tri);
         take(p.mt, units * tri);
@@ -1177,7 +1176,6 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
         take(p.gm, units * d * d * es);
         take(p.em, units * d * 64 * es);
         take(p.ym, units * d * 64 * es);
-        take(p.gmost, half * units * 8 * 4);
         take(p.vex, half * nseq * V * 8 * 4);
         take(p.gex, half * nseq * V * 8 * 4);
     }
@@ -1216,7 +1214,6 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     a.p = ws + p.p; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
     a.at = ws + p.at; a.mt = ws + p.mt;
     a.sm = ws + p.sm; a.gm = ws + p.gm; a.em = ws + p.em; a.ym = ws + p.ym;
-    a.vmost = reinterpret_cast<float*>(ws + p.vmost); a.gmost = reinterpret_cast<float*>(ws + p.gmost);
     a.vex = reinterpret_cast<int*>(ws + p.vex); a.gex = reinterpret_cast<int*>(ws + p.gex);
     a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 2 : 1;      // (delta_parts.h)
     a.np_b = dt == PATH_F32 ? 1 : a.state_in ? 2 : 1;
@@ -1267,7 +1264,6 @@ extern "C" path_status_t path_delta_train_bwd(const void* q, const void* k, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int bf = dt == PATH_BF16;
     if (T == 0 && !d_state_in) return PATH_OK;
-    if (bf && T > 0 && !hip_ok(launch_delta_most(a, d, st), "delta rule, size of the gradient")) return PATH_ERR_HIP;
     if (!hip_ok(launch_delta_scan(a, d, bf, 2, st), "delta rule, gradients of the states")) return PATH_ERR_HIP;
     return T == 0 || hip_ok(launch_delta_grad(a, d, bf, st), "delta rule, gradients of the chunks") ? PATH_OK : PATH_ERR_HIP;
 }

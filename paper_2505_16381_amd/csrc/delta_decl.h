@@ -34,7 +34,6 @@ struct DeltaArgs {
     long long ks, kt, kh, vs, vt, vh, ss, st, sh;      // element strides of sequence, token and head: q, k; v, o; beta, log_f
     float scale;
     int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
-    float *vmost, *gmost;                      // per (tile, head) [8]: largest finite |v|, |d_o| of the chunk, of each 16 value indices
     void *p, *m, *at, *mt;                     // per (tile, head): P and M as operand fragments; training: the transposes of A and M
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
     // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], E and Y, [value index][token]: fp32, or fp16 over
@@ -78,7 +77,6 @@ __device__ __forceinline__ bool delta_tile(const DeltaArgs& a, int tile, int lan
 }
 
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream);
-hipError_t launch_delta_most(const DeltaArgs& a, int d, hipStream_t stream);      // gmost of d_o (bf16)
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream);      // 0: o; 1: o, and what the backward needs; 2: backwards
 hipError_t launch_delta_grad(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);

@@ -24,36 +24,6 @@ __device__ __forceinline__ f32x4 block_mma(const float* A, int bi, int bk, f32x4
 __device__ __forceinline__ f32x4 mma_user(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma_user(f32x4 a, f32x4 b, f32x4 c) { return DeltaOps<float>::mma(a, b, c); }
 
-// largest finite |x| of 64 rows of d values, of each 16 columns, by 256 threads
-template <int D> __device__ __forceinline__ void most_of(const bf16_t* x, long long ld, int rows, float* out, float (*red)[8], int tid) {
-    constexpr int PPR = D / 8;      // pieces of 8 columns; a thread's are all in one place
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 64 * PPR / 256; ++i) {
-        const int r = (tid + 256 * i) / PPR;
-        if (r < rows) {
-            const bf16x8 f = *reinterpret_cast<const bf16x8*>(x + r * ld + tid % PPR * 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, delta_finite((float)f[e]));
-        }
-    }
-    m = fmaxf(m, __shfl_xor(m, 1));
-#pragma unroll
-    for (int i = PPR; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
-    if ((tid & 63) < PPR && !(tid & 1)) red[tid >> 6][(tid & 63) >> 1] = m;
-    __syncthreads();
-    if (tid < D / 16) out[tid] = fmaxf(fmaxf(red[0][tid], red[1][tid]), fmaxf(red[2][tid], red[3][tid]));
-}
-
-template <int D> __global__ __launch_bounds__(256) void delta_most_kernel(DeltaArgs a) {
-    __shared__ float red[4][8];
-    const int tid = threadIdx.x, tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.V), hv = blockIdx.x - tile * a.V;
-    int s, c;
-    DeltaSeq sq;
-    if (!delta_tile(a, tile, tid & 63, s, c, sq)) return;
-    most_of<D>(static_cast<const bf16_t*>(a.d_o) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + (long long)c * CHUNK * a.vt, a.vt, sq.len - c * CHUNK, a.gmost + ((size_t)tile * a.V + hv) * 8, red, tid);
-}
-
 template <typename T, int NP>
 __device__ __forceinline__ void store_frags(const float* X, bool transposed, void* out, size_t unit, int tid) {
     typedef DeltaOps<T> P;
@@ -89,7 +59,7 @@ template <typename F, typename T> __device__ __forceinline__ F row_frag(const T*
 // Four waves to a chunk, 16 rows each; K and Q come from memory as operands (a wave's four tiles of K overlap the others' in L1).  Bound by the chain of its phases,
 // so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone.
 template <typename T, int D, int NPF, int NPB>      // NPB = 0: no transposes
-__global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaArgs a) {
     typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept
     typedef typename Tr<T>::Frag Frag;
     constexpr int SL = sizeof(T) == 2 ? 32 : 16, FE = 16 / (int)sizeof(T);
@@ -97,8 +67,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     float* const N = reinterpret_cast<float*>(smem);
     float* const M = N + 64 * DP_LF;
     float* const rows = M + 64 * DP_LF;
-    float(*const red)[8] = reinterpret_cast<float(*)[8]>(rows + DELTA_ROWS * 64);
-    float* const Lm = rows + DELTA_ROWS * 64 + 32;      // training only
+    float* const Lm = rows + DELTA_ROWS * 64;      // training only
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.V), hv = blockIdx.x - tile * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
     int s, c;
@@ -149,10 +118,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
             }
         }
     }
-    if constexpr (sizeof(T) == 2)
-        most_of<D>(static_cast<const bf16_t*>(a.v) + delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, a.vt, left, a.vmost + unit * 8, red, tid);
-    else
-        __syncthreads();
+    __syncthreads();
     {
         float bh[4], bl[4];
 #pragma unroll
@@ -244,7 +210,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
 
 template <typename T, int D, int NPF, int NPB>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    constexpr size_t bytes = (size_t)((NPB > 0 ? 3 : 2) * 64 * DP_LF + DELTA_ROWS * 64 + 32) * 4;
+    constexpr size_t bytes = (size_t)((NPB > 0 ? 3 : 2) * 64 * DP_LF + DELTA_ROWS * 64) * 4;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_prep_kernel<T, D, NPF, NPB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
     delta_prep_kernel<T, D, NPF, NPB><<<dim3((unsigned)a.tiles * a.V), dim3(256), bytes, stream>>>(a);
@@ -259,12 +225,6 @@ static hipError_t launch_d(const DeltaArgs& a, int is_bf16, bool training, hipSt
 }
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream) {
     return d == 64 ? launch_d<64>(a, is_bf16, training, stream) : launch_d<128>(a, is_bf16, training, stream);
-}
-hipError_t launch_delta_most(const DeltaArgs& a, int d, hipStream_t stream) {
-    const dim3 grid((unsigned)a.tiles * a.V);
-    if (d == 64) delta_most_kernel<64><<<grid, dim3(256), 0, stream>>>(a);
-    else delta_most_kernel<128><<<grid, dim3(256), 0, stream>>>(a);
-    return hipGetLastError();
 }
 
 }  // namespace path

@@ -87,64 +87,29 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         from = a.state_in ? a.state_in + head : nullptr;
         to = a.state_out ? a.state_out + head : nullptr;
     }
-    // fp16's range leaves a state, its predictions' errors and U room to grow to 1000 times the largest value that comes in, ample for unit keys (whose steps change a state
-    // by no more than 2 |v|) unless thousands of tokens push the same way.  Where an operand went past its end all the same, the sequence is walked again with 2^8 or 2^16
-    // times the room; if neither helps, a value that came in was not finite, and the first powers stand.
+    // Operands start at 2^6 at most and may grow to fp16's end; those that are kept for the gradients of a chunk to 2^12, which leaves their products a place there.  Where one went
+    // past that, the sequence is walked again over the largest value of all its chunks, or, if that is what it had, with 2^8 or 2^16 times the room (states about keys
+    // of length one move by 2 |v| a token at most).  If nothing helps, a value that came in was not finite, and the first powers that held the others stand.
+    constexpr int ROOM = MODE == DELTA_O ? 10 : 6;
+    constexpr float END = MODE == DELTA_O ? 65504.f : 4096.f;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 3, n = lane & 15, g = lane >> 4;
     const bool chain = wave < 4;
     const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
-    int attempt = 0;
-    auto walk_again = [&]() {      // all waves ask, behind their last chunk
+    int attempt = 0, first_e[CT];
+#pragma unroll
+    for (int x = 0; x < CT; ++x) first_e[x] = 0;
+    auto walk_again = [&](bool past) {      // all waves ask, behind their last chunk
         if constexpr (!HALF) return false;
+        const bool any = __ballot(past) != 0;
+        if (lane == 0) reinterpret_cast<int*>(smem + L::X)[32 + wave] = any;
         __syncthreads();
-        const int4 past = *reinterpret_cast<const int4*>(smem + L::X + 128);
-        return __builtin_amdgcn_readfirstlane(past.x | past.y | past.z | past.w) != 0 && attempt++ < 3;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n |= reinterpret_cast<const int*>(smem + L::X)[32 + i];
+        return __builtin_amdgcn_readfirstlane(n) != 0 && attempt++ < 3;
     };
     f32x4 S[TW][CT];
     float down[CT], up[CT];
-    auto begin = [&](bool holds) {      // (a wave of the first four holds a part of the state)
-#pragma unroll
-        for (int t = 0; t < TW; ++t)
-#pragma unroll
-            for (int x = 0; x < CT; ++x)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) S[t][x][j] = holds && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
-
-        // the powers of two of the columns: down for what comes in, up for what goes out
-#pragma unroll
-        for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
-        if constexpr (HALF) {
-            float* const xs = reinterpret_cast<float*>(smem + L::X);
-            const float* const most = (BACK ? a.gmost : a.vmost) + ((size_t)tile0 * a.V + hv) * 8 + part * CT;
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {
-                float m = 0.f;
-                for (int i = tid; i < NC; i += 512) m = fmaxf(m, most[(size_t)i * a.V * 8 + x]);
-                if (holds)
-#pragma unroll
-                for (int t = 0; t < TW; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) m = fmaxf(m, delta_finite(S[t][x][j]));
-#pragma unroll
-                for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
-                if (lane == 0) xs[x * 8 + wave] = m;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int x = 0; x < CT; ++x) {
-                float m = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) m = fmaxf(m, xs[x * 8 + i]);
-                const int e = __builtin_amdgcn_readfirstlane(delta_exponent(m)) + (attempt < 3 ? 8 * attempt : 0);
-                down[x] = delta_power(-e);
-                up[x] = delta_power(e);
-                if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
-#pragma unroll
-                for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
-            }
-        }
-    };
-
     // an exchange area's fragment, slabs of one requested together (left to itself the compiler waits for each on its own), and one tile of a slab as operands into it
     auto frags = [&](int area, DeltaParts<C, NP> (&f)[CS][CT]) {
 #pragma unroll
@@ -191,6 +156,69 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         for (int i = 0, c = first; i < NC; i += 2, c += 2 * step) {
             body(std::integral_constant<int, 0>{}, i, c);
             if (i + 1 < NC) body(std::integral_constant<int, 1>{}, i + 1, c + step);
+        }
+    };
+    // The first state, and the powers of two of the columns: down for what comes in, up for what goes out.  They are those of the first state and of the first chunk that holds anything
+    // but zeros (a look at all of V would read it twice); a sequence that outgrows them is walked again.
+    auto begin = [&](bool holds) {      // (a wave of the first four holds a part of the state)
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[t][x][j] = holds && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
+#pragma unroll
+        for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
+        if constexpr (HALF) {
+            float* const xs = reinterpret_cast<float*>(smem + L::X);
+            float m[CT], all[CT];
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                all[x] = m[x] = 0.f;
+                if (holds)
+#pragma unroll
+                    for (int t = 0; t < TW; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) m[x] = fmaxf(m[x], delta_finite(S[t][x][j]));
+            }
+            for (int i = 0, c = first; i < (NC > 0 ? NC : 1); ++i, c += step) {
+                if (NC > 0 && wave < 2 * CT) {      // a piece of eight columns to a thread
+                    const UserFrag f = delta_load16<UserFrag>(buffer(vb + (long long)c * CHUNK * vrow, vrow, c), tid / (2 * CT) * vrow + tid % (2 * CT) * 16);
+                    float y = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y = fmaxf(y, delta_finite((float)f[e]));
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) m[x] = fmaxf(m[x], CT == 1 || (lane >> 1 & 1) == x ? y : 0.f);
+                }
+#pragma unroll
+                for (int x = 0; x < CT; ++x) {
+#pragma unroll
+                    for (int z = 1; z < 64; z *= 2) m[x] = fmaxf(m[x], __shfl_xor(m[x], z));
+                    if (lane == 0) xs[x * 8 + wave] = m[x];
+                }
+                __syncthreads();
+                float any = 0.f;
+#pragma unroll
+                for (int x = 0; x < CT; ++x) {
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) all[x] = fmaxf(all[x], xs[x * 8 + z]);
+                    any = fmaxf(any, all[x]);
+                }
+                if (attempt == 0 && __builtin_amdgcn_readfirstlane(any > 0.f)) break;
+                __syncthreads();
+            }
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                int e = __builtin_amdgcn_readfirstlane(delta_exponent(all[x]));
+                if (attempt == 0) first_e[x] = e;
+                else if (attempt < 3) e += 8 * (attempt - (e > first_e[x]));
+                else if (e - first_e[x] <= ROOM) e = first_e[x];
+                down[x] = delta_power(-e);
+                up[x] = delta_power(e);
+                if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
+#pragma unroll
+                for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
+            }
         }
     };
     const unsigned row_at = P::row(wv, n) * krow + 16 * g;
@@ -456,18 +484,14 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             put_state();
             if (CHAIN_STAGES) stage(std::integral_constant<int, 1 - T2>{}, next);
         });
-        if (HALF) {
-            bool past = most_out > 65504.f;
+        bool past = most_out > END;
 #pragma unroll
-            for (int t = 0; t < TW; ++t)
+        for (int t = 0; t < TW; ++t)
 #pragma unroll
-                for (int x = 0; x < CT; ++x)
+            for (int x = 0; x < CT; ++x)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) past |= (__float_as_uint(S[t][x][j]) & 0x7f800000u) == 0x7f800000u;
-            const bool any = __ballot(past) != 0;
-            if (lane == 0) reinterpret_cast<int*>(smem + L::X)[32 + wv] = any;
-        }
-        if (walk_again()) continue;
+                for (int j = 0; j < 4; ++j) past |= (__float_as_uint(S[t][x][j]) & 0x7f800000u) == 0x7f800000u;
+        if (walk_again(past)) continue;
         if (to) {
 #pragma unroll
             for (int t = 0; t < TW; ++t)
@@ -527,10 +551,11 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             on += dv;
             stage(std::integral_constant<int, 1 - T2>{}, next);
         });
-        if (!walk_again()) return;
+        if (!walk_again(false)) return;
     }
     if (BACK) for (;;) {
         begin(false);
+        float most_out = 0.f;
         if (NC > 0) {
         // Of the chunk that the first four waves come to next: M^T dO and Q^T diag(scale gamma) dO, in fp32.  The first goes out behind the second barrier (they have read
         // the one before), the second, held back, behind the first barrier of the next round.
@@ -574,6 +599,9 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             load_slice(qn, then, qt[T2]);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
+                if (HALF)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) most_out = fmaxf(most_out, fabsf(V[x][j]));
                 put(one_part, L::O, wv, x, V[x]);
                 put(all_parts, L::OG, wv, x, V[x] * (ga4[T2] * a.scale));
             }
@@ -616,7 +644,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         if (NC & 1) round(std::integral_constant<int, 1>{}, NC, first + NC * step);
         else round(std::integral_constant<int, 0>{}, NC, first + NC * step);
         }
-        if (!walk_again()) return;
+        if (!walk_again(most_out > END)) return;
     }
 }
 
