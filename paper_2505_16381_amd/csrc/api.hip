@@ -1150,7 +1150,7 @@ extern "C" path_status_t path_paged_plan(const int* cached, const int* new_token
 
 // ---- gated delta rule ----
 namespace {
-struct DeltaPlan { long long tiles; size_t p, m, rows, at, mt, sm, gm, em, ym, vex, gex, total; };
+struct DeltaPlan { long long tiles; size_t p, m, rows, parts, at, mt, sm, gm, em, ym, vex, gex, total; };
 }  // namespace
 
 // Launches of fewer than 2^32 threads: 256 per tile and head, 4096 per sequence and value head (the states: 512 for each 16 columns).
@@ -1160,7 +1160,7 @@ static bool delta_shape_ok(int nseq, int T, int L, int H, int group, int d) {
     return V <= 65535 && nseq * V <= (1 << 19) && tiles * V < (1 << 23);
 }
 // tiles: a packed batch's; sequences of one length need no more (n ceil(L / 64) <= n L / 64 + n)
-static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool training) {
+static DeltaPlan delta_plan(int nseq, int T, int L, int V, int d, size_t es, bool training) {
     DeltaPlan p{};
     p.tiles = (long long)T / CHUNK + nseq;
     size_t off = 0;
@@ -1169,6 +1169,8 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
     take(p.p, units * tri);
     take(p.m, units * tri);
     take(p.rows, units * DELTA_ROWS * 64 * 4);
+    // What up to 4096 / d segments do to a state, two d x d matrices each (delta_segments).  All calls with sequences long enough have room for it: a smaller call must not need more than a larger one.
+    take(p.parts, L > (DELTA_CUT - 1) * CHUNK ? 2ull * 4096 * d * 4 : 0);
     if (training) {
         take(p.at, units * tri);
         take(p.mt, units * tri);
@@ -1184,7 +1186,7 @@ static DeltaPlan delta_plan(int nseq, int T, int V, int d, size_t es, bool train
 }
 extern "C" size_t path_delta_workspace_bytes(int nseq, int T, int max_len, int H, int group, int d, path_dtype_t dt, int training) {
     if ((dt != PATH_F32 && dt != PATH_BF16) || !delta_shape_ok(nseq, T, max_len, H, group, d)) return 0;
-    return delta_plan(nseq, T, H * group, d, dt == PATH_F32 ? 4 : 2, training != 0).total;
+    return delta_plan(nseq, T, max_len, H * group, d, dt == PATH_F32 ? 4 : 2, training != 0).total;
 }
 
 // The arguments' checks and everything in DeltaArgs that follows from sizes and workspace.
@@ -1197,7 +1199,7 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     a.V = a.H * a.G;
     a.NC = (int)(((long long)a.L + CHUNK - 1) / CHUNK);
     const size_t es = dt == PATH_F32 ? 4 : 2;
-    const DeltaPlan p = delta_plan(a.nseq, a.T, a.V, d, es, training);
+    const DeltaPlan p = delta_plan(a.nseq, a.T, a.L, a.V, d, es, training);
     if (workspace_bytes < p.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return PATH_ERR_WORKSPACE;
     a.tiles = a.cu ? (int)p.tiles : a.nseq * a.NC;
     const long long L = a.L, H = a.H, V = a.V;
@@ -1212,6 +1214,10 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     }
     char* const ws = static_cast<char*>(workspace);
     a.p = ws + p.p; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
+    a.parts = reinterpret_cast<float*>(ws + p.parts);
+    const long long chunks = ((long long)(a.L < a.T ? a.L : a.T) + CHUNK - 1) / CHUNK;
+    a.nseg = training ? 1 : delta_segments((long long)a.nseq * a.V, d, chunks);
+    a.seg = (int)((chunks + a.nseg - 1) / a.nseg);
     a.at = ws + p.at; a.mt = ws + p.mt;
     a.sm = ws + p.sm; a.gm = ws + p.gm; a.em = ws + p.em; a.ym = ws + p.ym;
     a.vex = reinterpret_cast<int*>(ws + p.vex); a.gex = reinterpret_cast<int*>(ws + p.gex);

@@ -18,6 +18,7 @@
 namespace path {
 
 constexpr int DELTA_FEW = 8;       // a sequence with up to so many new tokens is taken token by token (served calls)
+constexpr int DELTA_CUT = 36;      // sequences of so many chunks are cut into segments where heads are few
 constexpr int DELTA_ROWS = 5;      // numbers kept per token between the kernels: beta, gamma, rho, b rounded to 32 bits, and what that rounding left
 
 struct DeltaArgs {
@@ -33,6 +34,8 @@ struct DeltaArgs {
     int few;                                   // sequences of up to `few` tokens are not the chunk kernels'
     long long ks, kt, kh, vs, vt, vh, ss, st, sh;      // element strides of sequence, token and head: q, k; v, o; beta, log_f
     float scale;
+    int nseg, seg;                             // segments of the longest sequence, chunks of a segment (outputs alone; 1: sequences are not cut)
+    float* parts;                              // [nseq * V][nseg - 1][2][d][d]: what the segments do to a state
     int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
     void *p, *m, *at, *mt;                     // per (tile, head): P and M as operand fragments; training: the transposes of A and M
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
@@ -78,6 +81,7 @@ __device__ __forceinline__ bool delta_tile(const DeltaArgs& a, int tile, int lan
 
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream);
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream);      // 0: o; 1: o, and what the backward needs; 2: backwards
+int delta_segments(long long units, int d, long long chunks);
 hipError_t launch_delta_grad(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 

@@ -10,7 +10,7 @@
 
 namespace path {
 
-enum { DELTA_O = 0, DELTA_KEEP = 1, DELTA_BACK = 2 };      // forward; forward that keeps what the backward needs; backwards
+enum { DELTA_O = 0, DELTA_KEEP = 1, DELTA_BACK = 2, DELTA_PART = 3 };      // forward; forward that keeps what the backward needs; backwards; what segments do to a state
 
 template <typename T> struct DeltaOperand { typedef T type; };
 template <> struct DeltaOperand<bf16_t> { typedef half_t type; };
@@ -24,7 +24,7 @@ struct ScanLds {
     static constexpr bool BACK = MODE == DELTA_BACK, HALF = sizeof(T) == 2;
     // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the operand of the gradient's update, and Y to be kept); forward E, to be kept; backwards d_o
     // and diag(gamma) d_o as operands, and what they add up to, in fp32
-    static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (MODE != DELTA_O ? CS * CT * 1024 : 0);
+    static constexpr int AREA = CS * NP * CT * 1024, S = 0, Y = S + NS * NP * CT * 1024, U = Y + AREA, V = U + AREA, O = V + AREA, OG = O + (MODE == DELTA_KEEP || BACK ? CS * CT * 1024 : 0);
     static constexpr int DU = OG + (BACK ? AREA : 0), DG = DU + (BACK ? 4 * CT * 1024 : 0), X = DG + (BACK ? 4 * TW * CT * 1024 : 0);
     // K and the tokens' numbers, two chunks; a wave's own tokens of V (16-bit), its own columns of Q (backwards)
     static constexpr int KT = X + 256, NUM = KT + 2 * DeltaTile<C, D>::BYTES, VT = NUM + 2 * 768, QT = VT + (HALF ? (BACK ? 8 : 4) * CT * 512 : 0);
@@ -61,13 +61,25 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     constexpr int NS = L::NS, CS = L::CS, TW = L::TW, ES = sizeof(T);
     constexpr bool BACK = MODE == DELTA_BACK, HALF = ES == 2;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    // With few heads a sequence is cut into segments of `seg` chunks.  A segment does S -> A S + B: one launch walks all but the last from zeros, for B (the first one from the given state,
+    // whose copy it leaves in place of its A), and, of V = 0, from the unit matrix, for A; the next walks all at once, each from the state that those before it make.
+    constexpr bool PART = MODE == DELTA_PART;
+    const int nseg = MODE == DELTA_O ? a.nseg : PART ? a.nseg - 1 : 1, parts = D / 16 / CT;
     int unit, part;
-    if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, D / 16 / CT, a.nseq * a.V, unit, part)) return;
+    if (!xcd_deal(blockIdx.x >> 3, blockIdx.x & 7, parts * (PART ? 2 : 1), a.nseq * a.V * nseg, unit, part)) return;
+    const int at_seg = __builtin_amdgcn_readfirstlane(unit % nseg);
+    unit = __builtin_amdgcn_readfirstlane(unit / nseg);
+    const bool linear = PART && part >= parts;      // (the one for A)
+    if (linear) part -= parts;
     const int s = __builtin_amdgcn_readfirstlane(unit / a.V), hv = unit - s * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
     const DeltaSeq sq = delta_seq(a, s);
     const int len = __builtin_amdgcn_readfirstlane(sq.len), tile0 = __builtin_amdgcn_readfirstlane(sq.tile0);
     if (a.slots && len <= a.few) return;
-    const int NC = (len + CHUNK - 1) / CHUNK;
+    const int all = (len + CHUNK - 1) / CHUNK, c0 = MODE == DELTA_O || PART ? at_seg * a.seg : 0;
+    const bool last = MODE == DELTA_KEEP || BACK || all - c0 <= a.seg, cut = MODE == DELTA_O && all > a.seg;      // the sequence's last segment; it has others
+    if (at_seg > 0 && c0 >= all) return;
+    if (PART && last) return;
+    const int NC = last ? all - c0 : a.seg;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     // the first state: of a pool's slot, given, or zeros
@@ -87,11 +99,16 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         from = a.state_in ? a.state_in + head : nullptr;
         to = a.state_out ? a.state_out + head : nullptr;
     }
+    float* const joint = MODE == DELTA_O || PART ? a.parts + ((size_t)s * a.V + hv) * (a.nseg - 1) * 2 * D * D : nullptr;      // per segment B, A
+    if (PART && at_seg > 0) from = nullptr;
+    if (PART) to = joint + ((size_t)at_seg * 2 + linear) * D * D;
+    if (cut) from = joint + (at_seg > 0 ? 0 : D * D);      // (the given state itself may be overwritten by now)
+    if (!last && !PART) to = nullptr;
     // Operands start at 2^6 at most and may grow to fp16's end; those that are kept for the gradients of a chunk to 2^12, which leaves their products a place there.  Where one went
     // past that, the sequence is walked again over the largest value of all its chunks, or, if that is what it had, with 2^8 or 2^16 times the room (states about keys
     // of length one move by 2 |v| a token at most).  If nothing helps, a value that came in was not finite, and the first powers that held the others stand.
-    constexpr int ROOM = MODE == DELTA_O ? 10 : 6;
-    constexpr float END = MODE == DELTA_O ? 65504.f : 4096.f;
+    constexpr int ROOM = MODE == DELTA_KEEP || BACK ? 6 : 10;
+    constexpr float END = MODE == DELTA_KEEP || BACK ? 4096.f : 65504.f;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 3, n = lane & 15, g = lane >> 4;
     const bool chain = wave < 4;
     const int col = 16 * part * CT + n;      // the lane's value index (and + 16)
@@ -145,8 +162,19 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     const unsigned krow = (unsigned)a.kt * ES, vrow = (unsigned)a.vt * ES;
     // (Pointers to a chunk's rows and matrices move with the chunks: made anew by multiplications they took a fifth of a chunk's time.)
     auto buffer = [&](const char* p, unsigned row, int c) { return delta_buffer(p, len - c * CHUNK, row); };
-    const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : 0;
-    auto after = [&](int c) { const int y = c + step; return y >= 0 && y < NC ? y : c; };      // (behind the last chunk: that one again)
+    if (PART && linear && at_seg == 0) {
+        for (int t = 0; chain && t < TW; ++t)
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const size_t at = (size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x;
+                    to[at] = from ? from[at] : 0.f;
+                }
+        return;
+    }
+    const int step = BACK ? -1 : 1, first = BACK ? NC - 1 : c0;
+    auto after = [&](int c) { const int y = c + step; return y >= c0 && y < c0 + NC ? y : c; };      // (behind the last chunk: that one again)
     auto at_first = [&](const char* base, unsigned row) { return base + (long long)(first > 0 ? first : 0) * CHUNK * row; };
     const size_t unit0 = (size_t)(tile0 + (first > 0 ? first : 0)) * a.V + hv;
     constexpr int TRI = NP * P::NLOW * 1024;
@@ -158,6 +186,46 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             if (i + 1 < NC) body(std::integral_constant<int, 1>{}, i + 1, c + step);
         }
     };
+    // a later segment's first state: S <- A S + B over the segments before it, in fp32; S as operands by way of the exchange areas
+    auto joined = [&](bool holds) {
+        for (int i = 1; i < at_seg; ++i) {
+            const float* const B = joint + (size_t)i * 2 * D * D;
+            const float* const A = B + D * D;
+            if (holds) {
+                f32x4 m[TW][D / 16];
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int z = 0; z < D / 16; ++z) m[t][z] = *reinterpret_cast<const f32x4*>(A + (size_t)P::row(TW * wv + t, n) * D + P::row(z, 4 * g));
+                f32x4 y[TW][CT];
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) y[t][x][j] = B[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x];
+                        *reinterpret_cast<f32x4*>(smem + ((TW * wv + t) * CT + x) * 1024 + lane * 16) = S[t][x];
+                    }
+                __syncthreads();
+#pragma unroll
+                for (int z = 0; z < D / 16; ++z)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) {
+                        const f32x4 b = *reinterpret_cast<const f32x4*>(smem + (z * CT + x) * 1024 + lane * 16);
+#pragma unroll
+                        for (int t = 0; t < TW; ++t) y[t][x] = DeltaOps<float>::mma(m[t][z], b, y[t][x]);
+                    }
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) S[t][x] = y[t][x];
+                __syncthreads();
+            } else {
+                __syncthreads();
+                __syncthreads();
+            }
+        }
+    };
     // The first state, and the powers of two of the columns: down for what comes in, up for what goes out.  They are those of the first state and of the first chunk that holds anything
     // but zeros (a look at all of V would read it twice); a sequence that outgrows them is walked again.
     auto begin = [&](bool holds) {      // (a wave of the first four holds a part of the state)
@@ -167,6 +235,14 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             for (int x = 0; x < CT; ++x)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) S[t][x][j] = holds && from ? from[(size_t)P::row(TW * wv + t, 4 * g + j) * D + col + 16 * x] : 0.f;
+        if (PART && linear && at_seg > 0 && holds)
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+#pragma unroll
+                for (int x = 0; x < CT; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[t][x][j] = P::row(TW * wv + t, 4 * g + j) == col + 16 * x ? 1.f : 0.f;
+        if (cut) joined(holds);
 #pragma unroll
         for (int x = 0; x < CT; ++x) down[x] = up[x] = 1.f;
         if constexpr (HALF) {
@@ -182,7 +258,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                         for (int j = 0; j < 4; ++j) m[x] = fmaxf(m[x], delta_finite(S[t][x][j]));
             }
             for (int i = 0, c = first; i < (NC > 0 ? NC : 1); ++i, c += step) {
-                if (NC > 0 && wave < 2 * CT) {      // a piece of eight columns to a thread
+                if (NC > 0 && wave < 2 * CT && !linear) {      // a piece of eight columns to a thread
                     const UserFrag f = delta_load16<UserFrag>(buffer(vb + (long long)c * CHUNK * vrow, vrow, c), tid / (2 * CT) * vrow + tid % (2 * CT) * 16);
                     float y = 0.f;
 #pragma unroll
@@ -215,7 +291,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                 else if (e - first_e[x] <= ROOM) e = first_e[x];
                 down[x] = delta_power(-e);
                 up[x] = delta_power(e);
-                if (MODE != DELTA_O && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
+                if ((MODE == DELTA_KEEP || BACK) && tid == 0) (BACK ? a.gex : a.vex)[((size_t)s * a.V + hv) * 8 + part * CT + x] = e;
 #pragma unroll
                 for (int t = 0; t < TW; ++t) S[t][x] = S[t][x] * down[x];
             }
@@ -431,7 +507,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
             if (!BACK) {
                 const f32x4 ga4 = numbers(c, 1);
 #pragma unroll
-                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, V[x] - ga4 * y[x]);
+                for (int x = 0; x < CT; ++x) put(all_parts, L::Y, wv, x, (PART && linear ? zero : V[x]) - ga4 * y[x]);
             } else {      // dU = diag(rho) K G + M^T dO
                 const f32x4 rh = numbers(c, 2);
 #pragma unroll
@@ -456,7 +532,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                     if (MODE == DELTA_KEEP) put(one_part, L::O, wv, x, U[x]);
                     U[x] = be * U[x];
                     put(all_parts, L::U, wv, x, U[x] * w);
-                    put(all_parts, L::V, wv, x, U[x]);
+                    if (!PART) put(all_parts, L::V, wv, x, U[x]);
                 } else {      // (U: the gradient's Y)
                     put(one_part, L::V, wv, x, U[x]);
                     U[x] = be * U[x];
@@ -502,6 +578,17 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         }
         return;
     }
+    if (PART) for (;;) {
+        begin(false);
+        begin_tile();
+        in_turn([&](auto turn, int i, int c) {
+            lds_barrier();
+            lds_barrier();
+            lds_barrier();
+            stage(std::integral_constant<int, 1 - decltype(turn)::value>{}, after(c));
+        });
+        if (!walk_again(false)) return;
+    }
     if (!BACK) for (;;) {
         begin(false);
         begin_tile();
@@ -509,7 +596,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
         Operand Qh[RS];
         DeltaParts<C, NP> M[2][CS];
         const char *qn = at_first(qb, krow), *mn = gm + unit0 * TRI;
-        char* on = ob;
+        char* on = ob + c0 * dv;
         int ahead = first;
         if (NC > 0) {
             load_rows(qn, first, Q[0]);
@@ -653,13 +740,14 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
     typedef ScanLds<T, D, NP, CT, MODE> L;
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, NP, CT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
     if (attr != hipSuccess) return attr;
-    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(D / 16 / CT, a.nseq * a.V)), dim3(512), L::BYTES, stream>>>(a);
+    const int nseg = MODE == DELTA_O ? a.nseg : MODE == DELTA_PART ? a.nseg - 1 : 1, parts = D / 16 / CT * (MODE == DELTA_PART ? 2 : 1);
+    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(parts, a.nseq * a.V * nseg)), dim3(512), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D, int NP, int MODE>
 static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
     if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers)
-        if ((long long)a.nseq * a.V * (D / 32) >= 256) return launch<T, D, NP, 2, MODE>(a, stream);
+        if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 32) >= 256) return launch<T, D, NP, 2, MODE>(a, stream);
     return launch<T, D, NP, 1, MODE>(a, stream);
 }
 template <int D, int MODE>
@@ -667,9 +755,26 @@ static hipError_t launch_np(const DeltaArgs& a, int is_bf16, hipStream_t stream)
     if (!is_bf16) return launch_ct<float, D, 1, MODE>(a, stream);
     return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 2 ? launch_ct<bf16_t, D, 2, MODE>(a, stream) : launch_ct<bf16_t, D, 1, MODE>(a, stream);
 }
+template <int D> static hipError_t launch_mode(const DeltaArgs& a, int is_bf16, int mode, hipStream_t stream) {
+    if (mode == DELTA_KEEP) return launch_np<D, DELTA_KEEP>(a, is_bf16, stream);
+    if (mode == DELTA_BACK) return launch_np<D, DELTA_BACK>(a, is_bf16, stream);
+    if (a.nseg > 1)
+        if (const hipError_t e = launch_np<D, DELTA_PART>(a, is_bf16, stream)) return e;
+    return launch_np<D, DELTA_O>(a, is_bf16, stream);
+}
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream) {
-    if (d == 64) return mode == DELTA_O ? launch_np<64, DELTA_O>(a, is_bf16, stream) : mode == DELTA_KEEP ? launch_np<64, DELTA_KEEP>(a, is_bf16, stream) : launch_np<64, DELTA_BACK>(a, is_bf16, stream);
-    return mode == DELTA_O ? launch_np<128, DELTA_O>(a, is_bf16, stream) : mode == DELTA_KEEP ? launch_np<128, DELTA_KEEP>(a, is_bf16, stream) : launch_np<128, DELTA_BACK>(a, is_bf16, stream);
+    return d == 64 ? launch_mode<64>(a, is_bf16, mode, stream) : launch_mode<128>(a, is_bf16, mode, stream);
+}
+
+// Segments of sequences whose longest has `chunks`.  Heads are dealt to 8 XCDs of 32 CUs, a workgroup takes a CU: both launches are to fit at once.  Beyond the root of 0.6 times the chunks
+// the joining of states costs more than shorter segments gain, and two segments gain nothing.  Times in us, both launches and the matrices of the chunks, d = 128, one sequence:
+//   8 heads of 16384 tokens   1 segment 302, 3: 246, 5 (taken): 172, 6 (does not fit): 203       16 heads of 8192   1: 170, 3 (taken): 148, 4: 164
+//   4 heads of 4096           1: 82, 3: 74, 6 (taken): 60, 12: 74                                1 head of 2560    1: 55, 4 (taken): 50, 6: 47, 12: 56
+int delta_segments(long long units, int d, long long chunks) {
+    int n = 1;
+    if (chunks < DELTA_CUT) return 1;
+    while ((units * n + 7) / 8 * (d / 16) <= 32 && (units * (n + 1) + 7) / 8 * (d / 32) <= 32 && 10ll * (n + 1) * (n + 1) <= 6 * chunks) ++n;
+    return n >= 3 ? n : 1;
 }
 
 }  // namespace path

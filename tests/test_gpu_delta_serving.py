@@ -72,6 +72,14 @@ def test_heads_and_gates(gpu, H, G, gates, d):
     serve(gpu, [1, 5, 90, 2], [4, 0, 9, 1], H, G, d, "bf16", gates, seed=H)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_long_prompts(gpu, dtype):
+    """Prompts of few heads, cut into segments; beside short ones, in fresh, carried and no slots."""
+    serve(gpu, [2500, 1, 800, 0], [7, 7, 0, 7], 1, 2, 64, dtype, seed=1)
+    serve(gpu, [2500, 9, 2400], [0, 7, 7], 1, 1, 128, dtype, seed=2, slots=[3, -1, 0])
+    serve(gpu, [2400], [7], 1, 1, 64, dtype, seed=3, max_new=10000)
+
+
 def test_slots_that_are_none(gpu):
     """A sequence whose slot is outside the pool starts from zeros and is not kept."""
     serve(gpu, [1, 4, 70, 2, 80], [3, 3, 3, 3, 3], 2, 2, 64, slots=[-1, 2, 99, 0, 1], seed=3)
