@@ -20,10 +20,19 @@ __device__ __forceinline__ long long wave_sum(long long x) {
 }
 __device__ __forceinline__ int held(int x) { return x < 0 ? 0 : x; }
 
-// sum of x[0 .. n), not below 0 each, by a wave
-__device__ __forceinline__ long long sum_before(const int* x, int n, int lane) {
+// sum of x[0 .. n), not below 0 each, by a wave, N reads of a lane together
+template <int N> __device__ __forceinline__ long long sum_before(const int* x, int n, int lane) {
     long long y = 0;
-    for (int i = lane; i < n; i += 64) y += held(x[i]);
+    for (int i0 = 0; i0 < n; i0 += 64 * N) {
+        int v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0;
+            if (i0 + 64 * i < n) v[i] = x[i0 + 64 * i + lane < n ? i0 + 64 * i + lane : n - 1];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) y += i0 + 64 * i + lane < n ? held(v[i]) : 0;
+    }
     return wave_sum(y);
 }
 
@@ -42,15 +51,31 @@ __device__ __forceinline__ Row row_of(const PlanArgs& a, int s, long long start)
 __device__ __forceinline__ bool page_ok(const PlanArgs& a, int e) { return e >= 0 && e < a.num_pages; }
 __device__ __forceinline__ int free_at_first(const PlanArgs& a) { const int c = a.scratch[0]; return c < 0 ? 0 : c > a.num_pages ? a.num_pages : c; }
 
+// Entries j0 .. of a row, 64 apart per lane, N of a lane requested together.  One after the other, 2048 of them took 10 us, the latency of 32 reads, eight at a time 6; in the kernel of one workgroup, whose
+// rows are short, the longer code costs 1.5 us instead.
+template <int N> __device__ __forceinline__ void read_ahead(const PlanArgs& a, const Row& r, int j0, int lane, int (&e)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = j0 + 64 * i + lane;
+        e[i] = -1;
+        if (j0 + 64 * i < a.per_seq) e[i] = r.entries[j < a.per_seq ? j : a.per_seq - 1];
+    }
+}
+
 // What each sequence gives back and wants.
-__device__ void plan_count(const PlanArgs& a, int s, int lane) {
-    const Row r = row_of(a, s, sum_before(a.fresh, s, lane));
+template <int N> __device__ void plan_count(const PlanArgs& a, int s, int lane) {
+    const Row r = row_of(a, s, sum_before<N>(a.fresh, s, lane));
     int back = 0, need = 0;
-    for (int j = lane; j < a.per_seq; j += 64) {
-        if (j < r.have && j < r.want) continue;
-        const bool ok = page_ok(a, r.entries[j]);
-        back += ok && j >= r.want;
-        need += !ok && j >= r.have && j < r.want;
+    for (int j0 = (r.have < r.want ? r.have : r.want) / 64 * 64; j0 < a.per_seq; j0 += N * 64) {
+        int e[N];
+        read_ahead(a, r, j0, lane, e);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int j = j0 + 64 * i + lane;
+            const bool ok = page_ok(a, e[i]);
+            back += ok && j >= r.want && j < a.per_seq;
+            need += !ok && j >= r.have && j < r.want;
+        }
     }
     back = wave_sum(back);
     need = wave_sum(need);
@@ -63,26 +88,30 @@ __device__ void plan_count(const PlanArgs& a, int s, int lane) {
     }
 }
 // Pages go back.  (Entries that are no page, and what finds no room on the stack, go nowhere.)
-__device__ void plan_back(const PlanArgs& a, int s, int lane) {
+template <int N> __device__ void plan_back(const PlanArgs& a, int s, int lane) {
     const Row r = row_of(a, s, a.cu[s]);      // (held already: the same pages)
-    long long at = free_at_first(a) + sum_before(a.scratch + 1, s, lane);
-    for (int j0 = r.want / 64 * 64; j0 < a.per_seq; j0 += 64) {
-        const int j = j0 + lane;
-        const bool mine = j >= r.want && j < a.per_seq;
-        const int e = mine ? r.entries[j] : -1;
-        const unsigned long long ok = __ballot(mine && page_ok(a, e));
-        if (mine && page_ok(a, e)) {
-            const long long place = at + __popcll(ok & ((1ull << lane) - 1));
-            if (place < a.num_pages) a.free_pages[place] = e;
+    long long at = free_at_first(a) + sum_before<N>(a.scratch + 1, s, lane);
+    for (int j0 = r.want / 64 * 64; j0 < a.per_seq; j0 += N * 64) {
+        int e[N];
+        read_ahead(a, r, j0, lane, e);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int j = j0 + 64 * i + lane;
+            const bool mine = j >= r.want && j < a.per_seq, page = mine && page_ok(a, e[i]);
+            const unsigned long long ok = __ballot(page);
+            if (page) {
+                const long long place = at + __popcll(ok & ((1ull << lane) - 1));
+                if (place < a.num_pages) a.free_pages[place] = e[i];
+            }
+            if (mine && e[i] != -1) r.entries[j] = -1;
+            at += __popcll(ok);
         }
-        if (mine && e != -1) r.entries[j] = -1;
-        at += __popcll(ok);
     }
 }
 // Pages are taken.
-__device__ void plan_take(const PlanArgs& a, int s, int lane) {
+template <int N> __device__ void plan_take(const PlanArgs& a, int s, int lane) {
     const Row r = row_of(a, s, a.cu[s]);
-    const long long back = sum_before(a.scratch + 1, a.nseq, lane), before = sum_before(a.scratch + 1 + a.nseq, s, lane);
+    const long long back = sum_before<N>(a.scratch + 1, a.nseq, lane), before = sum_before<N>(a.scratch + 1 + a.nseq, s, lane);
     const long long all = free_at_first(a) + back, top = all < a.num_pages ? all : a.num_pages;
     const int need = a.scratch[1 + a.nseq + s];
     long long at = top - 1 - before;
@@ -128,20 +157,20 @@ __device__ void plan_map(const PlanArgs& a, long long t0, long long t1, int step
 
 __global__ __launch_bounds__(1024) void plan_small_kernel(PlanArgs a) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    for (int s = wv; s < a.nseq; s += 16) plan_count(a, s, lane);
+    for (int s = wv; s < a.nseq; s += 16) plan_count<1>(a, s, lane);
     __syncthreads();
-    for (int s = wv; s < a.nseq; s += 16) plan_back(a, s, lane);
+    for (int s = wv; s < a.nseq; s += 16) plan_back<1>(a, s, lane);
     __syncthreads();
-    for (int s = wv; s < a.nseq; s += 16) plan_take(a, s, lane);
+    for (int s = wv; s < a.nseq; s += 16) plan_take<1>(a, s, lane);
     __syncthreads();
     plan_map(a, threadIdx.x, a.T, 1024);
 }
 template <int PHASE> __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
     const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (s >= a.nseq) return;
-    if (PHASE == 0) plan_count(a, s, lane);
-    if (PHASE == 1) plan_back(a, s, lane);
-    if (PHASE == 2) plan_take(a, s, lane);
+    if (PHASE == 0) plan_count<8>(a, s, lane);
+    if (PHASE == 1) plan_back<8>(a, s, lane);
+    if (PHASE == 2) plan_take<8>(a, s, lane);
 }
 __global__ __launch_bounds__(256) void plan_map_kernel(PlanArgs a) {
     const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
