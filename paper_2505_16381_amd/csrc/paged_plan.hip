@@ -178,7 +178,9 @@ __global__ __launch_bounds__(256) void plan_map_kernel(PlanArgs a) {
 }
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t stream) {
-    if ((long long)a.nseq * a.per_seq <= 8192 && a.nseq <= 1024 && a.T <= 8192) {
+    // One workgroup has 16 waves, a row each: two rows to a wave are level with four launches (32 rows of 256 entries 10.7 us against 33 rows' 11.3 and three more starts, 16 of 64 6.3; 128 of 64 31 against
+    // 13, 512 of 16 148 against 15).
+    if ((long long)a.nseq * a.per_seq <= 8192 && a.nseq <= 32 && a.T <= 4096) {
         plan_small_kernel<<<dim3(1), dim3(1024), 0, stream>>>(a);
         return hipGetLastError();
     }
