@@ -433,7 +433,7 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
  *                         have different slots (the state of one that is named twice is undefined; no fault).
  * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16: states and sums in fp32, products of fp16 operands.  q and k are operands as they are (below 65504 in magnitude, as scale q.k has to
- * be); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as one fp16 number, or, where
+ * be; in steps of 2^-24); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as one fp16 number, or, where
  * fp32 states are handed out (forward: state_out or a pool; backward: state_in), as the sum of two: states are off by some 1e-6 of their size, o and the 16-bit gradients by
  * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
  * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A sequence in which

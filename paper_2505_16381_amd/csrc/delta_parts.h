@@ -7,8 +7,8 @@
 //     delta_row(t, m) = 32 (t / 2) + 8 (m / 4) + 4 (t % 2) + m % 4          (fp32: 16 t + m).
 //
 // With bf16 tensors the operands are fp16: q, k and what is computed from them as they are, and what hangs on v (states, U; backwards d_o, their gradients) over a power of two that
-// puts the largest finite value of the sequence, head and 16 columns between 32 and 64, so that values of any size have fp16's eleven bits (down to 2^-19 of the largest;
-// less below).  What is computed is multiplied as the sum of NP fp16 numbers, each the rounding of what the one before leaves.  NP = 1 (relative steps of 2^-12; o and gradients 4e-4 of their norm
+// puts the largest finite value of the first state and the first chunk, per sequence, head and 16 columns, between 32 and 64 (delta_scan.hip has what follows if later ones are larger), so
+// that values of any size have fp16's eleven bits (down to 2^-19 of the largest; less below).  What is computed is multiplied as the sum of NP fp16 numbers, each the rounding of what the one before leaves.  NP = 1 (relative steps of 2^-12; o and gradients 4e-4 of their norm
 // from 64 bits before they are rounded to bf16, which is 1.7e-3) where nothing but bf16 is handed out, NP = 2 (2^-23; 2e-7) where states are.  (Sums of bf16 numbers need two and three for
 // less, 5e-6 and 7e-8: forward of 4 x 16 heads, 8192 tokens, states 331 us.)
 #pragma once

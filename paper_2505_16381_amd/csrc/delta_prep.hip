@@ -57,7 +57,8 @@ template <typename F, typename T> __device__ __forceinline__ F row_frag(const T*
 }
 
 // Four waves to a chunk, 16 rows each; K and Q come from memory as operands (a wave's four tiles of K overlap the others' in L1).  Bound by the chain of its phases,
-// so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone.
+// so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone, and 128 registers (three of them spilled) let four in.  d = 128, 8192 tokens of 64 heads: 108 us, 3.5 TB/s
+// (K, Q in, P, M out: 378 MB); three workgroups 120.  With the transposes for training 158 us (three workgroups: a third matrix in LDS).
 template <typename T, int D, int NPF, int NPB>      // NPB = 0: no transposes
 __global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaArgs a) {
     typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept

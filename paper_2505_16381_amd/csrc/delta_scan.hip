@@ -4,6 +4,10 @@
 // with it the 16 tokens of one result tile; four more do what the chain of chunks does not wait for: the outputs (forward), and what d_o adds to dU and to the state's
 // gradient (backwards, a chunk ahead).  What one wave alone needs of K, Q, A and M comes from memory straight into its registers, a chunk ahead; what others need -- the
 // state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
+//
+// Bound by the latency of a chunk: two exchanges and four products that wait for one another.  d = 128, 64 heads of 8192 tokens, 32 columns: 211 us, 1.6 a chunk, 3.0 TB/s of its own traffic
+// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 342 us (1.05 GB), backwards 299 us (0.90 GB).  One wave per 16 columns and no exchange took three times as long
+// (64 dependent products a chunk); four waves for everything 314, since the outputs then stand in the chain; loads one chunk ahead 262.
 #include <type_traits>
 
 #include "delta_parts.h"
@@ -50,6 +54,19 @@ template <typename T> __device__ __forceinline__ void delta_store4(__amdgpu_buff
     else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), r, at, 0, 0);
 }
 
+// A packed batch's sequences in the order of their lengths, longest first (up to 64 of them; a whole wave asks): a long one that starts last would keep a few CUs busy alone.  16 heads of nine sequences
+// of 40 to 2999 tokens: 238 us in their own order, 212 in this (backwards 222, 198).
+__device__ __forceinline__ int delta_longest(const DeltaArgs& a, int turn, int lane) {
+    if (!a.cu || a.nseq == 1 || a.nseq > 64) return turn;
+    const int len = delta_seq(a, lane < a.nseq ? lane : 0).len;
+    int before = 0;
+    for (int i = 0; i < a.nseq; ++i) {
+        const int x = __builtin_amdgcn_readlane(len, i);
+        before += x > len || (x == len && i < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < a.nseq && before == turn));
+}
+
 template <typename T, int D, int NP, int CT, int MODE>
 __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     typedef typename DeltaOperand<T>::type C;
@@ -71,7 +88,8 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     unit = __builtin_amdgcn_readfirstlane(unit / nseg);
     const bool linear = PART && part >= parts;      // (the one for A)
     if (linear) part -= parts;
-    const int s = __builtin_amdgcn_readfirstlane(unit / a.V), hv = unit - s * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
+    const int turn = __builtin_amdgcn_readfirstlane(unit / a.V), s = delta_longest(a, turn, threadIdx.x & 63);
+    const int hv = unit - turn * a.V, hk = __builtin_amdgcn_readfirstlane(hv / a.G);
     const DeltaSeq sq = delta_seq(a, s);
     const int len = __builtin_amdgcn_readfirstlane(sq.len), tile0 = __builtin_amdgcn_readfirstlane(sq.tile0);
     if (a.slots && len <= a.few) return;
@@ -744,10 +762,12 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
     delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(parts, a.nseq * a.V * nseg)), dim3(512), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
+// 32 columns to a workgroup where those of 16 do not all find a CU: each chunk's K, Q and matrices then serve twice as many.  4096 tokens, d = 128, 16 against 32 columns, all kernels, us:
+// 32 heads 107 and 116 (training forward 148, 165), 48 heads 186 and 131 (259, 204), 64 heads 207 and 152 (309, 242).
 template <typename T, int D, int NP, int MODE>
 static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
     if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers)
-        if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 32) >= 256) return launch<T, D, NP, 2, MODE>(a, stream);
+        if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 16) > 256) return launch<T, D, NP, 2, MODE>(a, stream);
     return launch<T, D, NP, 1, MODE>(a, stream);
 }
 template <int D, int MODE>
