@@ -6,8 +6,8 @@
 // state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
 //
 // Bound by the latency of a chunk: two exchanges and four products that wait for one another.  d = 128, 64 heads of 8192 tokens, 32 columns: 211 us, 1.6 a chunk, 3.0 TB/s of its own traffic
-// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 342 us (1.05 GB), backwards 299 us (0.90 GB).  One wave per 16 columns and no exchange took three times as long
-// (64 dependent products a chunk); four waves for everything 314, since the outputs then stand in the chain; loads one chunk ahead 262.
+// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 342 us (1.05 GB), backwards 299 us (0.90 GB).  One wave per 16 columns, without exchanges (64 dependent products a
+// chunk), took 465 us, four waves for everything, over bf16 operands in more parts, 331, four more for the outputs and fp16 operands 256; loads one chunk ahead instead of two 262.
 #include <type_traits>
 
 #include "delta_parts.h"
