@@ -438,11 +438,11 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
  * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
- * below 2^-30 of the largest are lost.  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
+ * below 2^-30 of the largest are lost (in the gradients but dv: of the head's largest).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
  * log_f below -200 counts as -200; log_f > 0 is carried as it is.
  * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.
- * No atomics: the same bits every time.
+ * No atomics: the same bits every time.  Outputs overlap no input (state_out may be state_in).
  * workspace: path_delta_workspace_bytes(...) bytes (0 for sizes that are refused; training != 0 for the path_delta_train_* pair), 256-byte aligned; grows with every argument, so that one for the
  * largest call serves all smaller ones.
  * Errors: PATH_ERR_SHAPE for nseq, max_len, H or group < 1, T < 0, T != nseq * max_len without cu_seqlens, nseq * V > 2^19, (T / 64 + nseq) * V >= 2^23, V > 65535;

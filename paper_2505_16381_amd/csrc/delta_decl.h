@@ -67,12 +67,17 @@ __device__ __forceinline__ bool delta_tile(const DeltaArgs& a, int tile, int lan
     if (!a.cu) {
         s = __builtin_amdgcn_readfirstlane(tile / a.NC);
     } else {
-        int n = 0;
-        for (int s0 = 0; s0 < a.nseq; s0 += 64) {      // sequences whose first tile is not behind this one
-            const bool before = s0 + lane < a.nseq && delta_held(a.cu[s0 + lane < a.nseq ? s0 + lane : 0], a.T) / CHUNK + s0 + lane <= tile;
-            n += __popcll(__ballot(before));
-        }
-        s = n > 0 ? n - 1 : 0;
+        // the last sequence whose first tile is not behind this one, by 64 probes at a time: two reads that wait for one another for up to 4096 sequences
+        int lo = 0, n = a.nseq, step = 1;
+        do {
+            step = (n + 63) / 64;
+            const int i = lo + lane * step;
+            const bool before = lane * step < n && delta_held(a.cu[lane * step < n ? i : lo], a.T) / CHUNK + i <= tile;
+            const int k = __popcll(__ballot(before)), at = k > 0 ? (k - 1) * step : 0;
+            lo += at;
+            n = n - at < step ? n - at : step;
+        } while (step > 1);
+        s = lo;
     }
     q = delta_seq(a, s);
     c = tile - q.tile0;

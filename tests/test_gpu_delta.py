@@ -21,6 +21,7 @@ dbeta and dlog_f: r is the largest of the sequence's head where that is more tha
 |Y_t| |E_t|, and the last token has |Y| = |K G| = 7.8 and |E| up to 9.8 where the mean of |Y| over 130 tokens is 0.18 (one key for all tokens, gates of mean 1/2): 61 * 2^-24 = 3.6e-6 beside a
 mean dbeta of 0.21, of which 1e-5 is 2.1e-6.  Two rows of random values have |Y| |E| / sqrt(d) as their product, so the largest |dbeta| measures it.  dlog_f sums such products."""
 import math
+import random
 
 import pytest
 
@@ -150,6 +151,25 @@ def test_layouts(gpu, layout, d, dtype, G):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_without_gates_or_states(gpu, gates, state, d_state, dtype):
     train(gpu, [90, 130], 2, 2, 64, dtype, gates=gates, state=state, d_state=d_state, seed=4)
+
+
+@pytest.mark.parametrize("n", [64, 65, 300, 4200])
+def test_many_sequences(gpu, n):
+    """Chunks are found among as many sequences as there are: empty ones, short ones and some of several chunks."""
+    rng = random.Random(n)
+    lengths = [rng.choice([0, 0, 1, 2, 3]) for _ in range(n)]
+    for i in (0, 63, n // 2, n - 1):
+        lengths[i] = rng.choice([64, 65, 130])
+
+    # dlog_f of a sequence of one token is what is left of gamma <S, G> and what the token reads and writes, of which the first is a sum of 4096 products of 0.3 by 1, each off by
+    # 0.58 * sqrt(2) * 2^-12 (S and G as single fp16 numbers): 64 * 0.3 * 2e-4 = 3.8e-3 in deviation, 1.9e-2 at five of them, with as much from the others 2.7e-2.
+    # dbeta of one is a single Y.E with |Y| = |K G| = 8 and |E| = 8.4: 67 / 8 * 2e-4 = 1.7e-3, five of them 8.4e-3.
+    # fp32: 67 * 2^-24 for each factor; <S, G> is of the size of 64 * 0.3 = 19, off by 2^-24 of that for each of some 17 steps of its sum.
+    def check(torch, name, got, want, cu, f32):
+        close(torch, name, got, want, cu, f32, least={"dlog_f": 17 * 19 * 2 ** -24, "dbeta": 2 * 67 * 2 ** -24}.get(name, 1e-30) if f32 else {"dlog_f": 2.7e-2, "dbeta": 8.4e-3}.get(name, 1e-30))
+
+    train(gpu, lengths, 1, 2, 64, seed=n, check=check)
+    train(gpu, lengths, 1, 1, 64, "fp32", seed=n, check=check)
 
 
 def test_many_workgroups(gpu):
