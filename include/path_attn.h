@@ -422,7 +422,7 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  * Shapes: q, k, dq, dk [B,H,L,d], v, o, d_o, dv [B,V,L,d], beta, log_f, dbeta, dlog_f [B,V,L] (PATH_LAYOUT_BHLD), or the same with the token axis before the heads
  * (PATH_LAYOUT_BLHD), with nseq = B, max_len = L, T = B * L, cu_seqlens NULL; or packed: [T,H,d], [T,V,d], [T,V] (PATH_LAYOUT_BLHD), sequence s being the tokens
  * cu_seqlens[s] .. cu_seqlens[s+1]-1 (DEVICE int32 [nseq + 1], not decreasing), none longer than max_len; offsets and lengths past T and max_len are held to them.  Rows that belong to no sequence are left
- * as they are.  Sequences of no tokens: allowed.
+ * as they are.  Sequences of no tokens: allowed, T = 0 too (pointers to tokens may be NULL then).
  *   path_delta_fwd        o; state_in [nseq,V,d,d] = first states (NULL: zeros), state_out = last ones (NULL: not wanted; may be state_in).
  *   path_delta_train_fwd  the same, leaving in `workspace` what the gradients need.
  *   path_delta_train_bwd  gradients of sum(d_o * o) + sum(d_state_out * state_out) (d_state_out NULL: zeros), from the workspace of path_delta_train_fwd on the same
@@ -438,7 +438,7 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
  * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
- * below 2^-30 of the largest are lost (in the gradients but dv: of the head's largest).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
+ * below 2^-19 of the largest lose bits, below 2^-30 they are lost (in the gradients but dv by the head's largest, and where two such meet sooner).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
  * log_f below -200 counts as -200; log_f > 0 is carried as it is.
  * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.

@@ -1191,7 +1191,7 @@ extern "C" size_t path_delta_workspace_bytes(int nseq, int T, int max_len, int H
 
 // The arguments' checks and everything in DeltaArgs that follows from sizes and workspace.
 static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt, bool training, void* workspace, size_t workspace_bytes) {
-    if (!a.q || !a.k || !a.v || !a.beta || !workspace) return PATH_ERR_NULL;
+    if ((a.T != 0 && (!a.q || !a.k || !a.v || !a.beta)) || !workspace) return PATH_ERR_NULL;      // (a batch of no tokens carries its states on)
     if (dt != PATH_F32 && dt != PATH_BF16) return PATH_ERR_DTYPE;
     if (!delta_shape_ok(a.nseq, a.T, a.L, a.H, a.G, d)) return PATH_ERR_SHAPE;
     if (!layout_ok(layout) || !(a.scale > 0.f) || (a.cu && layout != PATH_LAYOUT_BLHD)) return PATH_ERR_UNSUPPORTED;
@@ -1227,7 +1227,7 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
 }
 
 static path_status_t delta_forward(DeltaArgs a, int d, int layout, path_dtype_t dt, bool training, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!a.o) return PATH_ERR_NULL;
+    if (a.T != 0 && !a.o) return PATH_ERR_NULL;
     if (const path_status_t e = delta_args(a, d, layout, dt, training, workspace, workspace_bytes)) return e;
     for (const void* ptr : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.state_in, (const void*)a.state_out}) if (misaligned(ptr)) return PATH_ERR_ALIGN;
     clear_inherited_error();
@@ -1262,7 +1262,7 @@ extern "C" path_status_t path_delta_train_bwd(const void* q, const void* k, cons
     a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_seqlens; a.state_in = state_in;
     a.d_o = d_o; a.d_state = d_state_out; a.dq = dq; a.dk = dk; a.dv = dv; a.dbeta = dbeta; a.dlog_f = dlog_f; a.d_state_in = d_state_in;
     a.nseq = nseq; a.T = T; a.L = max_len; a.H = H; a.G = group; a.scale = scale;
-    if (!d_o || !dq || !dk || !dv || !dbeta || !log_f != !dlog_f || !state_in != !d_state_in) return PATH_ERR_NULL;
+    if ((T != 0 && (!d_o || !dq || !dk || !dv || !dbeta || !log_f != !dlog_f)) || !state_in != !d_state_in) return PATH_ERR_NULL;
     if (const path_status_t e = delta_args(a, d, layout, dt, true, workspace, workspace_bytes)) return e;
     for (const void* ptr : {q, k, v, d_o, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)state_in, (const void*)d_state_out, (const void*)d_state_in})
         if (misaligned(ptr)) return PATH_ERR_ALIGN;

@@ -153,6 +153,23 @@ def test_without_gates_or_states(gpu, gates, state, d_state, dtype):
     train(gpu, [90, 130], 2, 2, 64, dtype, gates=gates, state=state, d_state=d_state, seed=4)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_no_tokens(gpu, dtype):
+    """A packed batch of empty sequences hands its states on, and their gradients back."""
+    torch, pa = gpu
+    y = to_gpu(dm.batch([0, 0], 2, 2, 64, dtype))
+    ins, how = [y[n] for n in ("q", "k", "v", "beta")], dict(log_f=y["log_f"], cu_seqlens=y["cu"], max_len=1)
+    assert y["q"].numel() == 0
+    o, last = pa.path_delta_fwd(*ins, state_in=y["state"], final_state=True, **how)
+    assert o.shape == y["v"].shape and torch.equal(last, y["state"])
+    assert (pa.path_delta_fwd(*ins, final_state=True, **how)[1] == 0).all() and pa.path_delta_fwd(*ins, **how).numel() == 0
+    ws = torch.empty(pa.path_delta_workspace_bytes(2, 0, 1, 2, 2, 64, 1 if dtype == "bf16" else 0, True), dtype=torch.uint8, device="cuda")
+    o, last = pa.path_delta_train_fwd(*ins, state_in=y["state"], final_state=True, workspace=ws, **how)
+    got = pa.path_delta_train_bwd(*ins, y["d_o"], ws, state_in=y["state"], d_state_out=y["d_state"], **how)
+    assert torch.equal(last, y["state"]) and torch.equal(got[-1], y["d_state"]) and all(t.numel() == 0 for t in got[:-1])
+    assert all(t.numel() == 0 for t in pa.path_delta_train_bwd(*ins, y["d_o"], ws, **how))
+
+
 @pytest.mark.parametrize("n", [64, 65, 300, 4200])
 def test_many_sequences(gpu, n):
     """Chunks are found among as many sequences as there are: empty ones, short ones and some of several chunks."""
