@@ -215,10 +215,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     if (GROUP)
 #pragma unroll
         for (int b = 0; b < RB; ++b) dq[b] = dk[b] = zero16();
-    // the wave's 32 columns of 64 rows: 16 bytes a lane, rows lane / 4 + 16 i
+    // the wave's 32 columns of 64 rows, from fragments of 16 rows (delta_scan.hip): 16 bytes a lane, rows lane / 4 + 16 i
     auto slice_rows = [&](const half_t* x, halfx8 (&f)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + (size_t)(lane / 4 + 16 * i) * D + lane % 4 * 8);
+        for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + i * CB * 512 + (lane % 4 * 16 + lane / 4) * 8);
     };
     auto slice_tokens = [&](const bf16_t* x, bf16x8 (&f)[4]) {
 #pragma unroll
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         const int l32 = lane & 31, h = lane >> 5;
         const size_t u = (size_t)tile * a.V + hv;
         const long long vat = delta_at(a, sq, s, a.vs, a.vt) + hv * a.vh + t0 * a.vt, sat = delta_at(a, sq, s, a.ss, a.st) + hv * a.sh + t0 * a.st;
-        const half_t *const sg = static_cast<const half_t*>(a.sm) + u * D * D + 32 * cb, *const gg = static_cast<const half_t*>(a.gm) + u * D * D + 32 * cb;
+        const half_t *const sg = static_cast<const half_t*>(a.sm) + u * D * D + 512 * cb, *const gg = static_cast<const half_t*>(a.gm) + u * D * D + 512 * cb;
         const half_t *const eg = static_cast<const half_t*>(a.em) + u * D * 64, *const yg = static_cast<const half_t*>(a.ym) + u * D * 64;
         const int *const vex = a.vex + ((size_t)s * a.V + hv) * 8, *const gex = a.gex + ((size_t)s * a.V + hv) * 8;
         int ev = vex[0], eq = gex[0];      // the largest exponents: of S and E, of G, Y and dO
@@ -279,9 +279,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         {
             halfx8 ef[NP], yf[NP];
             bf16x8 of[NP];
+            const int y = 32 * (wv & 1) + 8 * (lane >> 4);      // the first of the eight tokens of the thread's pieces of E and Y
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int p = tid + i * 256, r = p / (D / 8);
+                const int p = tid + i * 256, r = p / (D / 8);      // of dO; E and Y: fragments
                 ef[i] = *reinterpret_cast<const halfx8*>(eg + p * 8);
                 yf[i] = *reinterpret_cast<const halfx8*>(yg + p * 8);
 #pragma unroll
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             }
             slice_rows(sg, sf);
             slice_rows(gg, gf);
-            const f32x4 b0 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8), b1 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + (tid & 7) * 8 + 4);
+            const f32x4 b0 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + y), b1 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + y + 4);
             halfx8 be;      // of the eight tokens of the thread's pieces
 #pragma unroll
             for (int e = 0; e < 8; ++e) be[e] = (half_t)(e < 4 ? b0[e & 3] : b1[e & 3]);
@@ -299,8 +300,8 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             float db[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int p = tid + i * 256, r = p >> 3, y = (p & 7) * 8, ro = p / (D / 8), xo = p % (D / 8) * 8;
-                const halfx8 e1 = ef[i] * half_power(vex[r >> 4] - ev), y1 = yf[i] * half_power(gex[r >> 4] - eq);
+                const int p = tid + i * 256, vt = (wv >> 1) + 2 * i, r = 16 * vt + (lane & 15), ro = p / (D / 8), xo = p % (D / 8) * 8;
+                const halfx8 e1 = ef[i] * half_power(vex[vt] - ev), y1 = yf[i] * half_power(gex[vt] - eq);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) db[e] += (float)e1[e] * (float)y1[e];
                 *reinterpret_cast<halfx8*>(smem + C::U + 2 * TurnedTile<64>::at(r, y)) = e1 * be;
@@ -313,10 +314,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int z = 8; z < 64; z *= 2) db[e] += __shfl_xor(db[e], z);
-            if (lane < 8)
+                for (int z = 1; z < 16; z *= 2) db[e] += __shfl_xor(db[e], z);
+            if ((lane & 15) == 0)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dbs[wv * 64 + lane * 8 + e] = db[e];
+                for (int e = 0; e < 8; ++e) dbs[wv * 64 + y + e] = db[e];
         }
         __syncthreads();
 
@@ -511,7 +512,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 if (lane + z < 64) l += y;
             }
             if (lane < left) {
-                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)(((dbs[lane] + dbs[64 + lane]) + (dbs[128 + lane] + dbs[192 + lane])) * up);
+                static_cast<bf16_t*>(a.dbeta)[sat + lane * a.st] = (bf16_t)((dbs[(lane >> 5) * 64 + lane] + dbs[((lane >> 5) + 2) * 64 + lane]) * up);      // (of the two waves that have the token's half)
                 if (a.dlog_f) static_cast<bf16_t*>(a.dlog_f)[sat + lane * a.st] = (bf16_t)(l + ((kus[0] + kus[1]) + (kus[2] + kus[3])));
             }
         }
