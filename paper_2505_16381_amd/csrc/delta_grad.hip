@@ -215,10 +215,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     if (GROUP)
 #pragma unroll
         for (int b = 0; b < RB; ++b) dq[b] = dk[b] = zero16();
-    // the wave's 32 columns of 64 rows, from fragments of 16 rows (delta_scan.hip): 16 bytes a lane, rows lane / 4 + 16 i
+    // the wave's 32 columns of 64 rows, from fragments of 16 rows (delta_scan.hip): 16 bytes a lane, row lane % 16 + 16 i
     auto slice_rows = [&](const half_t* x, halfx8 (&f)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + i * CB * 512 + (lane % 4 * 16 + lane / 4) * 8);
+        for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const halfx8*>(x + i * CB * 512 + lane * 8);
     };
     auto slice_tokens = [&](const bf16_t* x, bf16x8 (&f)[4]) {
 #pragma unroll
@@ -255,6 +255,12 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<halfx8*>(slot + (lane / 4 + 16 * i) * 32 + lane % 4 * 8) = f[i];
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto frags_to_slot = [&](const halfx8 (&f)[4]) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<halfx8*>(slot + ((lane & 15) + 16 * i) * 32 + (lane >> 4) * 8) = f[i];
         __builtin_amdgcn_wave_barrier();
     };
 #pragma unroll 1
@@ -352,13 +358,12 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             for (int half = 0; half < D / 64; ++half) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = 64 * half + lane / 4 + 16 * i;
-                    sf[i] = sf[i] * half_power(vex[r >> 4] - ev);
-                    gf[i] = gf[i] * half_power(gex[r >> 4] - eq);
+                    sf[i] = sf[i] * half_power(vex[4 * half + i] - ev);
+                    gf[i] = gf[i] * half_power(gex[4 * half + i] - eq);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += (float)sf[i][e] * (float)gf[i][e];
                 }
-                to_slot(sf);
+                frags_to_slot(sf);
                 if (half + 1 < D / 64) slice_rows(sg + (size_t)64 * D, sf);
 #pragma unroll
                 for (int sl = 0; sl < 4; ++sl) {
@@ -377,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                         }
                     }
                 }
-                to_slot(gf);
+                frags_to_slot(gf);
                 if (half + 1 < D / 64) slice_rows(gg + (size_t)64 * D, gf);
 #pragma unroll
                 for (int sl = 0; sl < 4; ++sl) {
