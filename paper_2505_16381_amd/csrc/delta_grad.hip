@@ -189,8 +189,8 @@ template <int D> struct Grad16 {
 
 // ---- bf16: 32x32x16 products of fp16 operands; U, Y, dO (then Gq and Gk in its place) in LDS, S and G by way of 4 KB of a wave's own ----
 //
-// A wave has 32 key indices; two workgroups share a CU, so that one's loads stand beside the other's products.  Bound by memory: d = 128, 64 heads of 8192 tokens 440 us, 3.7 TB/s of its own traffic
-// (1.61 GB: S, G, E, Y, K, Q, dO in, dq, dk, dv out); 16 value heads of 8 key heads over 15000 tokens, whose groups of two add up in registers, 309 us.  With S and G whole in LDS (one workgroup
+// A wave has 32 key indices; two workgroups share a CU, so that one's loads stand beside the other's products.  Bound by memory: d = 128, 64 heads of 8192 tokens 407 to 450 us from run to run, 3.6 TB/s and more of its own traffic
+// (1.61 GB: S, G, E, Y, K, Q, dO in, dq, dk, dv out); 16 value heads of 8 key heads over 15000 tokens, whose groups of two add up in registers, 294 us.  With S and G whole in LDS (one workgroup
 // per CU) it took 1098 us, by way of a wave's own 4 KB 561, with row sums in registers that no index selects and gradients out by whole pieces 429.
 template <int D, bool GROUP>
 __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {

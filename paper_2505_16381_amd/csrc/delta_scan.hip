@@ -6,7 +6,7 @@
 // state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
 //
 // Bound by the latency of a chunk: two exchanges and four products that wait for one another.  d = 128, 64 heads of 8192 tokens, 32 columns: 211 us, 1.6 a chunk, 3.0 TB/s of its own traffic
-// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 342 us (1.05 GB), backwards 299 us (0.90 GB).  One wave per 16 columns, without exchanges (64 dependent products a
+// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 300 us (1.05 GB), backwards 293 us (0.90 GB).  One wave per 16 columns, without exchanges (64 dependent products a
 // chunk), took 465 us, four waves for everything, over bf16 operands in more parts, 331, four more for the outputs and fp16 operands 256; loads one chunk ahead instead of two 262.
 #include <type_traits>
 
@@ -55,7 +55,7 @@ template <typename T> __device__ __forceinline__ void delta_store4(__amdgpu_buff
 }
 
 // A packed batch's sequences in the order of their lengths, longest first (up to 64 of them; a whole wave asks): a long one that starts last would keep a few CUs busy alone.  16 heads of nine sequences
-// of 40 to 2999 tokens: 238 us in their own order, 212 in this (backwards 222, 198).
+// of 40 to 2999 tokens: 238 us in their own order, 212 in this (backwards 222, 198; both before what is kept went out as fragments).
 __device__ __forceinline__ int delta_longest(const DeltaArgs& a, int turn, int lane) {
     if (!a.cu || a.nseq == 1 || a.nseq > 64) return turn;
     const int len = delta_seq(a, lane < a.nseq ? lane : 0).len;
