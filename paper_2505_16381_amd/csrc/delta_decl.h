@@ -39,8 +39,8 @@ struct DeltaArgs {
     int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
     void *p, *m, *at, *mt;                     // per (tile, head): P and M as operand fragments; training: the transposes of A and M
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
-    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], E and Y, [value index][token]: fp32, or fp16 over
-    // the powers of two that the scans chose, per (sequence, head) and 16 value indices
+    // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], E and Y, [value index][token]: fp32 in rows, or fp16, over the powers of two that the scans
+    // chose per (sequence, head) and 16 value indices, in fragments of 16 value indices by 32: [d / 16][d / 32 or 2][lane][8]
     void *sm, *gm, *em, *ym;
     int *vex, *gex;                            // [nseq * V][8]: of S and E, of G and Y
     const void* d_o;
