@@ -307,11 +307,11 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int p = tid + i * 256, vt = (wv >> 1) + 2 * i, r = 16 * vt + (lane & 15), ro = p / (D / 8), xo = p % (D / 8) * 8;
-                const halfx8 e1 = ef[i] * half_power(vex[vt] - ev), y1 = yf[i] * half_power(gex[vt] - eq);
+                const halfx8 e1 = ef[i] * half_power(vex[vt] - ev), y1 = yf[i] * half_power(gex[vt] - eq);      // (Y goes to LDS over its own columns' power: dv is made of it)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) db[e] += (float)e1[e] * (float)y1[e];
                 *reinterpret_cast<halfx8*>(smem + C::U + 2 * TurnedTile<64>::at(r, y)) = e1 * be;
-                *reinterpret_cast<halfx8*>(smem + C::Y + 2 * TurnedTile<64>::at(r, y)) = y1;
+                *reinterpret_cast<halfx8*>(smem + C::Y + 2 * TurnedTile<64>::at(r, y)) = yf[i];
                 halfx8 o1;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o1[e] = (half_t)((float)of[i][e] * wo);
@@ -352,7 +352,6 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 wu[b] = (half_t)rows[128 + r];
                 q1[b] = rd[b] = wr[b] = zero16();
             }
-            const float wdv = delta_power(eq);
             bf16_t* const dvp = static_cast<bf16_t*>(a.dv) + vat;
 #pragma unroll 1
             for (int half = 0; half < D / 64; ++half) {
@@ -368,11 +367,14 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int sl = 0; sl < 4; ++sl) {
                     const halfx8 f = slot_frag(sl);
+                    const int ey = gex[4 * half + sl];      // of these 16 value indices
+                    const half_t hy = half_power(ey - eq);
+                    const float wdv = delta_power(ey);
 #pragma unroll
                     for (int b = 0; b < RB; ++b) {
                         const halfx8 y = u_frag(C::Y, rb0 + b, 4 * half + sl);
                         q1[b] = Tr<half_t>::mma(o_frag(rb0 + b, 4 * half + sl) * wg[b], f, q1[b]);
-                        rd[b] = Tr<half_t>::mma(y * wy[b], f, rd[b]);
+                        rd[b] = Tr<half_t>::mma(y * hy * wy[b], f, rd[b]);
                         if ((RB == 2 ? sl : sl & 1) == cb) {      // dv = beta Y: 8 value indices of the lane's token; the waves take turns
                             const int r = 32 * (rb0 + b) + l32;
                             bf16x8 v;
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
                 for (int sl = 0; sl < D / 16; ++sl) {
                     const halfx8 f = u_frag(C::U, bi, sl);
-                    acc = Tr<half_t>::mma(job < 3 ? u_frag(C::Y, br, sl) : o_frag(br, sl), f, acc);
+                    acc = Tr<half_t>::mma(job < 3 ? u_frag(C::Y, br, sl) * half_power(gex[sl] - eq) : o_frag(br, sl), f, acc);
                 }
                 const int i = 32 * bi + l32;
                 const float ih = rows[192 + i], il = rows[256 + i];
