@@ -433,10 +433,11 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
  *                         have different slots (the state of one that is named twice is undefined; no fault).
  * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16: states and sums in fp32, products of fp16 operands.  q and k are operands as they are (below 65504 in magnitude, as scale q.k has to
- * be; in steps of 2^-24); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as one fp16 number, or, where
- * fp32 states are handed out (forward: state_out or a pool; backward: state_in), as the sum of two: states are off by some 1e-6 of their size, o and the 16-bit gradients by
- * some 2e-3.  Single operands (11 bits) are rounded relative to the state, not to a step: with beta near 2 over near-equal keys, where a chunk's steps cancel, the error grows with
- * their number (to percents at 64 equal keys and beta = 2); two parts or PATH_F32 keep such states to 1e-4.  A sequence in which
+ * be; in steps of 2^-24); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as the sum of two
+ * fp16 numbers: states are off by some 1e-6 of their size, o and the 16-bit gradients by their own rounding and little more; o has the same bits whether states are handed out or not.  With beta near 2 over near-equal keys,
+ * where a chunk's steps cancel, the error grows with their number: states to 1e-4 at 64 equal keys and beta = 2.  What the gradients of a chunk start from (its state, the gradient behind it, E and Y of its tokens) is kept
+ * as one fp16 number each: before they are rounded dq, dk, dv and dbeta are off by up to 8e-4 of their norm, dlog_f, in which such sums cancel, by 6e-3 of its norm over keys whose products are 0.95 (beta near 2), and any of them by
+ * up to 64 steps of 2^-11 of a chunk's largest where all its tokens have one key and values that alternate. A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
  * below 2^-19 of the largest lose bits, below 2^-30 they are lost (in the gradients but dv by the head's largest, and where two such meet sooner).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
  * log_f below -200 counts as -200; log_f > 0 is carried as it is.

@@ -1221,8 +1221,6 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     a.at = ws + p.at; a.mt = ws + p.mt;
     a.sm = ws + p.sm; a.gm = ws + p.gm; a.em = ws + p.em; a.ym = ws + p.ym;
     a.vex = reinterpret_cast<int*>(ws + p.vex); a.gex = reinterpret_cast<int*>(ws + p.gex);
-    a.np_f = dt == PATH_F32 ? 1 : a.state_out || a.states ? 2 : 1;      // (delta_parts.h)
-    a.np_b = dt == PATH_F32 ? 1 : a.state_in ? 2 : 1;
     return PATH_OK;
 }
 

@@ -36,7 +36,6 @@ struct DeltaArgs {
     float scale;
     int nseg, seg;                             // segments of the longest sequence, chunks of a segment (outputs alone; 1: sequences are not cut)
     float* parts;                              // [nseq * V][nseg - 1][2][d][d]: what the segments do to a state
-    int np_f, np_b;                            // parts of the operands of the forward, and of those kept for the backward
     void *p, *m, *at, *mt;                     // per (tile, head): P and M as operand fragments; training: the transposes of A and M
     float* rows;                               // per (tile, head): [DELTA_ROWS][64]
     // training: per (tile, head) the state before the chunk and the gradient behind it, [value index][key index], E and Y, [value index][token]: fp32 in rows, or fp16, over the powers of two that the scans

@@ -8,9 +8,10 @@
 //
 // With bf16 tensors the operands are fp16: q, k and what is computed from them as they are, and what hangs on v (states, U; backwards d_o, their gradients) over a power of two that
 // puts the largest finite value of the first state and the first chunk, per sequence, head and 16 columns, between 32 and 64 (delta_scan.hip has what follows if later ones are larger), so
-// that values of any size have fp16's eleven bits (down to 2^-19 of the largest; less below).  What is computed is multiplied as the sum of NP fp16 numbers, each the rounding of what the one before leaves.  NP = 1 (relative steps of 2^-12; o and gradients 4e-4 of their norm
-// from 64 bits before they are rounded to bf16, which is 1.7e-3) where nothing but bf16 is handed out, NP = 2 (2^-23; 2e-7) where states are.  (Sums of bf16 numbers need two and three for
-// less, 5e-6 and 7e-8: forward of 4 x 16 heads, 8192 tokens, states 331 us.)
+// that values of any size have fp16's eleven bits (down to 2^-19 of the largest; less below).  What is computed is multiplied as the sum of NP = 2 fp16 numbers, the second
+// the rounding of what the first leaves (relative steps of 2^-23; o and gradients 2e-7 of their norm from 64 bits before they are rounded).  Single ones (2^-12) are rounded relative to the state and to P's
+// rows, not to a step of a token: 4e-4 of the norm over random keys and betas below 1, but 5e-3, three times bf16's own rounding, over keys whose products are 0.95 with betas near 2, and more the longer a
+// chunk's steps cancel.  (They took 304 us where two take 385: forward of 4 x 16 heads, 8192 tokens.  Sums of bf16 numbers need three for as much: states 331 us of 737 in all.)
 #pragma once
 #include "delta_decl.h"
 
@@ -19,6 +20,7 @@ namespace path {
 template <typename T> struct DeltaOps;
 template <> struct DeltaOps<half_t> {
     static constexpr int SL = 32, FE = 8, TPS = 2;      // contraction indices of a slab, elements of a fragment, result tiles that make a slab
+    static constexpr int NP = 2;                        // numbers that an operand is the sum of
     static constexpr int NLOW = 6;                      // fragments of a 64 x 64 lower (or upper) triangular operand
     typedef halfx8 Frag;
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -29,7 +31,7 @@ template <> struct DeltaOps<half_t> {
     static constexpr __device__ __forceinline__ int up_at(int t, int s) { return t < 2 ? 2 * t + s : 2 + t; }                 // t < 2: slabs 0, 1
 };
 template <> struct DeltaOps<float> {
-    static constexpr int SL = 16, FE = 4, TPS = 1, NLOW = 10;
+    static constexpr int SL = 16, FE = 4, TPS = 1, NP = 1, NLOW = 10;
     typedef f32x4 Frag;
     static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
 #pragma unroll

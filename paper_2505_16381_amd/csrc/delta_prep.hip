@@ -24,9 +24,10 @@ __device__ __forceinline__ f32x4 block_mma(const float* A, int bi, int bk, f32x4
 __device__ __forceinline__ f32x4 mma_user(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma_user(f32x4 a, f32x4 b, f32x4 c) { return DeltaOps<float>::mma(a, b, c); }
 
-template <typename T, int NP>
+template <typename T>
 __device__ __forceinline__ void store_frags(const float* X, bool transposed, void* out, size_t unit, int tid) {
     typedef DeltaOps<T> P;
+    constexpr int NP = P::NP;
     typename P::Frag* const dst = reinterpret_cast<typename P::Frag*>(out) + unit * NP * P::NLOW * 64;
     constexpr int NT = 64 / 16, NS = 64 / P::SL;
     for (int i = tid; i < P::NLOW * 64; i += 256) {
@@ -59,8 +60,8 @@ template <typename F, typename T> __device__ __forceinline__ F row_frag(const T*
 // Four waves to a chunk, 16 rows each; K and Q come from memory as operands (a wave's four tiles of K overlap the others' in L1).  Bound by the chain of its phases,
 // so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone, and 128 registers (three of them spilled) let four in.  d = 128, 8192 tokens of 64 heads: 108 us, 3.5 TB/s
 // (K, Q in, P, M out: 378 MB); three workgroups 120.  With the transposes for training 158 us (three workgroups: a third matrix in LDS).
-template <typename T, int D, int NPF, int NPB>      // NPB = 0: no transposes
-__global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaArgs a) {
+template <typename T, int D, bool TRAIN>      // TRAIN: the transposes, for the gradients
+__global__ __launch_bounds__(256, TRAIN ? 3 : 4) void delta_prep_kernel(DeltaArgs a) {
     typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept
     typedef typename Tr<T>::Frag Frag;
     constexpr int SL = sizeof(T) == 2 ? 32 : 16, FE = 16 / (int)sizeof(T);
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaA
                 const float w = ib <= wv ? expf((bh[j] - ih) + (bl[j] - il)) : 0.f, l = i < r ? w * kk[ib][j] : 0.f;
                 N[r * DP_LF + i] = l * be;
                 M[r * DP_LF + i] = i <= r ? a.scale * w * qk[ib][j] : 0.f;
-                if (NPB > 0) Lm[r * DP_LF + i] = l;
+                if (TRAIN) Lm[r * DP_LF + i] = l;
             }
         }
     }
@@ -183,10 +184,10 @@ __global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaA
         for (int j = 0; j < 4; ++j) N[(16 * bi + 4 * g + j) * DP_LF + 16 * bj + n] = -x[j];
     }
     __syncthreads();
-    store_frags<C, NPF>(N, false, a.p, unit, tid);
-    store_frags<C, NPF>(M, false, a.m, unit, tid);
-    if constexpr (NPB > 0) {
-        store_frags<C, NPB>(M, true, a.mt, unit, tid);
+    store_frags<C>(N, false, a.p, unit, tid);
+    store_frags<C>(M, false, a.m, unit, tid);
+    if constexpr (TRAIN) {
+        store_frags<C>(M, true, a.mt, unit, tid);
         // A = I - diag(beta) P L, rows 16 wv ..
         f32x4 x[4];
 #pragma unroll
@@ -205,24 +206,22 @@ __global__ __launch_bounds__(256, NPB > 0 ? 3 : 4) void delta_prep_kernel(DeltaA
                 N[r * DP_LF + i] = (r == i ? 1.f : 0.f) - rows[r] * x[bj][j];
             }
         __syncthreads();
-        store_frags<C, NPB>(N, true, a.at, unit, tid);
+        store_frags<C>(N, true, a.at, unit, tid);
     }
 }
 
-template <typename T, int D, int NPF, int NPB>
+template <typename T, int D, bool TRAIN>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    constexpr size_t bytes = (size_t)((NPB > 0 ? 3 : 2) * 64 * DP_LF + DELTA_ROWS * 64) * 4;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_prep_kernel<T, D, NPF, NPB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    constexpr size_t bytes = (size_t)((TRAIN ? 3 : 2) * 64 * DP_LF + DELTA_ROWS * 64) * 4;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_prep_kernel<T, D, TRAIN>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (attr != hipSuccess) return attr;
-    delta_prep_kernel<T, D, NPF, NPB><<<dim3((unsigned)a.tiles * a.V), dim3(256), bytes, stream>>>(a);
+    delta_prep_kernel<T, D, TRAIN><<<dim3((unsigned)a.tiles * a.V), dim3(256), bytes, stream>>>(a);
     return hipGetLastError();
 }
 template <int D>
 static hipError_t launch_d(const DeltaArgs& a, int is_bf16, bool training, hipStream_t stream) {
-    if (!is_bf16) return training ? launch<float, D, 1, 1>(a, stream) : launch<float, D, 1, 0>(a, stream);
-    if (!training) return a.np_f == 2 ? launch<bf16_t, D, 2, 0>(a, stream) : launch<bf16_t, D, 1, 0>(a, stream);
-    if (a.np_f == 2) return a.np_b == 2 ? launch<bf16_t, D, 2, 2>(a, stream) : launch<bf16_t, D, 2, 1>(a, stream);
-    return a.np_b == 2 ? launch<bf16_t, D, 1, 2>(a, stream) : launch<bf16_t, D, 1, 1>(a, stream);
+    if (!is_bf16) return training ? launch<float, D, true>(a, stream) : launch<float, D, false>(a, stream);
+    return training ? launch<bf16_t, D, true>(a, stream) : launch<bf16_t, D, false>(a, stream);
 }
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream) {
     return d == 64 ? launch_d<64>(a, is_bf16, training, stream) : launch_d<128>(a, is_bf16, training, stream);

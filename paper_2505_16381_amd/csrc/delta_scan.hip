@@ -19,11 +19,11 @@ enum { DELTA_O = 0, DELTA_KEEP = 1, DELTA_BACK = 2, DELTA_PART = 3 };      // fo
 template <typename T> struct DeltaOperand { typedef T type; };
 template <> struct DeltaOperand<bf16_t> { typedef half_t type; };
 
-template <typename T, int D, int NP, int CT, int MODE>
+template <typename T, int D, int CT, int MODE>
 struct ScanLds {
     typedef typename DeltaOperand<T>::type C;
     typedef DeltaOps<C> P;
-    static constexpr int NS = D / P::SL, CS = 64 / P::SL;                      // slabs of the state's rows, of a chunk
+    static constexpr int NP = P::NP, NS = D / P::SL, CS = 64 / P::SL;                      // slabs of the state's rows, of a chunk
     static constexpr int TW = D / 64;                                          // state tiles of a wave
     static constexpr bool BACK = MODE == DELTA_BACK, HALF = sizeof(T) == 2;
     // exchange areas: state; predictions' errors (dU); diag(rho) U, U (the operand of the gradient's update, and Y to be kept); forward E, to be kept; backwards d_o
@@ -67,15 +67,15 @@ __device__ __forceinline__ int delta_longest(const DeltaArgs& a, int turn, int l
     return __builtin_ctzll(__ballot(lane < a.nseq && before == turn));
 }
 
-template <typename T, int D, int NP, int CT, int MODE>
+template <typename T, int D, int CT, int MODE>
 __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     typedef typename DeltaOperand<T>::type C;
     typedef DeltaOps<C> P;
     typedef typename P::Frag Frag;
     typedef decltype(delta_operand(typename Tr<T>::Frag())) Operand;
     typedef typename Tr<T>::Frag UserFrag;
-    typedef ScanLds<T, D, NP, CT, MODE> L;
-    constexpr int NS = L::NS, CS = L::CS, TW = L::TW, ES = sizeof(T);
+    typedef ScanLds<T, D, CT, MODE> L;
+    constexpr int NP = P::NP, NS = L::NS, CS = L::CS, TW = L::TW, ES = sizeof(T);
     constexpr bool BACK = MODE == DELTA_BACK, HALF = ES == 2;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     // With few heads a sequence is cut into segments of `seg` chunks.  A segment does S -> A S + B: one launch walks all but the last from zeros, for B (the first one from the given state,
@@ -756,34 +756,33 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
     }
 }
 
-template <typename T, int D, int NP, int CT, int MODE>
+template <typename T, int D, int CT, int MODE>
 static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
-    typedef ScanLds<T, D, NP, CT, MODE> L;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, NP, CT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+    typedef ScanLds<T, D, CT, MODE> L;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&delta_scan_kernel<T, D, CT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
     if (attr != hipSuccess) return attr;
     const int nseg = MODE == DELTA_O ? a.nseg : MODE == DELTA_PART ? a.nseg - 1 : 1, parts = D / 16 / CT * (MODE == DELTA_PART ? 2 : 1);
-    delta_scan_kernel<T, D, NP, CT, MODE><<<dim3(xcd_deal_grid(parts, a.nseq * a.V * nseg)), dim3(512), L::BYTES, stream>>>(a);
+    delta_scan_kernel<T, D, CT, MODE><<<dim3(xcd_deal_grid(parts, a.nseq * a.V * nseg)), dim3(512), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
 // 32 columns to a workgroup where those of 16 do not all find a CU: each chunk's K, Q and matrices then serve twice as many.  4096 tokens, d = 128, 16 against 32 columns, all kernels, us:
 // 32 heads 107 and 116 (training forward 148, 165), 48 heads 186 and 131 (259, 204), 64 heads 207 and 152 (309, 242).
-template <typename T, int D, int NP, int MODE>
+template <typename T, int D, int MODE>
 static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
     if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers)
-        if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 16) > 256) return launch<T, D, NP, 2, MODE>(a, stream);
-    return launch<T, D, NP, 1, MODE>(a, stream);
+        if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 16) > 256) return launch<T, D, 2, MODE>(a, stream);
+    return launch<T, D, 1, MODE>(a, stream);
 }
 template <int D, int MODE>
-static hipError_t launch_np(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
-    if (!is_bf16) return launch_ct<float, D, 1, MODE>(a, stream);
-    return (MODE == DELTA_BACK ? a.np_b : a.np_f) == 2 ? launch_ct<bf16_t, D, 2, MODE>(a, stream) : launch_ct<bf16_t, D, 1, MODE>(a, stream);
+static hipError_t launch_type(const DeltaArgs& a, int is_bf16, hipStream_t stream) {
+    return is_bf16 ? launch_ct<bf16_t, D, MODE>(a, stream) : launch_ct<float, D, MODE>(a, stream);
 }
 template <int D> static hipError_t launch_mode(const DeltaArgs& a, int is_bf16, int mode, hipStream_t stream) {
-    if (mode == DELTA_KEEP) return launch_np<D, DELTA_KEEP>(a, is_bf16, stream);
-    if (mode == DELTA_BACK) return launch_np<D, DELTA_BACK>(a, is_bf16, stream);
+    if (mode == DELTA_KEEP) return launch_type<D, DELTA_KEEP>(a, is_bf16, stream);
+    if (mode == DELTA_BACK) return launch_type<D, DELTA_BACK>(a, is_bf16, stream);
     if (a.nseg > 1)
-        if (const hipError_t e = launch_np<D, DELTA_PART>(a, is_bf16, stream)) return e;
-    return launch_np<D, DELTA_O>(a, is_bf16, stream);
+        if (const hipError_t e = launch_type<D, DELTA_PART>(a, is_bf16, stream)) return e;
+    return launch_type<D, DELTA_O>(a, is_bf16, stream);
 }
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream) {
     return d == 64 ? launch_mode<64>(a, is_bf16, mode, stream) : launch_mode<128>(a, is_bf16, mode, stream);

@@ -48,3 +48,62 @@ def test_small_columns_of_a_head(gpu, down, d, dtype, G):
             close(torch, n, got[n][..., part], want[n][..., part], x["cu"].tolist(), dtype == "fp32")
     for n in ("dq", "dk", "dbeta", "dlog_f"):
         close(torch, n, got[n], want[n], x["cu"].tolist(), dtype == "fp32")
+
+
+def wide_betas(torch, x):
+    """beta = 2 sigmoid(N(2, 1)), as the attention's own inputs have it: half of all above 1.76."""
+    g = torch.Generator().manual_seed(5)
+    x["beta"] = (2 * torch.sigmoid(2 + torch.randn(x["beta"].shape, generator=g))).to(x["q"].dtype)
+
+
+def keys_alike(torch, x, part):
+    """Unit keys and queries whose products are `part` on average."""
+    g = torch.Generator().manual_seed(6)
+    m = torch.nn.functional.normalize(torch.randn(1, *x["k"].shape[1:], generator=g), dim=-1)
+    for n in ("q", "k"):
+        x[n] = torch.nn.functional.normalize(part ** 0.5 * m + (1 - part) ** 0.5 * x[n].float(), dim=-1).to(x["v"].dtype)
+
+
+@pytest.mark.parametrize("alike", [0.0, 0.7, 0.95])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("state", [True, False])
+def test_wide_betas_and_keys_alike(gpu, alike, d, state):
+    """Sums that cancel: betas near 2 over keys that resemble each other, no gates.  Bars on the root mean square of a head's error, beside what rounding the exact result once to bf16 makes of it (the two
+    are independent, their squares add up; a per cent for the draw of 4e4 values and more):
+      o               sums of products of operands of 22 bits; rows of P add up to 66 at most (two equal keys, beta 2, add 2 |E| a step), so 66 * 2^-22 * sqrt(8): 4.5e-5 of the norm, half of 1e-4.
+      dv              Y, kept as one fp16 number: at most 2^-11, over a binade 0.58 * 0.7 of that in deviation, 2e-4; and o's: 3e-4 at most.
+      dq, dk, dbeta   up to eight such roundings: 8e-4."""
+    torch, pa = gpu
+    x = dm.batch([640], 2, 1, d, seed=3)
+    wide_betas(torch, x)
+    x["log_f"][:] = 0
+    if alike:
+        keys_alike(torch, x, alike)
+    got, want = pair(gpu, x, d, 2, 1, state=state)
+    for n, bar in (("o", 1e-4), ("dv", 3e-4), ("dq", 8e-4), ("dk", 8e-4), ("dbeta", 8e-4)):
+        for h in range(2):
+            a, w = got[n][:, h].double().cpu(), want[n][:, h]
+            size = float(w.square().mean())
+            off, least = float((a - w).square().mean()) / size, float((w.bfloat16().double() - w).square().mean()) / size
+            assert off <= 1.01 ** 2 * least + bar ** 2, (n, h, off ** 0.5, least ** 0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_outputs_do_not_depend_on_whether_states_are_wanted(gpu, d):
+    """The same bits of o, from the forward and the training forward, with the last states handed out or not; also where the state is 3000 times the values that come in."""
+    torch, pa = gpu
+    from test_gpu_delta import pushes_one_way
+    x = dm.batch([1500, 70], 2, 1, d, seed=1)
+    pushes_one_way(torch, x)
+    k = torch.zeros(d)
+    k[: d // 4] = (d // 4) ** -0.5 if d == 64 else 0.17578125      # 16 of 1/4: of length one; 32 of 45/256: 0.9944
+    x["k"][:], x["q"][:] = k.bfloat16(), k.bfloat16()
+    for z in (dm.batch([130, 1, 700], 2, 2, d, seed=4), x):
+        y, G = to_gpu(z), z["v"].shape[1] // 2
+        ins, L = [y[n] for n in ("q", "k", "v", "beta")], 1500
+        how = dict(log_f=y["log_f"], cu_seqlens=y["cu"], max_len=L)
+        ws = lambda: poison(torch, pa, z, 2, G, d, L, "bf16", True)
+        o, _ = pa.path_delta_train_fwd(*ins, final_state=True, workspace=ws(), **how)
+        close(torch, "o", o, dm.forward(z, d ** -0.5)[0], z["cu"].tolist(), False)
+        for other in (pa.path_delta_train_fwd(*ins, workspace=ws(), **how), pa.path_delta_fwd(*ins, **how), pa.path_delta_fwd(*ins, final_state=True, **how)[0]):
+            assert torch.equal(other, o)
