@@ -440,7 +440,8 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  * up to 64 steps of 2^-11 of a chunk's largest where all its tokens have one key and values that alternate. A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
  * below 2^-19 of the largest lose bits, below 2^-30 they are lost (in the gradients but dv by the head's largest, and where two such meet sooner).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
- * log_f below -200 counts as -200; log_f > 0 is carried as it is.
+ * log_f below -200 counts as -200.  log_f > 0 is carried as it is where no run of successive tokens adds up to more than 3 (states that grow 20 times).  Past that, PATH_F32 and what is taken token by token go on
+ * to fp32's end, but PATH_BF16 by chunks holds what has grown, and the matrices of a chunk, in fp16: bits are lost with every doubling, gradients first, and from about 7 (gradients) and 11 on infinities and NaN come out.
  * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.
  * No atomics: the same bits every time.  Outputs overlap no input (state_out may be state_in).

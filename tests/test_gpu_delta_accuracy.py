@@ -107,3 +107,46 @@ def test_outputs_do_not_depend_on_whether_states_are_wanted(gpu, d):
         close(torch, "o", o, dm.forward(z, d ** -0.5)[0], z["cu"].tolist(), False)
         for other in (pa.path_delta_train_fwd(*ins, workspace=ws(), **how), pa.path_delta_fwd(*ins, **how), pa.path_delta_fwd(*ins, final_state=True, **how)[0]):
             assert torch.equal(other, o)
+
+
+def largest_states(torch, x, scale):
+    """The root mean square of each sequence's head's state, and of its gradient, where it is largest: [nseq,V,1,1] each."""
+    kept, cu, rms = [], x["cu"].tolist(), lambda t: t.square().mean((-1, -2), keepdim=True).sqrt()
+    dm.forward(x, scale, x["state"], kept)
+    G = x["v"].shape[1] // x["q"].shape[1]
+    q, k = (x[n].double().repeat_interleave(G, 1) for n in ("q", "k"))
+    beta, f, d_o = x["beta"].double(), torch.exp(x["log_f"].double()), x["d_o"].double()
+    states, grads = [], []
+    for s, (a, b) in enumerate(zip(cu, cu[1:])):
+        states.append(torch.stack([rms(t) for t in kept[a:b]]).amax(0))
+        g, sizes = x["d_state"][s].double(), []
+        for t in range(b - 1, a - 1, -1):
+            sizes.append(rms(g))
+            g = g + scale * q[t, :, :, None] * d_o[t, :, None]
+            g = f[t, :, None, None] * (g - k[t, :, :, None] * (beta[t, :, None] * torch.einsum("hij,hi->hj", g, k[t]))[:, None])
+        grads.append(torch.stack(sizes).amax(0))
+    return torch.stack(states), torch.stack(grads)
+
+
+@pytest.mark.parametrize("up,down,period", [(0.15, -0.16, 40), (0.3, -0.3, 14), (0.02, -0.02, 200), (0.43, -3.0, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("G", [1, 2])
+def test_gates_that_grow(gpu, up, down, period, d, dtype, G):
+    """log_f above zero for a while, and below for as long, no run of tokens adding up to more than 3: states and gradients grow up to e^3 times (within seven tokens, or twenty) and fall again.  The bars are
+    the usual ones; those of the states are relative to the largest that a head's state gets to in the sequence, for operands of two fp16 numbers end with fp16's smallest steps: an entry of P that has fallen
+    to e^-3 is off by 2^-25 as one of size one is, and is multiplied with rows that hang on the state at its largest."""
+    torch, pa = gpu
+    x = dm.batch([200, 70], 2, G, d, dtype, seed=13)
+    at = torch.arange(270)
+    rises = at % period < period // 2 if down > -3 else at % period < period - 1
+    x["log_f"][:] = torch.where(rises, up, down)[:, None].to(x["log_f"].dtype)
+    x["log_f"][:, 1] = 0
+    got, want = pair(gpu, x, d, 2, G, dtype)
+    sizes = dict(zip(("state", "d_state"), largest_states(torch, x, d ** -0.5)))
+    for n in got:
+        if n in sizes and dtype == "bf16":
+            off = (got[n].double().cpu() - want[n]).abs()
+            assert (off <= (1e-5 if n == "state" else 2e-5) * sizes[n]).all(), (n, float((off / sizes[n]).max()))
+        else:
+            close(torch, n, got[n], want[n], x["cu"].tolist(), dtype == "fp32")
