@@ -807,7 +807,8 @@ def _delta_fwd(name, q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, s
 def path_delta_fwd(q, k, v, beta, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, final_state=False, o=None, state_out=None,
                    workspace=None, stream=None):
     """Gated delta rule: q, k [B,H,L,d], v [B,H*group,L,d], beta (and log_f) [B,H*group,L], or with the tokens before the heads (``layout``), or packed [T,heads,d] with
-    cu_seqlens [nseq+1] (int32, on the GPU) and max_len, a bound on the lengths.  Returns o, and the last states [nseq,H*group,d,d] (fp32) with ``final_state`` or ``state_out``."""
+    cu_seqlens [nseq+1] (int32, on the GPU) and max_len, a bound on the lengths.  Returns o, and the last states [nseq,H*group,d,d] (fp32) with ``final_state`` or ``state_out``.  Rows of o that
+    belong to no sequence are left as they are."""
     return _delta_fwd("path_delta_fwd", q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, state_in, final_state, o, state_out, workspace, stream)
 
 
@@ -819,22 +820,32 @@ def path_delta_train_fwd(q, k, v, beta, log_f=None, scale=None, layout=PATH_LAYO
     return _delta_fwd("path_delta_train_fwd", q, k, v, beta, log_f, scale, layout, cu_seqlens, max_len, state_in, final_state, o, state_out, workspace, stream)
 
 
-def path_delta_train_bwd(q, k, v, beta, d_o, workspace, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, d_state_out=None, stream=None):
-    """(dq, dk, dv, dbeta[, dlog_f][, d_state_in]) from the workspace of path_delta_train_fwd on the same tensors; d_state_out: gradient of the last states."""
+def path_delta_train_bwd(q, k, v, beta, d_o, workspace, log_f=None, scale=None, layout=PATH_LAYOUT_BHLD, cu_seqlens=None, max_len=None, state_in=None, d_state_out=None, stream=None,
+                         dq=None, dk=None, dv=None, dbeta=None, dlog_f=None, d_state_in=None):
+    """(dq, dk, dv, dbeta[, dlog_f][, d_state_in]) from the workspace of path_delta_train_fwd on the same tensors; d_state_out: gradient of the last states.  Gradients that are not
+    given are made.  Rows that belong to no sequence are left as they are: a batch with such rows brings its own gradients, cleared."""
     import torch
+    if workspace is None:
+        raise ValueError("the workspace is the one that path_delta_train_fwd left: it has to be given")
+    if (dlog_f is not None and log_f is None) or (d_state_in is not None and state_in is None):
+        raise ValueError("dlog_f goes with log_f, d_state_in with state_in")
     nseq, T, L, H, G, d, layout, shapes = _delta_sizes(q, v, cu_seqlens, max_len, layout)
     dt, st = _dt_of(q), (nseq, H * G, d, d)
-    dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("d_state_out", d_state_out, st)], [("d_o", d_o, shapes[1])], shapes)
+    out = [("dq", dq, q, shapes[0]), ("dk", dk, k, shapes[0]), ("dv", dv, v, shapes[1]), ("dbeta", dbeta, beta, shapes[2])]
+    if log_f is not None:
+        out.append(("dlog_f", dlog_f, log_f, shapes[2]))
+    dev = _delta_look(q, k, v, beta, log_f, cu_seqlens, [("state_in", state_in, st), ("d_state_out", d_state_out, st), ("d_state_in", d_state_in, st)],
+                      [("d_o", d_o, shapes[1]), *[(name, t, shape) for name, t, _, shape in out if t is not None]], shapes)
     _scratch(workspace, None, None, q, stream, "q")
-    made = lambda like: _paged_made(like, like.shape, like.dtype, stream, True)
-    out = [made(q), made(k), made(v), made(beta)]
-    dlog_f = made(log_f) if log_f is not None else None
-    d_state_in = made(state_in) if state_in is not None else None
+    made = lambda t, like: _paged_made(like, like.shape, like.dtype, stream, True) if t is None else t
+    out = [made(t, like) for _, t, like, _ in out]
+    if state_in is not None:
+        d_state_in = made(d_state_in, state_in)
     if T > 0 or d_state_in is not None:
         _call_on(dev, "path_delta_train_bwd", (q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), _opt(log_f), _opt(cu_seqlens), _opt(state_in), d_o.data_ptr(), _opt(d_state_out),
-                                               *[x.data_ptr() for x in out], _opt(dlog_f), _opt(d_state_in), nseq, T, L, H, G, d, layout, float(d ** -0.5 if scale is None else scale), dt,
-                                               workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
-    return (*out, *[x for x in (dlog_f, d_state_in) if x is not None])
+                                               *[x.data_ptr() for x in out[:4]], out[4].data_ptr() if log_f is not None else None, _opt(d_state_in), nseq, T, L, H, G, d, layout,
+                                               float(d ** -0.5 if scale is None else scale), dt, workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
+    return (*out, d_state_in) if d_state_in is not None else tuple(out)
 
 
 def path_delta_extend(q, k, v, beta, states, slots, cached, cu_new, max_new, log_f=None, scale=None, o=None, workspace=None, stream=None):
