@@ -1278,7 +1278,7 @@ extern "C" path_status_t path_delta_extend(const void* q, const void* k, const v
     a.q = q; a.k = k; a.v = v; a.beta = beta; a.log_f = log_f; a.cu = cu_new; a.o = o; a.states = states; a.slots = slots; a.cached = cached; a.num_slots = num_slots;
     a.nseq = nseq; a.T = T; a.L = max_new; a.H = H; a.G = group; a.scale = scale;
     a.few = DELTA_FEW;
-    if (!states || !slots || !cached || !cu_new || !o) return PATH_ERR_NULL;
+    if (!states || !slots || !cached || !cu_new || (T != 0 && !o)) return PATH_ERR_NULL;
     if (const path_status_t e = delta_args(a, d, PATH_LAYOUT_BLHD, dt, false, workspace, workspace_bytes)) return e;
     if (num_slots < 1) return PATH_ERR_SHAPE;
     for (const void* ptr : {q, k, v, (const void*)o, (const void*)states}) if (misaligned(ptr)) return PATH_ERR_ALIGN;

@@ -22,3 +22,13 @@ def test_gradients_and_workspace_are_looked_at():
         pa.path_delta_train_bwd(*ins, ws, **{**how, "state_in": None}, d_state_in=torch.empty_like(x["state"]))
     with pytest.raises(ValueError, match="GPU"):
         pa.path_delta_train_bwd(*ins, ws, **how, dq=torch.empty_like(x["q"]))
+
+
+def test_an_empty_step_needs_no_tokens():
+    """T = 0: pointers to tokens may be NULL, for served calls too; what they carry on has to be there."""
+    import ctypes
+    at = 0x1000      # never read
+    call = lambda tokens, o, states=at, T=0: pa.load_library().path_delta_extend(*[tokens] * 4, tokens, states, at, at, at, o, 2, T, 10, 4, 2, 1, 64, ctypes.c_float(0.1), 1, at, 1 << 40, None)
+    assert call(None, None) == 0 and call(at, at) == 0
+    assert call(None, None, states=None) == 1
+    assert call(at, None, T=20) == 1 and call(None, at, T=20) == 1
