@@ -160,9 +160,9 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
 
 // ---- bf16: 32x32 products of fp16 operands of one part, over the powers of two of the scans ----
 //
-// A wave has 32 key indices of dq and dk, of all 64 tokens (d = 64: of 32).  E (as U), Y and dO are in LDS for everybody; the wave's columns of S, G, K and Q pass through
+// A wave has 32 key indices of dq and dk, of all 64 tokens (d = 64: of 32).  E, Y and dO are in LDS for everybody; the wave's columns of S, G, K and Q pass through
 // 4 KB of its own, half a state at a time, the next piece on its way in registers meanwhile: no barrier from the first product to the last but the two around Gq and Gk, and two
-// workgroups on a CU.  Factors of a token (gamma, beta, rho) are multiplied into the operand whose rows the tokens are.
+// workgroups on a CU.  Factors of a token (gamma, beta, rho) are multiplied into results, in 32 bits: into operands, each would be one rounding to 11 bits more, and gates above one could carry them past fp16's end.
 
 // sums over the 32 lanes of a half-wave of each of 16 values; lane l32 gets the value l32 / 2
 __device__ __forceinline__ float sum16(float (&v)[16], int l32) {
@@ -183,11 +183,12 @@ __device__ __forceinline__ half_t half_power(int e) { return e < -24 ? (half_t)0
 template <int D> struct Grad16 {
     static constexpr int RB = D / 64, CB = D / 32;                     // blocks of 32 tokens of a wave, of 32 key indices of a head
     static constexpr int TOK = 64 * D * 2, G2 = 64 * 64 * 2;            // bytes of a tokens' matrix, of Gq
-    static constexpr int U = 0, Y = TOK, O = 2 * TOK, SLOT = O + (TOK > 2 * G2 ? TOK : 2 * G2), ROWS = SLOT + 4 * 4096, RED = ROWS + DELTA_ROWS * 256;
+    static constexpr int E = 0, Y = TOK, O = 2 * TOK, SLOT = O + (TOK > 2 * G2 ? TOK : 2 * G2), ROWS = SLOT + 4 * 4096, RED = ROWS + DELTA_ROWS * 256;
     static constexpr int BYTES = RED + (4 * 64 + CB * 64 + 16) * 4;
+    static_assert(2 * G2 <= O - E, "the second parts of Gq and Gk lie in E's and Y's place");
 };
 
-// ---- bf16: 32x32x16 products of fp16 operands; U, Y, dO (then Gq and Gk in its place) in LDS, S and G by way of 4 KB of a wave's own ----
+// ---- bf16: 32x32x16 products of fp16 operands; E, Y, dO (then Gq and Gk in their place) in LDS, S and G by way of 4 KB of a wave's own ----
 //
 // A wave has 32 key indices; two workgroups share a CU, so that one's loads stand beside the other's products.  Bound by memory: d = 128, 64 heads of 8192 tokens 407 to 450 us from run to run, 3.6 TB/s and more of its own traffic
 // (1.61 GB: S, G, E, Y, K, Q, dO in, dq, dk, dv out); 16 value heads of 8 key heads over 15000 tokens, whose groups of two add up in registers, 294 us.  With S and G whole in LDS (one workgroup
@@ -195,7 +196,7 @@ template <int D> struct Grad16 {
 template <int D, bool GROUP>
 __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     typedef Grad16<D> C;
-    typedef TurnedLane<64> Lane;      // of U, Y, Gq, Gk
+    typedef TurnedLane<64> Lane;      // of E, Y, Gq, Gk
     constexpr int RB = C::RB, CB = C::CB, NP = 64 * D / 8 / 256;      // 16-byte pieces of a tokens' matrix per thread
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     float* const rows = reinterpret_cast<float*>(smem + C::ROWS);
@@ -297,10 +298,6 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             }
             slice_rows(sg, sf);
             slice_rows(gg, gf);
-            const f32x4 b0 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + y), b1 = *reinterpret_cast<const f32x4*>(a.rows + u * DELTA_ROWS * 64 + y + 4);
-            halfx8 be;      // of the eight tokens of the thread's pieces
-#pragma unroll
-            for (int e = 0; e < 8; ++e) be[e] = (half_t)(e < 4 ? b0[e & 3] : b1[e & 3]);
             for (int i = tid; i < DELTA_ROWS * 64; i += 256) rows[i] = a.rows[u * DELTA_ROWS * 64 + i];
             const float wo = delta_power(-eq);
             float db[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -310,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 const halfx8 e1 = ef[i] * half_power(vex[vt] - ev), y1 = yf[i] * half_power(gex[vt] - eq);      // (Y goes to LDS over its own columns' power: dv is made of it)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) db[e] += (float)e1[e] * (float)y1[e];
-                *reinterpret_cast<halfx8*>(smem + C::U + 2 * TurnedTile<64>::at(r, y)) = e1 * be;
+                *reinterpret_cast<halfx8*>(smem + C::E + 2 * TurnedTile<64>::at(r, y)) = e1;
                 *reinterpret_cast<halfx8*>(smem + C::Y + 2 * TurnedTile<64>::at(r, y)) = yf[i];
                 halfx8 o1;
 #pragma unroll
@@ -341,15 +338,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         f32x16 q1[RB], rd[RB], wr[RB];
         float sum = 0.f;      // <S, G>, over 2^(ev + eq)
         {
-            half_t wg[RB], wy[RB], wu[RB];      // of the lane's tokens
-            float bt[RB];
+            float bt[RB];      // beta of the lane's tokens
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const int r = 32 * (rb0 + b) + l32;
-                bt[b] = rows[r];
-                wg[b] = (half_t)rows[64 + r];
-                wy[b] = (half_t)(-rows[64 + r] * rows[r]);
-                wu[b] = (half_t)rows[128 + r];
+                bt[b] = rows[32 * (rb0 + b) + l32];
                 q1[b] = rd[b] = wr[b] = zero16();
             }
             bf16_t* const dvp = static_cast<bf16_t*>(a.dv) + vat;
@@ -373,8 +365,8 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
                     for (int b = 0; b < RB; ++b) {
                         const halfx8 y = u_frag(C::Y, rb0 + b, 4 * half + sl);
-                        q1[b] = Tr<half_t>::mma(o_frag(rb0 + b, 4 * half + sl) * wg[b], f, q1[b]);
-                        rd[b] = Tr<half_t>::mma(y * hy * wy[b], f, rd[b]);
+                        q1[b] = Tr<half_t>::mma(o_frag(rb0 + b, 4 * half + sl), f, q1[b]);
+                        rd[b] = Tr<half_t>::mma(y * hy, f, rd[b]);
                         if ((RB == 2 ? sl : sl & 1) == cb) {      // dv = beta Y: 8 value indices of the lane's token; the waves take turns
                             const int r = 32 * (rb0 + b) + l32;
                             bf16x8 v;
@@ -390,15 +382,16 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 for (int sl = 0; sl < 4; ++sl) {
                     const halfx8 f = slot_frag(sl);
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) wr[b] = Tr<half_t>::mma(u_frag(C::U, rb0 + b, 4 * half + sl) * wu[b], f, wr[b]);
+                    for (int b = 0; b < RB; ++b) wr[b] = Tr<half_t>::mma(u_frag(C::E, rb0 + b, 4 * half + sl), f, wr[b]);
                 }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 kr[4];
         slice_tokens(kp, kr);
-        // X and N of the lower 32x32 blocks
-        halfx8 res[2][2];
+        // X and N of the lower 32x32 blocks.  Gq and Gk are sums of two fp16 numbers: in dlog_f they add up, times products of keys, over pairs of tokens, and over keys alike those sums cancel where independent
+        // roundings of the pairs do not (single ones left dlog_f off by 6e-3 of its norm at products of 0.95).  The second parts take E's and Y's place.
+        halfx8 res[2][2], rest[2][2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
@@ -406,11 +399,11 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 f32x16 acc = zero16();
 #pragma unroll
                 for (int sl = 0; sl < D / 16; ++sl) {
-                    const halfx8 f = u_frag(C::U, bi, sl);
+                    const halfx8 f = u_frag(C::E, bi, sl);
                     acc = Tr<half_t>::mma(job < 3 ? u_frag(C::Y, br, sl) * half_power(gex[sl] - eq) : o_frag(br, sl), f, acc);
                 }
                 const int i = 32 * bi + l32;
-                const float ih = rows[192 + i], il = rows[256 + i];
+                const float ih = rows[192 + i], il = rows[256 + i], ib = rows[i];
 #pragma unroll
                 for (int j4 = 0; j4 < 16; j4 += 4) {
                     const int r0 = 32 * br + acc_row(j4, h);
@@ -418,24 +411,34 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         // (a power of two: its rounding and that of the exponent, 1e-5, are nothing beside the operand's; 2^-16: sums of 128 products stay far from fp16's end, one factor's growth included)
-                        const float w = __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f - 16.f);
+                        const float w = ib * __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f - 16.f);
                         const float y = job < 3 ? (i < r0 + j ? -rb[j] * w * acc[j4 + j] : 0.f) : (i <= r0 + j ? w * acc[j4 + j] : 0.f);
-                        res[n][j4 / 8][(j4 + j) % 8] = (half_t)y;
+                        const half_t y1 = (half_t)y;
+                        res[n][j4 / 8][(j4 + j) % 8] = y1;
+                        rest[n][j4 / 8][(j4 + j) % 8] = (half_t)(y - (float)y1);
                     }
                 }
             }
         }
-        __syncthreads();      // (dO has been read: Gq and Gk take its place)
+        __syncthreads();      // (E, Y and dO have been read: Gq and Gk take their places)
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
             if (job < 6) {
                 half_t* const to = reinterpret_cast<half_t*>(smem + C::O + (job < 3 ? C::G2 : 0));
+                half_t* const to2 = reinterpret_cast<half_t*>(smem + C::E + (job < 3 ? C::G2 : 0));
 #pragma unroll
-                for (int j = 0; j < 16; ++j) to[TurnedTile<64>::at(32 * br + acc_row(j, h), 32 * bi + l32)] = res[n][j / 8][j % 8];
+                for (int j = 0; j < 16; ++j) {
+                    const int i = TurnedTile<64>::at(32 * br + acc_row(j, h), 32 * bi + l32);
+                    to[i] = res[n][j / 8][j % 8];
+                    to2[i] = rest[n][j / 8][j % 8];
+                }
                 if (b == 1)      // the upper block
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) to[TurnedTile<64>::at(acc_row(j, h), 32 + l32)] = (half_t)0.f;
+                    for (int j = 0; j < 16; ++j) {
+                        const int i = TurnedTile<64>::at(acc_row(j, h), 32 + l32);
+                        to[i] = to2[i] = (half_t)0.f;
+                    }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -450,11 +453,18 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                kug += (float)slot[(32 * (rb0 + b) + acc_row(j, h)) * 32 + l32] * wr[b][j];
-                q1[b][j] *= 0x1p-16f;
-                rd[b][j] *= 0x1p-16f;
-                wr[b][j] *= 0x1p-16f;
+            for (int j4 = 0; j4 < 16; j4 += 4) {
+                const int r0 = 32 * (rb0 + b) + acc_row(j4, h);
+                const f32x4 be = *reinterpret_cast<const f32x4*>(rows + r0), ga = *reinterpret_cast<const f32x4*>(rows + 64 + r0), rh = *reinterpret_cast<const f32x4*>(rows + 128 + r0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j4 + e;
+                    wr[b][j] *= rh[e] * be[e];
+                    kug += (float)slot[(r0 + e) * 32 + l32] * wr[b][j];
+                    q1[b][j] *= 0x1p-16f * ga[e];
+                    rd[b][j] *= -0x1p-16f * ga[e] * be[e];
+                    wr[b][j] *= 0x1p-16f;
+                }
             }
         kug = (kug + (rb0 == 0 ? rows[64 + 63] * sum : 0.f)) * up;
 #pragma unroll
@@ -465,10 +475,15 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 const int br = rb0 + b;
                 // (Gq and Gk are lower triangular: 32 tokens are before or behind the others)
                 if (br == 1 || sl < 2) {
-                    q1[b] = Tr<half_t>::mma(nat(C::O, br, sl), f, q1[b]);
-                    rd[b] = Tr<half_t>::mma(nat(C::O + C::G2, br, sl), f, rd[b]);
+#pragma unroll
+                    for (const int part : {C::E, C::O}) {
+                        q1[b] = Tr<half_t>::mma(nat(part, br, sl), f, q1[b]);
+                        rd[b] = Tr<half_t>::mma(nat(part + C::G2, br, sl), f, rd[b]);
+                    }
                 }
-                if (br == 0 || sl >= 2) wr[b] = Tr<half_t>::mma(u_frag(C::O + C::G2, br, sl), f, wr[b]);
+                if (br == 0 || sl >= 2)
+#pragma unroll
+                    for (const int part : {C::E, C::O}) wr[b] = Tr<half_t>::mma(u_frag(part + C::G2, br, sl), f, wr[b]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -485,7 +500,9 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
             const halfx8 f = slot_frag(sl);
 #pragma unroll
             for (int b = 0; b < RB; ++b)
-                if (rb0 + b == 0 || sl >= 2) wr[b] = Tr<half_t>::mma(u_frag(C::O, rb0 + b, sl), f, wr[b]);
+                if (rb0 + b == 0 || sl >= 2)
+#pragma unroll
+                    for (const int part : {C::E, C::O}) wr[b] = Tr<half_t>::mma(u_frag(part, rb0 + b, sl), f, wr[b]);
         }
 #pragma unroll
         for (int b = 0; b < RB; ++b) {

@@ -109,6 +109,59 @@ def test_outputs_do_not_depend_on_whether_states_are_wanted(gpu, d):
             assert torch.equal(other, o)
 
 
+def gate_gradients(torch, x, head, rounded):
+    """dlog_f of a value head of one sequence whose length is a multiple of 64, by the chunks' formulas in 64 bits; `rounded`: what the chunks' gradients start from -- the state before, the gradient behind,
+    E and Y -- rounded to fp16 (over 2^-4: values of size one, as over their power of two)."""
+    G, d = x["v"].shape[1] // x["q"].shape[1], x["v"].shape[2]
+    q, k = (x[n][:, head // G].double() for n in ("q", "k"))
+    v, beta, log_f, d_o = (x[n][:, head].double() for n in ("v", "beta", "log_f", "d_o"))
+    kept = (lambda t: (16 * t).half().double() / 16) if rounded else (lambda t: t)
+    S, g, chunks, eye, out = torch.zeros(d, d).double(), torch.zeros(d, d).double(), [], torch.eye(64).double(), torch.zeros_like(beta)
+    for c in range(0, len(q), 64):
+        sl = slice(c, c + 64)
+        K, b = k[sl], torch.cumsum(log_f[sl], 0)
+        D = torch.exp(b[:, None] - b).tril()
+        L, M = (D * (K @ K.T)).tril(-1), d ** -0.5 * D * (q[sl] @ K.T)
+        P = torch.linalg.inv(eye + L * beta[sl])
+        E = P @ (v[sl] - torch.exp(b)[:, None] * (K @ S))
+        chunks.append((sl, b, D, L, M, P, S, E))
+        S = torch.exp(b[-1]) * S + K.T @ (torch.exp(b[-1] - b)[:, None] * (beta[sl, None] * E))
+    for sl, b, D, L, M, P, S, E in reversed(chunks):
+        K, Q, be, dO, gamma, rho = k[sl], q[sl], beta[sl, None], d_o[sl], torch.exp(b)[:, None], torch.exp(b[-1] - b)[:, None]
+        Y = (eye - be * (P @ L)).T @ (M.T @ dO + rho * (K @ g))
+        Sr, gr, Er, Yr = kept(S), kept(g), kept(E), kept(Y)
+        Gq, Gk = d ** -0.5 * (dO @ (be * Er).T * D).tril(), -(be * (Yr @ (be * Er).T) * D).tril(-1)
+        dq, read, UG = Gq @ K + d ** -0.5 * gamma * (dO @ Sr.T), Gk @ K - gamma * be * (Yr @ Sr.T), rho * (be * Er) @ gr.T
+        sums = (Q * dq).sum(1) + (K * (read - Gk.T @ K - Gq.T @ Q - UG)).sum(1)
+        out[sl] = torch.flip(torch.cumsum(torch.flip(sums, [0]), 0), [0]) + gamma[-1] * (Sr * gr).sum() + (K * UG).sum()
+        g = gamma[-1] * g + Q.T @ (d ** -0.5 * gamma * dO) - K.T @ (gamma * be * Y)
+    return out
+
+
+@pytest.mark.parametrize("beta", [1, 2])
+@pytest.mark.parametrize("alike", [0.7, 0.95])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2])
+def test_gradients_of_gates_over_keys_alike(gpu, beta, alike, d, G):
+    """dlog_f adds up Gq_ri (q_r . k_i) and Gk_ri (k_r . k_i) over the pairs i < t <= r of a chunk.  Over keys alike all products are near one and the pairs' weights cancel, so an independent error of each weight
+    does not: 2^-12 of them left 6e-3 of the result.  The bar: what rounding the state, its gradient, E and Y to single fp16 numbers, the only ones that are, makes of the result in 64 bits; 1.5 times that for another draw
+    of some 640 roundings and what two-part operands add (they are 2^11 times better), beside the result's own rounding and a tenth of it."""
+    torch, pa = gpu
+    x = dm.batch([640], 2, G, d, seed=3)
+    if beta == 2:
+        wide_betas(torch, x)
+    x["log_f"][:] = 0
+    keys_alike(torch, x, alike)
+    got, want = pair(gpu, x, d, 2, G, state=False)
+    for h in range(2 * G):
+        a, w = got["dlog_f"][:, h].double().cpu(), want["dlog_f"][:, h]
+        assert (gate_gradients(torch, x, h, False) - w).abs().max() <= 1e-10 * w.abs().max()
+        size = float(w.square().mean())
+        off, least = float((a - w).square().mean()) / size, float((w.bfloat16().double() - w).square().mean()) / size
+        kept = float((gate_gradients(torch, x, h, True) - w).square().mean()) / size
+        assert off <= 1.1 ** 2 * least + 1.5 ** 2 * kept, (h, off ** 0.5, least ** 0.5, kept ** 0.5)
+
+
 def largest_states(torch, x, scale):
     """The root mean square of each sequence's head's state, and of its gradient, where it is largest: [nseq,V,1,1] each."""
     kept, cu, rms = [], x["cu"].tolist(), lambda t: t.square().mean((-1, -2), keepdim=True).sqrt()
