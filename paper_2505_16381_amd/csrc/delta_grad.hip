@@ -391,7 +391,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         slice_tokens(kp, kr);
         // X and N of the lower 32x32 blocks.  Gq and Gk are sums of two fp16 numbers: in dlog_f they add up, times products of keys, over pairs of tokens, and over keys alike those sums cancel where independent
         // roundings of the pairs do not (single ones left dlog_f off by 6e-3 of its norm at products of 0.95).  The second parts take E's and Y's place.
-        halfx8 res[2][2], rest[2][2];
+        // (Those of a wave's first block wait in the 4 KB of its own.)
+        halfx8 res[4];      // first parts, second parts
+        halfx8* const parked = reinterpret_cast<halfx8*>(slot);
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
@@ -414,24 +417,30 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                         const float w = ib * __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f - 16.f);
                         const float y = job < 3 ? (i < r0 + j ? -rb[j] * w * acc[j4 + j] : 0.f) : (i <= r0 + j ? w * acc[j4 + j] : 0.f);
                         const half_t y1 = (half_t)y;
-                        res[n][j4 / 8][(j4 + j) % 8] = y1;
-                        rest[n][j4 / 8][(j4 + j) % 8] = (half_t)(y - (float)y1);
+                        res[j4 / 8][(j4 + j) % 8] = y1;
+                        res[2 + j4 / 8][(j4 + j) % 8] = (half_t)(y - (float)y1);
                     }
                 }
+                if (n == 0)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) parked[p * 64 + lane] = res[p];
             }
         }
         __syncthreads();      // (E, Y and dO have been read: Gq and Gk take their places)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 1; n >= 0; --n) {
             const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
+            if (n == 0)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) res[p] = parked[p * 64 + lane];
             if (job < 6) {
                 half_t* const to = reinterpret_cast<half_t*>(smem + C::O + (job < 3 ? C::G2 : 0));
                 half_t* const to2 = reinterpret_cast<half_t*>(smem + C::E + (job < 3 ? C::G2 : 0));
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int i = TurnedTile<64>::at(32 * br + acc_row(j, h), 32 * bi + l32);
-                    to[i] = res[n][j / 8][j % 8];
-                    to2[i] = rest[n][j / 8][j % 8];
+                    to[i] = res[j / 8][j % 8];
+                    to2[i] = res[2 + j / 8][j % 8];
                 }
                 if (b == 1)      // the upper block
 #pragma unroll
