@@ -1216,7 +1216,7 @@ static path_status_t delta_args(DeltaArgs& a, int d, int layout, path_dtype_t dt
     a.p = ws + p.p; a.m = ws + p.m; a.rows = reinterpret_cast<float*>(ws + p.rows);
     a.parts = reinterpret_cast<float*>(ws + p.parts);
     const long long chunks = ((long long)(a.L < a.T ? a.L : a.T) + CHUNK - 1) / CHUNK;
-    a.nseg = training ? 1 : delta_segments((long long)a.nseq * a.V, d, chunks);
+    a.nseg = training ? 1 : delta_segments((long long)a.nseq * a.V, d, dt == PATH_BF16, chunks);
     a.seg = (int)((chunks + a.nseg - 1) / a.nseg);
     a.at = ws + p.at; a.mt = ws + p.mt;
     a.sm = ws + p.sm; a.gm = ws + p.gm; a.em = ws + p.em; a.ym = ws + p.ym;

@@ -85,7 +85,7 @@ __device__ __forceinline__ bool delta_tile(const DeltaArgs& a, int tile, int lan
 
 hipError_t launch_delta_prep(const DeltaArgs& a, int d, int is_bf16, bool training, hipStream_t stream);
 hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, hipStream_t stream);      // 0: o; 1: o, and what the backward needs; 2: backwards
-int delta_segments(long long units, int d, long long chunks);
+int delta_segments(long long units, int d, int is_bf16, long long chunks);
 hipError_t launch_delta_grad(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaArgs& a, int d, int is_bf16, hipStream_t stream);
 

@@ -792,10 +792,12 @@ hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, h
 // the joining of states costs more than shorter segments gain, and two segments gain nothing.  Times in us, both launches and the matrices of the chunks, d = 128, one sequence:
 //   8 heads of 16384 tokens   1 segment 302, 3: 246, 5 (taken): 172, 6 (does not fit): 203       16 heads of 8192   1: 170, 3 (taken): 148, 4: 164
 //   4 heads of 4096           1: 82, 3: 74, 6 (taken): 60, 12: 74                                1 head of 2560    1: 55, 4 (taken): 50, 6: 47, 12: 56
-int delta_segments(long long units, int d, long long chunks) {
+// fp32 at d = 128, whose workgroups have 16 columns: 8 heads of 16384 3 segments (taken) 612, 5 (more than fit) 735; 4 heads of 4096 111, 127.
+int delta_segments(long long units, int d, int is_bf16, long long chunks) {
     int n = 1;
     if (chunks < DELTA_CUT) return 1;
-    while ((units * n + 7) / 8 * (d / 16) <= 32 && (units * (n + 1) + 7) / 8 * (d / 32) <= 32 && 10ll * (n + 1) * (n + 1) <= 6 * chunks) ++n;
+    const int cols = !is_bf16 && d == 128 ? 16 : 32;      // of a workgroup (launch_ct)
+    while ((units * n + 7) / 8 * (2 * d / cols) <= 32 && (units * (n + 1) + 7) / 8 * (d / cols) <= 32 && 10ll * (n + 1) * (n + 1) <= 6 * chunks) ++n;
     return n >= 3 ? n : 1;
 }
 
