@@ -436,12 +436,12 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  * be; in steps of 2^-24); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as the sum of two
  * fp16 numbers: states are off by some 1e-6 of their size, o and the 16-bit gradients by their own rounding and little more; o has the same bits whether states are handed out or not.  With beta near 2 over near-equal keys,
  * where a chunk's steps cancel, the error grows with their number: states to 1e-4 at 64 equal keys and beta = 2.  What the gradients of a chunk start from (its state, the gradient behind it, E and Y of its tokens) is kept
- * as one fp16 number each: before they are rounded dq, dk, dv and dbeta are off by up to 8e-4 of their norm, dlog_f, in which such sums cancel, by 6e-3 of its norm over keys whose products are 0.95 (beta near 2), and any of them by
- * up to 64 steps of 2^-11 of a chunk's largest where all its tokens have one key and values that alternate. A sequence in which
+ * as one fp16 number each: before they are rounded dq, dk, dv and dbeta are off by up to 8e-4 of their norm, dlog_f, in which such sums cancel, by 2e-3 (keys whose products are 0.95), and all of them by up to 2^-4 of their largest
+ * (dlog_f 2^-3) where the tokens of a chunk have one key, beta = 2 and values that alternate, in a state 3000 times their size. A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values
  * below 2^-19 of the largest lose bits, below 2^-30 they are lost (in the gradients but dv by the head's largest, and where two such meet sooner).  Keys longer than unit vectors with beta |k|^2 > 2 grow without bound, and past that come out infinite or NaN.
- * log_f below -200 counts as -200.  log_f > 0 is carried as it is where no run of successive tokens adds up to more than 3 (states that grow 20 times).  Past that, PATH_F32 and what is taken token by token go on
- * to fp32's end, but PATH_BF16 by chunks holds what has grown, and the matrices of a chunk, in fp16: bits are lost with every doubling, gradients first, and from about 7 (gradients) and 11 on infinities and NaN come out.
+ * log_f below -200 counts as -200; log_f > 0 is carried as it is.  The matrices of a chunk end with fp16's smallest step, 2^-24 (PATH_BF16): where a run of tokens within a chunk adds up to s > 0, states are off by up to
+ * 5 * 2^-25 e^s of the largest they get to, and from s = 11 on infinities and NaN may come out.
  * Infinities and NaN: by chunks, values that are not finite may spoil every row of the chunk of 64 tokens that they are in, and all later ones (gradients: all earlier ones too), of their
  * sequence and head; token by token, no row before them.
  * No atomics: the same bits every time.  Outputs overlap no input (state_out may be state_in).

@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     constexpr int RB = C::RB, CB = C::CB, NP = 64 * D / 8 / 256;      // 16-byte pieces of a tokens' matrix per thread
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     float* const rows = reinterpret_cast<float*>(smem + C::ROWS);
-    float *const dbs = reinterpret_cast<float*>(smem + C::RED), *const dls = dbs + 256, *const kus = dls + CB * 64;      // [wave][64], [column block][64], [wave]
+    float *const dbs = reinterpret_cast<float*>(smem + C::RED), *const dls = dbs + 256, *const kus = dls + CB * 64, *const mosts = kus + 4;      // [wave][64], [column block][64], [wave], [block of pairs]
     int tid = threadIdx.x, lane = tid & 63;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / a.H), hk = blockIdx.x - tile * a.H;
@@ -390,10 +390,10 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         bf16x8 kr[4];
         slice_tokens(kp, kr);
         // X and N of the lower 32x32 blocks.  Gq and Gk are sums of two fp16 numbers: in dlog_f they add up, times products of keys, over pairs of tokens, and over keys alike those sums cancel where independent
-        // roundings of the pairs do not (single ones left dlog_f off by 6e-3 of its norm at products of 0.95).  The second parts take E's and Y's place.
-        // (Those of a wave's first block wait in the 4 KB of its own.)
-        halfx8 res[4];      // first parts, second parts
-        halfx8* const parked = reinterpret_cast<halfx8*>(slot);
+        // roundings of the pairs do not (single ones left dlog_f off by 6e-3 of its norm at products of 0.95).  They are over a power of two of their own, from the largest of
+        // both: what they are made of may have been walked again with 2^16 times the room, and lie that much lower, or have grown.  The second parts take E's and Y's place.  A wave's first block waits in the 4 KB of its own.
+        f32x16 pairs;
+        f32x4* const parked = reinterpret_cast<f32x4*>(slot);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
@@ -407,40 +407,53 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                 }
                 const int i = 32 * bi + l32;
                 const float ih = rows[192 + i], il = rows[256 + i], ib = rows[i];
+                float top = 0.f;
 #pragma unroll
                 for (int j4 = 0; j4 < 16; j4 += 4) {
                     const int r0 = 32 * br + acc_row(j4, h);
                     const f32x4 rh = *reinterpret_cast<const f32x4*>(rows + 192 + r0), rl = *reinterpret_cast<const f32x4*>(rows + 256 + r0), rb = *reinterpret_cast<const f32x4*>(rows + r0);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        // (a power of two: its rounding and that of the exponent, 1e-5, are nothing beside the operand's; 2^-16: sums of 128 products stay far from fp16's end, one factor's growth included)
-                        const float w = ib * __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f - 16.f);
-                        const float y = job < 3 ? (i < r0 + j ? -rb[j] * w * acc[j4 + j] : 0.f) : (i <= r0 + j ? w * acc[j4 + j] : 0.f);
-                        const half_t y1 = (half_t)y;
-                        res[j4 / 8][(j4 + j) % 8] = y1;
-                        res[2 + j4 / 8][(j4 + j) % 8] = (half_t)(y - (float)y1);
+                        // (a power of two: its rounding and that of the exponent, 1e-5, are nothing beside those of E and Y)
+                        const float w = ib * __builtin_amdgcn_exp2f(((rh[j] - ih) + (rl[j] - il)) * 1.44269504088896340736f);
+                        pairs[j4 + j] = job < 3 ? (i < r0 + j ? -rb[j] * w * acc[j4 + j] : 0.f) : (i <= r0 + j ? w * acc[j4 + j] : 0.f);
+                        top = fmaxf(top, delta_finite(pairs[j4 + j]));
                     }
                 }
+#pragma unroll
+                for (int z = 1; z < 64; z *= 2) top = fmaxf(top, __shfl_xor(top, z));
+                if (lane == 0) mosts[job] = top;
                 if (n == 0)
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) parked[p * 64 + lane] = res[p];
+                    for (int p = 0; p < 4; ++p) parked[p * 64 + lane] = f32x4{pairs[4 * p], pairs[4 * p + 1], pairs[4 * p + 2], pairs[4 * p + 3]};
             }
         }
         __syncthreads();      // (E, Y and dO have been read: Gq and Gk take their places)
+        // the largest between 2^13 and 2^14: sums of two fp16 numbers are right to 2^-38 of it and more
+        float most = mosts[0];
+#pragma unroll
+        for (int i = 1; i < 6; ++i) most = fmaxf(most, mosts[i]);
+        const int above = most > 0.f ? 8 - delta_exponent(most) : 0, raised = __builtin_amdgcn_readfirstlane(above < -40 ? -40 : above > 40 ? 40 : above);
 #pragma unroll
         for (int n = 1; n >= 0; --n) {
             const int job = wv + 4 * n, b = job % 3, br = b ? 1 : 0, bi = b == 2 ? 1 : 0;
             if (n == 0)
 #pragma unroll
-                for (int p = 0; p < 4; ++p) res[p] = parked[p * 64 + lane];
+                for (int p = 0; p < 4; ++p) {
+                    const f32x4 x = parked[p * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pairs[4 * p + e] = x[e];
+                }
             if (job < 6) {
                 half_t* const to = reinterpret_cast<half_t*>(smem + C::O + (job < 3 ? C::G2 : 0));
                 half_t* const to2 = reinterpret_cast<half_t*>(smem + C::E + (job < 3 ? C::G2 : 0));
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int i = TurnedTile<64>::at(32 * br + acc_row(j, h), 32 * bi + l32);
-                    to[i] = res[j / 8][j % 8];
-                    to2[i] = res[2 + j / 8][j % 8];
+                    const float y = ldexpf(pairs[j], raised);
+                    const half_t y1 = (half_t)y;
+                    to[i] = y1;
+                    to2[i] = (half_t)(y - (float)y1);
                 }
                 if (b == 1)      // the upper block
 #pragma unroll
@@ -456,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
         to_slot(kf);
         slice_tokens(qp, kr);
         __syncthreads();
-        const float up = ldexpf(1.f, ev + eq), up16 = up * 65536.f;      // of every product of two of them, of Gq and Gk, which are 2^16 below theirs
+        const float up = ldexpf(1.f, ev + eq), upg = ldexpf(1.f, ev + eq - raised), wg = delta_power(raised);      // of every product of two of them, of Gq and Gk
         auto nat = [&](int mat, int b, int sl) { return *reinterpret_cast<const halfx8*>(smem + mat + at.nat_at(32 * b, 16 * sl)); };
         float kug = 0.f;
 #pragma unroll
@@ -470,9 +483,9 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
                     const int j = j4 + e;
                     wr[b][j] *= rh[e] * be[e];
                     kug += (float)slot[(r0 + e) * 32 + l32] * wr[b][j];
-                    q1[b][j] *= 0x1p-16f * ga[e];
-                    rd[b][j] *= -0x1p-16f * ga[e] * be[e];
-                    wr[b][j] *= 0x1p-16f;
+                    q1[b][j] *= wg * ga[e];
+                    rd[b][j] *= -wg * ga[e] * be[e];
+                    wr[b][j] *= wg;
                 }
             }
         kug = (kug + (rb0 == 0 ? rows[64 + 63] * sum : 0.f)) * up;
@@ -519,7 +532,7 @@ __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const int r = 32 * (rb0 + b) + acc_row(j, h);
-                const float d1 = q1[b][j] * up16, d2 = rd[b][j] * up16, d3 = wr[b][j] * up16;      // (dq without scale: so is Q with it)
+                const float d1 = q1[b][j] * upg, d2 = rd[b][j] * upg, d3 = wr[b][j] * upg;      // (dq without scale: so is Q with it)
                 pl[j] = (float)slot[r * 32 + l32] * d1 + (float)kl[b][j / 8][j % 8] * (d2 - d3);
                 q1[b][j] = a.scale * d1;
                 rd[b][j] = d2 + d3;

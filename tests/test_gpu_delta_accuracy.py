@@ -1,4 +1,6 @@
 """Gated delta rule on the GPU: values of unlike sizes within a head, against the token walk in 64 bits.  Bars as in test_gpu_delta.py, which derives them."""
+import math
+
 import pytest
 
 import delta_model as dm
@@ -203,3 +205,27 @@ def test_gates_that_grow(gpu, up, down, period, d, dtype, G):
             assert (off <= (1e-5 if n == "state" else 2e-5) * sizes[n]).all(), (n, float((off / sizes[n]).max()))
         else:
             close(torch, n, got[n], want[n], x["cu"].tolist(), dtype == "fp32")
+
+
+@pytest.mark.parametrize("up,down,period", [(0.45, -0.5, 40), (0.35, -0.36, 40), (1.4, -9.9, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2])
+def test_gates_that_grow_far(gpu, up, down, period, d, G):
+    """Runs of tokens within a chunk that add up to s = 7 to 9.8: gamma and rho alone would be past fp16's end as factors of operands.  o and the 16-bit gradients to the usual bars.  States, relative to the largest they get
+    to: an entry of P or M is off by up to 2^-25 whatever its size, hence by 2^-25 e^s of one that a run as long has taken to e^-s, and its product with a row of what has grown e^s times by as much; a row adds up 64 of them
+    in every chunk: sqrt(64) * 0.58 (the deviation), about 5."""
+    torch, pa = gpu
+    x = dm.batch([200, 70], 2, G, d, seed=13)
+    at = torch.arange(270)
+    saw = down > -3
+    x["log_f"][:] = torch.where(at % period < (period // 2 if saw else period - 1), up, down)[:, None].to(x["log_f"].dtype)
+    x["log_f"][:, 1] = 0
+    s = up * (period // 2 if saw else period - 1)
+    got, want = pair(gpu, x, d, 2, G)
+    sizes = dict(zip(("state", "d_state"), largest_states(torch, x, d ** -0.5)))
+    for n in got:
+        if n in sizes:
+            off = (got[n].double().cpu() - want[n]).abs()
+            assert (off <= (5 * 2.0 ** -25 * math.exp(s) + 1e-5) * sizes[n]).all(), (n, float((off / sizes[n]).max()))
+        else:
+            close(torch, n, got[n], want[n], x["cu"].tolist(), False)
