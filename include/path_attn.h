@@ -402,7 +402,8 @@ path_status_t path_paged_extend(const void* q, const void* k, const void* v, con
  *      put on the stack free_pages [num_pages], whose first free_count [1] entries are free; all of them become -1.
  *   2. entries of new tokens' pages -- from ceil(cached / page_size) on -- that are no page get the one on top of the stack; if it is empty they become -1 (a hole) and are
  *      counted in missing [nseq].  Entries of pages that already hold cached tokens are left as they are.
- *   3. cu_new [nseq + 1] = offsets of the packed new tokens; slots [T] (64 bits) = page * page_size + place in it of every new token; -1 where there is no page, and for t behind
+ *   3. cu_new [nseq + 1] = offsets of the packed new tokens; slots [T] (64 bits; for caches of the caller's own beside these: the path_paged_* calls read the table, and path_delta_extend's slots are another thing) =
+ *      page * page_size + place in it of every new token; -1 where there is no page, and for t behind
  *      the last new token.  T bounds the new tokens: offsets end at it, and tokens behind it take no part.  Tokens past pages_per_seq * page_size get no slot.
  * Pages go back before any is taken, both in the order of the table (sequence after sequence): the result is always the same.  A page is in one entry only (a page in two
  * entries goes back twice); what finds no room on the stack is dropped.  free_count outside 0 .. num_pages is held to it.
@@ -431,11 +432,13 @@ path_status_t path_paged_plan(const int* cached, const int* new_tokens, int* pag
  *   path_delta_extend     serving: packed new tokens (as cu_new of the path_paged_* calls, at most max_new a sequence) for states in a pool [num_slots,V,d,d], carried on in place.
  *                         slots [nseq] (DEVICE int32): the sequence's state; outside 0 .. num_slots - 1: starts from zeros and is not kept.  cached [nseq] (DEVICE int32, as in the
  *                         path_paged_* calls): tokens before these; 0: starts from zeros whatever the slot holds.  No new tokens: the slot is left as it is.  Two sequences of one call
- *                         have different slots (the state of one that is named twice is undefined; no fault).
+ *                         have different slots (the state of one that is named twice is undefined; no fault).  A state moves on over every token of the call: where drafts may be dropped, the caller copies the state
+ *                         before, or takes the drafts once they stay.
  * Arithmetic: PATH_F32 in 32 bits throughout.  PATH_BF16: states and sums in fp32, products of fp16 operands.  q and k are operands as they are (below 65504 in magnitude, as scale q.k has to
  * be; in steps of 2^-24); what comes of v, d_o and the states is held over a power of two per sequence, head and 16 value indices, chosen from the largest finite value of the first state and of the first chunk that is not all zeros, as the sum of two
  * fp16 numbers: states are off by some 1e-6 of their size, o and the 16-bit gradients by their own rounding and little more; o has the same bits whether states are handed out or not.  With beta near 2 over near-equal keys,
- * where a chunk's steps cancel, the error grows with their number: states to 1e-4 at 64 equal keys and beta = 2.  What the gradients of a chunk start from (its state, the gradient behind it, E and Y of its tokens) is kept
+ * where a chunk's steps cancel, the error grows with their number: states to 1e-4 at 64 equal keys and beta = 2, and where nothing is forgotten it adds up from chunk to chunk (to 1e-3, and 4e-2 of
+ * the gradients, after ten such chunks; PATH_F32 too: the matrices of such a chunk are nearly singular to 32 bits).  What the gradients of a chunk start from (its state, the gradient behind it, E and Y of its tokens) is kept
  * as one fp16 number each: before they are rounded dq, dk, dv and dbeta are off by up to 8e-4 of their norm, dlog_f, in which such sums cancel, by 2e-3 (keys whose products are 0.95), and all of them by up to 2^-4 of their largest
  * (dlog_f 2^-3) where the tokens of a chunk have one key, beta = 2 and values that alternate, in a state 3000 times their size. A sequence in which
  * anything outgrows that (1000 times; 64 times where gradients are wanted) is walked again over the largest value of all its chunks, then with 2^8 and 2^16 times the room.  Values

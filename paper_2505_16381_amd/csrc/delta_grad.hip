@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a) {
         }
 }
 
-// ---- bf16: 32x32 products of fp16 operands of one part, over the powers of two of the scans ----
+// ---- bf16: 32x32 products of fp16 operands of one part (Gq and Gk: of two), over the powers of two of the scans ----
 //
 // A wave has 32 key indices of dq and dk, of all 64 tokens (d = 64: of 32).  E, Y and dO are in LDS for everybody; the wave's columns of S, G, K and Q pass through
 // 4 KB of its own, half a state at a time, the next piece on its way in registers meanwhile: no barrier from the first product to the last but the two around Gq and Gk, and two
@@ -190,9 +190,10 @@ template <int D> struct Grad16 {
 
 // ---- bf16: 32x32x16 products of fp16 operands; E, Y, dO (then Gq and Gk in their place) in LDS, S and G by way of 4 KB of a wave's own ----
 //
-// A wave has 32 key indices; two workgroups share a CU, so that one's loads stand beside the other's products.  Bound by memory: d = 128, 64 heads of 8192 tokens 407 to 450 us from run to run, 3.6 TB/s and more of its own traffic
-// (1.61 GB: S, G, E, Y, K, Q, dO in, dq, dk, dv out); 16 value heads of 8 key heads over 15000 tokens, whose groups of two add up in registers, 294 us.  With S and G whole in LDS (one workgroup
-// per CU) it took 1098 us, by way of a wave's own 4 KB 561, with row sums in registers that no index selects and gradients out by whole pieces 429.
+// A wave has 32 key indices; two workgroups share a CU, so that one's loads stand beside the other's products.  Bound by memory, and by the chain of a chunk's phases: d = 128, 64 heads of 8192 tokens 484 to 529 us from run to run, 3.0 TB/s and more of its own traffic
+// (1.61 GB: S, G, E, Y, K, Q, dO in, dq, dk, dv out); 16 value heads of 8 key heads over 15000 tokens, whose groups of two add up in registers (97 of them spilled, 384 bytes a lane), 352 us.  With Gq and Gk as single
+// numbers 407 to 450 us, in groups 292.  Before that: with S and G whole in LDS (one workgroup per CU) 1098 us, by way of a wave's own 4 KB 561, with row sums in registers that no index selects and gradients out by whole
+// pieces 429.
 template <int D, bool GROUP>
 __global__ __launch_bounds__(256, 2) void delta_grad16_kernel(DeltaArgs a) {
     typedef Grad16<D> C;

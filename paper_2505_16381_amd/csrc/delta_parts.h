@@ -11,7 +11,7 @@
 // that values of any size have fp16's eleven bits (down to 2^-19 of the largest; less below).  What is computed is multiplied as the sum of NP = 2 fp16 numbers, the second
 // the rounding of what the first leaves (relative steps of 2^-23; o and gradients 2e-7 of their norm from 64 bits before they are rounded).  Single ones (2^-12) are rounded relative to the state and to P's
 // rows, not to a step of a token: 4e-4 of the norm over random keys and betas below 1, but 5e-3, three times bf16's own rounding, over keys whose products are 0.95 with betas near 2, and more the longer a
-// chunk's steps cancel.  (They took 304 us where two take 385: forward of 4 x 16 heads, 8192 tokens.  Sums of bf16 numbers need three for as much: states 331 us of 737 in all.)
+// chunk's steps cancel.  (They took 304 us where two take 388: forward of 4 x 16 heads, 8192 tokens.  Sums of bf16 numbers need three for as much: states 331 us of 737 in all.)
 #pragma once
 #include "delta_decl.h"
 

@@ -58,8 +58,8 @@ template <typename F, typename T> __device__ __forceinline__ F row_frag(const T*
 }
 
 // Four waves to a chunk, 16 rows each; K and Q come from memory as operands (a wave's four tiles of K overlap the others' in L1).  Bound by the chain of its phases,
-// so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone, and 128 registers (three of them spilled) let four in.  d = 128, 8192 tokens of 64 heads: 108 us, 3.5 TB/s
-// (K, Q in, P, M out: 378 MB); three workgroups 120.  With the transposes for training 158 us (three workgroups: a third matrix in LDS).
+// so by how many workgroups a CU holds: LDS has the 64 x 64 matrices alone, and 128 registers (three of them spilled, of fp32 at d = 128 eight) let four in.  d = 128, 8192 tokens of 64 heads: 119 us, 4.0 TB/s
+// (K, Q in, P, M out: 478 MB; with operands of one part 108, where three workgroups took 120).  With the transposes for training 176 us (three workgroups: a third matrix in LDS).
 template <typename T, int D, bool TRAIN>      // TRAIN: the transposes, for the gradients
 __global__ __launch_bounds__(256, TRAIN ? 3 : 4) void delta_prep_kernel(DeltaArgs a) {
     typedef typename std::conditional<sizeof(T) == 2, half_t, float>::type C;      // of the operands that are kept

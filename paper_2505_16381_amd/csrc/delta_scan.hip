@@ -5,9 +5,9 @@
 // gradient (backwards, a chunk ahead).  What one wave alone needs of K, Q, A and M comes from memory straight into its registers, a chunk ahead; what others need -- the
 // state, the predictions' errors, U -- is exchanged through LDS as operands, split once.  Three barriers a chunk.
 //
-// Bound by the latency of a chunk: two exchanges and four products that wait for one another.  d = 128, 64 heads of 8192 tokens, 32 columns: 211 us, 1.6 a chunk, 3.0 TB/s of its own traffic
-// (642 MB: K, Q, V, P, M in, o out); with what the backward needs 300 us (1.05 GB), backwards 293 us (0.90 GB).  One wave per 16 columns, without exchanges (64 dependent products a
-// chunk), took 465 us, four waves for everything, over bf16 operands in more parts, 331, four more for the outputs and fp16 operands 256; loads one chunk ahead instead of two 262.
+// Bound by the latency of a chunk: two exchanges and four products that wait for one another.  d = 128, 64 heads of 8192 tokens, 32 columns: 302 us, 2.3 a chunk, 2.4 TB/s of its own traffic
+// (738 MB: K, Q, V, P, M in, o out); with what the backward needs 380 us (1.14 GB), backwards 363 us (1.0 GB).  Of the way there, with operands of one part, which take 211 us: one wave per 16 columns, without exchanges
+// (64 dependent products a chunk), 465 us, four waves for everything, over bf16 operands in more parts, 331, four more for the outputs and fp16 operands 256; loads one chunk ahead instead of two 262.
 #include <type_traits>
 
 #include "delta_parts.h"
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(512, 1) void delta_scan_kernel(DeltaArgs a) {
                 for (int x = 0; x < CT; ++x) o[x] = decltype(turned)::value ? delta_mma(y[sl][x], m[sl], o[x]) : delta_mma(m[sl], y[sl][x], o[x]);
     };
     // A state's or token matrix's slabs to memory for the chunk's gradients; the waves take turns.  fp32: the lane's row of the transposed matrix; fp16: fragments as they are, 1 KB each, by value indices and
-    // slabs (rows instead, of which a fragment has 64 bytes each, took 342 us where this takes 300).
+    // slabs (rows instead, of which a fragment has 64 bytes each, took 342 us where this took 300, both with operands of one part).
     auto keep = [&](void* out, int area, size_t u, int np, int slabs) {
         const int ld = slabs * P::SL;
         for (int sl = wv; sl < slabs; sl += 4)
@@ -765,11 +765,11 @@ static hipError_t launch(const DeltaArgs& a, hipStream_t stream) {
     delta_scan_kernel<T, D, CT, MODE><<<dim3(xcd_deal_grid(parts, a.nseq * a.V * nseg)), dim3(512), L::BYTES, stream>>>(a);
     return hipGetLastError();
 }
-// 32 columns to a workgroup where those of 16 do not all find a CU: each chunk's K, Q and matrices then serve twice as many.  4096 tokens, d = 128, 16 against 32 columns, all kernels, us:
-// 32 heads 107 and 116 (training forward 148, 165), 48 heads 186 and 131 (259, 204), 64 heads 207 and 152 (309, 242).
+// 32 columns to a workgroup where those of 16 do not all find a CU: each chunk's K, Q and matrices then serve twice as many.  4096 tokens, d = 128, 16 against 32 columns, uncut, all kernels, us:
+// 32 heads 125 and 153 (training forward 159, 181), 40 heads 210 and 160 (276, 209), 64 heads 254 and 196 (351, 260).
 template <typename T, int D, int MODE>
 static hipError_t launch_ct(const DeltaArgs& a, hipStream_t stream) {
-    if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers)
+    if constexpr (sizeof(T) == 2 || D == 64)      // (fp32 at d = 128: 32 columns do not fit the registers; 16 spill 62, of the training pair 74 and 48)
         if (MODE == DELTA_PART || a.nseg > 1 || (long long)a.nseq * a.V * (D / 16) > 256) return launch<T, D, 2, MODE>(a, stream);
     return launch<T, D, 1, MODE>(a, stream);
 }
@@ -790,8 +790,8 @@ hipError_t launch_delta_scan(const DeltaArgs& a, int d, int is_bf16, int mode, h
 
 // Segments of sequences whose longest has `chunks`.  Heads are dealt to 8 XCDs of 32 CUs, a workgroup takes a CU: both launches are to fit at once.  Beyond the root of 0.6 times the chunks
 // the joining of states costs more than shorter segments gain, and two segments gain nothing.  Times in us, both launches and the matrices of the chunks, d = 128, one sequence:
-//   8 heads of 16384 tokens   1 segment 302, 3: 246, 5 (taken): 172, 6 (does not fit): 203       16 heads of 8192   1: 170, 3 (taken): 148, 4: 164
-//   4 heads of 4096           1: 82, 3: 74, 6 (taken): 60, 12: 74                                1 head of 2560    1: 55, 4 (taken): 50, 6: 47, 12: 56
+//   8 heads of 16384 tokens   1 segment 358, 2: 442, 3: 312, 4: 251, 5 (taken): 215, 6 (does not fit): 250       16 heads of 8192   1: 199, 2: 245, 3 (taken): 182, 4: 199
+//   4 heads of 4096           1: 95, 3: 93, 4: 81, 6 (taken): 69, 12: 81                                          1 head of 2560     1: 64, 4 (taken): 59, 6: 54, 12: 61
 // fp32 at d = 128, whose workgroups have 16 columns: 8 heads of 16384 3 segments (taken) 612, 5 (more than fit) 735; 4 heads of 4096 111, 127.
 int delta_segments(long long units, int d, int is_bf16, long long chunks) {
     int n = 1;
